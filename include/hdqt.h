@@ -75,6 +75,10 @@ typedef enum { HDQT_GEMM_FWD = 0, HDQT_GEMM_BWD_INPUT = 1, HDQT_GEMM_BWD_WEIGHT 
 #define HDQT_ESCRATCH (-14)        /* hdqt_gemm_fwd_static: the shape needs more scratch than the
                                       library's fixed device array holds */
 
+#define HDQT_EINVAL_DTYPE (-15)    /* unknown element type */
+#define HDQT_EINVAL_OPTION (-16)   /* unknown reduction, activation or kind of norm, or a number (eps,
+                                      max_norm) out of its range */
+
 /* One quantized operand; names follow the paper's quantizer Q. */
 typedef struct {
     int32_t b;          /* bit width of the integer codes, 2..8 (the paper's b)            */
@@ -496,6 +500,104 @@ int hdqt_layer_bwd(const float *G, const float *W, const void *saved, float *dX,
                    int64_t M, int64_t K, int64_t N, const hdqt_params_t *bwd_input,
                    const hdqt_params_t *bwd_weight, void *workspace, size_t workspace_bytes,
                    void *stream);
+
+/*
+ * The operators around the integer products of a training step (no steps of the paper): the
+ * classifier's loss, the normalisation between layers, the clipping of the gradients.  They work in
+ * floating point.  Differences from the conventions above: tensors are fp32 or bfloat16
+ * (hdqt_dtype_t), a pointer needs the alignment of its elements only (16 bytes are faster), and
+ * infinities and NaN are taken as the formulas take them.  Products, sums, softmax statistics, means and
+ * variances are held in 32 bits or more; a bfloat16 output is rounded once, to nearest even.  Results do
+ * not depend on the order in which workgroups finish.
+ */
+typedef enum { HDQT_F32 = 0, HDQT_BF16 = 1 } hdqt_dtype_t;
+typedef enum { HDQT_REDUCE_NONE = 0, HDQT_REDUCE_MEAN = 1, HDQT_REDUCE_SUM = 2 } hdqt_reduction_t;
+typedef enum { HDQT_ACT_NONE = 0, HDQT_ACT_RELU = 1, HDQT_ACT_SILU = 2 } hdqt_act_t;
+typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
+
+/*
+ * Softmax cross entropy of a linear classifier of N classes over K features, M rows:
+ *     z = X W + bias,   lse_i = log sum_j exp(z_ij),   l_i = lse_i - z_i,target(i)
+ *     loss = l (HDQT_REDUCE_NONE, M values), sum_i l_i, or sum_i l_i / max(1, rows that count)
+ * and its gradients, with g_i = dloss (a value for each row, or one) times the row's share in the loss:
+ *     dz_ij = g_i (exp(z_ij - lse_i) - [j = target(i)]),   dX = dz W^T,   dW = X^T dz,   dbias_j = sum_i dz_ij
+ * The logits are not kept: they are formed tile by tile, and in the backward pass again, in pieces of the
+ * classes whose dz lies in the workspace (at most 256 MB of it, or 1024 classes).
+ *   X         [M, K], rows ldx >= K elements apart; W [K, N], rows ldw >= N apart (a head that has more
+ *             classes than are in use); both of `dtype`
+ *   bias      [N] of bias_dtype, or NULL.  Minus infinity takes a class out: probability and gradient zero
+ *   target    int64 [M], a class or ignore_index (any value): such a row has loss and gradients zero and does
+ *             not count.  Any other value makes the row's loss and gradients NaN.  A target that is taken out
+ *             has loss plus infinity; a logit of plus infinity or NaN makes the row's loss and gradients NaN
+ *   saved     hdqt_xent_saved_size(M) bytes, 4-byte aligned, written by the forward call, read by the
+ *             backward call with the same arguments; private to the library
+ *   dX, dW    [M, K] and [K, N], dense, of `dtype`; dbias [N] of bias_dtype; any may be NULL (one must not)
+ *   dloss     fp32, M values for HDQT_REDUCE_NONE, else one; NULL: ones
+ *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd}_workspace_size (0 for invalid arguments)
+ * hdqt_xent_step is the forward and the backward call with dloss = 1; its workspace is the larger of the two.
+ * bfloat16: products of bfloat16 with sums in 32 bits; dz is rounded to bfloat16 before its products.
+ * fp32: as exact as products in 32 bits.
+ */
+size_t hdqt_xent_saved_size(int64_t M);
+size_t hdqt_xent_fwd_workspace_size(int64_t M, int64_t K, int64_t N, int dtype);
+size_t hdqt_xent_bwd_workspace_size(int64_t M, int64_t K, int64_t N, int dtype);
+int hdqt_xent_fwd(const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias, const int64_t *target,
+                  int64_t ignore_index, int64_t M, int64_t K, int64_t N, int dtype, int bias_dtype, int reduction,
+                  float *loss, float *saved, void *workspace, size_t workspace_bytes, void *stream);
+int hdqt_xent_bwd(const float *dloss, const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias,
+                  const int64_t *target, int64_t ignore_index, int64_t M, int64_t K, int64_t N, int dtype,
+                  int bias_dtype, int reduction, const float *saved, void *dX, void *dW, void *dbias, void *workspace,
+                  size_t workspace_bytes, void *stream);
+int hdqt_xent_step(const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias, const int64_t *target,
+                   int64_t ignore_index, int64_t M, int64_t K, int64_t N, int dtype, int bias_dtype, int reduction,
+                   float *loss, float *saved, void *dX, void *dW, void *dbias, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/*
+ * Group normalisation with an activation, channels innermost: x [B, P, C] (what a layer's product leaves:
+ * B images of P pixels), G groups of C/G channels, mean and variance over a group's pixels and channels,
+ *     xh = (x - mean) / sqrt(var + eps),   pre = xh weight + bias,   y = act(pre)
+ * and its gradients, xh and pre formed again from x:
+ *     d = dy act'(pre),   dbias = sum d,   dweight = sum d xh (over images and pixels),
+ *     dx = (weight d - mean(weight d) - xh mean(weight d xh)) / sqrt(var + eps)
+ *   x, y, dy, dx   of `dtype`, dense; y may be x, dx may be dy.  weight, bias, dweight, dbias [C] of
+ *                  param_dtype; weight NULL: ones, bias NULL: zeros
+ *   act            max(pre, 0) has the derivative 0 at 0; pre / (1 + exp(-pre)) for HDQT_ACT_SILU
+ *   saved          fp32 [B, G, 2], 8-byte aligned: mean and 1 / sqrt(var + eps), written by the forward call
+ *   dx, dweight, dbias   any may be NULL (one must not)
+ *   workspace      16-byte aligned, hdqt_groupnorm_workspace_size (0 for invalid arguments)
+ * HDQT_EINVAL_DIM for B above 65535, C above 65536, P of 2^31 or more, G that does not divide C, B G above 2^23.
+ */
+size_t hdqt_groupnorm_workspace_size(int64_t B, int64_t P, int C, int G, int dtype, int backward);
+int hdqt_groupnorm_fwd(const void *x, const void *weight, const void *bias, void *y, float *saved, int64_t B,
+                       int64_t P, int C, int G, float eps, int act, int dtype, int param_dtype, void *workspace,
+                       size_t workspace_bytes, void *stream);
+int hdqt_groupnorm_bwd(const void *dy, const void *x, const void *weight, const void *bias, const float *saved,
+                       void *dx, void *dweight, void *dbias, int64_t B, int64_t P, int C, int G, int act, int dtype,
+                       int param_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The global norm of many tensors and their clipping by it:
+ *     n = sqrt(sum of all elements' squares) (HDQT_NORM_2) or max |g| (HDQT_NORM_MAX)
+ *     c = min(1, max_norm / (n + eps)),   dst = c src
+ *   tensors   HOST memory, read before the call returns: the addresses travel with the launches, so a call can
+ *             be captured.  Tensors of both types may be mixed, any number of them, empty ones too.  dst may
+ *             be src; then nothing is written where c is 1.  hdqt_grad_norm does not look at dst
+ *   norm      fp32, one value (device).  An infinite norm gives c = 0, a NaN among the elements c = NaN
+ *   workspace 16-byte aligned, hdqt_clip_grad_norm_workspace_size (0 for invalid arguments) for both calls
+ */
+typedef struct {
+    const void *src;
+    void *dst;
+    int64_t elements;
+    int32_t dtype;      /* hdqt_dtype_t */
+    int32_t reserved;
+} hdqt_tensor_t;
+size_t hdqt_clip_grad_norm_workspace_size(const hdqt_tensor_t *tensors, int64_t count);
+int hdqt_grad_norm(const hdqt_tensor_t *tensors, int64_t count, int kind, float *norm, void *workspace,
+                   size_t workspace_bytes, void *stream);
+int hdqt_clip_grad_norm(const hdqt_tensor_t *tensors, int64_t count, float max_norm, float eps, int kind, float *norm,
+                        void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Optional per-kernel timing, for benchmarks.  While enabled, every kernel the

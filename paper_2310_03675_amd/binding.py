@@ -5,6 +5,7 @@ PyTorch is used for device memory and streams; nothing here computes.  If the
 library is missing the import of a function fails loudly: there is no CPU or
 PyTorch fallback.
 """
+import contextlib
 import ctypes as C
 import importlib
 import os
@@ -58,6 +59,9 @@ EXPORTED = [
     "hdqt_gemm_fwd_static", "hdqt_gemm_fwd_static_max_bytes",
     "hdqt_gemm_bwd_input_masked", "hdqt_layer_bwd_masked", "hdqt_conv_bwd_masked",
     "hdqt_probe_matrix_clock", "hdqt_wall_clock_khz",
+    "hdqt_xent_saved_size", "hdqt_xent_fwd_workspace_size", "hdqt_xent_bwd_workspace_size", "hdqt_xent_fwd",
+    "hdqt_xent_bwd", "hdqt_xent_step", "hdqt_groupnorm_workspace_size", "hdqt_groupnorm_fwd", "hdqt_groupnorm_bwd",
+    "hdqt_clip_grad_norm_workspace_size", "hdqt_grad_norm", "hdqt_clip_grad_norm",
 ]
 
 
@@ -90,6 +94,11 @@ class CLayout(C.Structure):
 
 class CKernelTime(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int64), ("total_ms", C.c_double)]
+
+
+class CTensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("elements", C.c_int64), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
 
 
 @dataclass
@@ -221,6 +230,31 @@ def load() -> C.CDLL:
     lib.hdqt_gemm_fwd_static.argtypes = [vp, vp, vp, i64, i64, i64, C.POINTER(CParams), vp, vp]
     lib.hdqt_gemm_fwd_static_max_bytes.restype = sz
     lib.hdqt_gemm_fwd_static_max_bytes.argtypes = []
+    f32 = C.c_float
+    lib.hdqt_xent_saved_size.restype = sz
+    lib.hdqt_xent_saved_size.argtypes = [i64]
+    for name in ("hdqt_xent_fwd_workspace_size", "hdqt_xent_bwd_workspace_size"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [i64, i64, i64, i32]
+    rows = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, i32]        # X ... reduction
+    lib.hdqt_xent_fwd.restype = i32
+    lib.hdqt_xent_fwd.argtypes = rows + [vp, vp, vp, sz, vp]
+    lib.hdqt_xent_bwd.restype = i32
+    lib.hdqt_xent_bwd.argtypes = [vp] + rows + [vp, vp, vp, vp, vp, sz, vp]
+    lib.hdqt_xent_step.restype = i32
+    lib.hdqt_xent_step.argtypes = rows + [vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.hdqt_groupnorm_workspace_size.restype = sz
+    lib.hdqt_groupnorm_workspace_size.argtypes = [i64, i64, i32, i32, i32, i32]
+    lib.hdqt_groupnorm_fwd.restype = i32
+    lib.hdqt_groupnorm_fwd.argtypes = [vp] * 5 + [i64, i64, i32, i32, f32, i32, i32, i32, vp, sz, vp]
+    lib.hdqt_groupnorm_bwd.restype = i32
+    lib.hdqt_groupnorm_bwd.argtypes = [vp] * 8 + [i64, i64, i32, i32, i32, i32, i32, vp, sz, vp]
+    lib.hdqt_clip_grad_norm_workspace_size.restype = sz
+    lib.hdqt_clip_grad_norm_workspace_size.argtypes = [C.POINTER(CTensor), i64]
+    lib.hdqt_grad_norm.restype = i32
+    lib.hdqt_grad_norm.argtypes = [C.POINTER(CTensor), i64, i32, vp, vp, sz, vp]
+    lib.hdqt_clip_grad_norm.restype = i32
+    lib.hdqt_clip_grad_norm.argtypes = [C.POINTER(CTensor), i64, f32, f32, i32, vp, vp, sz, vp]
     lib.hdqt_strerror.restype = C.c_char_p
     lib.hdqt_strerror.argtypes = [i32]
     lib.hdqt_last_hip_error.restype = i32
@@ -243,9 +277,9 @@ def profile_enable(on: bool) -> None:
 
 def profile_collect() -> dict:
     """-> {kernel name: (launches, total milliseconds)} since the last collect."""
-    rows = (CKernelTime * 32)()
-    n = load().hdqt_profile_collect(rows, 32)
-    return {rows[i].name.decode(): (rows[i].launches, rows[i].total_ms) for i in range(min(n, 32))}
+    rows = (CKernelTime * 64)()
+    n = load().hdqt_profile_collect(rows, 64)
+    return {rows[i].name.decode(): (rows[i].launches, rows[i].total_ms) for i in range(min(n, 64))}
 
 
 def n_eff(D: int, had_block: int) -> int:
@@ -792,3 +826,264 @@ def gemm_requant(kind: int, P: torch.Tensor, Q: torch.Tensor, M: int, K: int, N:
     if rc:
         raise HdqtError(rc, "hdqt_gemm_requant")
     return out, acc, workspace
+
+
+# ---- the operators around the products of a training step --------------------------------------
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+REDUCTIONS = {"none": 0, "mean": 1, "sum": 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
+NORMS = {2.0: 0, float("inf"): 1}
+
+
+def _of(table: dict, key, what: str) -> int:
+    if key not in table:
+        raise ValueError(f"{what} must be one of {sorted(map(str, table))}, not {key}")
+    return table[key]
+
+
+def _dtype(t: torch.Tensor) -> int:
+    return _of(_DTYPES, t.dtype, "the element type")
+
+
+def _check_out(what: str, t: torch.Tensor, shape, dtype, device) -> None:
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _rows(what: str, t: torch.Tensor) -> int:
+    """Distance of a matrix's rows, which are dense and do not overlap."""
+    if t.dim() != 2 or not t.is_cuda or t.numel() == 0:
+        raise ValueError(f"{what} must be a matrix with elements in device memory")
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{what} must have dense rows (strides {t.stride()})")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _xent_args(X, W, target, bias, ignore_index, reduction):
+    ldx, ldw = _rows("X", X), _rows("W", W)
+    (M, K), N = X.shape, W.shape[1]
+    if W.shape[0] != K or W.dtype != X.dtype or W.device != X.device:
+        raise ValueError(f"W must be [{K}, classes] of {X.dtype} on {X.device}")
+    _check_out("target", target, (M,), torch.int64, X.device)
+    if bias is not None:
+        if bias.dtype not in (torch.float32, X.dtype):
+            raise ValueError(f"bias must be float32 or {X.dtype}")
+        _check_out("bias", bias, (N,), bias.dtype, X.device)
+    return (M, K, N), (_ptr(X), ldx, _ptr(W), ldw, _ptr(bias), _ptr(target), ignore_index, M, K, N, _dtype(X),
+                       _dtype(X if bias is None else bias), _of(REDUCTIONS, reduction, "reduction"))
+
+
+def _bytes(n: int, device) -> torch.Tensor:
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+_HERE_AND_NOW = contextlib.nullcontext()
+
+
+def _place(device, stream):
+    """Where a call runs and allocates: the given stream, whose memory a call's own buffers then are, or the current
+    stream of the tensors' device."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return _HERE_AND_NOW if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def xent_fwd(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, bias: Optional[torch.Tensor] = None,
+             ignore_index: int = -100, reduction: str = "mean", workspace: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_xent_fwd -> (loss fp32 [] or [M], saved): softmax cross entropy of the classifier X W + bias,
+    X [M, K], W [K, N] (fp32 or bfloat16, dense rows, which may lie apart), target int64 [M]."""
+    (M, K, N), args = _xent_args(X, W, target, bias, ignore_index, reduction)
+    _check_dev(workspace)
+    with _place(X.device, stream):
+        loss = torch.empty((M,) if reduction == "none" else (), dtype=torch.float32, device=X.device)
+        saved = torch.empty(M + 1, dtype=torch.float32, device=X.device)
+        if workspace is None:
+            workspace = _bytes(load().hdqt_xent_fwd_workspace_size(M, K, N, args[10]), X.device)
+        rc = load().hdqt_xent_fwd(*args, _ptr(loss), _ptr(saved), _ptr(workspace), workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_xent_fwd")
+        return loss, saved
+
+
+def _xent_grads(X, W, bias, need):
+    new = lambda want, t, shape: torch.empty(shape, dtype=t.dtype, device=t.device) if want and t is not None else None
+    return new(need[0], X, X.shape), new(need[1], W, W.shape), new(need[2], bias, (W.shape[1],))
+
+
+def xent_bwd(dloss: Optional[torch.Tensor], X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, saved: torch.Tensor,
+             bias: Optional[torch.Tensor] = None, ignore_index: int = -100, reduction: str = "mean",
+             need=(True, True, True), workspace: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_xent_bwd -> (dX, dW, dbias), those that `need` asks for and None in the place of others.  dloss: fp32, one
+    value or (reduction "none") M; None: ones.  saved: of xent_fwd with the same arguments."""
+    (M, K, N), args = _xent_args(X, W, target, bias, ignore_index, reduction)
+    _check_dev(workspace)
+    _check_out("saved", saved, (M + 1,), torch.float32, X.device)
+    if dloss is not None:
+        _check_out("dloss", dloss, (M,) if reduction == "none" else (), torch.float32, X.device)
+    with _place(X.device, stream):
+        dX, dW, db = _xent_grads(X, W, bias, need)
+        if workspace is None:
+            workspace = _bytes(load().hdqt_xent_bwd_workspace_size(M, K, N, args[10]), X.device)
+        rc = load().hdqt_xent_bwd(_ptr(dloss), *args, _ptr(saved), _ptr(dX), _ptr(dW), _ptr(db), _ptr(workspace),
+                                  workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_xent_bwd")
+        return dX, dW, db
+
+
+def xent_step(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, bias: Optional[torch.Tensor] = None,
+              ignore_index: int = -100, reduction: str = "mean", need=(True, True, True),
+              workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_xent_step -> (loss, dX, dW, dbias): xent_fwd and xent_bwd (with dloss = 1) in one call."""
+    (M, K, N), args = _xent_args(X, W, target, bias, ignore_index, reduction)
+    _check_dev(workspace)
+    with _place(X.device, stream):
+        loss = torch.empty((M,) if reduction == "none" else (), dtype=torch.float32, device=X.device)
+        dX, dW, db = _xent_grads(X, W, bias, need)
+        saved = torch.empty(M + 1, dtype=torch.float32, device=X.device)
+        if workspace is None:
+            lib = load()
+            workspace = _bytes(max(lib.hdqt_xent_fwd_workspace_size(M, K, N, args[10]),
+                                   lib.hdqt_xent_bwd_workspace_size(M, K, N, args[10])), X.device)
+        rc = load().hdqt_xent_step(*args, _ptr(loss), _ptr(saved), _ptr(dX), _ptr(dW), _ptr(db), _ptr(workspace),
+                                   workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_xent_step")
+        return loss, dX, dW, db
+
+
+def _norm_sizes(x, groups, weight, bias):
+    if x.dim() < 2 or not x.is_cuda or not x.is_contiguous():
+        raise ValueError("x must be a contiguous device tensor [images, ..., channels]")
+    if x.numel() == 0:
+        raise HdqtError(-2, "hdqt_groupnorm")
+    B, C_ = x.shape[0], x.shape[-1]
+    given = [t for t in (weight, bias) if t is not None]
+    for t in given:
+        if t.dtype not in (torch.float32, x.dtype) or t.dtype != given[0].dtype:
+            raise ValueError(f"weight and bias must be float32 or {x.dtype}, both the same")
+        _check_out("weight and bias", t, (C_,), t.dtype, x.device)
+    return B, x.numel() // (B * C_), C_, given[0].dtype if given else torch.float32
+
+
+def _norm_workspace(x, B, P, C_, groups, backward):
+    return _bytes(load().hdqt_groupnorm_workspace_size(B, P, C_, groups, _dtype(x), int(backward)), x.device)
+
+
+def groupnorm_fwd(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = None,
+                  bias: Optional[torch.Tensor] = None, eps: float = 1e-5, act: str = "none",
+                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_groupnorm_fwd -> (y, saved fp32 [images, groups, 2]): x [images, ..., channels] (fp32 or bfloat16)
+    normalised over each group's pixels and channels, act "none", "relu" or "silu" behind it.  out may be x."""
+    B, P, C_, pdt = _norm_sizes(x, groups, weight, bias)
+    _check_dev(workspace)
+    with _place(x.device, stream):
+        if out is None:
+            out = torch.empty_like(x)
+        _check_out("out", out, x.shape, x.dtype, x.device)
+        saved = torch.empty((B, max(groups, 1), 2), dtype=torch.float32, device=x.device)
+        if workspace is None:
+            workspace = _norm_workspace(x, B, P, C_, groups, False)
+        rc = load().hdqt_groupnorm_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(out), _ptr(saved), B, P, C_, groups, eps,
+                                       _of(ACTIVATIONS, act, "act"), _dtype(x), _DTYPES[pdt], _ptr(workspace),
+                                       workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_groupnorm_fwd")
+        return out, saved
+
+
+def groupnorm_bwd(dy: torch.Tensor, x: torch.Tensor, saved: torch.Tensor, groups: int,
+                  weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, act: str = "none",
+                  need=(True, True, True), out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_groupnorm_bwd -> (dx, dweight, dbias), those that `need` asks for.  dweight and dbias are of the
+    parameters' type (fp32 without parameters).  out, for dx, may be dy."""
+    B, P, C_, pdt = _norm_sizes(x, groups, weight, bias)
+    _check_dev(workspace)
+    _check_out("dy", dy, x.shape, x.dtype, x.device)
+    _check_out("saved", saved, (B, groups, 2), torch.float32, x.device)
+    with _place(x.device, stream):
+        dx = None
+        if need[0]:
+            dx = torch.empty_like(x) if out is None else out
+            _check_out("out", dx, x.shape, x.dtype, x.device)
+        dw, db = (torch.empty(C_, dtype=pdt, device=x.device) if want else None for want in need[1:])
+        if workspace is None:
+            workspace = _norm_workspace(x, B, P, C_, groups, True)
+        rc = load().hdqt_groupnorm_bwd(_ptr(dy), _ptr(x), _ptr(weight), _ptr(bias), _ptr(saved), _ptr(dx), _ptr(dw), _ptr(db),
+                                       B, P, C_, groups, _of(ACTIVATIONS, act, "act"), _dtype(x), _DTYPES[pdt],
+                                       _ptr(workspace), workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_groupnorm_bwd")
+        return dx, dw, db
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether t's elements fill a range of memory, in whatever order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda v: v[1]):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+def _tensors(grads, out):
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if len(out) != len(grads):
+        raise ValueError(f"{len(grads)} tensors, but {len(out)} outputs")
+    if not grads:
+        raise ValueError("no tensors")
+    device = grads[0].device
+    rows = (CTensor * len(grads))()
+    for row, g, o in zip(rows, grads, out):
+        for t in (g, o):
+            # (any dense order of the elements will do, the same on both sides)
+            if not t.is_cuda or t.device != device or not _dense(t):
+                raise ValueError("tensors must be dense device tensors, all on one device")
+        if o is not g and (o.dtype != g.dtype or o.shape != g.shape or
+                           (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))):
+            raise ValueError("an output must have its tensor's type, shape and strides")
+        row.src, row.dst, row.elements, row.dtype = g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g)
+    return rows, len(grads), device
+
+
+def grad_norm(grads, norm_type: float = 2.0, workspace: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """hdqt_grad_norm -> fp32 []: the norm (2 or inf) of all elements of the tensors together."""
+    rows, n, device = _tensors(grads, None)
+    _check_dev(workspace)
+    kind = _of(NORMS, float(norm_type), "norm_type")
+    with _place(device, stream):
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        if workspace is None:
+            workspace = _bytes(load().hdqt_clip_grad_norm_workspace_size(rows, n), device)
+        rc = load().hdqt_grad_norm(rows, n, kind, _ptr(norm), _ptr(workspace), workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_grad_norm")
+        return norm
+
+
+def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, eps: float = 1e-6, out=None,
+                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """hdqt_clip_grad_norm -> the norm before clipping, fp32 [] on the device (nothing waits for it).  The tensors are
+    multiplied by min(1, max_norm / (norm + eps)), in place or into `out`."""
+    rows, n, device = _tensors(grads, out)
+    _check_dev(workspace)
+    kind = _of(NORMS, float(norm_type), "norm_type")
+    with _place(device, stream):
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        if workspace is None:
+            workspace = _bytes(load().hdqt_clip_grad_norm_workspace_size(rows, n), device)
+        rc = load().hdqt_clip_grad_norm(rows, n, max_norm, eps, kind, _ptr(norm), _ptr(workspace), workspace.numel(),
+                                        _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_clip_grad_norm")
+        return norm

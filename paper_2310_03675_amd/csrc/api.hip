@@ -8,9 +8,15 @@
 #include <limits.h>
 #include <mutex>
 
-namespace {
+static thread_local int g_last_hip_error = 0;
 
-thread_local int g_last_hip_error = 0;
+int hdqt::hip_fail(hipError_t e)
+{
+    g_last_hip_error = (int)e;
+    return HDQT_EHIP;
+}
+
+namespace {
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
@@ -104,11 +110,7 @@ int log2i(int v)
     return k;
 }
 
-int hip_fail(hipError_t e)
-{
-    g_last_hip_error = (int)e;
-    return HDQT_EHIP;
-}
+using hdqt::hip_fail;
 
 // Parts the contraction is split into when the output has too few tiles to fill the chip.
 // The matmul kernels keep two workgroups per CU resident (512 on the chip); every part
@@ -1604,6 +1606,8 @@ const char* hdqt_strerror(int code)
     case HDQT_EHIP: return "a HIP call failed (see hdqt_last_hip_error)";
     case HDQT_ESCRATCH: return "the shape needs more scratch than the library's fixed device array holds";
     case HDQT_EINVAL_GEOMETRY: return "convolution geometry or layer shape not taken by the activation-source kernels";
+    case HDQT_EINVAL_DTYPE: return "unknown element type";
+    case HDQT_EINVAL_OPTION: return "unknown reduction, activation or kind of norm, or a number out of its range";
     default: return "unknown error code";
     }
 }

@@ -1,0 +1,222 @@
+"""Group normalisation with an activation, channels innermost, against 64 bits.
+
+Tolerances, 2-norm of the difference over 2-norm of the result.  fp32: some ten roundings of 2^-24 between x and y or dx,
+and sums whose error is that of a few partial sums: 2e-6 (32 roundings).  bfloat16, of 8 significant bits: one rounding of at most 2^-8 more.
+dx is a difference (zero for groups of one element): against the 2-norm of its first term.  dweight and dbias: sums of terms of either sign, whose result may be smaller than its terms by the square root of their
+number; against the 2-norm over the terms' own, 2e-6."""
+import pytest
+import torch
+
+from paper_2310_03675_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def inputs(shape, dtype, seed=0, mean=0.5, std=1.0, pdtype=F32):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g)
+    C = shape[-1]
+    return ((r(*shape) * std + mean + r(C)).to(dtype).cuda(), r(*shape).to(dtype).cuda(), (1 + 0.3 * r(C)).to(pdtype).cuda(),
+            (0.3 * r(C)).to(pdtype).cuda())
+
+
+def reference(x, dy, w, b, G, act, eps=1e-5):
+    x, dy = x.double().cpu().reshape(x.shape[0], -1, x.shape[-1]), dy.double().cpu().reshape(x.shape[0], -1, x.shape[-1])
+    B_, P, C = x.shape
+    w = torch.ones(C, dtype=torch.float64) if w is None else w.double().cpu()
+    b = torch.zeros(C, dtype=torch.float64) if b is None else b.double().cpu()
+    v = x.reshape(B_, P, G, C // G)
+    mu = v.mean((1, 3), keepdim=True)
+    rstd = 1 / torch.sqrt((v - mu).square().mean((1, 3), keepdim=True) + eps)
+    xh = ((v - mu) * rstd).reshape(B_, P, C)
+    pre = xh * w + b
+    s = torch.sigmoid(pre)
+    y = {"none": pre, "relu": pre.clamp_min(0), "silu": pre * s}[act]
+    d = dy * {"none": torch.ones_like(pre), "relu": (pre > 0).double(), "silu": s * (1 + pre * (1 - s))}[act]
+    wd = (d * w).reshape(B_, P, G, C // G)
+    xg = xh.reshape(B_, P, G, C // G)
+    dx = rstd * (wd - wd.mean((1, 3), keepdim=True) - xg * (wd * xg).mean((1, 3), keepdim=True))
+    return dict(y=y, dx=dx.reshape(B_, P, C), dw=(d * xh).sum((0, 1)), db=d.sum((0, 1)),
+                dx_terms=(rstd * wd).norm(), dw_terms=(d * xh).square().sum().sqrt(), db_terms=d.square().sum().sqrt(), pre=pre)
+
+
+def near(got, want, tol, norm=None):
+    d, n = (got.double().cpu().reshape(want.shape) - want).norm(), want.norm() if norm is None else norm
+    assert d <= tol * n + 1e-30, (float(d / n), tol)
+
+
+def check(shape, G, dtype, act, w="given", pdtype=F32, seed=0, mean=0.5, std=1.0):
+    x, dy, wt, bs = inputs(shape, dtype, seed, mean, std, pdtype)
+    if w == "none":
+        wt = bs = None
+    if act == "relu":      # (an element whose pre-activation is within rounding of the corner has two right derivatives)
+        dy = dy * (reference(x, dy, wt, bs, G, act)["pre"].abs() > 1e-4).reshape(dy.shape).to(dy)
+    want = reference(x, dy, wt, bs, G, act)
+    x0, dy0 = x.clone(), dy.clone()
+    y, saved = B.groupnorm_fwd(x, G, wt, bs, act=act)
+    dx, dw, db = B.groupnorm_bwd(dy, x, saved, G, wt, bs, act=act)
+    assert torch.equal(x, x0) and torch.equal(dy, dy0)
+    tol = 2e-6 if dtype == F32 else 2e-6 + 2.0 ** -8
+    near(y, want["y"], tol)
+    near(dx, want["dx"], tol, norm=want["dx_terms"])
+    more = 0.0 if pdtype == F32 else 2.0 ** -8
+    near(dw, want["dw"], 1.0, norm=2e-6 * want["dw_terms"] + more * want["dw"].norm())
+    near(db, want["db"], 1.0, norm=2e-6 * want["db_terms"] + more * want["db"].norm())
+    # alone, and in place
+    assert B.groupnorm_bwd(dy, x, saved, G, wt, bs, act=act, need=(True, False, False))[1:] == (None, None)
+    only = B.groupnorm_bwd(dy, x, saved, G, wt, bs, act=act, need=(False, True, False))
+    assert only[0] is None and torch.equal(only[1], dw)
+    dx2, _, _ = B.groupnorm_bwd(dy, x, saved, G, wt, bs, act=act, out=dy)
+    assert dx2 is dy and torch.equal(dx2, dx)
+    y2, _ = B.groupnorm_fwd(x, G, wt, bs, act=act, out=x)
+    assert y2 is x and torch.equal(y2, y)
+
+
+SHAPES = [((1, 1, 1), 1), ((2, 1, 8), 2), ((1, 1, 64), 64), ((3, 2, 5), 1), ((3, 7, 15), 5), ((2, 49, 96), 3), ((128, 4, 4, 512), 32),
+          ((4, 32, 32, 64), 32), ((2, 64, 64, 40), 8), ((5, 33, 7, 12), 3), ((1, 5000, 24), 4), ((2, 17, 2056), 8), ((1, 9, 4100), 10),
+          ((2, 300, 320), 32), ((300, 3, 16), 4), ((1, 70000, 8), 2), ((7, 1, 33), 33), ((2, 100, 130), 1), ((1, 20001, 129), 3)]
+
+
+@pytest.mark.parametrize("shape,G", SHAPES, ids=str)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+def test_against_64_bits(shape, G, dtype, act):
+    check(shape, G, dtype, act)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_parameters(dtype):
+    check((4, 50, 32), 4, dtype, "silu", w="none")
+    check((4, 50, 32), 4, dtype, "none", w="none")
+    if dtype == BF16:
+        check((4, 50, 32), 4, dtype, "silu", pdtype=BF16)
+
+
+def test_large_mean():
+    """A mean that is many deviations away costs the bits it takes from x - mean, and no more: x has 24 bits, the mean
+    takes 10 of them from the deviation; the variance must not lose 20."""
+    x = (torch.randn(2, 3000, 16, generator=torch.Generator().manual_seed(3)) + 1000.0).cuda()
+    y, saved = B.groupnorm_fwd(x, 4)
+    v = x.double().cpu().reshape(2, 3000, 4, 4)
+    mu, var = v.mean((1, 3)), v.var((1, 3), unbiased=False)
+    assert torch.allclose(saved[..., 0].double().cpu(), mu, rtol=2.0 ** -22, atol=0)
+    assert torch.allclose(saved[..., 1].double().cpu(), 1 / torch.sqrt(var + 1e-5), rtol=1e-5, atol=0)
+    want = ((v - mu[:, None, :, None]) / torch.sqrt(var + 1e-5)[:, None, :, None]).reshape(2, 3000, 16)
+    assert float((y.double().cpu() - want).norm() / want.norm()) < 1000 * 2.0 ** -23
+
+
+def test_first_value_far_off():
+    x = torch.randn(1, 4096, 8, generator=torch.Generator().manual_seed(4))
+    x[0, 0] = 3000.0
+    x = x.cuda()
+    _, saved = B.groupnorm_fwd(x, 2)
+    v = x.double().cpu().reshape(1, 4096, 2, 4)
+    var = v.var((1, 3), unbiased=False)
+    assert torch.allclose(saved[..., 1].double().cpu(), 1 / torch.sqrt(var + 1e-5), rtol=1e-5, atol=0)
+
+
+def test_constant_groups_and_one_element():
+    x = torch.full((2, 10, 8), 3.0, device="cuda")
+    w, b = torch.full((8,), 2.0, device="cuda"), torch.full((8,), 0.25, device="cuda")
+    y, saved = B.groupnorm_fwd(x, 2, w, b)
+    assert bool((y == 0.25).all()) and bool((saved[..., 0] == 3.0).all())
+    dy = torch.randn_like(x)
+    dx, dw, db = B.groupnorm_bwd(dy, x, saved, 2, w, b)
+    assert bool((dw == 0).all()) and bool(dx.isfinite().all())
+    one = torch.tensor([[[7.0]]], device="cuda")
+    y, saved = B.groupnorm_fwd(one, 1)
+    assert float(y) == 0.0
+    assert float(B.groupnorm_bwd(one, one, saved, 1)[0]) == 0.0
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+def test_values_that_are_not_finite_stay_in_their_group(act):
+    x = torch.randn(3, 40, 16, device="cuda")
+    clean, _ = B.groupnorm_fwd(x, 4, act=act)
+    for bad in (float("nan"), float("inf")):
+        v = x.clone()
+        v[1, 5, 6] = bad
+        y, _ = B.groupnorm_fwd(v, 4, act=act)
+        hit = torch.zeros(3, 40, 16, dtype=torch.bool)
+        hit[1, :, 4:8] = True
+        assert torch.equal(y.cpu()[~hit], clean.cpu()[~hit]) and bool(y[1, 5, 6].isnan())
+
+
+def test_gradient_by_differences():
+    """The directional derivative of sum(y * r) against (f(x + h d) - f(x - h d)) / 2h in 64 bits of the fp32 outputs: h^2
+    from the third derivative (h = 1/64: 2.4e-4 of it, which is of the first's size) and 2^-24 / h from rounding: 2e-3."""
+    x, r, w, b = inputs((2, 30, 12), F32, 9)
+    d, h = torch.randn(2, 30, 12, generator=torch.Generator().manual_seed(1)).cuda(), 1 / 64
+    y, saved = B.groupnorm_fwd(x, 3, w, b, act="silu")
+    dx, dw, db = B.groupnorm_bwd(r, x, saved, 3, w, b, act="silu")
+    f = lambda x, w, b: float((B.groupnorm_fwd(x, 3, w, b, act="silu")[0].double() * r.double()).sum())
+    e = torch.randn(12, generator=torch.Generator().manual_seed(2)).cuda()
+    for got, plus, minus in ((float((dx.double() * d.double()).sum()), (x + h * d, w, b), (x - h * d, w, b)),
+                             (float((dw.double() * e.double()).sum()), (x, w + h * e, b), (x, w - h * e, b)),
+                             (float((db.double() * e.double()).sum()), (x, w, b + h * e), (x, w, b - h * e))):
+        assert got == pytest.approx((f(*plus) - f(*minus)) / (2 * h), rel=2e-3, abs=2e-2)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_parts_of_other_tensors(dtype):
+    whole = torch.randn(4 * 30 * 16 + 1, device="cuda").to(dtype)
+    x = whole[1:].reshape(4, 30, 16)
+    y, saved = B.groupnorm_fwd(x, 4, act="silu")
+    z, other = B.groupnorm_fwd(x.clone(), 4, act="silu")
+    tol = 1e-5 if dtype == F32 else 2.0 ** -8
+    assert torch.allclose(y.float(), z.float(), rtol=tol, atol=tol) and torch.allclose(saved, other, rtol=1e-6, atol=1e-6)
+
+
+def test_refusals():
+    x = torch.randn(2, 6, 8, device="cuda")
+    for call in (lambda: B.groupnorm_fwd(x.transpose(1, 2), 2), lambda: B.groupnorm_fwd(x.half(), 2),
+                 lambda: B.groupnorm_fwd(x, 2, act="tanh"), lambda: B.groupnorm_fwd(x, 2, torch.ones(7, device="cuda")),
+                 lambda: B.groupnorm_fwd(x, 2, out=torch.empty(2, 6, 9, device="cuda")),
+                 lambda: B.groupnorm_fwd(x, 2, torch.ones(8, device="cuda"), torch.ones(8, device="cuda", dtype=BF16))):
+        with pytest.raises(ValueError):
+            call()
+    for groups in (0, 3, -2):
+        with pytest.raises(B.HdqtError):
+            B.groupnorm_fwd(x, groups)
+    with pytest.raises(B.HdqtError):
+        B.groupnorm_fwd(torch.empty(0, 6, 8, device="cuda"), 2)
+
+
+def test_beyond_32_bits():
+    x = torch.empty(2, 1 << 24, 72, dtype=BF16, device="cuda")       # 2.4 G elements, 1.2 G an image
+    x.normal_(generator=torch.Generator(device="cuda").manual_seed(0))
+    x[1] += 1.0
+    y, saved = B.groupnorm_fwd(x, 3)
+    mean, rstd = saved[..., 0].cpu(), saved[..., 1].cpu()
+    assert torch.allclose(mean, torch.tensor([[0.0] * 3, [1.0] * 3]), atol=1e-3) and torch.allclose(rstd, torch.ones(2, 3), atol=1e-3)
+    for image in (0, 1):
+        v = x[image, -5:].float().cpu()
+        want = (v - mean[image].repeat_interleave(24)) * rstd[image].repeat_interleave(24)
+        assert torch.allclose(y[image, -5:].float().cpu(), want, atol=2e-2)
+    del y
+    dx, dw, db = B.groupnorm_bwd(x, x, saved, 3)                     # dy = x: d xh = xh^2 / rstd + mean xh
+    assert torch.allclose(db.cpu(), torch.full((72,), float(1 << 24)), rtol=1e-2)
+    assert torch.allclose(dw.cpu(), torch.full((72,), 2.0 * (1 << 24)), rtol=1e-2)
+    assert float(dx[1, -5:].float().abs().max()) < 0.1               # dy is an affine function of xh
+
+
+def test_graph_and_streams():
+    x, dy, w, b = inputs((4, 100, 48), F32, 5)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y0, s0 = B.groupnorm_fwd(x, 4, w, b, act="silu", stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, saved = B.groupnorm_fwd(x, 4, w, b, act="silu")
+        grads = B.groupnorm_bwd(dy, x, saved, 4, w, b, act="silu")
+    for k in range(4):
+        x.normal_()
+        dy.normal_()
+        y1, s1 = B.groupnorm_fwd(x, 4, w, b, act="silu")
+        want = B.groupnorm_bwd(dy, x, s1, 4, w, b, act="silu")
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, y1) and all(torch.equal(p, q) for p, q in zip(grads, want))

@@ -1,0 +1,284 @@
+"""Softmax cross entropy of a linear classifier, against 64 bits.
+
+Tolerances, 2-norm of the difference over 2-norm of the result.  fp32: a logit of size |z| <= 8 over K terms has an error of
+about sqrt(K) 2^-24 |z|, K <= 4096: 3e-5 at most and 4e-6 for K = 512; so have its exponential and the gradients: 1e-5 up
+to K = 1000, 4e-5 beyond; the loss, in which the logits' errors are averaged or stand alone: the same of (1 + |z|).
+bfloat16, of 8 significant bits: dz rounded once (2^-8 at most), the gradients once more: 2^-7, and where a gradient's terms cancel (dbias, a
+single class) against the 2-norm of its terms."""
+import math
+
+import pytest
+import torch
+
+from paper_2310_03675_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+IGNORE = -100
+
+
+def inputs(M, K, N, dtype, bias=True, ignored=0.0, spare=0, lead=0, seed=0, bdtype=None):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g)
+    X = r(M, K + lead).to(dtype).cuda()[:, lead:]
+    W = (r(K, N + spare) * 1.5 / math.sqrt(K)).to(dtype).cuda()[:, :N]
+    b = (r(N) * 0.5).to(bdtype or dtype).cuda() if bias else None
+    t = torch.randint(0, N, (M,), generator=g)
+    if ignored:
+        t[torch.rand(M, generator=g) < ignored] = IGNORE
+    return X, W, b, t.cuda()
+
+
+def reference(X, W, b, t, reduction="mean", dloss=None):
+    X, W, t = X.double().cpu(), W.double().cpu(), t.cpu()
+    z = X @ W + (0 if b is None else b.double().cpu())
+    lse = torch.logsumexp(z, 1)
+    keep = t != IGNORE
+    rows = torch.where(keep, lse - z.gather(1, t.clamp_min(0)[:, None])[:, 0], torch.zeros_like(lse))
+    share = 1.0 / max(1, int(keep.sum())) if reduction == "mean" else 1.0
+    loss = rows if reduction == "none" else rows.sum() * share
+    g = keep.double() * share * (1.0 if dloss is None else dloss.double().cpu())
+    dz = torch.exp(z - lse[:, None])
+    dz[torch.arange(len(t)), t.clamp_min(0)] -= 1
+    dz = dz * g[:, None]
+    return loss, dz @ W.t(), X.t() @ dz, dz.sum(0), dz
+
+
+def tolerance(dtype, K):
+    return (1e-5 if K <= 1000 else 4e-5) if dtype == F32 else 2.0 ** -7 + 4e-5
+
+
+def near(got, want, tol, floor=0.0):
+    d = float((got.double().cpu() - want).norm())
+    assert d <= tol * max(float(want.norm()), floor) + 1e-12, (d / (float(want.norm()) + 1e-300), tol)
+
+
+def check(M, K, N, dtype, reduction="mean", dloss=False, **kw):
+    X, W, b, t = inputs(M, K, N, dtype, **kw)
+    g = None
+    if dloss:
+        g = (torch.randn((M,) if reduction == "none" else (), generator=torch.Generator().manual_seed(7)) + 2).cuda()
+    want, dX, dW, db, dz = reference(X, W, b, t, reduction, g)
+    tol, args = tolerance(dtype, K), dict(bias=b, ignore_index=IGNORE, reduction=reduction)
+    before = [v.clone() for v in (X, W)]
+    loss, saved = B.xent_fwd(X, W, t, **args)
+    near(loss, want, 1e-5 if K <= 1000 else 4e-5, floor=math.sqrt(loss.numel()))
+    got = B.xent_bwd(g, X, W, t, saved, **args)
+    assert torch.equal(before[0], X) and torch.equal(before[1], W)
+    assert got[0].dtype == X.dtype and got[1].dtype == W.dtype and tuple(got[1].shape) == (K, N)
+    # (N = 1: every gradient is zero up to the rounding of 1 - 1)
+    floor = float(dz.norm()) + (1.0 if N == 1 else 0.0) * 2.0 ** -7
+    near(got[0], dX, tol, floor * 0.5)
+    near(got[1], dW, tol, floor * 0.5)
+    if b is not None:
+        near(got[2], db, tol, floor)
+    else:
+        assert got[2] is None
+    if not dloss:
+        step = B.xent_step(X, W, t, **args)
+        assert torch.equal(step[0], loss) and all(p is q or torch.equal(p, q) for p, q in zip(step[1:], got))
+    only = B.xent_bwd(g, X, W, t, saved, need=(False, True, False), **args)
+    assert only[0] is None and only[2] is None and torch.equal(only[1], got[1])
+    only = B.xent_bwd(g, X, W, t, saved, need=(True, False, False), **args)
+    assert only[1] is None and torch.equal(only[0], got[0])
+
+
+SIZES = [(1, 561, 11), (1, 1, 1), (1, 1, 2), (3, 7, 5), (128, 512, 100), (2, 33, 1000), (64, 64, 64), (65, 65, 65), (63, 129, 127),
+         (200, 64, 129), (257, 96, 300), (300, 1000, 2), (777, 320, 1007), (1000, 40, 10007), (5, 2048, 4099), (512, 256, 2048),
+         (130, 1023, 513), (33, 4096, 50), (1, 300, 33000), (2049, 24, 31)]
+
+
+@pytest.mark.parametrize("M,K,N", SIZES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_against_64_bits(M, K, N, dtype):
+    check(M, K, N, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("reduction", ["none", "mean", "sum"])
+@pytest.mark.parametrize("M,K,N", [(70, 48, 90), (300, 264, 1200)])
+def test_reductions_ignored_rows_and_gradients_of_the_loss(dtype, reduction, M, K, N):
+    check(M, K, N, dtype, reduction, ignored=0.3)
+    check(M, K, N, dtype, reduction, dloss=True, ignored=0.3, bias=False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,K,N,spare,lead", [(40, 64, 96, 32, 0), (40, 64, 97, 3, 0), (100, 61, 200, 1, 3), (130, 128, 1000, 24, 8), (1, 64, 64, 64, 64)])
+def test_rows_that_lie_apart(dtype, M, K, N, spare, lead):
+    check(M, K, N, dtype, spare=spare, lead=lead)
+
+
+def test_bias_of_32_bits_behind_bfloat16():
+    check(100, 64, 300, BF16, bdtype=F32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_many_pieces_of_the_classes(dtype):
+    """More rows and classes than a piece's part of the workspace: the input gradient is added up over pieces."""
+    M, K, N = 40000, 32, 4321
+    X, W, b, t = inputs(M, K, N, dtype, ignored=0.1)
+    need = B.load().hdqt_xent_bwd_workspace_size(M, K, N, B._DTYPES[dtype])
+    assert need < 4 * M * N                                     # (not the logits)
+    loss, dX, dW, db = B.xent_step(X, W, t, bias=b, ignore_index=IGNORE)
+    want, dX1, dW1, db1, dz = reference(X, W, b, t)
+    tol = tolerance(dtype, K)
+    near(loss, want, 1e-5)
+    near(dX, dX1, tol)
+    near(dW, dW1, tol, float(dz.norm()))
+    near(db, db1, tol, float(dz.norm()))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_no_row_counts(dtype):
+    X, W, b, t = inputs(40, 32, 50, dtype)
+    t.fill_(IGNORE)
+    for reduction in ("mean", "sum", "none"):
+        loss, dX, dW, db = B.xent_step(X, W, t, bias=b, reduction=reduction)
+        assert bool((loss == 0).all()) and not dX.any() and not dW.any() and not db.any()
+    t[3] = 7
+    loss, dX, dW, db = B.xent_step(X, W, t, bias=b)
+    near(loss, reference(X, W, b, t)[0], 1e-5)
+    assert dX[3].any() and not dX[:3].any() and not dX[4:].any()
+    # another number to ignore, a class among them
+    loss7, dX7, _, _ = B.xent_step(X, W, t, bias=b, ignore_index=7)
+    assert not dX7[3].any() and bool(loss7.isnan())             # (-100 is no class then)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,K,N", [(70, 40, 150), (300, 264, 700)])
+def test_classes_taken_out(dtype, M, K, N):
+    """Minus infinity, and the type's lowest value, as a class's bias: no probability, no gradient."""
+    X, W, b, t = inputs(M, K, N, dtype)
+    out = torch.zeros(N, dtype=torch.bool)
+    out[N // 2:] = True
+    t = t % (N // 2)
+    small = reference(X, W[:, :N // 2], b[:N // 2], t)
+    for lowest in (-math.inf, torch.finfo(dtype).min / 2):
+        v = b.clone()
+        v[out.cuda()] = lowest
+        loss, dX, dW, db = B.xent_step(X, W, t, bias=v)
+        near(loss, small[0], 1e-5)
+        near(dX, small[1], tolerance(dtype, K))
+        near(dW[:, :N // 2], small[2], tolerance(dtype, K), float(small[4].norm()))
+        assert not dW[:, N // 2:].any() and not db[out.cuda()].any()
+    # a target that is taken out: the loss is infinite, the gradient that of the others' probabilities
+    v = b.clone()
+    v[out.cuda()] = -math.inf
+    t2 = t.clone()
+    t2[5] = N - 1
+    loss, dX, dW, db = B.xent_step(X, W, t2, bias=v, reduction="none")
+    assert float(loss[5]) == math.inf and bool(loss[:5].isfinite().all()) and bool(dX.isfinite().all())
+    # every class
+    loss, dX, dW, db = B.xent_step(X, W, t, bias=torch.full_like(b, -math.inf), reduction="none")
+    assert bool((loss == math.inf).all()) and bool(dX.isfinite().all()) and bool(dW.isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_values_that_are_not_finite_stay_in_their_row(dtype):
+    X, W, b, t = inputs(70, 40, 150, dtype)
+    clean, dX0, _, _ = B.xent_step(X, W, t, bias=b, reduction="none")
+    X2 = X.clone()
+    X2[9, 3] = math.nan
+    loss, dX, _, _ = B.xent_step(X2, W, t, bias=b, reduction="none")
+    rest = torch.arange(70) != 9
+    assert bool(loss[9].isnan()) and torch.equal(loss.cpu()[rest], clean.cpu()[rest])
+    assert bool(dX[9].isnan().all()) and torch.equal(dX.cpu()[rest], dX0.cpu()[rest])
+    v = b.clone()
+    v[11] = math.inf
+    loss, dX, _, _ = B.xent_step(X, W, t, bias=v, reduction="none")
+    assert bool(loss.isnan().all()) and bool(dX.isnan().all())
+    for bad in (150, -1, 1 << 40, -(1 << 40)):                  # no classes
+        t2 = t.clone()
+        t2[9] = bad
+        loss, dX, dW, _ = B.xent_step(X, W, t2, bias=b, reduction="none")
+        assert bool(loss[9].isnan()) and bool(dX[9].isnan().all()) and torch.equal(loss.cpu()[rest], clean.cpu()[rest])
+        # a row that is ignored may hold anything
+        loss, dX, dW, _ = B.xent_step(X, W, t2, bias=b, reduction="none", ignore_index=bad)
+        assert float(loss[9]) == 0.0 and not dX[9].any() and bool(dW.isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large_logits(dtype):
+    """Logits of +-3e4: exponentials only relative to the largest."""
+    X, W, b, t = inputs(60, 32, 80, dtype)
+    X = X * 8192
+    loss, dX, dW, _ = B.xent_step(X, W, t, bias=b)
+    want = reference(X, W, b, t)
+    near(loss, want[0], 1e-5)
+    assert bool(dX.isfinite().all()) and bool(dW.isfinite().all())
+    tiny = X * 1e-30
+    loss, dX, _, _ = B.xent_step(tiny.contiguous(), W, t)
+    near(loss, reference(tiny, W, None, t)[0], 1e-5)
+    near(dX, reference(tiny, W, None, t)[1], tolerance(dtype, 32))
+
+
+def test_gradient_by_differences():
+    """Directional derivatives against (f(x + h d) - f(x - h d)) / 2h with h = 1/128: a third derivative of the first's size
+    gives 1e-5, 2^-23 |loss| / h 5e-5: 1e-3 of the derivative plus 2e-4."""
+    X, W, b, t = inputs(90, 48, 120, F32, ignored=0.2)
+    loss, dX, dW, db = B.xent_step(X, W, t, bias=b)
+    f = lambda X, W, b: float(B.xent_fwd(X, W, t, bias=b)[0])
+    g, h = torch.Generator().manual_seed(3), 1 / 128
+    d, e, c = (torch.randn(v.shape, generator=g).cuda() for v in (X, W, b))
+    for got, plus, minus in ((dX * d, (X + h * d, W, b), (X - h * d, W, b)), (dW * e, (X, W + h * e, b), (X, W - h * e, b)),
+                             (db * c, (X, W, b + h * c), (X, W, b - h * c))):
+        assert float(got.double().sum()) == pytest.approx((f(*plus) - f(*minus)) / (2 * h), rel=1e-3, abs=2e-4)
+
+
+def test_refusals():
+    X, W, b, t = inputs(8, 16, 20, F32)
+    for call in (lambda: B.xent_fwd(X.t(), W, t), lambda: B.xent_fwd(X, W.t().contiguous().t(), t), lambda: B.xent_fwd(X, W, t.int()),
+                 lambda: B.xent_fwd(X, W.to(BF16), t), lambda: B.xent_fwd(X, W[:8], t), lambda: B.xent_fwd(X, W, t[:4]),
+                 lambda: B.xent_fwd(X, W, t, bias=b[:4]), lambda: B.xent_fwd(X, W, t, bias=b.half()),
+                 lambda: B.xent_fwd(X, W, t, reduction="max"), lambda: B.xent_fwd(X.double(), W.double(), t),
+                 lambda: B.xent_fwd(X[:0], W, t[:0]), lambda: B.xent_fwd(X, W[:, :0], t),
+                 lambda: B.xent_fwd(X[:1].expand(8, 16), W, t),
+                 lambda: B.xent_bwd(torch.ones(8, device="cuda"), X, W, t, torch.zeros(9, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_beyond_32_bits():
+    """A weight of 5 GB: its last rows and classes take part."""
+    M, K, N = 16, 2048, 1_300_007
+    W = torch.zeros(K, N, dtype=BF16, device="cuda")
+    W[:, -7:] = 0.01
+    W[-1, 5] = 1.0
+    X = torch.randn(M, K, generator=torch.Generator().manual_seed(0)).to(BF16).cuda()
+    t = torch.full((M,), N - 3, device="cuda")
+    t[1] = 5
+    loss, dX, dW, _ = B.xent_step(X, W, t)
+    cols = torch.tensor([5] + list(range(N - 7, N)))
+    z = torch.zeros(M, N, dtype=torch.float64)
+    z[:, cols] = X.double().cpu() @ W[:, cols.cuda()].double().cpu()
+    lse = torch.logsumexp(z, 1)
+    want = (lse - z.gather(1, t.cpu()[:, None])[:, 0]).mean()
+    assert float(loss) == pytest.approx(float(want), rel=1e-5)
+    dz = torch.exp(z[:, cols] - lse[:, None])
+    for i in range(M):
+        dz[i, list(cols).index(int(t[i]))] -= 1
+    dz /= M
+    near(dW[:, cols.cuda()], X.double().cpu().t() @ dz, 2.0 ** -7)
+    near(dX, dz @ W[:, cols.cuda()].double().cpu().t(), 2.0 ** -7)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,K,N", [(33, 64, 70), (600, 256, 3000)])
+def test_graph_and_streams(dtype, M, K, N):
+    X, W, b, t = inputs(M, K, N, dtype)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    first = B.xent_step(X, W, t, bias=b, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(p, q) for p, q in zip(first, B.xent_step(X, W, t, bias=b)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = B.xent_step(X, W, t, bias=b)
+    for k in range(4):
+        X.normal_()
+        t.random_(0, N)
+        want = B.xent_step(X, W, t, bias=b)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
