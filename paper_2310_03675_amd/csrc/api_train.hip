@@ -227,7 +227,7 @@ static int run_xent(hdqt::XentArgs a, bool forward, bool backward, void* workspa
     const hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
     if (forward) e = hdqt::launch_xent_fwd(a, workspace, st);
-    if (backward && e == hipSuccess) e = hdqt::launch_xent_bwd(a, workspace, st);
+    if (backward && e == hipSuccess) e = hdqt::launch_xent_bwd(a, workspace, forward, st);
     return e == hipSuccess ? HDQT_OK : hip_fail(e);
 }
 

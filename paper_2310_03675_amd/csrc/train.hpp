@@ -124,6 +124,7 @@ struct XentArgs {
 };
 size_t xent_workspace(const XentArgs& a, bool backward);
 hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, hipStream_t stream);
-hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, hipStream_t stream);
+// forward: the forward pass has just run in the same workspace
+hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hipStream_t stream);
 
 } // namespace hdqt
