@@ -236,7 +236,7 @@ enum KernelId {
     K_GEMM_RAGGED, K_GEMM_SMALL, K_COL2IM, K_TRANSPOSE, K_EXPAND,
     K_CLIP_NORM, K_CLIP_FINISH, K_CLIP_SCALE, K_NORM_FWD_SUMS, K_NORM_FWD_FINISH, K_NORM_FWD, K_NORM_BWD_SUMS,
     K_NORM_BWD_FINISH, K_NORM_BWD, K_XENT_LOGITS, K_XENT_LOSS, K_XENT_DLOGITS, K_XENT_DX, K_XENT_DW, K_XENT_DBIAS,
-    K_XENT_PACK, K_XENT_ADD_PARTS,
+    K_XENT_PACK, K_XENT_ADD_PARTS, K_NORM_PARAMS,
     K_COUNT
 };
 bool quantize_fast_eligible(const QuantArgs& q);

@@ -39,7 +39,7 @@ const char* kernel_name(int id)
         "gemm_tiled_ragged", "gemm_small_batch", "col2im", "transpose", "gemm_expand",
         "clip_norm", "clip_finish", "clip_scale", "groupnorm_fwd_sums", "groupnorm_fwd_finish", "groupnorm_fwd",
         "groupnorm_bwd_sums", "groupnorm_bwd_finish", "groupnorm_bwd", "xent_logits", "xent_loss", "xent_dlogits",
-        "xent_dx", "xent_dw", "xent_dbias", "xent_pack", "xent_add_parts"};
+        "xent_dx", "xent_dw", "xent_dbias", "xent_pack", "xent_add_parts", "groupnorm_params"};
     return (id >= 0 && id < K_COUNT) ? names[id] : "?";
 }
 
