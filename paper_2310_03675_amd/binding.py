@@ -894,6 +894,10 @@ def xent_fwd(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, bias: Optio
              stream: Optional[torch.cuda.Stream] = None):
     """hdqt_xent_fwd -> (loss fp32 [] or [M], saved): softmax cross entropy of the classifier X W + bias,
     X [M, K], W [K, N] (fp32 or bfloat16, dense rows, which may lie apart), target int64 [M]."""
+    if workspace is None and stream is None:
+        r = _native(_host.xent_fwd(X, W, target, bias, ignore_index, REDUCTIONS.get(reduction)), "hdqt_xent_fwd")
+        if r is not None:
+            return r
     (M, K, N), args = _xent_args(X, W, target, bias, ignore_index, reduction)
     _check_dev(workspace)
     with _place(X.device, stream):
@@ -918,6 +922,10 @@ def xent_bwd(dloss: Optional[torch.Tensor], X: torch.Tensor, W: torch.Tensor, ta
              stream: Optional[torch.cuda.Stream] = None):
     """hdqt_xent_bwd -> (dX, dW, dbias), those that `need` asks for and None in the place of others.  dloss: fp32, one
     value or (reduction "none") M; None: ones.  saved: of xent_fwd with the same arguments."""
+    if workspace is None and stream is None:
+        r = _native(_host.xent_bwd(X, W, target, bias, ignore_index, REDUCTIONS.get(reduction), dloss, saved, need), "hdqt_xent_bwd")
+        if r is not None:
+            return r
     (M, K, N), args = _xent_args(X, W, target, bias, ignore_index, reduction)
     _check_dev(workspace)
     _check_out("saved", saved, (M + 1,), torch.float32, X.device)
@@ -938,6 +946,10 @@ def xent_step(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, bias: Opti
               ignore_index: int = -100, reduction: str = "mean", need=(True, True, True),
               workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """hdqt_xent_step -> (loss, dX, dW, dbias): xent_fwd and xent_bwd (with dloss = 1) in one call."""
+    if workspace is None and stream is None:
+        r = _native(_host.xent_step(X, W, target, bias, ignore_index, REDUCTIONS.get(reduction), need), "hdqt_xent_step")
+        if r is not None:
+            return r
     (M, K, N), args = _xent_args(X, W, target, bias, ignore_index, reduction)
     _check_dev(workspace)
     with _place(X.device, stream):
@@ -979,6 +991,10 @@ def groupnorm_fwd(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] =
                   stream: Optional[torch.cuda.Stream] = None):
     """hdqt_groupnorm_fwd -> (y, saved fp32 [images, groups, 2]): x [images, ..., channels] (fp32 or bfloat16)
     normalised over each group's pixels and channels, act "none", "relu" or "silu" behind it.  out may be x."""
+    if out is None and workspace is None and stream is None:
+        r = _native(_host.groupnorm_fwd(x, groups, weight, bias, eps, ACTIVATIONS.get(act)), "hdqt_groupnorm_fwd")
+        if r is not None:
+            return r
     B, P, C_, pdt = _norm_sizes(x, groups, weight, bias)
     _check_dev(workspace)
     with _place(x.device, stream):
@@ -1002,6 +1018,10 @@ def groupnorm_bwd(dy: torch.Tensor, x: torch.Tensor, saved: torch.Tensor, groups
                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """hdqt_groupnorm_bwd -> (dx, dweight, dbias), those that `need` asks for.  dweight and dbias are of the
     parameters' type (fp32 without parameters).  out, for dx, may be dy."""
+    if out is None and workspace is None and stream is None:
+        r = _native(_host.groupnorm_bwd(dy, x, saved, groups, weight, bias, ACTIVATIONS.get(act), need), "hdqt_groupnorm_bwd")
+        if r is not None:
+            return r
     B, P, C_, pdt = _norm_sizes(x, groups, weight, bias)
     _check_dev(workspace)
     _check_out("dy", dy, x.shape, x.dtype, x.device)
@@ -1058,9 +1078,13 @@ def _tensors(grads, out):
 def grad_norm(grads, norm_type: float = 2.0, workspace: Optional[torch.Tensor] = None,
               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """hdqt_grad_norm -> fp32 []: the norm (2 or inf) of all elements of the tensors together."""
+    kind = _of(NORMS, float(norm_type), "norm_type")
+    if workspace is None and stream is None:
+        r = _native(_host.grad_norm(grads, kind), "hdqt_grad_norm")
+        if r is not None:
+            return r
     rows, n, device = _tensors(grads, None)
     _check_dev(workspace)
-    kind = _of(NORMS, float(norm_type), "norm_type")
     with _place(device, stream):
         norm = torch.empty((), dtype=torch.float32, device=device)
         if workspace is None:
@@ -1075,9 +1099,13 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, eps: float = 
                    workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """hdqt_clip_grad_norm -> the norm before clipping, fp32 [] on the device (nothing waits for it).  The tensors are
     multiplied by min(1, max_norm / (norm + eps)), in place or into `out`."""
+    kind = _of(NORMS, float(norm_type), "norm_type")
+    if workspace is None and stream is None:
+        r = _native(_host.clip_grad_norm(grads, out, max_norm, eps, kind), "hdqt_clip_grad_norm")
+        if r is not None:
+            return r
     rows, n, device = _tensors(grads, out)
     _check_dev(workspace)
-    kind = _of(NORMS, float(norm_type), "norm_type")
     with _place(device, stream):
         norm = torch.empty((), dtype=torch.float32, device=device)
         if workspace is None:

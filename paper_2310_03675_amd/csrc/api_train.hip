@@ -88,10 +88,14 @@ int run_clip(const hdqt_tensor_t* tensors, int64_t count, int kind, bool clip, f
     double* parts = reinterpret_cast<double*>(static_cast<char*>(workspace) + 256);
     hipError_t e = each_table(tensors, count, call.plan, clip,
                               [&](const hdqt::ClipTable& t) { return hdqt::launch_clip_norm(t, kind == HDQT_NORM_MAX, parts, st); });
-    if (e == hipSuccess) e = hdqt::launch_clip_finish(parts, call.plan.pieces, kind == HDQT_NORM_MAX, max_norm, eps, norm, scale, st);
+    const bool largest = kind == HDQT_NORM_MAX;
+    const uint32_t pieces = call.plan.pieces;
+    if (e == hipSuccess && !(clip && hdqt::clip_scales_alone(pieces)))
+        e = hdqt::launch_clip_finish(parts, pieces, largest, max_norm, eps, norm, scale, st);
     if (e == hipSuccess && clip)
-        e = each_table(tensors, count, call.plan, clip,
-                       [&](const hdqt::ClipTable& t) { return hdqt::launch_clip_scale(t, scale, st); });
+        e = each_table(tensors, count, call.plan, clip, [&](const hdqt::ClipTable& t) {
+            return hdqt::launch_clip_scale(t, parts, pieces, largest, max_norm, eps, norm, scale, st);
+        });
     return e == hipSuccess ? HDQT_OK : hip_fail(e);
 }
 

@@ -15,6 +15,7 @@
 #include <dlfcn.h>
 
 #include <optional>
+#include <vector>
 
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -42,6 +43,16 @@ struct Library {
     decltype(&hdqt_layer_bwd_masked) bwd_masked;
     decltype(&hdqt_conv_bwd) conv_bwd;
     decltype(&hdqt_conv_bwd_masked) conv_bwd_masked;
+    decltype(&hdqt_xent_fwd_workspace_size) xent_fwd_workspace_size, xent_bwd_workspace_size;
+    decltype(&hdqt_xent_fwd) xent_fwd;
+    decltype(&hdqt_xent_bwd) xent_bwd;
+    decltype(&hdqt_xent_step) xent_step;
+    decltype(&hdqt_groupnorm_workspace_size) norm_workspace_size;
+    decltype(&hdqt_groupnorm_fwd) norm_fwd;
+    decltype(&hdqt_groupnorm_bwd) norm_bwd;
+    decltype(&hdqt_clip_grad_norm_workspace_size) clip_workspace_size;
+    decltype(&hdqt_grad_norm) grad_norm;
+    decltype(&hdqt_clip_grad_norm) clip;
 } lib;
 PyObject *get_device, *get_stream;           // torch's: the current device, its current stream's handle
 
@@ -381,6 +392,272 @@ PyObject* conv_bwd(PyObject* const* a)
     return tuple(Result(std::move(dAct)), Result(std::move(dW)));
 }
 
+// ---- the operators around the products: on the current device and its current stream, workspaces of their own ----
+
+int type_of(const at::Tensor& t)
+{
+    if (t.scalar_type() == at::kFloat) return HDQT_F32;
+    if (t.scalar_type() == at::kBFloat16) return HDQT_BF16;
+    throw Other();
+}
+
+const at::Tensor& on_device(PyObject* o)
+{
+    if (!THPVariable_CheckExact(o)) throw Other();
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) throw Other();
+    return t;
+}
+
+// the current stream, where the current device is the tensor's
+void* stream_of(const at::Tensor& t)
+{
+    PyObject* device = PyObject_CallNoArgs(get_device);
+    if (!device) throw Other();
+    const bool here = PyLong_AsLong(device) == t.get_device();
+    PyObject* h = here ? PyObject_CallOneArg(get_stream, device) : nullptr;
+    Py_DECREF(device);
+    if (!h) throw Other();
+    void* p = PyLong_AsVoidPtr(h);
+    Py_DECREF(h);
+    if (PyErr_Occurred()) throw Other();
+    return p;
+}
+
+// contiguous, of this type, shape and device
+const at::Tensor& like(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor& beside)
+{
+    const at::Tensor& t = tensor(o, type);
+    if (t.sizes() != shape || t.device() != beside.device()) throw Other();
+    return t;
+}
+
+// which of three results are asked for
+struct Need {
+    bool k[3];
+    explicit Need(PyObject* o)
+    {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) throw Other();
+        for (int i = 0; i < 3; ++i) {
+            PyObject* b = PyTuple_GET_ITEM(o, i);
+            if (!PyBool_Check(b)) throw Other();
+            k[i] = b == Py_True;
+        }
+    }
+};
+
+double number(PyObject* o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) throw Other();
+    return v;
+}
+
+int64_t row_step(const at::Tensor& t)
+{
+    if (t.dim() != 2 || t.numel() == 0 || (t.size(1) > 1 && t.stride(1) != 1) || (t.size(0) > 1 && t.stride(0) < t.size(1))) throw Other();
+    return t.size(0) > 1 ? t.stride(0) : t.size(1);
+}
+
+// X, W, target, bias | None, ignore_index, reduction
+struct Classifier {
+    const at::Tensor &X, &W, &target;
+    const at::Tensor* bias;
+    int64_t ldx, ldw, M, K, N, ignore;
+    int dtype, bias_dtype, reduction;
+    void* stream;
+    at::Tensor grads[3], ws;
+    explicit Classifier(PyObject* const* a) : X(on_device(a[0])), W(on_device(a[1])), target(on_device(a[2]))
+    {
+        dtype = type_of(X);
+        ldx = row_step(X);
+        ldw = row_step(W);
+        M = X.size(0); K = X.size(1); N = W.size(1);
+        if (W.scalar_type() != X.scalar_type() || W.size(0) != K || W.device() != X.device()) throw Other();
+        like(a[2], at::kLong, {M}, X);
+        bias = a[3] == Py_None ? nullptr : &on_device(a[3]);
+        bias_dtype = bias ? type_of(*bias) : dtype;
+        if (bias) {
+            if (bias_dtype == HDQT_BF16 && dtype != HDQT_BF16) throw Other();
+            like(a[3], bias->scalar_type(), {N}, X);
+        }
+        ignore = integer(a[4]);
+        reduction = (int)integer(a[5]);
+        stream = stream_of(X);
+    }
+    at::Tensor loss() const
+    {
+        return reduction == HDQT_REDUCE_NONE ? fresh({M}, at::kFloat, X) : fresh({}, at::kFloat, X);
+    }
+    void make_grads(const Need& need)
+    {
+        if (need.k[0]) grads[0] = fresh({M, K}, X.scalar_type(), X);
+        if (need.k[1]) grads[1] = fresh({K, N}, X.scalar_type(), X);
+        if (need.k[2] && bias) grads[2] = fresh({N}, bias->scalar_type(), X);
+    }
+    void* grad(int k) const { return grads[k].defined() ? address(grads[k]) : nullptr; }
+    void make_workspace(size_t n) { ws = bytes(n, X); }
+};
+
+// xent_fwd(X, W, target, bias, ignore_index, reduction) -> (loss, saved)
+PyObject* xent_fwd(PyObject* const* a)
+{
+    Classifier c(a);
+    at::Tensor loss = c.loss(), saved = fresh({c.M + 1}, at::kFloat, c.X);
+    c.make_workspace(lib.xent_fwd_workspace_size(c.M, c.K, c.N, c.dtype));
+    const int rc = unlocked([&] {
+        return lib.xent_fwd(address(c.X), c.ldx, address(c.W), c.ldw, address(c.bias), (const int64_t*)address(c.target), c.ignore, c.M, c.K,
+                            c.N, c.dtype, c.bias_dtype, c.reduction, (float*)address(loss), (float*)address(saved), address(c.ws),
+                            (size_t)c.ws.numel(), c.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(Result(std::move(loss)), Result(std::move(saved)));
+}
+
+// xent_step(X, W, target, bias, ignore_index, reduction, need) -> (loss, dX, dW, dbias)
+PyObject* xent_step(PyObject* const* a)
+{
+    Classifier c(a);
+    c.make_grads(Need(a[6]));
+    at::Tensor loss = c.loss(), saved = fresh({c.M + 1}, at::kFloat, c.X);
+    const size_t f = lib.xent_fwd_workspace_size(c.M, c.K, c.N, c.dtype), b = lib.xent_bwd_workspace_size(c.M, c.K, c.N, c.dtype);
+    c.make_workspace(f > b ? f : b);
+    const int rc = unlocked([&] {
+        return lib.xent_step(address(c.X), c.ldx, address(c.W), c.ldw, address(c.bias), (const int64_t*)address(c.target), c.ignore, c.M, c.K,
+                             c.N, c.dtype, c.bias_dtype, c.reduction, (float*)address(loss), (float*)address(saved), c.grad(0), c.grad(1),
+                             c.grad(2), address(c.ws), (size_t)c.ws.numel(), c.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(Result(std::move(loss)), Result(std::move(c.grads[0])), Result(std::move(c.grads[1])), Result(std::move(c.grads[2])));
+}
+
+// xent_bwd(X, W, target, bias, ignore_index, reduction, dloss | None, saved, need) -> (dX, dW, dbias)
+PyObject* xent_bwd(PyObject* const* a)
+{
+    Classifier c(a);
+    const at::Tensor* dloss = nullptr;
+    if (a[6] != Py_None) dloss = c.reduction == HDQT_REDUCE_NONE ? &like(a[6], at::kFloat, {c.M}, c.X) : &like(a[6], at::kFloat, {}, c.X);
+    const at::Tensor& saved = like(a[7], at::kFloat, {c.M + 1}, c.X);
+    c.make_grads(Need(a[8]));
+    c.make_workspace(lib.xent_bwd_workspace_size(c.M, c.K, c.N, c.dtype));
+    const int rc = unlocked([&] {
+        return lib.xent_bwd((const float*)address(dloss), address(c.X), c.ldx, address(c.W), c.ldw, address(c.bias),
+                            (const int64_t*)address(c.target), c.ignore, c.M, c.K, c.N, c.dtype, c.bias_dtype, c.reduction,
+                            (const float*)address(saved), c.grad(0), c.grad(1), c.grad(2), address(c.ws), (size_t)c.ws.numel(), c.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(Result(std::move(c.grads[0])), Result(std::move(c.grads[1])), Result(std::move(c.grads[2])));
+}
+
+// x [images, ..., channels], groups, weight | None, bias | None
+struct Normed {
+    const at::Tensor& x;
+    const at::Tensor *weight, *bias;
+    int64_t B, P, C, groups;
+    int dtype, param_dtype;
+    at::ScalarType param_type;
+    void* stream;
+    Normed(PyObject* px, PyObject* g, PyObject* w, PyObject* b) : x(on_device(px))
+    {
+        dtype = type_of(x);
+        if (x.dim() < 2 || x.numel() == 0 || !x.is_contiguous()) throw Other();
+        B = x.size(0); C = x.size(-1); P = x.numel() / (B * C);
+        groups = integer(g);
+        if (groups < 1 || groups > C || C > INT32_MAX) throw Other();
+        weight = w == Py_None ? nullptr : &on_device(w);
+        bias = b == Py_None ? nullptr : &on_device(b);
+        const at::Tensor* one = weight ? weight : bias;
+        param_dtype = one ? type_of(*one) : HDQT_F32;
+        param_type = one ? one->scalar_type() : at::kFloat;
+        if (param_dtype == HDQT_BF16 && dtype != HDQT_BF16) throw Other();
+        if (weight) like(w, param_type, {C}, x);
+        if (bias) like(b, param_type, {C}, x);
+        stream = stream_of(x);
+    }
+    at::Tensor workspace(int backward) const { return bytes(lib.norm_workspace_size(B, P, (int)C, (int)groups, dtype, backward), x); }
+};
+
+// groupnorm_fwd(x, groups, weight, bias, eps, act) -> (y, saved)
+PyObject* groupnorm_fwd(PyObject* const* a)
+{
+    const Normed n(a[0], a[1], a[2], a[3]);
+    const float eps = (float)number(a[4]);
+    const int act = (int)integer(a[5]);
+    at::Tensor y = fresh(n.x.sizes(), n.x.scalar_type(), n.x), saved = fresh({n.B, n.groups, 2}, at::kFloat, n.x), ws = n.workspace(0);
+    const int rc = unlocked([&] {
+        return lib.norm_fwd(address(n.x), address(n.weight), address(n.bias), address(y), (float*)address(saved), n.B, n.P, (int)n.C,
+                            (int)n.groups, eps, act, n.dtype, n.param_dtype, address(ws), (size_t)ws.numel(), n.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(Result(std::move(y)), Result(std::move(saved)));
+}
+
+// groupnorm_bwd(dy, x, saved, groups, weight, bias, act, need) -> (dx, dweight, dbias)
+PyObject* groupnorm_bwd(PyObject* const* a)
+{
+    const Normed n(a[1], a[3], a[4], a[5]);
+    const at::Tensor &dy = like(a[0], n.x.scalar_type(), n.x.sizes(), n.x), &saved = like(a[2], at::kFloat, {n.B, n.groups, 2}, n.x);
+    const int act = (int)integer(a[6]);
+    const Need need(a[7]);
+    at::Tensor out[3], ws = n.workspace(1);
+    if (need.k[0]) out[0] = fresh(n.x.sizes(), n.x.scalar_type(), n.x);
+    for (int k = 1; k < 3; ++k)
+        if (need.k[k]) out[k] = fresh({n.C}, n.param_type, n.x);
+    auto at = [&](int k) { return out[k].defined() ? address(out[k]) : nullptr; };
+    const int rc = unlocked([&] {
+        return lib.norm_bwd(address(dy), address(n.x), address(n.weight), address(n.bias), (const float*)address(saved), at(0), at(1), at(2),
+                            n.B, n.P, (int)n.C, (int)n.groups, act, n.dtype, n.param_dtype, address(ws), (size_t)ws.numel(), n.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(Result(std::move(out[0])), Result(std::move(out[1])), Result(std::move(out[2])));
+}
+
+// a list's or a tuple's tensors, contiguous and all on one device, and the outputs beside them
+struct Gradients {
+    std::vector<hdqt_tensor_t> rows;
+    const at::Tensor* first = nullptr;
+    Gradients(PyObject* grads, PyObject* out)
+    {
+        auto size = [](PyObject* o) { return PyList_CheckExact(o) ? PyList_GET_SIZE(o) : PyTuple_CheckExact(o) ? PyTuple_GET_SIZE(o) : -1; };
+        auto item = [](PyObject* o, Py_ssize_t k) { return PyList_CheckExact(o) ? PyList_GET_ITEM(o, k) : PyTuple_GET_ITEM(o, k); };
+        const Py_ssize_t n = size(grads);
+        if (n < 1 || (out != Py_None && size(out) != n)) throw Other();
+        rows.reserve((size_t)n);
+        for (Py_ssize_t k = 0; k < n; ++k) {
+            const at::Tensor& g = on_device(item(grads, k));
+            const at::Tensor& o = out == Py_None ? g : on_device(item(out, k));
+            if (!first) first = &g;
+            if (!g.is_contiguous() || g.device() != first->device()) throw Other();
+            if (&o != &g && (!o.is_contiguous() || o.device() != g.device() || o.scalar_type() != g.scalar_type() || o.sizes() != g.sizes()))
+                throw Other();
+            rows.push_back({address(g), address(o), g.numel(), type_of(g), 0});
+        }
+    }
+};
+
+PyObject* norm_of(const Gradients& g, int64_t kind, bool clip, float max_norm, float eps)
+{
+    void* stream = stream_of(*g.first);
+    at::Tensor norm = fresh({}, at::kFloat, *g.first), ws = bytes(lib.clip_workspace_size(g.rows.data(), (int64_t)g.rows.size()), *g.first);
+    const int rc = unlocked([&] {
+        return clip ? lib.clip(g.rows.data(), (int64_t)g.rows.size(), max_norm, eps, (int)kind, (float*)address(norm), address(ws),
+                               (size_t)ws.numel(), stream)
+                    : lib.grad_norm(g.rows.data(), (int64_t)g.rows.size(), (int)kind, (float*)address(norm), address(ws), (size_t)ws.numel(),
+                                    stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return THPVariable_Wrap(std::move(norm));
+}
+
+// grad_norm(grads, kind) -> norm
+PyObject* grad_norm(PyObject* const* a) { return norm_of(Gradients(a[0], Py_None), integer(a[1]), false, 0.0f, 0.0f); }
+
+// clip_grad_norm(grads, out | None, max_norm, eps, kind) -> norm
+PyObject* clip_grad_norm(PyObject* const* a)
+{
+    return norm_of(Gradients(a[0], a[1]), integer(a[4]), true, (float)number(a[2]), (float)number(a[3]));
+}
+
 // What a function may throw (a call of another form; whatever an allocation or a tensor without
 // memory of its own raises, which the other way raises again) ends here.  So do the interpreter's errors that
 // only say that a member is missing or no number; any other (an interrupt or a time limit's exception out of
@@ -436,6 +713,17 @@ PyObject* bind(PyObject*, PyObject* args)
     find(l.bwd_masked, "hdqt_layer_bwd_masked");
     find(l.conv_bwd, "hdqt_conv_bwd");
     find(l.conv_bwd_masked, "hdqt_conv_bwd_masked");
+    find(l.xent_fwd_workspace_size, "hdqt_xent_fwd_workspace_size");
+    find(l.xent_bwd_workspace_size, "hdqt_xent_bwd_workspace_size");
+    find(l.xent_fwd, "hdqt_xent_fwd");
+    find(l.xent_bwd, "hdqt_xent_bwd");
+    find(l.xent_step, "hdqt_xent_step");
+    find(l.norm_workspace_size, "hdqt_groupnorm_workspace_size");
+    find(l.norm_fwd, "hdqt_groupnorm_fwd");
+    find(l.norm_bwd, "hdqt_groupnorm_bwd");
+    find(l.clip_workspace_size, "hdqt_clip_grad_norm_workspace_size");
+    find(l.grad_norm, "hdqt_grad_norm");
+    find(l.clip, "hdqt_clip_grad_norm");
     if (!all) return PyErr_Format(PyExc_ImportError, "%s lacks functions of include/hdqt.h", path);
     Py_INCREF(device);
     Py_INCREF(stream);
@@ -449,7 +737,9 @@ PyObject* bind(PyObject*, PyObject* args)
 PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, nullptr},
     HDQT_ENTRY(quantize, 6), HDQT_ENTRY(gemm, 14), HDQT_ENTRY(layer_step, 9), HDQT_ENTRY(layer_fwd, 8),
-    HDQT_ENTRY(layer_bwd, 10), HDQT_ENTRY(conv_fwd, 7), HDQT_ENTRY(conv_bwd, 10),
+    HDQT_ENTRY(layer_bwd, 10), HDQT_ENTRY(conv_fwd, 7), HDQT_ENTRY(conv_bwd, 10), HDQT_ENTRY(xent_fwd, 6), HDQT_ENTRY(xent_step, 7),
+    HDQT_ENTRY(xent_bwd, 9), HDQT_ENTRY(groupnorm_fwd, 6), HDQT_ENTRY(groupnorm_bwd, 8), HDQT_ENTRY(grad_norm, 2),
+    HDQT_ENTRY(clip_grad_norm, 5),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -85,7 +85,10 @@ bool plan_clip(F bytes, int64_t count, ClipPlan* plan)
 hipError_t launch_clip_norm(const ClipTable& t, bool largest, double* parts, hipStream_t stream);
 hipError_t launch_clip_finish(const double* parts, uint32_t pieces, bool largest, float max_norm, float eps, float* norm,
                               float* scale, hipStream_t stream);
-hipError_t launch_clip_scale(const ClipTable& t, const float* scale, hipStream_t stream);
+// whether the product's workgroups add the pieces' sums up themselves; else launch_clip_finish goes before
+inline bool clip_scales_alone(uint32_t pieces) { return pieces > 0 && pieces <= 2048; }
+hipError_t launch_clip_scale(const ClipTable& t, const double* parts, uint32_t pieces, bool largest, float max_norm, float eps,
+                             float* norm, const float* scale, hipStream_t stream);
 
 // ---- groupnorm.hip ----
 
