@@ -230,7 +230,7 @@ static int run_xent(hdqt::XentArgs a, bool forward, bool backward, void* workspa
     if (off(workspace, 256)) return HDQT_EALIGN;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
-    if (forward) e = hdqt::launch_xent_fwd(a, workspace, st);
+    if (forward) e = hdqt::launch_xent_fwd(a, workspace, backward, st);
     if (backward && e == hipSuccess) e = hdqt::launch_xent_bwd(a, workspace, forward, st);
     return e == hipSuccess ? HDQT_OK : hip_fail(e);
 }

@@ -3,8 +3,9 @@
 //
 // An operand lies in memory with its contraction along the rows (kAlong) or down them (kDown); both ways come to LDS by loads
 // that write there directly, 16 bytes a lane, and neither needs a copy in another order: fragments of kDown are read by
-// the transposing LDS reads of this chip.  fp32 operands are three bfloat16 matrices (planes) that add up to them, 8
-// bits each, and the product the six products of planes that are not below 2^-24 of the whole, smallest first.
+// the transposing LDS reads of this chip.  fp32 operands (P = 3) are three bfloat16 matrices, planes, that add up to them, 8
+// bits each, and the product is the six products of planes that are not below 2^-24 of the whole, smallest first; a stage
+// holds all planes, so that six products share the loads and the LDS reads of six planes.
 #pragma once
 #include "train.hpp"
 
@@ -15,40 +16,36 @@ namespace bf16 {
 
 enum Mode { kAlong, kDown };
 
-// An operand in memory, bfloat16: rows `step` elements apart, 16-byte aligned with step a multiple of 8, and so is what a row
-// holds (zeros behind the end, where there is padding).  kAlong: a row is a line of the product; kDown: a line is a column.
+// An operand in memory, bfloat16: rows `step` elements apart, 16-byte aligned with step a multiple of 8.
+// One plane: what a row holds is a multiple of 8 (zeros behind the end, where there is padding).
+// Three: 32 codes of a plane stand together, [row][column / 32][plane][column % 32], and a row is a multiple of 32 columns.
+// kAlong: a row is a line of the product; kDown: a line is a column.
 struct Side {
     const uint16_t* p;
-    int64_t step, plane;            // elements from a row, from a plane, to the next
+    int64_t step;
 };
 
 struct Args {
     Side A, B;
     int64_t RA, RB, D;              // lines of A, of B; contraction
-    int terms;                      // 1, or 6 products of planes
     uint32_t n_at, n_bt, tiles, per_xcd;
     Divisor group, out_tiles;
-    uint32_t stages, part_stages, parts;        // of 64 along the contraction
+    uint32_t stages, part_stages, parts;        // of stage_of(P) along the contraction
 };
 
 constexpr uint32_t kOutside = 0x80000000u;
-constexpr int kStage = 64;          // of the contraction
+constexpr int stage_of(int planes) { return planes == 1 ? 64 : 32; }
 
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-// planes of the six products, smallest first
-__device__ __forceinline__ int plane_a(int term) { return (0x201100 >> (4 * (5 - term))) & 3; }
-__device__ __forceinline__ int plane_b(int term) { return (0x021010 >> (4 * (5 - term))) & 3; }
-
-inline Args plan(const Side& A, const Side& B, int64_t RA, int64_t RB, int64_t D, bool planes, int ta, int tb, uint32_t parts)
+inline Args plan(const Side& A, const Side& B, int64_t RA, int64_t RB, int64_t D, int planes, int ta, int tb, uint32_t parts)
 {
     Args g{};
-    g.A = A; g.B = B; g.RA = RA; g.RB = RB; g.D = D; g.terms = planes ? 6 : 1;
+    g.A = A; g.B = B; g.RA = RA; g.RB = RB; g.D = D;
     g.n_at = (uint32_t)((RA + ta - 1) / ta); g.n_bt = (uint32_t)((RB + tb - 1) / tb);
-    g.stages = (uint32_t)((D + kStage - 1) / kStage);
+    g.stages = (uint32_t)((D + stage_of(planes) - 1) / stage_of(planes));
     g.part_stages = (g.stages + parts - 1) / parts;
     g.parts = (g.stages + g.part_stages - 1) / g.part_stages;
     g.tiles = g.n_at * g.n_bt * g.parts;
@@ -80,18 +77,23 @@ __device__ __forceinline__ Place place_of(const Args& g)
     return p;
 }
 
-// One operand of a workgroup: T lines of it, brought by WAVES waves.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const uint16_t* from, int64_t elements)
+{
+    const int64_t bytes = 2 * elements;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(from), 0,
+                                             bytes <= 0 ? 0 : bytes < (int64_t)kOutside ? (int)bytes : (int)(kOutside - 1), 0x00020000);
+}
+
+// One operand of a workgroup, T lines of it, brought by WAVES waves: a stage to LDS.
 //
-// In LDS a stage is T rows of 64 codes (kAlong) or 64 rows of T (kDown), and a row's 16-byte pieces are turned by the row's
+// One plane: T rows of 64 codes (kAlong) or 64 rows of T (kDown), and a row's 16-byte pieces are turned by the row's
 // number, so that what a fragment's reads touch together lies in different banks.
-template <int MODE, int T, int WAVES>
+template <int P, int MODE, int T, int WAVES>
 struct Panel {
-    static constexpr int kRowBytes = MODE == kAlong ? 2 * kStage : 2 * T;
-    static constexpr int kPieces = kRowBytes / 16;
+    static constexpr int kStage = 64, kRowBytes = MODE == kAlong ? 2 * kStage : 2 * T, kPieces = kRowBytes / 16;
     static constexpr int kBytes = 2 * kStage * T;
     static constexpr int kLoads = kBytes / (1024 * WAVES);          // of a wave, 1 KB each
-    static_assert(kLoads >= 1 && kPieces >= 8 && 1024 % kRowBytes == 0, "a load is whole rows");
-    static constexpr int kRowsOfLoad = 1024 / kRowBytes;
+    static_assert(P == 1 && kLoads >= 1 && kPieces >= 8 && 1024 % kRowBytes == 0, "a load is whole rows");
 
     static __device__ __forceinline__ int turn(int row)
     {
@@ -100,19 +102,18 @@ struct Panel {
     }
 
     uint32_t off[kLoads];           // of a lane's piece, from the stage's first byte
-    int64_t lines_left, d;
+    int64_t lines_left, d, step;
     const uint16_t* base;
-    int64_t step, plane;
     int col[kLoads > 1 ? 2 : 1];    // kAlong: first code of a lane's piece in even and odd loads
 
     __device__ __forceinline__ Panel(const Side& s, int64_t lines, int64_t line0, int64_t D, int wave, int lane)
     {
-        step = s.step; plane = s.plane; d = D;
+        step = s.step; d = D;
         lines_left = lines - line0;
         base = s.p + (MODE == kAlong ? line0 * s.step : line0);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int row = (wave * kLoads + j) * kRowsOfLoad + lane / kPieces;
+            const int row = (wave * kLoads + j) * (1024 / kRowBytes) + lane / kPieces;
             const int piece = (lane % kPieces) ^ turn(row);
             off[j] = (uint32_t)row * (uint32_t)step * 2 + 16 * piece;
             if (MODE == kAlong) col[j & (kLoads > 1)] = 8 * piece;          // (turns repeat every 16 rows: two loads)
@@ -120,17 +121,11 @@ struct Panel {
         }
     }
 
-    // stage `s` of plane `pl` to LDS
-    template <class L>
-    __device__ __forceinline__ void bring(L* lds, uint32_t s, int pl, int wave) const
+    __device__ __forceinline__ void bring(uint8_t* lds, uint32_t s, int wave) const
     {
         const int64_t at = (int64_t)s * kStage;
-        const uint16_t* from = base + pl * plane + (MODE == kAlong ? at : at * step);
-        // elements from here to the operand's end
         const int64_t rows = MODE == kAlong ? lines_left : d - at, width = MODE == kAlong ? d - at : lines_left;
-        const int64_t bytes = 2 * ((rows - 1) * step + (width + 7) / 8 * 8);
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<uint16_t*>(from), 0, bytes <= 0 ? 0 : bytes < (int64_t)kOutside ? (int)bytes : (int)(kOutside - 1), 0x00020000);
+        const __amdgpu_buffer_rsrc_t rs = range_of(base + (MODE == kAlong ? at : at * step), (rows - 1) * step + (width + 7) / 8 * 8);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             uint32_t o = off[j];
@@ -141,9 +136,57 @@ struct Panel {
     }
 };
 
+// Three planes, 32 of the contraction: T rows of 192 bytes (kAlong; neighbours of two pieces change places every four rows) or
+// 32 rows of 6 T (kDown; blocks of 32 columns are turned by the row's number).
+template <int MODE, int T, int WAVES>
+struct Panel<3, MODE, T, WAVES> {
+    static constexpr int kStage = 32, kPieces = MODE == kAlong ? 12 : 12 * T / 32, kBytes = 192 * T;
+    static constexpr int kLoads = kBytes / (1024 * WAVES);
+    static_assert(kLoads >= 1 && kLoads * 1024 * WAVES == kBytes && T % 128 == 0, "whole loads, four blocks of columns");
+
+    uint32_t off[kLoads];
+    int64_t rows_left, step;        // kDown: rows of the whole contraction
+    const uint16_t* base;
+    int64_t width;                  // of a row from the base on
+
+    __device__ __forceinline__ Panel(const Side& s, int64_t lines, int64_t line0, int64_t D, int wave, int lane)
+    {
+        step = s.step;
+        rows_left = MODE == kAlong ? lines - line0 : D;
+        base = s.p + (MODE == kAlong ? line0 * s.step : 3 * line0);
+        width = MODE == kAlong ? step : step - 3 * line0;
+        const int64_t room = 3 * ((lines - line0 + 31) / 32 * 32);      // (kDown: the columns that there are)
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int g = (wave * kLoads + j) * 64 + lane, row = g / kPieces, at = g % kPieces;
+            const int piece = MODE == kAlong ? at ^ ((row >> 2) & 1) : ((at / 12) ^ (row & 3)) * 12 + at % 12;
+            off[j] = (uint32_t)row * (uint32_t)step * 2 + 16 * piece;
+            if (MODE == kDown && 8 * piece >= room) off[j] = kOutside;
+        }
+    }
+
+    __device__ __forceinline__ void bring(uint8_t* lds, uint32_t s, int wave) const
+    {
+        const int64_t at = (int64_t)s * kStage;
+        const __amdgpu_buffer_rsrc_t rs = MODE == kAlong ? range_of(base + 3 * at, (rows_left - 1) * step + width - 3 * at)
+                                                         : range_of(base + at * step, (rows_left - at - 1) * step + width);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rs, (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + j) * 1024), 16, off[j], 0, 0, 0);
+    }
+};
+
+__device__ __forceinline__ v8b read_turned(const uint8_t* lds, int row_bytes)
+{
+    typedef __attribute__((address_space(3))) v4s* local;
+    const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((local)lds), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((local)(lds + 4 * row_bytes));
+    return __builtin_bit_cast(v8b, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
 // Fragments of a wave's lines: N blocks of 32, sixteen of the contraction at a time (lane: line lane % 32, the eight codes
-// from 8 (lane / 32) on).
-template <int MODE, int T, int N>
+// from 8 (lane / 32) on).  kDown: sixteen lanes read four rows of 16 codes, and lane i gets column i.
+template <int P, int MODE, int T, int N>
 struct Fragments {
     uint32_t at[MODE == kAlong ? 4 : N];
     __device__ __forceinline__ Fragments(int line0, int lane)
@@ -153,9 +196,8 @@ struct Fragments {
 #pragma unroll
             for (int q = 0; q < 4; ++q) at[q] = row * 128 + 16 * ((2 * q + (lane >> 5)) ^ ((row >> 1) & 7));
         } else {
-            // sixteen lanes read four rows of 16 codes; lane i gets column i
             const int k = 8 * (lane >> 5) + ((lane >> 2) & 3);
-            const int turn = Panel<MODE, T, 1>::turn(k);
+            const int turn = Panel<P, MODE, T, 1>::turn(k);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int column = line0 + 32 * i + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
@@ -163,75 +205,114 @@ struct Fragments {
             }
         }
     }
-    template <class L>
-    __device__ __forceinline__ v8b read(const L* lds, int i, int q) const
+    __device__ __forceinline__ v8b read(const uint8_t* lds, int i, int q, int) const
     {
-        if constexpr (MODE == kAlong) {
-            return *reinterpret_cast<const v8b*>(lds + at[q] + 4096 * i);
-        } else {
-            typedef __attribute__((address_space(3))) v4s* local;
-            const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((local)(lds + at[i] + 32 * T * q));
-            const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((local)(lds + at[i] + 32 * T * q + 8 * T));
-            return __builtin_bit_cast(v8b, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
+        if constexpr (MODE == kAlong) return *reinterpret_cast<const v8b*>(lds + at[q] + 4096 * i);
+        else return read_turned(lds + at[i] + 32 * T * q, 2 * T);
     }
 };
 
-// The part's sums: acc[i][j], block i of the wave's lines of A and j of B.  The two stages in LDS are objects of their own, so
-// that the compiler knows which loads a read must wait for.  A wave waits for its own part of a stage, and for its own
-// reads of the buffer that is brought next, in front of the barrier.
-template <int MA, int MB, int TA, int TB, int WA, int WB, class LA, class LB>
-__device__ __forceinline__ void multiply(const Args& g, const Place& p, LA* a0, LA* a1, LB* b0, LB* b1, int wave, int lane,
-                                         v16f (&acc)[TA / WA / 32][TB / WB / 32])
-{
-    constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
-    const Panel<MA, TA, WA * WB> pa(g.A, g.RA, (int64_t)p.at * TA, g.D, wave, lane);
-    const Panel<MB, TB, WA * WB> pb(g.B, g.RB, (int64_t)p.bt * TB, g.D, wave, lane);
-    const Fragments<MA, TA, NA> fa((wave / WB) * (TA / WA), lane);
-    const Fragments<MB, TB, NB> fb((wave % WB) * (TB / WB), lane);
-    uint32_t s = 0;                 // what is brought next
-    int term = 0;
-    auto bring = [&](LA* a, LB* b) {
-        const bool one = g.terms == 1;
-        pa.bring(a, p.first + s, one ? 0 : plane_a(term), wave);
-        pb.bring(b, p.first + s, one ? 0 : plane_b(term), wave);
-        if (++s == p.n) { s = 0; ++term; }
-    };
-    auto arrived = [] {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);         // vmcnt(0) lgkmcnt(0), as the compiler's own bookkeeping takes it
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    };
-    auto products = [&](const LA* a, const LB* b) {
+template <int MODE, int T, int N>
+struct Fragments<3, MODE, T, N> {
+    uint32_t at[MODE == kAlong ? 1 : N];
+    __device__ __forceinline__ Fragments(int line0, int lane)
+    {
+        if constexpr (MODE == kAlong) {
+            const int row = line0 + (lane & 31);
+            at[0] = row * 192 + 16 * ((lane >> 5) ^ ((row >> 2) & 1));
+        } else {
+            const int m = (lane >> 2) & 3, k = 8 * (lane >> 5) + m;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            __builtin_amdgcn_sched_barrier(0);
-            v8b x[NA], y[NB];
-#pragma unroll
-            for (int j = 0; j < NB; ++j) y[j] = fb.read(b, j, q);
-#pragma unroll
-            for (int i = 0; i < NA; ++i) x[i] = fa.read(a, i, q);
-#pragma unroll
-            for (int i = 0; i < NA; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], y[j], acc[i][j], 0, 0, 0);
-        }
-    };
-    const uint32_t total = p.n * (uint32_t)g.terms;
-    bring(a0, b0);
-    for (uint32_t done = 0; done < total; done += 2) {
-        arrived();
-        if (done + 1 < total) bring(a1, b1);
-        products(a0, b0);
-        if (done + 1 < total) {
-            arrived();
-            if (done + 2 < total) bring(a0, b0);
-            products(a1, b1);
+            for (int i = 0; i < N; ++i)
+                at[i] = k * 6 * T + 192 * (((line0 >> 5) + i) ^ m) + 2 * (16 * ((lane >> 4) & 1) + 4 * (lane & 3));
         }
     }
-    // (what follows may write where the last stage lies)
-    arrived();
+    __device__ __forceinline__ v8b read(const uint8_t* lds, int i, int q, int plane) const
+    {
+        if constexpr (MODE == kAlong) return *reinterpret_cast<const v8b*>(lds + at[0] + 6144 * i + 32 * q + 64 * plane);
+        else return read_turned(lds + at[i] + 96 * T * q + 64 * plane, 6 * T);
+    }
+};
+
+// A wave's loads but the last FLYING have arrived, and all it reads from LDS; then every wave's.  (The wait is one that the
+// compiler's own bookkeeping takes in.)
+template <int FLYING>
+__device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (FLYING & 15) | (FLYING >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <int S>
+struct Stages {
+    uint8_t *a[S], *b[S];
+};
+
+// The part's sums: acc[i][j], block i of the wave's lines of A and j of B.  S stages in LDS, objects of their own, so that the
+// compiler knows which loads a read must wait for.  A wave waits for its own part of a stage, and for its own reads of the
+// buffer that is brought next, in front of the barrier.
+template <int P, int MA, int MB, int TA, int TB, int WA, int WB, int S, int NA, int NB>
+__device__ __forceinline__ void multiply(const Args& g, const Place& p, const Stages<S>& lds, int wave, int lane,
+                                         v16f (&acc)[NA][NB])
+{
+#ifdef __HIP_DEVICE_COMPILE__       // (the host's pass has no use for the body, nor all of its builtins)
+    static_assert(NA == TA / WA / 32 && NB == TB / WB / 32, "a wave's blocks");
+    typedef Panel<P, MA, TA, WA * WB> PanelA;
+    typedef Panel<P, MB, TB, WA * WB> PanelB;
+    constexpr int kLoads = PanelA::kLoads + PanelB::kLoads;
+    const PanelA pa(g.A, g.RA, (int64_t)p.at * TA, g.D, wave, lane);
+    const PanelB pb(g.B, g.RB, (int64_t)p.bt * TB, g.D, wave, lane);
+    const Fragments<P, MA, TA, NA> fa((wave / WB) * (TA / WA), lane);
+    const Fragments<P, MB, TB, NB> fb((wave % WB) * (TB / WB), lane);
+    auto bring = [&](uint32_t s, uint8_t* a, uint8_t* b) {
+        pa.bring(a, p.first + s, wave);
+        pb.bring(b, p.first + s, wave);
+    };
+    auto products = [&](const uint8_t* a, const uint8_t* b) {
+#pragma unroll
+        for (int q = 0; q < stage_of(P) / 16; ++q) {
+            __builtin_amdgcn_sched_barrier(0);
+            v8b x[NA][P], y[NB][P];
+#pragma unroll
+            for (int k = P - 1; k >= 0; --k) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j) y[j][k] = fb.read(b, j, q, k);
+#pragma unroll
+                for (int i = 0; i < NA; ++i) x[i][k] = fa.read(a, i, q, k);
+            }
+            auto term = [&](int ka, int kb) {
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][ka], y[j][kb], acc[i][j], 0, 0, 0);
+            };
+            if constexpr (P == 3) {
+                term(2, 0);
+                term(0, 2);
+                term(1, 1);
+                term(1, 0);
+                term(0, 1);
+            }
+            term(0, 0);
+        }
+    };
+    // (stages behind the last are brought as well, out of range or not used: the waits stay the same)
+#pragma unroll
+    for (int u = 0; u + 1 < S; ++u) bring(u, lds.a[u], lds.b[u]);
+    for (uint32_t s = 0;;) {
+#pragma unroll
+        for (int u = 0; u < S; ++u) {
+            wait_and_meet<(S - 2) * kLoads>();
+            bring(s + S - 1, lds.a[(u + S - 1) % S], lds.b[(u + S - 1) % S]);
+            products(lds.a[u], lds.b[u]);
+            if (++s == p.n) goto done;
+        }
+    }
+done:
+    wait_and_meet<0>();             // (what follows may write where a stage lies)
+#endif
 }
 
 } // namespace bf16

@@ -126,7 +126,8 @@ struct XentArgs {
     void *dX, *dW, *dbias;              // [M, K], [K, N], [N]; any may be null
 };
 size_t xent_workspace(const XentArgs& a, bool backward);
-hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, hipStream_t stream);
+// backward: the backward pass will run in the same workspace
+hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hipStream_t stream);
 // forward: the forward pass has just run in the same workspace
 hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hipStream_t stream);
 

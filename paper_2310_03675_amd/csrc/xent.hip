@@ -54,7 +54,7 @@ struct PackArgs {
     const void* src;
     int64_t rows, cols, ld;
     uint16_t* dst;
-    int64_t step, plane;
+    int64_t step;
 };
 
 __device__ __forceinline__ void split(float x, uint32_t (&part)[3])
@@ -71,11 +71,11 @@ template <int DT>
 __global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs a)
 {
     const int64_t c = 2 * ((int64_t)blockIdx.x * kThreads + threadIdx.x);
-    if (c >= a.step) return;
+    if (c >= (DT == kBf16 ? a.step : a.step / 3)) return;
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const int64_t from = row * a.ld + c;
         const float x = c < a.cols ? load_as<DT>(a.src, from) : 0.0f, y = c + 1 < a.cols ? load_as<DT>(a.src, from + 1) : 0.0f;
-        uint32_t* to = reinterpret_cast<uint32_t*>(a.dst + row * a.step + c);
+        uint32_t* to = reinterpret_cast<uint32_t*>(a.dst + row * a.step + (DT == kBf16 ? c : c / 32 * 96 + c % 32));
         if (DT == kBf16) {
             *to = __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xFFFF0000u);
         } else {
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs a)
             split(x, p);
             split(y, q);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) to[k * (a.plane / 2)] = p[k] | q[k] << 16;
+            for (int k = 0; k < 3; ++k) to[16 * k] = p[k] | q[k] << 16;
         }
     }
 }
@@ -101,7 +101,8 @@ struct RowArgs {
     const float *saved, *dloss;
     int each;                           // rows have a factor of their own
     uint16_t* dz;                       // [M][step], zeros behind the classes
-    int64_t step, plane;
+    int64_t step;
+    float* column;                      // [tiles of rows][classes]: dz's sums over a tile's rows; null: not wanted
 };
 
 __device__ __forceinline__ float larger_half(float v)
@@ -115,15 +116,36 @@ __device__ __forceinline__ float sum_halves(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// over lanes 0 .. 31 and over lanes 32 .. 63, in every one of them
+__device__ __forceinline__ float sum_of_32(float v)
+{
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true));        // lane ^ 1
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, true));        // lane ^ 2
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, true));       // the other four of eight
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, true));       // the other eight of sixteen
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// S stages of P planes' operands in LDS, each an object of its own
+#define HDQT_STAGES(P, S, TA, TB)                                                                            \
+    constexpr int kA = (P == 1 ? 128 : 192) * TA, kB = (P == 1 ? 128 : 192) * TB;                            \
+    __shared__ __align__(1024) uint8_t a0[kA], a1[kA], a2[S > 2 ? kA : 16], b0[kB], b1[kB], b2[S > 2 ? kB : 16]; \
+    bf16::Stages<S> stages;                                                                                  \
+    stages.a[0] = a0; stages.a[1] = a1; stages.b[0] = b0; stages.b[1] = b1;                                  \
+    if constexpr (S > 2) { stages.a[S - 1] = a2; stages.b[S - 1] = b2; }
+
 // Lines of A are classes (W, read down), lines of B rows (X): a lane then holds sums of one row of the logits, and the
 // maximum and the sum over classes stay inside it but for one exchange between the wave's halves.
-template <bool GRAD, bool PLANES, int TA, int TB, int WA, int WB>
+template <bool GRAD, int P, int TA, int TB, int WA, int WB, int S>
 __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2, 2))) void xent_logits_kernel(bf16::Args g, RowArgs r)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
-    __shared__ __align__(1024) uint8_t a0[128 * TA], a1[128 * TA], b0[128 * TB], b1[128 * TB];
+    constexpr bool kExact = P == 3;
+    HDQT_STAGES(P, S, TA, TB);
     __shared__ __align__(16) float bias[TA];
-    __shared__ float2 halves[WA][TB];
+    __shared__ float2 halves[GRAD ? 1 : WA][GRAD ? 1 : TB];
+    __shared__ float columns[GRAD ? WB : 1][GRAD ? TA : 1];
     const bf16::Place p = bf16::place_of(g);
     if (!p.there) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -132,7 +154,7 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2,
         bias[t] = c >= r.classes ? -INFINITY : r.bias ? any_load(r.bias, r.bias_dtype, c) : 0.0f;
     }
     v16f acc[NA][NB] = {};
-    bf16::multiply<kDown, kAlong, TA, TB, WA, WB>(g, p, a0, a1, b0, b1, wave, lane, acc);
+    bf16::multiply<P, kDown, kAlong, TA, TB, WA, WB, S>(g, p, stages, wave, lane, acc);
 
     const int class0 = (wave / WB) * (TA / WA), row0 = (wave % WB) * (TB / WB);
     auto column = [&](auto jj) {
@@ -172,7 +194,7 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
             for (int i = 0; i < NA; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += exp_of<PLANES>(acc[i][j][e] - base);
+                for (int e = 0; e < 16; ++e) sum += exp_of<kExact>(acc[i][j][e] - base);
             sum = sum_halves(sum);
             if (lane < 32) halves[wave / WB][row0 + 32 * j + lane] = make_float2(top, sum);
         } else {
@@ -182,7 +204,7 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
             for (int i = 0; i < NA; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] = exp_of<PLANES>(acc[i][j][e] - base);
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = exp_of<kExact>(acc[i][j][e] - base);
             if (any) {
 #pragma unroll
                 for (int i = 0; i < NA; ++i)
@@ -190,22 +212,26 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2,
                     for (int e = 0; e < 16; ++e)
                         if (at == 32 * i + 8 * (e >> 2) + (e & 3)) acc[i][j][e] -= 1.0f;
             }
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = counted ? acc[i][j][e] * each : 0.0f;
             if (there) {
-                uint16_t* to = r.dz + row * r.step + (int64_t)p.at * TA + class0 + 4 * (lane >> 5);
+                uint16_t* to = r.dz + row * r.step + P * ((int64_t)p.at * TA + class0) + 4 * (lane >> 5);
 #pragma unroll
                 for (int i = 0; i < NA; ++i)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         float v[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = counted ? acc[i][j][4 * q + e] * each : 0.0f;
-                        if constexpr (PLANES) {
+                        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+                        if constexpr (P == 3) {
                             uint32_t s[4][3];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) split(v[e], s[e]);
 #pragma unroll
                             for (int k = 0; k < 3; ++k)
-                                *reinterpret_cast<uint2*>(to + k * r.plane + 32 * i + 8 * q) =
+                                *reinterpret_cast<uint2*>(to + 96 * i + 32 * k + 8 * q) =
                                     make_uint2(s[0][k] | s[1][k] << 16, s[2][k] | s[3][k] << 16);
                         } else {
                             *reinterpret_cast<uint2*>(to + 32 * i + 8 * q) =
@@ -226,6 +252,25 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2,
             float2 v = halves[0][t];
             for (int w = 1; w < WA; ++w) join(v.x, v.y, halves[w][t].x, halves[w][t].y);
             r.pairs[(int64_t)p.at * r.M + row] = v;
+        }
+    } else if (r.column) {
+        // a class's sum over the tile's rows: this wave's, over the lanes of either half, then the waves side by side
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float s = acc[i][0][e];
+                if constexpr (NB > 1) s += acc[i][1][e];
+                s = sum_of_32(s);
+                if ((lane & 31) == 0) columns[wave % WB][class0 + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)] = s;
+            }
+        __syncthreads();
+        for (int t = threadIdx.x; t < TA; t += 64 * WA * WB) {
+            const int64_t c = (int64_t)p.at * TA + t;
+            if (c >= r.classes) continue;
+            float s = columns[0][t];
+            for (int w = 1; w < WB; ++w) s += columns[w][t];
+            r.column[(int64_t)p.bt * r.classes + c] = s;
         }
     }
 }
@@ -279,16 +324,16 @@ __device__ __forceinline__ void each_sum(v16f (&acc)[NA][NB], int64_t lines, int
     }
 }
 
-template <int MODE, int TA, int TB, int WA, int WB>
+template <int P, int MODE, int TA, int TB, int WA, int WB, int S>
 __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2, 2))) void xent_gradient_kernel(bf16::Args g, OutArgs o)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
-    __shared__ __align__(1024) uint8_t a0[128 * TA], a1[128 * TA], b0[128 * TB], b1[128 * TB];
+    HDQT_STAGES(P, S, TA, TB);
     const bf16::Place p = bf16::place_of(g);
     if (!p.there) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     v16f acc[NA][NB] = {};
-    bf16::multiply<MODE, MODE, TA, TB, WA, WB>(g, p, a0, a1, b0, b1, wave, lane, acc);
+    bf16::multiply<P, MODE, MODE, TA, TB, WA, WB, S>(g, p, stages, wave, lane, acc);
     const int64_t i0 = (int64_t)p.at * TA + (wave / WB) * (TA / WA), j0 = (int64_t)p.bt * TB + (wave % WB) * (TB / WB);
     const bool several = g.parts > 1;
     float* part = several ? o.slices + (int64_t)p.part * g.RA * g.RB : o.sums;
@@ -334,111 +379,380 @@ __global__ __launch_bounds__(kThreads) void xent_add_parts_kernel(OutArgs o, int
 
 // ---- sums over rows ----
 
-// a row's pairs joined: its log of the sum of exponentials and its loss
-__global__ __launch_bounds__(kThreads) void xent_rows_kernel(XentArgs a, const float2* pairs, int64_t tiles, const float* picked,
-                                                             float* rows)
-{
-    const int64_t row = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (row >= a.M) return;
-    float m = -INFINITY, l = 0.0f;
-    for (int64_t i = 0; i < tiles; ++i) {
-        const float2 p = pairs[i * a.M + row];
-        join(m, l, p.x, p.y);
-    }
-    const int64_t t = a.target[row];
-    // (no class left: minus infinity; a logit of plus infinity: no probabilities)
-    float lse = m == INFINITY ? NAN : l > 0.0f ? m + logf(l) : l != l ? l : m, loss = 0.0f;
-    if (t != a.ignore) {
-        if (t < 0 || t >= a.N) lse = NAN;                       // (a target that is no class: seen in the loss and the gradients)
-        const float z = t < 0 || t >= a.N ? NAN : picked[row];
-        loss = z == -INFINITY && lse == lse ? INFINITY : lse - z;
-    }
-    a.saved[row] = lse;
-    rows[row] = loss;
-}
-
-// one workgroup: the loss over all rows and a row's share in it
-__global__ __launch_bounds__(1024) void xent_total_kernel(XentArgs a, const float* rows)
+// A row's pairs joined, by `lanes` threads to a row: its log of the sum of exponentials and its loss.  Where one workgroup has
+// all rows it adds them up as well.
+struct TotalArgs {
+    int lanes;
+    int alone;
+};
+__device__ __forceinline__ void total_of(const XentArgs& a, double s, long long n)
 {
     __shared__ double sums[16];
     __shared__ long long counts[16];
-    double s = 0.0;
-    long long n = 0;
-    for (int64_t i = threadIdx.x; i < a.M; i += 1024) {
-        s += (double)rows[i];
-        n += a.target[i] != a.ignore;
-    }
     s = wave_sum(s);
     n = wave_sum(n);
     if ((threadIdx.x & 63) == 0) { sums[threadIdx.x >> 6] = s; counts[threadIdx.x >> 6] = n; }
     __syncthreads();
     if (threadIdx.x) return;
-    for (int w = 1; w < 16; ++w) { s += sums[w]; n += counts[w]; }
+    for (uint32_t w = 1; w < blockDim.x / kWave; ++w) { s += sums[w]; n += counts[w]; }
     const double share = a.reduction == kMean ? 1.0 / (double)(n > 0 ? n : 1) : 1.0;
     a.saved[a.M] = (float)share;
     if (a.reduction != kNone) a.loss[0] = (float)(s * share);
 }
 
-// db of a piece's classes: a column's sum, eight threads to two columns
-template <bool PLANES>
-__global__ __launch_bounds__(kThreads) void xent_dbias_kernel(RowArgs r, void* dbias, OutArgs o)
+__global__ __launch_bounds__(1024) void xent_rows_kernel(XentArgs a, const float2* pairs, int64_t tiles, const float* picked,
+                                                         float* rows, TotalArgs t)
 {
-    __shared__ float2 sums[8][32];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t col = 2 * ((int64_t)blockIdx.x * 32 + x);
-    float2 s = make_float2(0.0f, 0.0f);
-    if (col < r.classes)
-        for (int64_t i = y; i < r.M; i += 8)
-#pragma unroll
-            for (int k = PLANES ? 2 : 0; k >= 0; --k) {
-                const uint32_t v = *reinterpret_cast<const uint32_t*>(r.dz + k * r.plane + i * r.step + col);
-                s.x += from_bf16(v & 0xFFFFu);
-                s.y += __uint_as_float(v & 0xFFFF0000u);
+    const int lane = threadIdx.x & (t.lanes - 1), per = blockDim.x / t.lanes;
+    double sum = 0.0;
+    long long count = 0;
+    for (int64_t row0 = (int64_t)blockIdx.x * per; row0 < a.M; row0 += (int64_t)gridDim.x * per) {
+        const int64_t row = row0 + threadIdx.x / t.lanes;
+        const bool there = row < a.M;
+        float m = -INFINITY, l = 0.0f;
+        if (there)
+#pragma unroll 4
+            for (int64_t i = lane; i < tiles; i += t.lanes) {
+                const float2 p = pairs[i * a.M + row];
+                join(m, l, p.x, p.y);
             }
+        for (int k = 1; k < t.lanes; k <<= 1) {
+            const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
+            join(m, l, om, ol);
+        }
+        if (!there || lane) continue;
+        const int64_t target = a.target[row];
+        // (no class left: minus infinity; a logit of plus infinity: no probabilities)
+        float lse = m == INFINITY ? NAN : l > 0.0f ? m + logf(l) : l != l ? l : m, loss = 0.0f;
+        if (target != a.ignore) {
+            const bool none = target < 0 || target >= a.N;          // (no class: seen in the loss and the gradients)
+            if (none) lse = NAN;
+            const float z = none ? NAN : picked[row];
+            loss = z == -INFINITY && lse == lse ? INFINITY : lse - z;
+            ++count;
+        }
+        a.saved[row] = lse;
+        if (!t.alone || a.reduction == kNone) rows[row] = loss;
+        sum += (double)loss;
+    }
+    if (t.alone) total_of(a, sum, count);
+}
+
+// one workgroup: the loss over all rows and a row's share in it
+__global__ __launch_bounds__(1024) void xent_total_kernel(XentArgs a, const float* rows)
+{
+    double s = 0.0;
+    long long n = 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < a.M; i += 1024) {
+        s += (double)rows[i];
+        n += a.target[i] != a.ignore;
+    }
+    total_of(a, s, n);
+}
+
+// db of a piece's classes: the tiles' sums of a class, sixteen threads to it
+__global__ __launch_bounds__(kThreads) void xent_dbias_kernel(const float* column, int64_t tiles, int64_t classes, void* dbias, OutArgs o)
+{
+    __shared__ float sums[16][17];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + x;
+    float s = 0.0f;
+    if (c < classes)
+#pragma unroll 4
+        for (int64_t i = y; i < tiles; i += 16) s += column[i * classes + c];
     sums[y][x] = s;
     __syncthreads();
-    if (y) return;
-    for (int w = 1; w < 8; ++w) { s.x += sums[w][x].x; s.y += sums[w][x].y; }
-    const float factor = factor_of(o);
-    for (int e = 0; e < 2; ++e) {
-        if (col + e >= r.classes) continue;
-        const float v = (e ? s.y : s.x) * factor;
-        if (o.dtype == kBf16) store_as<kBf16>(dbias, col + e, v);
-        else store_as<kF32>(dbias, col + e, v);
+    if (y || c >= classes) return;
+    for (int w = 1; w < 16; ++w) s += sums[w][x];
+    s *= factor_of(o);
+    if (o.dtype == kBf16) store_as<kBf16>(dbias, c, s);
+    else store_as<kF32>(dbias, c, s);
+}
+
+// ---- small problems: straight from the operands, in 32 bits ----
+//
+// Packing, and products whose few tiles walk along the contraction one stage after the other, are most of what a small problem
+// takes (128 x 512 x 100: 110 us, of it 13 packing, 80 in two products of one tile).  Here a workgroup of eight waves has
+// 32 x 32 outputs, the waves share the contraction, sixteen bytes or four single elements a lane straight from memory, and
+// the 32-bit matrix instructions multiply.  The logits stay in the workspace (kSmallLogits at most), and the gradients'
+// products make dz from them as they read it: three launches forward and backward.
+
+constexpr int kSmallWaves = 8, kSmallTile = 32;
+constexpr int kSmallStep = 8 * kSmallWaves;         // of the contraction: eight to a wave, four to a half of its lanes
+constexpr int kSmallAhead = 4;                      // steps whose loads are in flight
+
+struct SmallArgs {
+    float* z;                           // [M][step], null: not wanted
+    int64_t step;
+    float2* pairs;                      // [tiles of classes][M]; null: not wanted
+    float* picked;
+    uint32_t x_tiles, x_parts;          // gradients: tiles of dX, parts of its contraction; dW's tiles behind them
+    uint32_t x_across, w_across;        // tiles side by side of dX (features), of the logits and dW (classes)
+    uint32_t w_first;                   // first tile down of dW (where only db is wanted: the one with the line of ones)
+    uint32_t w_tiles, w_parts;
+    float *slices, *w_slices;           // of dX, of dW and db in parts: [part][M][K], [part][K + 1][N]
+};
+
+// four neighbours in memory, those from `left` on zero
+template <int DT, bool VEC>
+__device__ __forceinline__ void load4(const void* p, int64_t at, int64_t left, float (&v)[4])
+{
+    if constexpr (VEC) {                // (left is a multiple of four)
+        if (left <= 0) {
+            v[0] = v[1] = v[2] = v[3] = 0.0f;
+        } else if (DT == kBf16) {
+            const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + at);
+            v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xFFFF0000u);
+            v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xFFFF0000u);
+        } else {
+            const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+            v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < left ? load_as<DT>(p, at + e) : 0.0f;
     }
+}
+
+// The waves' sums of a 32 x 32 block added up: f(register, sum) for the registers of this wave, in order of the waves.
+template <class F>
+__device__ __forceinline__ void join_waves(const v16f& acc, float (*lds)[16][64], int wave, int lane, F f)
+{
+#pragma unroll
+    for (int e = 0; e < 16; ++e) lds[wave][e][lane] = acc[e];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 16 / kSmallWaves; ++k) {
+        const int e = wave * (16 / kSmallWaves) + k;
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kSmallWaves; ++w) s += lds[w][e][lane];
+        f(e, s);
+    }
+}
+
+// Lines of A are classes, of B rows, as in the large products.
+template <int DT, bool VEC>
+__global__ __launch_bounds__(64 * kSmallWaves) void xent_small_logits_kernel(XentArgs a, SmallArgs k)
+{
+    __shared__ float lds[kSmallWaves][16][64];
+    __shared__ float z[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = lane & 31, half = lane >> 5;
+    const uint32_t down = blockIdx.x / k.w_across, across = blockIdx.x - down * k.w_across;
+    const int64_t class0 = (int64_t)across * kSmallTile, row0 = (int64_t)down * kSmallTile;
+    const int64_t c = class0 + line, row = row0 + line;
+    const bool class_there = c < a.N, row_there = row < a.M;
+    v16f acc = {};
+    for (int64_t base = 8 * wave; base < a.K; base += kSmallAhead * kSmallStep) {
+        float x[kSmallAhead][4], w[kSmallAhead][4];
+#pragma unroll
+        for (int u = 0; u < kSmallAhead; ++u) {
+            const int64_t at = base + u * kSmallStep + 4 * half;
+            load4<DT, VEC>(a.X, row * a.ldx + at, row_there ? a.K - at : 0, x[u]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[u][e] = class_there && at + e < a.K ? load_as<DT>(a.W, (at + e) * a.ldw + c) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < kSmallAhead; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(w[u][e], x[u][e], acc, 0, 0, 0);
+    }
+    join_waves(acc, lds, wave, lane, [&](int e, float s) {
+        const int64_t of = class0 + 8 * (e >> 2) + 4 * half + (e & 3);
+        z[e][lane] = of >= a.N ? -INFINITY : a.bias ? s + any_load(a.bias, a.bias_dtype, of) : s;
+    });
+    __syncthreads();
+    if (wave) return;
+    const int64_t target = row_there ? a.target[row] : -1;
+    float v[16], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        v[e] = z[e][lane];
+        top = fmaxf(top, v[e]);
+        if (k.pairs && row_there && target == class0 + 8 * (e >> 2) + 4 * half + (e & 3)) k.picked[row] = v[e];
+    }
+    if (k.z && row_there)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (class0 + 8 * q + 4 * half < a.N)
+                *reinterpret_cast<float4*>(k.z + row * k.step + class0 + 8 * q + 4 * half) =
+                    make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    if (!k.pairs) return;
+    top = larger_half(top);
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum += exp_of<true>(v[e] - base);
+    sum = sum_halves(sum);
+    if (row_there && half == 0) k.pairs[(int64_t)across * a.M + row] = make_float2(top, sum);
+}
+
+// dz of a logit
+__device__ __forceinline__ float small_dz(float z, int64_t c, int64_t target, float lse, float factor)
+{
+    const float base = lse == -INFINITY ? 0.0f : lse;
+    return (exp_of<true>(z - base) - (c == target ? 1.0f : 0.0f)) * factor;
+}
+// a part of a contraction: whole steps of all waves
+struct Share {
+    int64_t begin, end;
+};
+__device__ __forceinline__ Share share_of(int64_t length, uint32_t part, uint32_t parts)
+{
+    const int64_t steps = (length + kSmallStep - 1) / kSmallStep, per = (steps + parts - 1) / parts * kSmallStep, begin = part * per;
+    return {begin < length ? begin : length, begin + per < length ? begin + per : length};
+}
+__device__ __forceinline__ float row_factor(const XentArgs& a, int64_t row)
+{
+    return a.reduction == kNone && a.dloss ? a.dloss[row] : 1.0f;
+}
+
+// dX: lines of A are rows, of B features.  dW: lines of A features, and one of ones behind them, whose products are db; of B
+// classes.
+template <int DT, bool VEC>
+__global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(XentArgs a, SmallArgs k)
+{
+    __shared__ float lds[kSmallWaves][16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = lane & 31, half = lane >> 5;
+    v16f acc = {};
+    const float factor = (a.reduction == kNone ? 1.0f : (a.dloss ? *a.dloss : 1.0f)) * a.saved[a.M];
+    if (blockIdx.x < k.x_tiles * k.x_parts) {
+        const uint32_t part = blockIdx.x / k.x_tiles, tile = blockIdx.x - part * k.x_tiles, down = tile / k.x_across;
+        const int64_t row0 = (int64_t)down * kSmallTile, f0 = (int64_t)(tile - down * k.x_across) * kSmallTile;
+        const int64_t row = row0 + line, f = f0 + line;
+        const bool row_there = row < a.M, f_there = f < a.K;
+        const int64_t target = row_there ? a.target[row] : -1;
+        const bool counted = row_there && target != a.ignore;
+        const float lse = row_there ? a.saved[row] : 0.0f, each = counted ? row_factor(a, row) : 0.0f;
+        const Share share = share_of(a.N, part, k.x_parts);
+        for (int64_t base = share.begin + 8 * wave; base < share.end; base += kSmallAhead * kSmallStep) {
+            float z[kSmallAhead][4], w[kSmallAhead][4];
+#pragma unroll
+            for (int u = 0; u < kSmallAhead; ++u) {
+                const int64_t at = base + u * kSmallStep + 4 * half;
+                load4<kF32, true>(k.z, row * k.step + at, counted && at < share.end ? 4 : 0, z[u]);
+                load4<DT, VEC>(a.W, f * a.ldw + at, f_there ? share.end - at : 0, w[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kSmallAhead; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t c = base + u * kSmallStep + 4 * half + e;
+                    const float d = counted && c < share.end ? small_dz(z[u][e], c, target, lse, each) : 0.0f;
+                    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(d, w[u][e], acc, 0, 0, 0);
+                }
+        }
+        join_waves(acc, lds, wave, lane, [&](int e, float s) {
+            const int64_t i = row0 + 8 * (e >> 2) + 4 * half + (e & 3);
+            if (i >= a.M || !f_there) return;
+            if (k.x_parts > 1) k.slices[((int64_t)part * a.M + i) * a.K + f] = s;
+            else store_as<DT>(a.dX, i * a.K + f, s * factor);
+        });
+        return;
+    }
+    const uint32_t at_w = blockIdx.x - k.x_tiles * k.x_parts, part = at_w / k.w_tiles, tile = at_w - part * k.w_tiles, down = k.w_first + tile / k.w_across;
+    const int64_t f0 = (int64_t)down * kSmallTile, c0 = (int64_t)(tile % k.w_across) * kSmallTile;
+    const int64_t f = f0 + line, c = c0 + line;
+    const bool c_there = c < a.N;
+    const Share share = share_of(a.M, part, k.w_parts);
+    const bool each = a.reduction == kNone && a.dloss;
+    for (int64_t base = share.begin + 8 * wave; base < share.end; base += kSmallAhead / 2 * kSmallStep) {
+        float x[kSmallAhead / 2][4], z[kSmallAhead / 2][4], lse[kSmallAhead / 2][4], g[kSmallAhead / 2][4];
+        int64_t target[kSmallAhead / 2][4];
+#pragma unroll
+        for (int u = 0; u < kSmallAhead / 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t row = base + u * kSmallStep + 4 * half + e, r = row < share.end ? row : share.end - 1;
+                x[u][e] = row >= share.end ? 0.0f : f < a.K ? load_as<DT>(a.X, row * a.ldx + f) : f == a.K ? 1.0f : 0.0f;
+                z[u][e] = row < share.end && c_there ? k.z[row * k.step + c] : 0.0f;
+                target[u][e] = row < share.end ? a.target[r] : a.ignore;
+                lse[u][e] = a.saved[r];
+                g[u][e] = each ? a.dloss[r] : 1.0f;
+            }
+#pragma unroll
+        for (int u = 0; u < kSmallAhead / 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float d = target[u][e] != a.ignore && c_there ? small_dz(z[u][e], c, target[u][e], lse[u][e], g[u][e]) : 0.0f;
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[u][e], d, acc, 0, 0, 0);
+            }
+    }
+    join_waves(acc, lds, wave, lane, [&](int e, float s) {
+        const int64_t i = f0 + 8 * (e >> 2) + 4 * half + (e & 3);
+        if (!c_there) return;
+        if (k.w_parts > 1) {
+            if (i <= a.K) k.w_slices[((int64_t)part * (a.K + 1) + i) * a.N + c] = s;
+            return;
+        }
+        if (i < a.K && a.dW) store_as<DT>(a.dW, i * a.N + c, s * factor);
+        if (i == a.K && a.dbias) {
+            if (a.bias_dtype == kBf16) store_as<kBf16>(a.dbias, c, s * factor);
+            else store_as<kF32>(a.dbias, c, s * factor);
+        }
+    });
+}
+
+// dX's parts added up, and dW's and db's behind them
+__global__ __launch_bounds__(kThreads) void xent_small_add_kernel(XentArgs a, SmallArgs k, int64_t of_x, int64_t of_w)
+{
+    const float factor = (a.reduction == kNone ? 1.0f : (a.dloss ? *a.dloss : 1.0f)) * a.saved[a.M];
+    int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (at >= of_x + of_w) return;
+    const bool x = at < of_x;
+    at -= x ? 0 : of_x;
+    const float* from = (x ? k.slices : k.w_slices) + at;
+    const int64_t size = x ? a.M * a.K : (a.K + 1) * a.N;
+    const uint32_t parts = x ? k.x_parts : k.w_parts;
+    float v = 0.0f;
+#pragma unroll 4
+    for (uint32_t i = 0; i < parts; ++i) v += from[i * size];
+    v *= factor;
+    const bool bias = !x && at >= a.K * a.N;
+    void* to = x ? a.dX : bias ? a.dbias : a.dW;
+    if (!to) return;
+    if (bias) at -= a.K * a.N;
+    if ((bias ? a.bias_dtype : a.dtype) == kBf16) store_as<kBf16>(to, at, v);
+    else store_as<kF32>(to, at, v);
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
-constexpr int kBig = 256, kMid = 128;
-
-// How a call is cut, and where its pieces of the workspace lie.
-struct Plan {
-    bool planes;                        // fp32
-    bool pack_x, pack_w;
-    int64_t piece;                      // classes of a piece
-    int64_t x_step, w_step, dz_step;    // of packed rows, of dz
-    size_t x, w, rest;                  // bytes of X packed, of a piece of W packed, of what lies behind them
-    size_t pairs, picked, rows;         // forward
-    size_t dz, sums, slices;            // backward
+// Tiles: large ones of 256 x 256 (one plane) or 256 x 128 (three), small ones of 128 x 128.
+struct Tile {
+    int a, b;
+    bool large;
 };
-
-// products of few tiles: the contraction in parts, so that there are about two workgroups for a compute unit, each part
-// at least 512 long
-uint32_t parts_of(int64_t RA, int64_t RB, int64_t D, int tile)
+Tile tile_of(int64_t RA, int64_t RB, int planes)
 {
-    const int64_t tiles = ((RA + tile - 1) / tile) * ((RB + tile - 1) / tile), full = tile == kBig ? 256 : 512;
+    const Tile big{256, planes == 1 ? 256 : 128, true};
+    const int64_t tiles = ((RA + big.a - 1) / big.a) * ((RB + big.b - 1) / big.b);
+    return tiles >= 192 ? big : Tile{128, 128, false};
+}
+
+// Products of few tiles: the contraction in parts, so that every compute unit has what workgroups it holds (two of the small
+// tiles of one plane, else one), each part at least 512 long.
+uint32_t parts_of(int64_t RA, int64_t RB, int64_t D, int planes)
+{
+    const Tile t = tile_of(RA, RB, planes);
+    const int64_t tiles = ((RA + t.a - 1) / t.a) * ((RB + t.b - 1) / t.b), full = t.large || planes > 1 ? 256 : 512;
+    const int64_t least = planes == 1 ? 512 : 128;
     int64_t parts = full / tiles;
-    if (parts > D / 512) parts = D / 512;
+    if (parts > D / least) parts = D / least;
     return (uint32_t)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
 }
 
-int tile_of(int64_t RA, int64_t RB)
-{
-    const int64_t tiles = ((RA + kBig - 1) / kBig) * ((RB + kBig - 1) / kBig);
-    return tiles >= 192 ? kBig : kMid;
-}
+// How a call is cut, and where its pieces of the workspace lie.
+struct Plan {
+    int planes;                         // 3: fp32
+    bool pack_x, pack_w;
+    int64_t piece;                      // classes of a piece
+    int64_t x_step, w_step, dz_step;    // of packed rows, of dz
+    size_t x, w;                        // bytes of X packed, of a piece of W packed
+    size_t pairs, picked, rows;         // forward
+    size_t dz, sums, slices, column;    // backward
+};
 
 bool whole(const void* p, int64_t ld, int64_t cols, int dtype)
 {
@@ -449,27 +763,28 @@ bool whole(const void* p, int64_t ld, int64_t cols, int dtype)
 Plan plan_of(const XentArgs& a, bool sizes)
 {
     Plan p{};
-    p.planes = a.dtype == kF32;
-    const int n = p.planes ? 3 : 1;
+    p.planes = a.dtype == kF32 ? 3 : 1;
     p.pack_x = sizes || !whole(a.X, a.ldx, a.K, a.dtype);
     p.pack_w = sizes || !whole(a.W, a.ldw, a.N, a.dtype);
     // dz of a piece stays within 128 MB, which the memory-side cache holds between its writer and its readers
-    p.piece = ((int64_t)128 << 20) / (2 * n * a.M) / kBig * kBig;
+    p.piece = ((int64_t)128 << 20) / (2 * p.planes * a.M) / 256 * 256;
     if (p.piece < 1024) p.piece = 1024;
     if (p.piece > 65536) p.piece = 65536;
     if (p.piece > a.N) p.piece = a.N;
-    p.x_step = up(a.K, 8);
-    p.w_step = up(p.piece, 8);
-    p.dz_step = up(p.piece, kBig);
-    p.x = p.pack_x ? up256(2 * (size_t)n * a.M * p.x_step) : 0;
-    p.w = p.pack_w ? up256(2 * (size_t)n * a.K * p.w_step) : 0;
-    p.pairs = up256(sizeof(float2) * ((a.N + kMid - 1) / kMid + (a.N + p.piece - 1) / p.piece) * a.M);
+    const int64_t unit = p.planes == 1 ? 8 : 32;
+    p.x_step = p.planes * up(a.K, unit);
+    p.w_step = p.planes * up(p.piece, unit);
+    p.dz_step = p.planes * up(p.piece, 256);
+    p.x = p.pack_x ? up256(2 * (size_t)a.M * p.x_step) : 0;
+    p.w = p.pack_w ? up256(2 * (size_t)a.K * p.w_step) : 0;
+    p.pairs = up256(sizeof(float2) * ((a.N + 127) / 128 + (a.N + p.piece - 1) / p.piece) * a.M);
     p.picked = p.rows = up256(sizeof(float) * a.M);
-    p.dz = up256(2 * (size_t)n * a.M * p.dz_step);
+    p.dz = up256(2 * (size_t)a.M * p.dz_step);
     p.sums = p.piece < a.N ? up256(sizeof(float) * a.M * a.K) : 0;
+    p.column = up256(sizeof(float) * (size_t)((a.M + 127) / 128) * p.piece);
     size_t most = 0;
     for (const int64_t classes : {p.piece, a.N - (a.N - 1) / p.piece * p.piece}) {          // (the last piece may be cut another way)
-        const uint32_t px = parts_of(a.M, a.K, classes, tile_of(a.M, a.K)), pw = parts_of(a.K, classes, a.M, tile_of(a.K, classes));
+        const uint32_t px = parts_of(a.M, a.K, classes, p.planes), pw = parts_of(a.K, classes, a.M, p.planes);
         const size_t sx = px > 1 ? (size_t)px * a.M * a.K : 0, sw = pw > 1 ? (size_t)pw * a.K * classes : 0;
         if (sx > most) most = sx;
         if (sw > most) most = sw;
@@ -480,8 +795,9 @@ Plan plan_of(const XentArgs& a, bool sizes)
 
 hipError_t launch_pack(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint16_t* dst, int64_t step, hipStream_t stream)
 {
-    const PackArgs a{src, rows, cols, ld, dst, step, rows * step};
-    const dim3 grid((uint32_t)((step / 2 + kThreads - 1) / kThreads), (uint32_t)(rows < 65535 ? rows : 65535));
+    const PackArgs a{src, rows, cols, ld, dst, step};
+    const int64_t pairs = (dtype == kBf16 ? step : step / 3) / 2;
+    const dim3 grid((uint32_t)((pairs + kThreads - 1) / kThreads), (uint32_t)(rows < 65535 ? rows : 65535));
     ProfileScope ps(K_XENT_PACK, stream);
     if (dtype == kBf16) hipLaunchKernelGGL(xent_pack_kernel<kBf16>, grid, dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL(xent_pack_kernel<kF32>, grid, dim3(kThreads), 0, stream, a);
@@ -489,28 +805,33 @@ hipError_t launch_pack(const void* src, int dtype, int64_t rows, int64_t cols, i
 }
 
 template <bool GRAD>
-hipError_t launch_logits(int tag, const bf16::Args& g, const RowArgs& r, int tile, hipStream_t stream)
+hipError_t launch_logits(int tag, const bf16::Args& g, const RowArgs& r, int planes, bool large, hipStream_t stream)
 {
     ProfileScope ps(tag, stream);
     const dim3 grid(8 * g.per_xcd);
-    if (tile == kBig) {
-        if (g.terms > 1) hipLaunchKernelGGL((xent_logits_kernel<GRAD, true, 256, 256, 2, 4>), grid, dim3(512), 0, stream, g, r);
-        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, false, 256, 256, 2, 4>), grid, dim3(512), 0, stream, g, r);
+    if (planes == 1) {
+        if (large) hipLaunchKernelGGL((xent_logits_kernel<GRAD, 1, 256, 256, 2, 4, 2>), grid, dim3(512), 0, stream, g, r);
+        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 1, 128, 128, 2, 2, 2>), grid, dim3(256), 0, stream, g, r);
     } else {
-        if (g.terms > 1) hipLaunchKernelGGL((xent_logits_kernel<GRAD, true, 128, 128, 2, 2>), grid, dim3(256), 0, stream, g, r);
-        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, false, 128, 128, 2, 2>), grid, dim3(256), 0, stream, g, r);
+        if (large) hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 256, 128, 4, 2, 2>), grid, dim3(512), 0, stream, g, r);
+        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 128, 128, 2, 4, 3>), grid, dim3(512), 0, stream, g, r);
     }
     return hipGetLastError();
 }
 
 template <int MODE>
-hipError_t launch_gradient(int tag, const bf16::Args& g, const OutArgs& o, int tile, hipStream_t stream)
+hipError_t launch_gradient(int tag, const bf16::Args& g, const OutArgs& o, int planes, bool large, hipStream_t stream)
 {
     {
         ProfileScope ps(tag, stream);
         const dim3 grid(8 * g.per_xcd);
-        if (tile == kBig) hipLaunchKernelGGL((xent_gradient_kernel<MODE, 256, 256, 2, 4>), grid, dim3(512), 0, stream, g, o);
-        else hipLaunchKernelGGL((xent_gradient_kernel<MODE, 128, 128, 2, 2>), grid, dim3(256), 0, stream, g, o);
+        if (planes == 1) {
+            if (large) hipLaunchKernelGGL((xent_gradient_kernel<1, MODE, 256, 256, 2, 4, 2>), grid, dim3(512), 0, stream, g, o);
+            else hipLaunchKernelGGL((xent_gradient_kernel<1, MODE, 128, 128, 2, 2, 2>), grid, dim3(256), 0, stream, g, o);
+        } else {
+            if (large) hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 256, 128, 4, 2, 2>), grid, dim3(512), 0, stream, g, o);
+            else hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 128, 128, 2, 4, 3>), grid, dim3(512), 0, stream, g, o);
+        }
     }
     if (g.parts > 1) {
         ProfileScope ps(K_XENT_ADD_PARTS, stream);
@@ -530,12 +851,29 @@ hipError_t operands_of(const XentArgs& a, const Plan& p, char* workspace, int64_
     const int64_t size = dtype_size(a.dtype);
     const char* w = static_cast<const char*>(a.W) + first * size;
     uint16_t *px = reinterpret_cast<uint16_t*>(workspace), *pw = reinterpret_cast<uint16_t*>(workspace + p.x);
-    o->x = p.pack_x ? bf16::Side{px, p.x_step, a.M * p.x_step} : bf16::Side{static_cast<const uint16_t*>(a.X), a.ldx, 0};
-    o->w = p.pack_w ? bf16::Side{pw, p.w_step, a.K * p.w_step} : bf16::Side{reinterpret_cast<const uint16_t*>(w), a.ldw, 0};
+    o->x = p.pack_x ? bf16::Side{px, p.x_step} : bf16::Side{static_cast<const uint16_t*>(a.X), a.ldx};
+    o->w = p.pack_w ? bf16::Side{pw, p.w_step} : bf16::Side{reinterpret_cast<const uint16_t*>(w), a.ldw};
     hipError_t e = hipSuccess;
     if (p.pack_x && !have_x) e = launch_pack(a.X, a.dtype, a.M, a.K, a.ldx, px, p.x_step, stream);
     if (p.pack_w && !have_w && e == hipSuccess) e = launch_pack(w, a.dtype, a.K, classes, a.ldw, pw, p.w_step, stream);
     return e;
+}
+
+// from the tiles' pairs to the loss
+hipError_t launch_rows(const XentArgs& a, const float2* pairs, int64_t tiles, const float* picked, float* rows, hipStream_t stream)
+{
+    ProfileScope ps(K_XENT_LOSS, stream);
+    TotalArgs t{1, 0};
+    while (t.lanes < 64 && 4 * t.lanes < tiles) t.lanes *= 2;
+    t.alone = a.M * t.lanes <= 2048;            // (two rounds of a workgroup at most: less than another launch)
+    if (t.alone) {
+        hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, stream, a, pairs, tiles, picked, rows, t);
+        return hipGetLastError();
+    }
+    const int64_t per = kThreads / t.lanes;
+    hipLaunchKernelGGL(xent_rows_kernel, dim3((uint32_t)((a.M + per - 1) / per)), dim3(kThreads), 0, stream, a, pairs, tiles, picked, rows, t);
+    hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, stream, a, rows);
+    return hipGetLastError();
 }
 
 RowArgs rows_of(const XentArgs& a, int64_t first, int64_t classes)
@@ -546,16 +884,131 @@ RowArgs rows_of(const XentArgs& a, int64_t first, int64_t classes)
     return r;
 }
 
+// ---- small problems ----
+
+constexpr int64_t kSmallLogits = (int64_t)8 << 20;          // of 4 bytes
+
+// (measured: see the kernels' comment)
+bool small_problem(const XentArgs& a)
+{
+    return a.M * a.N <= kSmallLogits && a.M * a.N <= ((int64_t)1 << 28) / a.K;
+}
+
+struct SmallPlan {
+    int64_t class_tiles, row_tiles, step;
+    uint32_t x_parts, w_parts;              // of dX's and dW's contractions
+    size_t z, pairs, picked, rows, x_slices, w_slices;
+};
+SmallPlan small_plan(const XentArgs& a)
+{
+    SmallPlan p{};
+    p.class_tiles = (a.N + kSmallTile - 1) / kSmallTile;
+    p.row_tiles = (a.M + kSmallTile - 1) / kSmallTile;
+    p.step = up(a.N, 4);
+    // where tiles are few several workgroups share a contraction: up to two for a compute unit, eight steps each at least
+    auto parts = [](int64_t tiles, int64_t length) {
+        const int64_t most = length / (8 * kSmallStep), n = 512 / tiles < most ? 512 / tiles : most;
+        return (uint32_t)(n < 1 ? 1 : n);
+    };
+    p.x_parts = parts(p.row_tiles * ((a.K + kSmallTile - 1) / kSmallTile), a.N);
+    p.w_parts = parts(p.class_tiles * (a.K / kSmallTile + 1), a.M);
+    p.z = up256(sizeof(float) * a.M * p.step);
+    p.pairs = up256(sizeof(float2) * p.class_tiles * a.M);
+    p.picked = p.rows = up256(sizeof(float) * a.M);
+    p.x_slices = p.x_parts > 1 ? up256(sizeof(float) * p.x_parts * a.M * a.K) : 0;
+    p.w_slices = p.w_parts > 1 ? up256(sizeof(float) * p.w_parts * (a.K + 1) * a.N) : 0;
+    return p;
+}
+
+// f(type, whole sixteen or eight bytes)
+template <class F>
+void with_small(const XentArgs& a, bool vec, F f)
+{
+    using std::integral_constant;
+    if (a.dtype == kBf16) {
+        if (vec) f(integral_constant<int, kBf16>{}, std::true_type{});
+        else f(integral_constant<int, kBf16>{}, std::false_type{});
+    } else {
+        if (vec) f(integral_constant<int, kF32>{}, std::true_type{});
+        else f(integral_constant<int, kF32>{}, std::false_type{});
+    }
+}
+bool fours(const void* p, int64_t ld, int64_t cols, int dtype)
+{
+    return reinterpret_cast<uintptr_t>(p) % (size_t)(4 * dtype_size(dtype)) == 0 && ld % 4 == 0 && cols % 4 == 0;
+}
+
+// forward: the loss; keep: the logits for the gradients
+hipError_t launch_small_logits(const XentArgs& a, const SmallPlan& p, char* at, bool forward, bool keep, hipStream_t stream)
+{
+    SmallArgs k{};
+    if (keep) k.z = reinterpret_cast<float*>(at);
+    k.step = p.step;
+    k.w_across = (uint32_t)p.class_tiles;
+    if (forward) {
+        k.pairs = reinterpret_cast<float2*>(at + p.z);
+        k.picked = reinterpret_cast<float*>(at + p.z + p.pairs);
+    }
+    {
+        ProfileScope ps(K_XENT_LOGITS, stream);
+        with_small(a, fours(a.X, a.ldx, a.K, a.dtype), [&](auto dt, auto vec) {
+            hipLaunchKernelGGL((xent_small_logits_kernel<dt.value, vec.value>), dim3((uint32_t)(p.class_tiles * p.row_tiles)),
+                               dim3(64 * kSmallWaves), 0, stream, a, k);
+        });
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !forward) return e;
+    float* rows = a.reduction == kNone ? a.loss : reinterpret_cast<float*>(at + p.z + p.pairs + p.picked);
+    return launch_rows(a, k.pairs, p.class_tiles, k.picked, rows, stream);
+}
+
+hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* at, hipStream_t stream)
+{
+    SmallArgs k{};
+    k.z = reinterpret_cast<float*>(at);
+    k.step = p.step;
+    k.x_across = (uint32_t)((a.K + kSmallTile - 1) / kSmallTile);
+    k.x_tiles = a.dX ? (uint32_t)p.row_tiles * k.x_across : 0;
+    k.x_parts = p.x_parts;
+    k.w_parts = p.w_parts;
+    k.w_across = (uint32_t)p.class_tiles;
+    k.slices = reinterpret_cast<float*>(at + p.z + p.pairs + p.picked + p.rows);
+    k.w_slices = k.slices + p.x_slices / sizeof(float);
+    // (the line of ones may begin a tile of its own)
+    const uint32_t w_end = (uint32_t)((a.K + (a.dbias ? 1 : 0) + kSmallTile - 1) / kSmallTile);
+    k.w_first = a.dW ? 0 : a.dbias ? w_end - 1 : w_end;
+    k.w_tiles = (w_end - k.w_first) * k.w_across;
+    {
+        ProfileScope ps(K_XENT_DX, stream);
+        with_small(a, fours(a.W, a.ldw, a.N, a.dtype), [&](auto dt, auto vec) {
+            hipLaunchKernelGGL((xent_small_gradients_kernel<dt.value, vec.value>), dim3(k.x_tiles * k.x_parts + k.w_tiles * k.w_parts), dim3(64 * kSmallWaves),
+                               0, stream, a, k);
+        });
+    }
+    const int64_t of_x = a.dX && p.x_parts > 1 ? a.M * a.K : 0, of_w = k.w_tiles && p.w_parts > 1 ? (a.K + 1) * a.N : 0;
+    if (of_x + of_w) {
+        ProfileScope ps(K_XENT_ADD_PARTS, stream);
+        hipLaunchKernelGGL(xent_small_add_kernel, dim3((uint32_t)((of_x + of_w + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, a, k,
+                           of_x, of_w);
+    }
+    return hipGetLastError();
+}
+
 } // namespace
 
 size_t xent_workspace(const XentArgs& a, bool backward)
 {
+    if (small_problem(a)) {
+        const SmallPlan p = small_plan(a);
+        return p.z + p.pairs + p.picked + p.rows + (backward ? p.x_slices + p.w_slices : 0);
+    }
     const Plan p = plan_of(a, true);
-    return p.x + p.w + (backward ? p.dz + p.sums + p.slices : p.pairs + p.picked + p.rows);
+    return p.x + p.w + (backward ? p.dz + p.sums + p.slices + p.column : p.pairs + p.picked + p.rows);
 }
 
-hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, hipStream_t stream)
+hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hipStream_t stream)
 {
+    if (small_problem(a)) return launch_small_logits(a, small_plan(a), static_cast<char*>(workspace), true, backward, stream);
     const Plan p = plan_of(a, false);
     char* at = static_cast<char*>(workspace) + p.x + p.w;
     float2* pairs = reinterpret_cast<float2*>(at);
@@ -570,24 +1023,25 @@ hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, hipStream_t strea
         RowArgs r = rows_of(a, first, classes);
         r.pairs = pairs + tiles * a.M;
         r.picked = picked;
-        const int tile = tile_of(classes, a.M);
-        const bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, tile, tile, 1);
-        if ((e = launch_logits<false>(K_XENT_LOGITS, g, r, tile, stream)) != hipSuccess) return e;
+        const Tile t = tile_of(classes, a.M, p.planes);
+        const bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, t.a, t.b, 1);
+        if ((e = launch_logits<false>(K_XENT_LOGITS, g, r, p.planes, t.large, stream)) != hipSuccess) return e;
         tiles += g.n_at;
     }
-    ProfileScope ps(K_XENT_LOSS, stream);
-    hipLaunchKernelGGL(xent_rows_kernel, dim3((uint32_t)((a.M + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, a, pairs, tiles,
-                       picked, rows);
-    hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, stream, a, rows);
-    return hipGetLastError();
+    return launch_rows(a, pairs, tiles, picked, rows, stream);
 }
 
 // forward: the forward pass has just run in the same workspace
 hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hipStream_t stream)
 {
+    hipError_t e;
+    if (small_problem(a)) {
+        const SmallPlan s = small_plan(a);
+        if (!forward && (e = launch_small_logits(a, s, static_cast<char*>(workspace), false, true, stream)) != hipSuccess) return e;
+        return launch_small_gradients(a, s, static_cast<char*>(workspace), stream);
+    }
     const Plan p = plan_of(a, false);
     char* at = static_cast<char*>(workspace) + p.x + p.w;
-    hipError_t e;
     for (int64_t first = 0; first < a.N; first += p.piece) {
         const int64_t classes = a.N - first < p.piece ? a.N - first : p.piece;
         Operands o;
@@ -596,11 +1050,13 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
         RowArgs r = rows_of(a, first, classes);
         r.saved = a.saved; r.dloss = a.dloss; r.each = a.reduction == kNone;
         r.dz = reinterpret_cast<uint16_t*>(at);
-        r.step = p.dz_step; r.plane = a.M * p.dz_step;
-        int tile = tile_of(classes, a.M);
-        bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, tile, tile, 1);
-        if ((e = launch_logits<true>(K_XENT_DLOGITS, g, r, tile, stream)) != hipSuccess) return e;
-        const bf16::Side dz{r.dz, r.step, r.plane};
+        r.step = p.dz_step;
+        if (a.dbias) r.column = reinterpret_cast<float*>(at + p.dz + p.sums + p.slices);
+        Tile t = tile_of(classes, a.M, p.planes);
+        bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, t.a, t.b, 1);
+        const uint32_t row_tiles = g.n_bt;
+        if ((e = launch_logits<true>(K_XENT_DLOGITS, g, r, p.planes, t.large, stream)) != hipSuccess) return e;
+        const bf16::Side dz{r.dz, r.step};
         OutArgs out{};
         out.dtype = a.dtype; out.share = a.saved + a.M; out.dloss = r.each ? nullptr : a.dloss;
         out.slices = reinterpret_cast<float*>(at + p.dz + p.sums);
@@ -610,25 +1066,24 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
             x.out = a.dX; x.step = a.K;
             x.sums = p.sums ? reinterpret_cast<float*>(at + p.dz) : nullptr;
             x.first_piece = first == 0; x.last_piece = first + classes == a.N;
-            tile = tile_of(a.M, a.K);
-            g = bf16::plan(dz, o.w, a.M, a.K, classes, p.planes, tile, tile, parts_of(a.M, a.K, classes, tile));
-            if ((e = launch_gradient<kAlong>(K_XENT_DX, g, x, tile, stream)) != hipSuccess) return e;
+            t = tile_of(a.M, a.K, p.planes);
+            g = bf16::plan(dz, o.w, a.M, a.K, classes, p.planes, t.a, t.b, parts_of(a.M, a.K, classes, p.planes));
+            if ((e = launch_gradient<kAlong>(K_XENT_DX, g, x, p.planes, t.large, stream)) != hipSuccess) return e;
         }
         if (a.dW) {
             OutArgs w = out;
             w.out = static_cast<char*>(a.dW) + first * dtype_size(a.dtype); w.step = a.N;
-            tile = tile_of(a.K, classes);
-            g = bf16::plan(o.x, dz, a.K, classes, a.M, p.planes, tile, tile, parts_of(a.K, classes, a.M, tile));
-            if ((e = launch_gradient<kDown>(K_XENT_DW, g, w, tile, stream)) != hipSuccess) return e;
+            t = tile_of(a.K, classes, p.planes);
+            g = bf16::plan(o.x, dz, a.K, classes, a.M, p.planes, t.a, t.b, parts_of(a.K, classes, a.M, p.planes));
+            if ((e = launch_gradient<kDown>(K_XENT_DW, g, w, p.planes, t.large, stream)) != hipSuccess) return e;
         }
         if (a.dbias) {
             OutArgs b = out;
             b.dtype = a.bias_dtype;
             void* to = static_cast<char*>(a.dbias) + first * dtype_size(a.bias_dtype);
-            const dim3 grid((uint32_t)((classes + 63) / 64));
             ProfileScope ps(K_XENT_DBIAS, stream);
-            if (p.planes) hipLaunchKernelGGL(xent_dbias_kernel<true>, grid, dim3(kThreads), 0, stream, r, to, b);
-            else hipLaunchKernelGGL(xent_dbias_kernel<false>, grid, dim3(kThreads), 0, stream, r, to, b);
+            hipLaunchKernelGGL(xent_dbias_kernel, dim3((uint32_t)((classes + 15) / 16)), dim3(kThreads), 0, stream, r.column, row_tiles, classes,
+                               to, b);
             if ((e = hipGetLastError()) != hipSuccess) return e;
         }
     }
