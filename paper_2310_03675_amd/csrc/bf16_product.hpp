@@ -77,11 +77,13 @@ __device__ __forceinline__ Place place_of(const Args& g)
     return p;
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const uint16_t* from, int64_t elements)
+// (there: else nothing is in range.  A mask: a choice makes the compiler branch around the arithmetic, inside the loop)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t range_of(const uint16_t* from, int64_t elements, bool there)
 {
-    const int64_t bytes = 2 * elements;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(from), 0,
-                                             bytes <= 0 ? 0 : bytes < (int64_t)kOutside ? (int)bytes : (int)(kOutside - 1), 0x00020000);
+    int64_t bytes = 2 * elements;
+    bytes = bytes < 0 ? 0 : bytes;
+    bytes = bytes < (int64_t)kOutside ? bytes : (int64_t)kOutside - 1;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(from), 0, (int)bytes & -(int)there, 0x00020000);
 }
 
 // One operand of a workgroup, T lines of it, brought by WAVES waves: a stage to LDS.
@@ -121,11 +123,11 @@ struct Panel {
         }
     }
 
-    __device__ __forceinline__ void bring(uint8_t* lds, uint32_t s, int wave) const
+    __device__ __forceinline__ void bring(uint8_t* lds, uint32_t s, bool there, int wave) const
     {
         const int64_t at = (int64_t)s * kStage;
         const int64_t rows = MODE == kAlong ? lines_left : d - at, width = MODE == kAlong ? d - at : lines_left;
-        const __amdgpu_buffer_rsrc_t rs = range_of(base + (MODE == kAlong ? at : at * step), (rows - 1) * step + (width + 7) / 8 * 8);
+        const __amdgpu_buffer_rsrc_t rs = range_of(base + (MODE == kAlong ? at : at * step), (rows - 1) * step + (width + 7) / 8 * 8, there);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             uint32_t o = off[j];
@@ -165,11 +167,11 @@ struct Panel<3, MODE, T, WAVES> {
         }
     }
 
-    __device__ __forceinline__ void bring(uint8_t* lds, uint32_t s, int wave) const
+    __device__ __forceinline__ void bring(uint8_t* lds, uint32_t s, bool there, int wave) const
     {
         const int64_t at = (int64_t)s * kStage;
-        const __amdgpu_buffer_rsrc_t rs = MODE == kAlong ? range_of(base + 3 * at, (rows_left - 1) * step + width - 3 * at)
-                                                         : range_of(base + at * step, (rows_left - at - 1) * step + width);
+        const int64_t elements = MODE == kAlong ? (rows_left - 1) * step + width - 3 * at : (rows_left - at - 1) * step + width;
+        const __amdgpu_buffer_rsrc_t rs = range_of(base + (MODE == kAlong ? 3 * at : at * step), elements, there);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -267,50 +269,63 @@ __device__ __forceinline__ void multiply(const Args& g, const Place& p, const St
     const Fragments<P, MA, TA, NA> fa((wave / WB) * (TA / WA), lane);
     const Fragments<P, MB, TB, NB> fb((wave % WB) * (TB / WB), lane);
     auto bring = [&](uint32_t s, uint8_t* a, uint8_t* b) {
-        pa.bring(a, p.first + s, wave);
-        pb.bring(b, p.first + s, wave);
+        pa.bring(a, p.first + s, s < p.n, wave);
+        pb.bring(b, p.first + s, s < p.n, wave);
     };
-    auto products = [&](const uint8_t* a, const uint8_t* b) {
+    // fragments of sixteen of the contraction, two sets: one is read while the other is multiplied
+    struct Set {
+        v8b x[NA][P], y[NB][P];
+    } set[2];
+    auto read = [&](Set& f, int u, int q) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int q = 0; q < stage_of(P) / 16; ++q) {
-            __builtin_amdgcn_sched_barrier(0);
-            v8b x[NA][P], y[NB][P];
+        for (int k = P - 1; k >= 0; --k) {
 #pragma unroll
-            for (int k = P - 1; k >= 0; --k) {
+            for (int j = 0; j < NB; ++j) f.y[j][k] = fb.read(lds.b[u], j, q, k);
 #pragma unroll
-                for (int j = 0; j < NB; ++j) y[j][k] = fb.read(b, j, q, k);
-#pragma unroll
-                for (int i = 0; i < NA; ++i) x[i][k] = fa.read(a, i, q, k);
-            }
-            auto term = [&](int ka, int kb) {
-#pragma unroll
-                for (int i = 0; i < NA; ++i)
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][ka], y[j][kb], acc[i][j], 0, 0, 0);
-            };
-            if constexpr (P == 3) {
-                term(2, 0);
-                term(0, 2);
-                term(1, 1);
-                term(1, 0);
-                term(0, 1);
-            }
-            term(0, 0);
+            for (int i = 0; i < NA; ++i) f.x[i][k] = fa.read(lds.a[u], i, q, k);
         }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    // (stages behind the last are brought as well, out of range or not used: the waits stay the same)
+    auto products = [&](const Set& f) {
+        auto term = [&](int ka, int kb) {
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[i][ka], f.y[j][kb], acc[i][j], 0, 0, 0);
+        };
+        if constexpr (P == 3) {
+            term(2, 0);
+            term(0, 2);
+            term(1, 1);
+            term(1, 0);
+            term(0, 1);
+        }
+        term(0, 0);
+    };
+    constexpr int kSteps = stage_of(P) / 16;
+    static_assert(kSteps % 2 == 0, "the sets take turns");
+    // (stages behind the last are zeros: whole rounds of S, and the same waits everywhere)
 #pragma unroll
     for (int u = 0; u + 1 < S; ++u) bring(u, lds.a[u], lds.b[u]);
-    for (uint32_t s = 0;;) {
+    wait_and_meet<(S - 2) * kLoads>();
+    bring(S - 1, lds.a[S - 1], lds.b[S - 1]);
+    read(set[0], 0, 0);
+    for (uint32_t s = 0; s < p.n; s += S) {
 #pragma unroll
         for (int u = 0; u < S; ++u) {
+#pragma unroll
+            for (int q = 0; q + 1 < kSteps; ++q) {
+                read(set[(q + 1) & 1], u, q + 1);
+                products(set[q & 1]);
+            }
+            // the stage has been read: what is brought next goes into its place, while the last sixteen are multiplied
             wait_and_meet<(S - 2) * kLoads>();
-            bring(s + S - 1, lds.a[(u + S - 1) % S], lds.b[(u + S - 1) % S]);
-            products(lds.a[u], lds.b[u]);
-            if (++s == p.n) goto done;
+            bring(s + u + S, lds.a[u], lds.b[u]);
+            read(set[0], (u + 1) % S, 0);
+            products(set[1]);
         }
     }
-done:
     wait_and_meet<0>();             // (what follows may write where a stage lies)
 #endif
 }

@@ -67,23 +67,34 @@ __device__ __forceinline__ void split(float x, uint32_t (&part)[3])
     part[2] = to_bf16(rest - from_bf16(part[1]));
 }
 
+// A thread has two columns of kPackRows rows, all of whose loads are in flight.
+constexpr int kPackRows = 8;
 template <int DT>
 __global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs a)
 {
     const int64_t c = 2 * ((int64_t)blockIdx.x * kThreads + threadIdx.x);
     if (c >= (DT == kBf16 ? a.step : a.step / 3)) return;
-    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        const int64_t from = row * a.ld + c;
-        const float x = c < a.cols ? load_as<DT>(a.src, from) : 0.0f, y = c + 1 < a.cols ? load_as<DT>(a.src, from + 1) : 0.0f;
-        uint32_t* to = reinterpret_cast<uint32_t*>(a.dst + row * a.step + (DT == kBf16 ? c : c / 32 * 96 + c % 32));
-        if (DT == kBf16) {
-            *to = __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xFFFF0000u);
-        } else {
-            uint32_t p[3], q[3];
-            split(x, p);
-            split(y, q);
+    for (int64_t row0 = (int64_t)blockIdx.y * kPackRows; row0 < a.rows; row0 += (int64_t)gridDim.y * kPackRows) {
+        float x[kPackRows], y[kPackRows];
 #pragma unroll
-            for (int k = 0; k < 3; ++k) to[16 * k] = p[k] | q[k] << 16;
+        for (int i = 0; i < kPackRows; ++i) {
+            const int64_t from = (row0 + i) * a.ld + c;
+            x[i] = row0 + i < a.rows && c < a.cols ? load_as<DT>(a.src, from) : 0.0f;
+            y[i] = row0 + i < a.rows && c + 1 < a.cols ? load_as<DT>(a.src, from + 1) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kPackRows; ++i) {
+            if (row0 + i >= a.rows) break;
+            uint32_t* to = reinterpret_cast<uint32_t*>(a.dst + (row0 + i) * a.step + (DT == kBf16 ? c : c / 32 * 96 + c % 32));
+            if (DT == kBf16) {
+                *to = __float_as_uint(x[i]) >> 16 | (__float_as_uint(y[i]) & 0xFFFF0000u);
+            } else {
+                uint32_t p[3], q[3];
+                split(x[i], p);
+                split(y[i], q);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) to[16 * k] = p[k] | q[k] << 16;
+            }
         }
     }
 }
@@ -127,6 +138,9 @@ __device__ __forceinline__ float sum_of_32(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// waves to a SIMD: two workgroups of the small tile of one plane share a compute unit, of the others' LDS there is room for one
+constexpr int waves_of(int planes, int ta) { return 2; }
+
 // S stages of P planes' operands in LDS, each an object of its own
 #define HDQT_STAGES(P, S, TA, TB)                                                                            \
     constexpr int kA = (P == 1 ? 128 : 192) * TA, kB = (P == 1 ? 128 : 192) * TB;                            \
@@ -138,7 +152,7 @@ __device__ __forceinline__ float sum_of_32(float v)
 // Lines of A are classes (W, read down), lines of B rows (X): a lane then holds sums of one row of the logits, and the
 // maximum and the sum over classes stay inside it but for one exchange between the wave's halves.
 template <bool GRAD, int P, int TA, int TB, int WA, int WB, int S>
-__global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2, 2))) void xent_logits_kernel(bf16::Args g, RowArgs r)
+__global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(waves_of(P, TA), waves_of(P, TA)))) void xent_logits_kernel(bf16::Args g, RowArgs r)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
     constexpr bool kExact = P == 3;
@@ -243,7 +257,9 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2,
     };
     column(std::integral_constant<int, 0>{});
     if constexpr (NB > 1) column(std::integral_constant<int, 1>{});
-    static_assert(NB <= 2, "a call for each");
+    if constexpr (NB > 2) column(std::integral_constant<int, 2>{});
+    if constexpr (NB > 3) column(std::integral_constant<int, 3>{});
+    static_assert(NB <= 4, "a call for each");
     if constexpr (!GRAD) {
         __syncthreads();
         for (int t = threadIdx.x; t < TB; t += 64 * WA * WB) {
@@ -260,7 +276,8 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 float s = acc[i][0][e];
-                if constexpr (NB > 1) s += acc[i][1][e];
+#pragma unroll
+                for (int j = 1; j < NB; ++j) s += acc[i][j][e];
                 s = sum_of_32(s);
                 if ((lane & 31) == 0) columns[wave % WB][class0 + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)] = s;
             }
@@ -325,7 +342,7 @@ __device__ __forceinline__ void each_sum(v16f (&acc)[NA][NB], int64_t lines, int
 }
 
 template <int P, int MODE, int TA, int TB, int WA, int WB, int S>
-__global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2, 2))) void xent_gradient_kernel(bf16::Args g, OutArgs o)
+__global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(waves_of(P, TA), waves_of(P, TA)))) void xent_gradient_kernel(bf16::Args g, OutArgs o)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
     HDQT_STAGES(P, S, TA, TB);
@@ -747,9 +764,10 @@ uint32_t parts_of(int64_t RA, int64_t RB, int64_t D, int planes)
 struct Plan {
     int planes;                         // 3: fp32
     bool pack_x, pack_w;
+    bool whole_w;                       // W is packed as a whole, once for both directions
     int64_t piece;                      // classes of a piece
     int64_t x_step, w_step, dz_step;    // of packed rows, of dz
-    size_t x, w;                        // bytes of X packed, of a piece of W packed
+    size_t x, w;                        // bytes of X packed, of W or a piece of it packed
     size_t pairs, picked, rows;         // forward
     size_t dz, sums, slices, column;    // backward
 };
@@ -773,7 +791,8 @@ Plan plan_of(const XentArgs& a, bool sizes)
     if (p.piece > a.N) p.piece = a.N;
     const int64_t unit = p.planes == 1 ? 8 : 32;
     p.x_step = p.planes * up(a.K, unit);
-    p.w_step = p.planes * up(p.piece, unit);
+    p.whole_w = a.K * a.N <= ((int64_t)256 << 20) / (2 * p.planes);
+    p.w_step = p.planes * up(p.whole_w ? a.N : p.piece, unit);
     p.dz_step = p.planes * up(p.piece, 256);
     p.x = p.pack_x ? up256(2 * (size_t)a.M * p.x_step) : 0;
     p.w = p.pack_w ? up256(2 * (size_t)a.K * p.w_step) : 0;
@@ -797,7 +816,8 @@ hipError_t launch_pack(const void* src, int dtype, int64_t rows, int64_t cols, i
 {
     const PackArgs a{src, rows, cols, ld, dst, step};
     const int64_t pairs = (dtype == kBf16 ? step : step / 3) / 2;
-    const dim3 grid((uint32_t)((pairs + kThreads - 1) / kThreads), (uint32_t)(rows < 65535 ? rows : 65535));
+    const int64_t down = (rows + kPackRows - 1) / kPackRows;
+    const dim3 grid((uint32_t)((pairs + kThreads - 1) / kThreads), (uint32_t)(down < 65535 ? down : 65535));
     ProfileScope ps(K_XENT_PACK, stream);
     if (dtype == kBf16) hipLaunchKernelGGL(xent_pack_kernel<kBf16>, grid, dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL(xent_pack_kernel<kF32>, grid, dim3(kThreads), 0, stream, a);
@@ -841,22 +861,23 @@ hipError_t launch_gradient(int tag, const bf16::Args& g, const OutArgs& o, int p
     return hipGetLastError();
 }
 
-// X and a piece of W as the products take them
+// X and a piece of W as the products take them; `have`: another pass has just left them in this workspace
 struct Operands {
     bf16::Side x, w;
 };
-hipError_t operands_of(const XentArgs& a, const Plan& p, char* workspace, int64_t first, int64_t classes, bool have_x, bool have_w,
-                       Operands* o, hipStream_t stream)
+hipError_t operands_of(const XentArgs& a, const Plan& p, char* workspace, int64_t first, int64_t classes, bool have, Operands* o,
+                       hipStream_t stream)
 {
     const int64_t size = dtype_size(a.dtype);
     const char* w = static_cast<const char*>(a.W) + first * size;
     uint16_t *px = reinterpret_cast<uint16_t*>(workspace), *pw = reinterpret_cast<uint16_t*>(workspace + p.x);
     o->x = p.pack_x ? bf16::Side{px, p.x_step} : bf16::Side{static_cast<const uint16_t*>(a.X), a.ldx};
-    o->w = p.pack_w ? bf16::Side{pw, p.w_step} : bf16::Side{reinterpret_cast<const uint16_t*>(w), a.ldw};
+    o->w = p.pack_w ? bf16::Side{pw + (p.whole_w ? p.planes * first : 0), p.w_step} : bf16::Side{reinterpret_cast<const uint16_t*>(w), a.ldw};
     hipError_t e = hipSuccess;
-    if (p.pack_x && !have_x) e = launch_pack(a.X, a.dtype, a.M, a.K, a.ldx, px, p.x_step, stream);
-    if (p.pack_w && !have_w && e == hipSuccess) e = launch_pack(w, a.dtype, a.K, classes, a.ldw, pw, p.w_step, stream);
-    return e;
+    if (p.pack_x && !have && first == 0) e = launch_pack(a.X, a.dtype, a.M, a.K, a.ldx, px, p.x_step, stream);
+    if (!p.pack_w || e != hipSuccess) return e;
+    if (!p.whole_w) return have && p.piece == a.N ? e : launch_pack(w, a.dtype, a.K, classes, a.ldw, pw, p.w_step, stream);
+    return have || first ? e : launch_pack(a.W, a.dtype, a.K, a.N, a.ldw, pw, p.w_step, stream);
 }
 
 // from the tiles' pairs to the loss
@@ -1019,7 +1040,7 @@ hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hi
     for (int64_t first = 0; first < a.N; first += p.piece) {
         const int64_t classes = a.N - first < p.piece ? a.N - first : p.piece;
         Operands o;
-        if ((e = operands_of(a, p, static_cast<char*>(workspace), first, classes, first > 0, false, &o, stream)) != hipSuccess) return e;
+        if ((e = operands_of(a, p, static_cast<char*>(workspace), first, classes, false, &o, stream)) != hipSuccess) return e;
         RowArgs r = rows_of(a, first, classes);
         r.pairs = pairs + tiles * a.M;
         r.picked = picked;
@@ -1045,7 +1066,7 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
     for (int64_t first = 0; first < a.N; first += p.piece) {
         const int64_t classes = a.N - first < p.piece ? a.N - first : p.piece;
         Operands o;
-        if ((e = operands_of(a, p, static_cast<char*>(workspace), first, classes, forward || first > 0, forward && p.piece == a.N, &o, stream)) != hipSuccess)
+        if ((e = operands_of(a, p, static_cast<char*>(workspace), first, classes, forward, &o, stream)) != hipSuccess)
             return e;
         RowArgs r = rows_of(a, first, classes);
         r.saved = a.saved; r.dloss = a.dloss; r.each = a.reduction == kNone;
