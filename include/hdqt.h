@@ -533,14 +533,16 @@ typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
  *             backward call with the same arguments; private to the library
  *   dX, dW    [M, K] and [K, N], dense, of `dtype`; dbias [N] of bias_dtype; any may be NULL (one must not)
  *   dloss     fp32, M values for HDQT_REDUCE_NONE, else one; NULL: ones
- *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd}_workspace_size (0 for invalid arguments)
- * hdqt_xent_step is the forward and the backward call with dloss = 1; its workspace is the larger of the two.
+ *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd,step}_workspace_size (0 for invalid arguments)
+ * hdqt_xent_step is the forward and the backward call with dloss = 1.  Its backward half takes the logits from the
+ * forward half where those fit the workspace's bounds (fp32, all classes one piece; and small problems).
  * bfloat16: products of bfloat16 with sums in 32 bits; dz is rounded to bfloat16 before its products.
  * fp32: as exact as products in 32 bits.
  */
 size_t hdqt_xent_saved_size(int64_t M);
 size_t hdqt_xent_fwd_workspace_size(int64_t M, int64_t K, int64_t N, int dtype);
 size_t hdqt_xent_bwd_workspace_size(int64_t M, int64_t K, int64_t N, int dtype);
+size_t hdqt_xent_step_workspace_size(int64_t M, int64_t K, int64_t N, int dtype);
 int hdqt_xent_fwd(const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias, const int64_t *target,
                   int64_t ignore_index, int64_t M, int64_t K, int64_t N, int dtype, int bias_dtype, int reduction,
                   float *loss, float *saved, void *workspace, size_t workspace_bytes, void *stream);

@@ -59,7 +59,7 @@ EXPORTED = [
     "hdqt_gemm_fwd_static", "hdqt_gemm_fwd_static_max_bytes",
     "hdqt_gemm_bwd_input_masked", "hdqt_layer_bwd_masked", "hdqt_conv_bwd_masked",
     "hdqt_probe_matrix_clock", "hdqt_wall_clock_khz",
-    "hdqt_xent_saved_size", "hdqt_xent_fwd_workspace_size", "hdqt_xent_bwd_workspace_size", "hdqt_xent_fwd",
+    "hdqt_xent_saved_size", "hdqt_xent_fwd_workspace_size", "hdqt_xent_bwd_workspace_size", "hdqt_xent_step_workspace_size", "hdqt_xent_fwd",
     "hdqt_xent_bwd", "hdqt_xent_step", "hdqt_groupnorm_workspace_size", "hdqt_groupnorm_fwd", "hdqt_groupnorm_bwd",
     "hdqt_clip_grad_norm_workspace_size", "hdqt_grad_norm", "hdqt_clip_grad_norm",
 ]
@@ -233,7 +233,7 @@ def load() -> C.CDLL:
     f32 = C.c_float
     lib.hdqt_xent_saved_size.restype = sz
     lib.hdqt_xent_saved_size.argtypes = [i64]
-    for name in ("hdqt_xent_fwd_workspace_size", "hdqt_xent_bwd_workspace_size"):
+    for name in ("hdqt_xent_fwd_workspace_size", "hdqt_xent_bwd_workspace_size", "hdqt_xent_step_workspace_size"):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [i64, i64, i64, i32]
     rows = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, i32]        # X ... reduction
@@ -957,9 +957,7 @@ def xent_step(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, bias: Opti
         dX, dW, db = _xent_grads(X, W, bias, need)
         saved = torch.empty(M + 1, dtype=torch.float32, device=X.device)
         if workspace is None:
-            lib = load()
-            workspace = _bytes(max(lib.hdqt_xent_fwd_workspace_size(M, K, N, args[10]),
-                                   lib.hdqt_xent_bwd_workspace_size(M, K, N, args[10])), X.device)
+            workspace = _bytes(load().hdqt_xent_step_workspace_size(M, K, N, args[10]), X.device)
         rc = load().hdqt_xent_step(*args, _ptr(loss), _ptr(saved), _ptr(dX), _ptr(dW), _ptr(db), _ptr(workspace),
                                    workspace.numel(), _stream(None))
         if rc:

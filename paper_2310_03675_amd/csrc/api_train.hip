@@ -211,22 +211,26 @@ size_t hdqt_xent_saved_size(int64_t M) { return M < 1 || M >= kMaxDim ? 0 : size
 size_t hdqt_xent_fwd_workspace_size(int64_t M, int64_t K, int64_t N, int dtype)
 {
     const hdqt::XentArgs a = sizes_of(M, K, N, dtype, HDQT_REDUCE_MEAN);
-    return sized(a) ? hdqt::xent_workspace(a, false) : 0;
+    return sized(a) ? hdqt::xent_workspace(a, true, false) : 0;
 }
 
 size_t hdqt_xent_bwd_workspace_size(int64_t M, int64_t K, int64_t N, int dtype)
 {
     const hdqt::XentArgs a = sizes_of(M, K, N, dtype, HDQT_REDUCE_MEAN);
-    return sized(a) ? hdqt::xent_workspace(a, true) : 0;
+    return sized(a) ? hdqt::xent_workspace(a, false, true) : 0;
+}
+
+size_t hdqt_xent_step_workspace_size(int64_t M, int64_t K, int64_t N, int dtype)
+{
+    const hdqt::XentArgs a = sizes_of(M, K, N, dtype, HDQT_REDUCE_MEAN);
+    return sized(a) ? hdqt::xent_workspace(a, true, true) : 0;
 }
 
 static int run_xent(hdqt::XentArgs a, bool forward, bool backward, void* workspace, size_t workspace_bytes, void* stream)
 {
     const int rc = check_xent(a);
     if (rc) return rc;
-    size_t need = forward ? hdqt::xent_workspace(a, false) : 0;
-    if (backward && hdqt::xent_workspace(a, true) > need) need = hdqt::xent_workspace(a, true);
-    if (short_of(workspace, workspace_bytes, need)) return HDQT_EWORKSPACE;
+    if (short_of(workspace, workspace_bytes, hdqt::xent_workspace(a, forward, backward))) return HDQT_EWORKSPACE;
     if (off(workspace, 256)) return HDQT_EALIGN;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;

@@ -43,7 +43,7 @@ struct Library {
     decltype(&hdqt_layer_bwd_masked) bwd_masked;
     decltype(&hdqt_conv_bwd) conv_bwd;
     decltype(&hdqt_conv_bwd_masked) conv_bwd_masked;
-    decltype(&hdqt_xent_fwd_workspace_size) xent_fwd_workspace_size, xent_bwd_workspace_size;
+    decltype(&hdqt_xent_fwd_workspace_size) xent_fwd_workspace_size, xent_bwd_workspace_size, xent_step_workspace_size;
     decltype(&hdqt_xent_fwd) xent_fwd;
     decltype(&hdqt_xent_bwd) xent_bwd;
     decltype(&hdqt_xent_step) xent_step;
@@ -520,8 +520,7 @@ PyObject* xent_step(PyObject* const* a)
     Classifier c(a);
     c.make_grads(Need(a[6]));
     at::Tensor loss = c.loss(), saved = fresh({c.M + 1}, at::kFloat, c.X);
-    const size_t f = lib.xent_fwd_workspace_size(c.M, c.K, c.N, c.dtype), b = lib.xent_bwd_workspace_size(c.M, c.K, c.N, c.dtype);
-    c.make_workspace(f > b ? f : b);
+    c.make_workspace(lib.xent_step_workspace_size(c.M, c.K, c.N, c.dtype));
     const int rc = unlocked([&] {
         return lib.xent_step(address(c.X), c.ldx, address(c.W), c.ldw, address(c.bias), (const int64_t*)address(c.target), c.ignore, c.M, c.K,
                              c.N, c.dtype, c.bias_dtype, c.reduction, (float*)address(loss), (float*)address(saved), c.grad(0), c.grad(1),
@@ -715,6 +714,7 @@ PyObject* bind(PyObject*, PyObject* args)
     find(l.conv_bwd_masked, "hdqt_conv_bwd_masked");
     find(l.xent_fwd_workspace_size, "hdqt_xent_fwd_workspace_size");
     find(l.xent_bwd_workspace_size, "hdqt_xent_bwd_workspace_size");
+    find(l.xent_step_workspace_size, "hdqt_xent_step_workspace_size");
     find(l.xent_fwd, "hdqt_xent_fwd");
     find(l.xent_bwd, "hdqt_xent_bwd");
     find(l.xent_step, "hdqt_xent_step");

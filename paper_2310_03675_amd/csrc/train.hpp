@@ -125,7 +125,7 @@ struct XentArgs {
     const float* dloss;                 // its gradient, as many; null: ones
     void *dX, *dW, *dbias;              // [M, K], [K, N], [N]; any may be null
 };
-size_t xent_workspace(const XentArgs& a, bool backward);
+size_t xent_workspace(const XentArgs& a, bool forward, bool backward);        // both: a step
 // backward: the backward pass will run in the same workspace
 hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hipStream_t stream);
 // forward: the forward pass has just run in the same workspace

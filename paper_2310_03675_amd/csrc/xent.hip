@@ -114,6 +114,8 @@ struct RowArgs {
     uint16_t* dz;                       // [M][step], zeros behind the classes
     int64_t step;
     float* column;                      // [tiles of rows][classes]: dz's sums over a tile's rows; null: not wanted
+    float* z;                           // [M][z_step]: the logits, where the gradients that follow can have them; null: not kept
+    int64_t z_step;
 };
 
 __device__ __forceinline__ float larger_half(float v)
@@ -195,13 +197,23 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
                 }
             }
         if constexpr (!GRAD) {
-            if (any) {
+            if (any && r.pairs) {
 #pragma unroll
                 for (int i = 0; i < NA; ++i)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         if (at == 32 * i + 8 * (e >> 2) + (e & 3)) r.picked[row] = acc[i][j][e];
             }
+            if (P == 3 && r.z && there) {
+                float* to = r.z + row * r.z_step + (int64_t)p.at * TA + class0 + 4 * (lane >> 5);
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<float4*>(to + 32 * i + 8 * q) =
+                            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            }
+            if (!r.pairs) return;
             top = larger_half(top);
             const float base = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
@@ -261,6 +273,7 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
     if constexpr (NB > 3) column(std::integral_constant<int, 3>{});
     static_assert(NB <= 4, "a call for each");
     if constexpr (!GRAD) {
+        if (!r.pairs) return;           // (only the logits are wanted)
         __syncthreads();
         for (int t = threadIdx.x; t < TB; t += 64 * WA * WB) {
             const int64_t row = (int64_t)p.bt * TB + t;
@@ -290,6 +303,40 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
             r.column[(int64_t)p.bt * r.classes + c] = s;
         }
     }
+}
+
+// dz in planes from the logits, where the forward pass has kept them: a workgroup has kRowsOfDz rows of 1024 classes, a thread
+// four classes.
+constexpr int kRowsOfDz = 8;
+__global__ __launch_bounds__(kThreads) void xent_dz_kernel(RowArgs r)
+{
+    const int64_t c = 4 * ((int64_t)blockIdx.x * kThreads + threadIdx.x), row0 = (int64_t)blockIdx.y * kRowsOfDz;
+    if (c >= r.step / 3) return;
+    float column[4] = {};
+#pragma unroll 4
+    for (int64_t row = row0; row < row0 + kRowsOfDz && row < r.M; ++row) {
+        const int64_t target = r.target[row], at = target - r.first_class - c;
+        const bool counted = target != r.ignore;
+        const float lse = r.saved[row], base = lse == -INFINITY ? 0.0f : lse;
+        const float each = r.each && counted ? (r.dloss ? r.dloss[row] : 1.0f) : 1.0f;
+        // (behind the last class there is no logit in memory that anyone has written)
+        const float4 q = c < r.z_step ? *reinterpret_cast<const float4*>(r.z + row * r.z_step + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float z[4] = {q.x, q.y, q.z, q.w};
+        uint32_t s[4][3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float d = exp_of<true>(z[e] - base) - (at == e ? 1.0f : 0.0f), v = counted && c + e < r.classes ? d * each : 0.0f;
+            column[e] += v;
+            split(v, s[e]);
+        }
+        uint16_t* to = r.dz + row * r.step + c / 32 * 96 + c % 32;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(to + 32 * k) = make_uint2(s[0][k] | s[1][k] << 16, s[2][k] | s[3][k] << 16);
+    }
+    if (!r.column) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < r.classes) r.column[(int64_t)blockIdx.y * r.classes + c + e] = column[e];
 }
 
 // ---- gradients: dX (lines of A rows, of B features) and dW (lines of A features, of B classes) ----
@@ -381,16 +428,30 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
                          });
 }
 
+// (four neighbours at a time where rows of both sides come in whole 16 bytes)
+template <int V>
 __global__ __launch_bounds__(kThreads) void xent_add_parts_kernel(OutArgs o, int64_t RA, int64_t RB, uint32_t parts)
 {
     const float factor = factor_of(o);
+    const int64_t j = V * ((int64_t)blockIdx.x * kThreads + threadIdx.x), size = RA * RB;
+    if (j >= RB) return;
     for (int64_t i = blockIdx.y; i < RA; i += gridDim.y) {
-        const int64_t j = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-        if (j >= RB) continue;
-        float v = 0.0f;
-        for (uint32_t k = 0; k < parts; ++k) v += o.slices[((int64_t)k * RA + i) * RB + j];
-        if (o.dtype == kBf16) finish<kBf16>(o, i, j, RB, v, factor);
-        else finish<kF32>(o, i, j, RB, v, factor);
+        const float* from = o.slices + i * RB + j;
+        float v[V] = {};
+#pragma unroll 4
+        for (uint32_t k = 0; k < parts; ++k) {
+            if constexpr (V == 4) {
+                const float4 q = *reinterpret_cast<const float4*>(from + k * size);
+                v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
+            } else {
+                v[0] += from[k * size];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (o.dtype == kBf16) finish<kBf16>(o, i, j + e, RB, v[e], factor);
+            else finish<kF32>(o, i, j + e, RB, v[e], factor);
+        }
     }
 }
 
@@ -496,8 +557,9 @@ __global__ __launch_bounds__(kThreads) void xent_dbias_kernel(const float* colum
 // products make dz from them as they read it: three launches forward and backward.
 
 constexpr int kSmallWaves = 8, kSmallTile = 32;
-constexpr int kSmallStep = 8 * kSmallWaves;         // of the contraction: eight to a wave, four to a half of its lanes
-constexpr int kSmallAhead = 4;                      // steps whose loads are in flight
+constexpr int kSmallAhead = 4;                      // steps of eight of the contraction, four to a half of a wave's lanes, in flight
+constexpr int kSmallSpan = 8 * kSmallAhead;         // of the contraction, side by side: a whole line of memory in fp32
+constexpr int kSmallRound = kSmallSpan * kSmallWaves;
 
 struct SmallArgs {
     float* z;                           // [M][step], null: not wanted
@@ -561,11 +623,11 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_logits_kernel(Xen
     const int64_t c = class0 + line, row = row0 + line;
     const bool class_there = c < a.N, row_there = row < a.M;
     v16f acc = {};
-    for (int64_t base = 8 * wave; base < a.K; base += kSmallAhead * kSmallStep) {
+    for (int64_t base = kSmallSpan * wave; base < a.K; base += kSmallRound) {
         float x[kSmallAhead][4], w[kSmallAhead][4];
 #pragma unroll
         for (int u = 0; u < kSmallAhead; ++u) {
-            const int64_t at = base + u * kSmallStep + 4 * half;
+            const int64_t at = base + 8 * u + 4 * half;
             load4<DT, VEC>(a.X, row * a.ldx + at, row_there ? a.K - at : 0, x[u]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[u][e] = class_there && at + e < a.K ? load_as<DT>(a.W, (at + e) * a.ldw + c) : 0.0f;
@@ -610,13 +672,13 @@ __device__ __forceinline__ float small_dz(float z, int64_t c, int64_t target, fl
     const float base = lse == -INFINITY ? 0.0f : lse;
     return (exp_of<true>(z - base) - (c == target ? 1.0f : 0.0f)) * factor;
 }
-// a part of a contraction: whole steps of all waves
+// a part of a contraction: whole rounds of all waves
 struct Share {
     int64_t begin, end;
 };
 __device__ __forceinline__ Share share_of(int64_t length, uint32_t part, uint32_t parts)
 {
-    const int64_t steps = (length + kSmallStep - 1) / kSmallStep, per = (steps + parts - 1) / parts * kSmallStep, begin = part * per;
+    const int64_t rounds = (length + kSmallRound - 1) / kSmallRound, per = (rounds + parts - 1) / parts * kSmallRound, begin = part * per;
     return {begin < length ? begin : length, begin + per < length ? begin + per : length};
 }
 __device__ __forceinline__ float row_factor(const XentArgs& a, int64_t row)
@@ -642,11 +704,11 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
         const bool counted = row_there && target != a.ignore;
         const float lse = row_there ? a.saved[row] : 0.0f, each = counted ? row_factor(a, row) : 0.0f;
         const Share share = share_of(a.N, part, k.x_parts);
-        for (int64_t base = share.begin + 8 * wave; base < share.end; base += kSmallAhead * kSmallStep) {
+        for (int64_t base = share.begin + kSmallSpan * wave; base < share.end; base += kSmallRound) {
             float z[kSmallAhead][4], w[kSmallAhead][4];
 #pragma unroll
             for (int u = 0; u < kSmallAhead; ++u) {
-                const int64_t at = base + u * kSmallStep + 4 * half;
+                const int64_t at = base + 8 * u + 4 * half;
                 load4<kF32, true>(k.z, row * k.step + at, counted && at < share.end ? 4 : 0, z[u]);
                 load4<DT, VEC>(a.W, f * a.ldw + at, f_there ? share.end - at : 0, w[u]);
             }
@@ -654,7 +716,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
             for (int u = 0; u < kSmallAhead; ++u)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int64_t c = base + u * kSmallStep + 4 * half + e;
+                    const int64_t c = base + 8 * u + 4 * half + e;
                     const float d = counted && c < share.end ? small_dz(z[u][e], c, target, lse, each) : 0.0f;
                     acc = __builtin_amdgcn_mfma_f32_32x32x2f32(d, w[u][e], acc, 0, 0, 0);
                 }
@@ -673,14 +735,14 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
     const bool c_there = c < a.N;
     const Share share = share_of(a.M, part, k.w_parts);
     const bool each = a.reduction == kNone && a.dloss;
-    for (int64_t base = share.begin + 8 * wave; base < share.end; base += kSmallAhead / 2 * kSmallStep) {
+    for (int64_t base = share.begin + kSmallSpan / 2 * wave; base < share.end; base += kSmallRound / 2) {
         float x[kSmallAhead / 2][4], z[kSmallAhead / 2][4], lse[kSmallAhead / 2][4], g[kSmallAhead / 2][4];
         int64_t target[kSmallAhead / 2][4];
 #pragma unroll
         for (int u = 0; u < kSmallAhead / 2; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int64_t row = base + u * kSmallStep + 4 * half + e, r = row < share.end ? row : share.end - 1;
+                const int64_t row = base + 8 * u + 4 * half + e, r = row < share.end ? row : share.end - 1;
                 x[u][e] = row >= share.end ? 0.0f : f < a.K ? load_as<DT>(a.X, row * a.ldx + f) : f == a.K ? 1.0f : 0.0f;
                 z[u][e] = row < share.end && c_there ? k.z[row * k.step + c] : 0.0f;
                 target[u][e] = row < share.end ? a.target[r] : a.ignore;
@@ -710,6 +772,59 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
     });
 }
 
+// dW and db of few rows (up to MM): a thread has four classes' dz of all of them in registers and writes kOuterLines lines of
+// dW, so that only dW itself is moved (1 x 4096 x 128000 in fp32: 2 GB).
+constexpr int kOuterLines = 64, kOuterRows = 16;
+template <int DT, int MM>
+__global__ __launch_bounds__(kThreads) void xent_outer_kernel(XentArgs a, SmallArgs k)
+{
+    __shared__ float x[MM][kOuterLines];
+    const int64_t f0 = (int64_t)blockIdx.y * kOuterLines, c0 = (int64_t)blockIdx.x * (4 * kThreads) + threadIdx.x;
+    const float factor = (a.reduction == kNone ? 1.0f : (a.dloss ? *a.dloss : 1.0f)) * a.saved[a.M];
+    for (int i = threadIdx.x; i < MM * kOuterLines; i += kThreads) {
+        const int m = i / kOuterLines, f = i % kOuterLines;
+        x[m][f] = m < a.M && f0 + f < a.K ? load_as<DT>(a.X, m * a.ldx + f0 + f) : 0.0f;
+    }
+    float d[MM][4];
+#pragma unroll
+    for (int m = 0; m < MM; ++m) {
+        const bool counted = m < a.M && a.target[m < a.M ? m : 0] != a.ignore;
+        const int64_t target = counted ? a.target[m] : -1;
+        const float lse = counted ? a.saved[m] : 0.0f, each = counted ? row_factor(a, m) * factor : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t c = c0 + e * kThreads;
+            d[m][e] = counted && c < a.N ? small_dz(k.z[m * k.step + c], c, target, lse, each) : 0.0f;
+        }
+    }
+    __syncthreads();
+    if (a.dbias && blockIdx.y == 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t c = c0 + e * kThreads;
+            float s = 0.0f;
+#pragma unroll
+            for (int m = 0; m < MM; ++m) s += d[m][e];
+            if (c >= a.N) continue;
+            if (a.bias_dtype == kBf16) store_as<kBf16>(a.dbias, c, s);
+            else store_as<kF32>(a.dbias, c, s);
+        }
+    if (!a.dW) return;
+    const int lines = a.K - f0 < kOuterLines ? (int)(a.K - f0) : kOuterLines;
+    for (int f = 0; f < lines; ++f) {
+        float s[4] = {};
+#pragma unroll
+        for (int m = 0; m < MM; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = fmaf(x[m][f], d[m][e], s[e]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t c = c0 + e * kThreads;
+            if (c < a.N) store_as<DT>(a.dW, (f0 + f) * a.N + c, s[e]);
+        }
+    }
+}
+
 // dX's parts added up, and dW's and db's behind them
 __global__ __launch_bounds__(kThreads) void xent_small_add_kernel(XentArgs a, SmallArgs k, int64_t of_x, int64_t of_w)
 {
@@ -736,28 +851,37 @@ __global__ __launch_bounds__(kThreads) void xent_small_add_kernel(XentArgs a, Sm
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
-// Tiles: large ones of 256 x 256 (one plane) or 256 x 128 (three), small ones of 128 x 128.
-struct Tile {
+// How a product is cut: large tiles of 256 x 256 (one plane) or 256 x 128 (three), or small ones of 128 x 128, and the
+// contraction in parts, which another launch adds up.
+struct Cut {
     int a, b;
     bool large;
+    uint32_t parts;
+    double us;
 };
-Tile tile_of(int64_t RA, int64_t RB, int planes)
-{
-    const Tile big{256, planes == 1 ? 256 : 128, true};
-    const int64_t tiles = ((RA + big.a - 1) / big.a) * ((RB + big.b - 1) / big.b);
-    return tiles >= 192 ? big : Tile{128, 128, false};
-}
 
-// Products of few tiles: the contraction in parts, so that every compute unit has what workgroups it holds (two of the small
-// tiles of one plane, else one), each part at least 512 long.
-uint32_t parts_of(int64_t RA, int64_t RB, int64_t D, int planes)
+// The cut that a simple model of the time likes best, microseconds: rounds of the workgroups that the chip holds (256; 512 of the
+// small tiles of one plane), each as many stages as a part has, at what a stage takes on a full chip; and for parts the
+// sums written, read again at 4 TB/s, and a launch; 5 to begin and end a round.  (Stages measured, large and small tiles: 8192 x 4096 x 8192 in bfloat16
+// 1.85 and 1.05, 0.75 where a compute unit has one; in fp32 2.8 and 1.35.  What the model chooses between, forward, both ways:
+// 2048 cubed in bfloat16 51 and 30 us, 8192 x 4096 x 8192 474 and 537; in fp32 137 and 94, 512 x 1024 x 32768 174 and 196.)
+Cut cut_of(int64_t RA, int64_t RB, int64_t D, int planes, bool may_split)
 {
-    const Tile t = tile_of(RA, RB, planes);
-    const int64_t tiles = ((RA + t.a - 1) / t.a) * ((RB + t.b - 1) / t.b), full = t.large || planes > 1 ? 256 : 512;
-    const int64_t least = planes == 1 ? 512 : 128;
-    int64_t parts = full / tiles;
-    if (parts > D / least) parts = D / least;
-    return (uint32_t)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    Cut best{};
+    const int64_t stages = (D + bf16::stage_of(planes) - 1) / bf16::stage_of(planes);
+    for (const bool large : {true, false}) {
+        Cut c{large ? 256 : 128, large && planes == 1 ? 256 : 128, large, 1, 0.0};
+        const int64_t tiles = ((RA + c.a - 1) / c.a) * ((RB + c.b - 1) / c.b);
+        for (int64_t parts = 1; parts <= 64; ++parts) {
+            if (parts > 1 && (!may_split || tiles * parts > 1024 || stages < 4 * parts)) break;
+            const int64_t groups = tiles * parts, slots = !large && planes == 1 ? 512 : 256;
+            const double stage = large ? (planes == 1 ? 1.85 : 2.8) : planes == 1 ? (groups > 256 ? 1.05 : 0.75) : 1.35;
+            double t = (double)((groups + slots - 1) / slots) * ((double)((stages + parts - 1) / parts) * stage + 5.0);
+            if (parts > 1) t += 6.0 + 4.0 * (double)(2 * parts + 1) * (double)RA * (double)RB / 4.0e6;
+            if (best.a == 0 || t < best.us) { best = c; best.parts = (uint32_t)parts; best.us = t; }
+        }
+    }
+    return best;
 }
 
 // How a call is cut, and where its pieces of the workspace lie.
@@ -770,9 +894,10 @@ struct Plan {
     size_t x, w;                        // bytes of X packed, of W or a piece of it packed
     size_t pairs, picked, rows;         // forward
     size_t dz, sums, slices, column;    // backward
+    size_t z;                           // the logits, in front of those
 };
 
-bool whole(const void* p, int64_t ld, int64_t cols, int dtype)
+bool whole_rows(const void* p, int64_t ld, int64_t cols, int dtype)
 {
     return dtype == kBf16 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld < (int64_t)1 << 21;
 }
@@ -782,8 +907,8 @@ Plan plan_of(const XentArgs& a, bool sizes)
 {
     Plan p{};
     p.planes = a.dtype == kF32 ? 3 : 1;
-    p.pack_x = sizes || !whole(a.X, a.ldx, a.K, a.dtype);
-    p.pack_w = sizes || !whole(a.W, a.ldw, a.N, a.dtype);
+    p.pack_x = sizes || !whole_rows(a.X, a.ldx, a.K, a.dtype);
+    p.pack_w = sizes || !whole_rows(a.W, a.ldw, a.N, a.dtype);
     // dz of a piece stays within 128 MB, which the memory-side cache holds between its writer and its readers
     p.piece = ((int64_t)128 << 20) / (2 * p.planes * a.M) / 256 * 256;
     if (p.piece < 1024) p.piece = 1024;
@@ -800,11 +925,13 @@ Plan plan_of(const XentArgs& a, bool sizes)
     p.picked = p.rows = up256(sizeof(float) * a.M);
     p.dz = up256(2 * (size_t)a.M * p.dz_step);
     p.sums = p.piece < a.N ? up256(sizeof(float) * a.M * a.K) : 0;
-    p.column = up256(sizeof(float) * (size_t)((a.M + 127) / 128) * p.piece);
+    p.column = up256(sizeof(float) * (size_t)((a.M + kRowsOfDz - 1) / kRowsOfDz) * p.piece);
+    // in fp32, where the classes are one piece, a step keeps the logits: 4 bytes each, written and read, against six products
+    if (p.planes == 3 && p.piece == a.N) p.z = up256(sizeof(float) * (size_t)a.M * up(a.N, 256));
     size_t most = 0;
     for (const int64_t classes : {p.piece, a.N - (a.N - 1) / p.piece * p.piece}) {          // (the last piece may be cut another way)
-        const uint32_t px = parts_of(a.M, a.K, classes, p.planes), pw = parts_of(a.K, classes, a.M, p.planes);
-        const size_t sx = px > 1 ? (size_t)px * a.M * a.K : 0, sw = pw > 1 ? (size_t)pw * a.K * classes : 0;
+        const size_t px = cut_of(a.M, a.K, classes, p.planes, true).parts, pw = cut_of(a.K, classes, a.M, p.planes, true).parts;
+        const size_t sx = px > 1 ? px * a.M * a.K : 0, sw = pw > 1 ? pw * a.K * classes : 0;
         if (sx > most) most = sx;
         if (sw > most) most = sw;
     }
@@ -855,8 +982,13 @@ hipError_t launch_gradient(int tag, const bf16::Args& g, const OutArgs& o, int p
     }
     if (g.parts > 1) {
         ProfileScope ps(K_XENT_ADD_PARTS, stream);
-        hipLaunchKernelGGL(xent_add_parts_kernel, dim3((uint32_t)((g.RB + kThreads - 1) / kThreads), (uint32_t)(g.RA < 65535 ? g.RA : 65535)),
-                           dim3(kThreads), 0, stream, o, g.RA, g.RB, g.parts);
+        const uint32_t down = (uint32_t)(g.RA < 65535 ? g.RA : 65535);
+        if (g.RB % 4 == 0)
+            hipLaunchKernelGGL(xent_add_parts_kernel<4>, dim3((uint32_t)((g.RB / 4 + kThreads - 1) / kThreads), down), dim3(kThreads), 0, stream,
+                               o, g.RA, g.RB, g.parts);
+        else
+            hipLaunchKernelGGL(xent_add_parts_kernel<1>, dim3((uint32_t)((g.RB + kThreads - 1) / kThreads), down), dim3(kThreads), 0, stream,
+                               o, g.RA, g.RB, g.parts);
     }
     return hipGetLastError();
 }
@@ -909,10 +1041,20 @@ RowArgs rows_of(const XentArgs& a, int64_t first, int64_t classes)
 
 constexpr int64_t kSmallLogits = (int64_t)8 << 20;          // of 4 bytes
 
-// (measured: see the kernels' comment)
+// Whether a problem is small.  bfloat16: the large products' seven launches are what they take (128 x 512 x 1000 44 us, here 35;
+// 512 x 512 x 100 49 and 32; 2048 x 512 x 100 52 and 53), unless W is large, whose single elements are read here (1 x 512 x 33000
+// 72 and 118).  fp32: by the time of a step, microseconds, here three products at 50 TFLOP/s on whole tiles and a fifth
+// more, there the cuts' and what the packing and the logits move at 4 TB/s (512 x 2048 x 1000 152 us, the large products
+// 178; 2048 x 512 x 1000 175 and 136; 8192 x 2048 x 100 412 and 240; 1 x 4096 x 128000 1543 and 4763).
 bool small_problem(const XentArgs& a)
 {
-    return a.M * a.N <= kSmallLogits && a.M * a.N <= ((int64_t)1 << 28) / a.K;
+    if (a.M * a.N > kSmallLogits) return false;
+    if (a.dtype == kBf16) return a.K * a.N <= ((int64_t)3 << 19) && a.M * a.N <= ((int64_t)1 << 26) / a.K;
+    const double kn = (double)a.K * (double)a.N, mk = (double)a.M * (double)a.K, mn = (double)a.M * (double)a.N;
+    const double here = 18.0 + 3.6 * (double)up(a.M, kSmallTile) * (double)up(a.N, kSmallTile) * (double)a.K / 25.0e6;
+    const double large = 60.0 + cut_of(a.N, a.M, a.K, 3, false).us + cut_of(a.M, a.K, a.N, 3, true).us + cut_of(a.K, a.N, a.M, 3, true).us +
+                         (10.0 * (kn + mk) + 14.0 * mn) / 4.0e6;
+    return here <= large;
 }
 
 struct SmallPlan {
@@ -926,9 +1068,9 @@ SmallPlan small_plan(const XentArgs& a)
     p.class_tiles = (a.N + kSmallTile - 1) / kSmallTile;
     p.row_tiles = (a.M + kSmallTile - 1) / kSmallTile;
     p.step = up(a.N, 4);
-    // where tiles are few several workgroups share a contraction: up to two for a compute unit, eight steps each at least
+    // where tiles are few several workgroups share a contraction: up to two for a compute unit, two rounds each at least
     auto parts = [](int64_t tiles, int64_t length) {
-        const int64_t most = length / (8 * kSmallStep), n = 512 / tiles < most ? 512 / tiles : most;
+        const int64_t most = length / (2 * kSmallRound), n = 512 / tiles < most ? 512 / tiles : most;
         return (uint32_t)(n < 1 ? 1 : n);
     };
     p.x_parts = parts(p.row_tiles * ((a.K + kSmallTile - 1) / kSmallTile), a.N);
@@ -999,7 +1141,17 @@ hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* a
     const uint32_t w_end = (uint32_t)((a.K + (a.dbias ? 1 : 0) + kSmallTile - 1) / kSmallTile);
     k.w_first = a.dW ? 0 : a.dbias ? w_end - 1 : w_end;
     k.w_tiles = (w_end - k.w_first) * k.w_across;
-    {
+    if (k.w_tiles && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20) {         // (of fewer outputs a launch more is not worth it)
+        k.w_tiles = 0;
+        const dim3 grid((uint32_t)((a.N + 4 * kThreads - 1) / (4 * kThreads)), a.dW ? (uint32_t)((a.K + kOuterLines - 1) / kOuterLines) : 1);
+        ProfileScope ps(K_XENT_DW, stream);
+        with_small(a, false, [&](auto dt, auto) {
+            if (a.M <= 2) hipLaunchKernelGGL((xent_outer_kernel<dt.value, 2>), grid, dim3(kThreads), 0, stream, a, k);
+            else if (a.M <= 8) hipLaunchKernelGGL((xent_outer_kernel<dt.value, 8>), grid, dim3(kThreads), 0, stream, a, k);
+            else hipLaunchKernelGGL((xent_outer_kernel<dt.value, kOuterRows>), grid, dim3(kThreads), 0, stream, a, k);
+        });
+    }
+    if (k.x_tiles || k.w_tiles) {
         ProfileScope ps(K_XENT_DX, stream);
         with_small(a, fours(a.W, a.ldw, a.N, a.dtype), [&](auto dt, auto vec) {
             hipLaunchKernelGGL((xent_small_gradients_kernel<dt.value, vec.value>), dim3(k.x_tiles * k.x_parts + k.w_tiles * k.w_parts), dim3(64 * kSmallWaves),
@@ -1017,14 +1169,15 @@ hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* a
 
 } // namespace
 
-size_t xent_workspace(const XentArgs& a, bool backward)
+size_t xent_workspace(const XentArgs& a, bool forward, bool backward)
 {
     if (small_problem(a)) {
         const SmallPlan p = small_plan(a);
         return p.z + p.pairs + p.picked + p.rows + (backward ? p.x_slices + p.w_slices : 0);
     }
     const Plan p = plan_of(a, true);
-    return p.x + p.w + (backward ? p.dz + p.sums + p.slices + p.column : p.pairs + p.picked + p.rows);
+    const size_t f = forward ? p.pairs + p.picked + p.rows : 0, b = backward ? p.dz + p.sums + p.slices + p.column : 0;
+    return p.x + p.w + (backward ? p.z : 0) + (f > b ? f : b);
 }
 
 hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hipStream_t stream)
@@ -1032,9 +1185,10 @@ hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hi
     if (small_problem(a)) return launch_small_logits(a, small_plan(a), static_cast<char*>(workspace), true, backward, stream);
     const Plan p = plan_of(a, false);
     char* at = static_cast<char*>(workspace) + p.x + p.w;
-    float2* pairs = reinterpret_cast<float2*>(at);
-    float* picked = reinterpret_cast<float*>(at + p.pairs);
-    float* rows = a.reduction == kNone ? a.loss : reinterpret_cast<float*>(at + p.pairs + p.picked);
+    char* rest = at + (backward ? p.z : 0);
+    float2* pairs = reinterpret_cast<float2*>(rest);
+    float* picked = reinterpret_cast<float*>(rest + p.pairs);
+    float* rows = a.reduction == kNone ? a.loss : reinterpret_cast<float*>(rest + p.pairs + p.picked);
     hipError_t e;
     int64_t tiles = 0;
     for (int64_t first = 0; first < a.N; first += p.piece) {
@@ -1044,7 +1198,9 @@ hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hi
         RowArgs r = rows_of(a, first, classes);
         r.pairs = pairs + tiles * a.M;
         r.picked = picked;
-        const Tile t = tile_of(classes, a.M, p.planes);
+        if (backward && p.z) r.z = reinterpret_cast<float*>(at);
+        r.z_step = up(a.N, 256);
+        const Cut t = cut_of(classes, a.M, a.K, p.planes, false);
         const bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, t.a, t.b, 1);
         if ((e = launch_logits<false>(K_XENT_LOGITS, g, r, p.planes, t.large, stream)) != hipSuccess) return e;
         tiles += g.n_at;
@@ -1062,7 +1218,8 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
         return launch_small_gradients(a, s, static_cast<char*>(workspace), stream);
     }
     const Plan p = plan_of(a, false);
-    char* at = static_cast<char*>(workspace) + p.x + p.w;
+    float* z = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.x + p.w);
+    char* at = reinterpret_cast<char*>(z) + p.z;
     for (int64_t first = 0; first < a.N; first += p.piece) {
         const int64_t classes = a.N - first < p.piece ? a.N - first : p.piece;
         Operands o;
@@ -1073,10 +1230,22 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
         r.dz = reinterpret_cast<uint16_t*>(at);
         r.step = p.dz_step;
         if (a.dbias) r.column = reinterpret_cast<float*>(at + p.dz + p.sums + p.slices);
-        Tile t = tile_of(classes, a.M, p.planes);
+        Cut t = cut_of(classes, a.M, a.K, p.planes, false);
         bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, t.a, t.b, 1);
-        const uint32_t row_tiles = g.n_bt;
-        if ((e = launch_logits<true>(K_XENT_DLOGITS, g, r, p.planes, t.large, stream)) != hipSuccess) return e;
+        uint32_t row_tiles = g.n_bt;
+        if (p.z) {
+            r.z = z;
+            r.z_step = up(a.N, 256);
+            if (!forward && (e = launch_logits<false>(K_XENT_LOGITS, g, r, p.planes, t.large, stream)) != hipSuccess) return e;
+            row_tiles = (uint32_t)((a.M + kRowsOfDz - 1) / kRowsOfDz);
+            ProfileScope ps(K_XENT_DLOGITS, stream);
+            hipLaunchKernelGGL(xent_dz_kernel, dim3((uint32_t)((p.dz_step / 3 + 4 * kThreads - 1) / (4 * kThreads)), row_tiles), dim3(kThreads), 0,
+                               stream, r);
+            e = hipGetLastError();
+        } else {
+            e = launch_logits<true>(K_XENT_DLOGITS, g, r, p.planes, t.large, stream);
+        }
+        if (e != hipSuccess) return e;
         const bf16::Side dz{r.dz, r.step};
         OutArgs out{};
         out.dtype = a.dtype; out.share = a.saved + a.M; out.dloss = r.each ? nullptr : a.dloss;
@@ -1087,15 +1256,15 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
             x.out = a.dX; x.step = a.K;
             x.sums = p.sums ? reinterpret_cast<float*>(at + p.dz) : nullptr;
             x.first_piece = first == 0; x.last_piece = first + classes == a.N;
-            t = tile_of(a.M, a.K, p.planes);
-            g = bf16::plan(dz, o.w, a.M, a.K, classes, p.planes, t.a, t.b, parts_of(a.M, a.K, classes, p.planes));
+            t = cut_of(a.M, a.K, classes, p.planes, true);
+            g = bf16::plan(dz, o.w, a.M, a.K, classes, p.planes, t.a, t.b, t.parts);
             if ((e = launch_gradient<kAlong>(K_XENT_DX, g, x, p.planes, t.large, stream)) != hipSuccess) return e;
         }
         if (a.dW) {
             OutArgs w = out;
             w.out = static_cast<char*>(a.dW) + first * dtype_size(a.dtype); w.step = a.N;
-            t = tile_of(a.K, classes, p.planes);
-            g = bf16::plan(o.x, dz, a.K, classes, a.M, p.planes, t.a, t.b, parts_of(a.K, classes, a.M, p.planes));
+            t = cut_of(a.K, classes, a.M, p.planes, true);
+            g = bf16::plan(o.x, dz, a.K, classes, a.M, p.planes, t.a, t.b, t.parts);
             if ((e = launch_gradient<kDown>(K_XENT_DW, g, w, p.planes, t.large, stream)) != hipSuccess) return e;
         }
         if (a.dbias) {

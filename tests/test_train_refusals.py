@@ -50,7 +50,7 @@ def test_xent_refusals(name):
 def test_xent_sizes():
     lib = B.load()
     assert lib.hdqt_xent_saved_size(0) == 0 and lib.hdqt_xent_saved_size(7) >= 28
-    for f in (lib.hdqt_xent_fwd_workspace_size, lib.hdqt_xent_bwd_workspace_size):
+    for f in (lib.hdqt_xent_fwd_workspace_size, lib.hdqt_xent_bwd_workspace_size, lib.hdqt_xent_step_workspace_size):
         assert f(0, 64, 100, 0) == 0 and f(32, 64, 100, 5) == 0 and f(1 << 23, 64, 100, 0) == 0
         assert 0 < f(32, 64, 100, 0) < 1 << 20
     # what the backward call holds does not grow with the logits
