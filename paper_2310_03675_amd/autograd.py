@@ -251,6 +251,102 @@ class Unfold(torch.autograd.Function):
         return dAct, None, None, None
 
 
+class CrossEntropy(torch.autograd.Function):
+    """Softmax cross entropy of the classifier X W + bias (hdqt_xent_fwd / hdqt_xent_bwd): the logits are not kept
+    between the passes, nor formed as a whole.  X [M, K], W [K, N], both fp32 or bfloat16, target int64 [M]."""
+
+    @staticmethod
+    def forward(ctx, X, W, bias, target, ignore_index: int, reduction: str):
+        loss, saved = B.xent_fwd(X, W, target, bias, ignore_index, reduction)
+        ctx.save_for_backward(X, W, bias, target, saved)
+        ctx.how = ignore_index, reduction
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        X, W, bias, target, saved = ctx.saved_tensors
+        dX, dW, db = B.xent_bwd(dloss.contiguous(), X, W, target, saved, bias, *ctx.how, need=tuple(ctx.needs_input_grad[:3]))
+        return dX, dW, db, None, None, None
+
+
+class GroupNorm(torch.autograd.Function):
+    """Group normalisation with an activation, x [images, ..., channels] contiguous (hdqt_groupnorm_fwd /
+    hdqt_groupnorm_bwd): x and the groups' statistics are what is kept for the backward pass."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups: int, eps: float, act: str):
+        y, saved = B.groupnorm_fwd(x, groups, weight, bias, eps, act)
+        ctx.save_for_backward(x, weight, bias, saved)
+        ctx.how = groups, act
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, saved = ctx.saved_tensors
+        groups, act = ctx.how
+        dx, dw, db = B.groupnorm_bwd(dy.contiguous(), x, saved, groups, weight, bias, act, need=tuple(ctx.needs_input_grad[:3]))
+        return dx, dw, db, None, None, None
+
+
+class GroupNormAct(torch.nn.Module):
+    """y = act(group norm(x)), act "none", "relu" or "silu", on activations [B, C, H, W] as layers hand them on: what comes
+    out of a layer's product has its channels innermost, which is how this reads and leaves them (an
+    activation in channel planes is copied first)."""
+
+    def __init__(self, groups: int, channels: int, eps: float = 1e-5, act: str = "none", device=None):
+        super().__init__()
+        if channels % groups:
+            raise ValueError(f"{channels} channels are no whole groups of {groups}")
+        self.groups, self.eps, self.act = groups, eps, act
+        self.weight = torch.nn.Parameter(torch.ones(channels, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(channels, device=device))
+
+    def forward(self, x):
+        y = GroupNorm.apply(x.permute(0, 2, 3, 1).contiguous(), self.weight, self.bias, self.groups, self.eps, self.act)
+        return y.permute(0, 3, 1, 2)
+
+
+class ClassifierLoss(torch.nn.Module):
+    """A linear classifier and its softmax cross entropy in one, for heads that grow with the tasks of class incremental
+    training: `classes` of its columns are in use, the weight keeps room for the rest.  forward(x, target) is the
+    loss; logits(x), for evaluation, is PyTorch's product."""
+
+    def __init__(self, in_features: int, num_classes: int, bias: bool = True, classes: Optional[int] = None, ignore_index: int = -100,
+                 reduction: str = "mean", device=None):
+        super().__init__()
+        w = torch.empty(in_features, num_classes, device=device)
+        torch.nn.init.normal_(w, std=in_features ** -0.5)
+        self.weight = torch.nn.Parameter(w)
+        self.bias = torch.nn.Parameter(torch.zeros(num_classes, device=device)) if bias else None
+        self.classes = num_classes if classes is None else classes
+        self.ignore_index, self.reduction = ignore_index, reduction
+
+    def _used(self):
+        n = self.classes
+        return self.weight[:, :n], None if self.bias is None else self.bias[:n]
+
+    def forward(self, x, target):
+        W, b = self._used()
+        return CrossEntropy.apply(x.reshape(-1, x.shape[-1]).contiguous(), W, b, target.reshape(-1).contiguous(), self.ignore_index,
+                                  self.reduction)
+
+    def logits(self, x):
+        W, b = self._used()
+        z = x @ W
+        return z if b is None else z + b
+
+
+def clip_gradients(parameters, max_norm: float, norm_type: float = 2.0, eps: float = 1e-6) -> torch.Tensor:
+    """The norm of the parameters' gradients together, which are multiplied in place by min(1, max_norm / (norm + eps))
+    (hdqt_clip_grad_norm).  The norm stays on the device: nothing waits for it."""
+    grads = [p.grad for p in parameters if p.grad is not None]
+    if not grads:
+        return torch.zeros(())
+    return B.clip_grad_norm(grads, max_norm, norm_type, eps)
+
+
 class HdqtLinear(torch.nn.Module):
     """y = x W + bias with the matmul and its gradients quantized; inputs of any
     leading shape are flattened to [M, K]."""
