@@ -533,7 +533,10 @@ typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
  *             backward call with the same arguments; private to the library
  *   dX, dW    [M, K] and [K, N], dense, of `dtype`; dbias [N] of bias_dtype; any may be NULL (one must not)
  *   dloss     fp32, M values for HDQT_REDUCE_NONE, else one; NULL: ones
- *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd,step}_workspace_size (0 for invalid arguments)
+ *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd,step}_workspace_size (0 for invalid arguments): besides the above, X
+ *             and W (as a whole up to 256 MB, else a piece) in the form that the products take, where they are fp32 or
+ *             their rows are no whole 16 bytes
+ * HDQT_EINVAL_DIM for K above 2^21, M or N above 4 194 240.
  * hdqt_xent_step is the forward and the backward call with dloss = 1.  Its backward half takes the logits from the
  * forward half where those fit the workspace's bounds (fp32, all classes one piece; and small problems).
  * bfloat16: products of bfloat16 with sums in 32 bits; dz is rounded to bfloat16 before its products.

@@ -11,6 +11,7 @@ using hdqt::hip_fail;
 
 constexpr int64_t kMaxDim = (int64_t)65535 * 64 + 1;        // as for the products
 constexpr int64_t kMaxElems = (int64_t)1 << 40;
+constexpr int64_t kMaxFeatures = (int64_t)1 << 21;          // of a classifier: 128 rows of three planes within 32 bits of bytes
 
 bool known_dtype(int d) { return d == HDQT_F32 || d == HDQT_BF16; }
 bool off(const void* p, int64_t size) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)size != 0; }
@@ -119,7 +120,7 @@ int check_xent(const hdqt::XentArgs& a)
 {
     if (!a.X || !a.W || !a.target || !a.saved) return HDQT_EINVAL_NULL;
     if (!known_dtype(a.dtype) || !known_dtype(a.bias_dtype)) return HDQT_EINVAL_DTYPE;
-    if (a.M < 1 || a.K < 1 || a.N < 1 || a.M >= kMaxDim || a.K >= kMaxDim || a.N >= kMaxDim) return HDQT_EINVAL_DIM;
+    if (a.M < 1 || a.K < 1 || a.N < 1 || a.M >= kMaxDim || a.K > kMaxFeatures || a.N >= kMaxDim) return HDQT_EINVAL_DIM;
     if (a.ldx < a.K || a.ldw < a.N || a.ldx > kMaxElems / a.M || a.ldw > kMaxElems / a.K) return HDQT_EINVAL_DIM;
     if (a.reduction != HDQT_REDUCE_NONE && a.reduction != HDQT_REDUCE_MEAN && a.reduction != HDQT_REDUCE_SUM) return HDQT_EINVAL_OPTION;
     const int64_t size = hdqt::dtype_size(a.dtype), bsize = hdqt::dtype_size(a.bias_dtype);
@@ -141,7 +142,7 @@ hdqt::XentArgs sizes_of(int64_t M, int64_t K, int64_t N, int dtype, int reductio
 
 bool sized(const hdqt::XentArgs& a)
 {
-    return a.M >= 1 && a.K >= 1 && a.N >= 1 && a.M < kMaxDim && a.K < kMaxDim && a.N < kMaxDim && known_dtype(a.dtype) &&
+    return a.M >= 1 && a.K >= 1 && a.N >= 1 && a.M < kMaxDim && a.K <= kMaxFeatures && a.N < kMaxDim && known_dtype(a.dtype) &&
            a.K <= kMaxElems / a.M && a.N <= kMaxElems / a.K;
 }
 

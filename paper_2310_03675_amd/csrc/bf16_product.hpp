@@ -144,7 +144,8 @@ template <int MODE, int T, int WAVES>
 struct Panel<3, MODE, T, WAVES> {
     static constexpr int kStage = 32, kPieces = MODE == kAlong ? 12 : 12 * T / 32, kBytes = 192 * T;
     static constexpr int kLoads = kBytes / (1024 * WAVES);
-    static_assert(kLoads >= 1 && kLoads * 1024 * WAVES == kBytes && T % 128 == 0, "whole loads, four blocks of columns");
+    static_assert(kLoads >= 1 && kLoads * 1024 * WAVES == kBytes && T % 64 == 0, "whole loads, blocks of columns to turn");
+    static constexpr int kTurns = T >= 128 ? 3 : 1;          // (of two blocks only pairs of rows are kept apart)
 
     uint32_t off[kLoads];
     int64_t rows_left, step;        // kDown: rows of the whole contraction
@@ -161,7 +162,7 @@ struct Panel<3, MODE, T, WAVES> {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int g = (wave * kLoads + j) * 64 + lane, row = g / kPieces, at = g % kPieces;
-            const int piece = MODE == kAlong ? at ^ ((row >> 2) & 1) : ((at / 12) ^ (row & 3)) * 12 + at % 12;
+            const int piece = MODE == kAlong ? at ^ ((row >> 2) & 1) : ((at / 12) ^ (row & kTurns)) * 12 + at % 12;
             off[j] = (uint32_t)row * (uint32_t)step * 2 + 16 * piece;
             if (MODE == kDown && 8 * piece >= room) off[j] = kOutside;
         }
@@ -226,7 +227,7 @@ struct Fragments<3, MODE, T, N> {
             const int m = (lane >> 2) & 3, k = 8 * (lane >> 5) + m;
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                at[i] = k * 6 * T + 192 * (((line0 >> 5) + i) ^ m) + 2 * (16 * ((lane >> 4) & 1) + 4 * (lane & 3));
+                at[i] = k * 6 * T + 192 * (((line0 >> 5) + i) ^ (m & (T >= 128 ? 3 : 1))) + 2 * (16 * ((lane >> 4) & 1) + 4 * (lane & 3));
         }
     }
     __device__ __forceinline__ v8b read(const uint8_t* lds, int i, int q, int plane) const

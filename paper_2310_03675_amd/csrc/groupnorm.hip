@@ -120,6 +120,40 @@ __device__ __forceinline__ void join(float& n, float& mean, float& m2, float on,
     n = sum;
 }
 
+// 16 bytes of a tensor, or one element in x
+template <int DT, int V>
+__device__ __forceinline__ uint4 hold(const void* p, int64_t i)
+{
+    if constexpr (V == 1) return make_uint4(DT == kBf16 ? static_cast<const uint16_t*>(p)[i] : static_cast<const uint32_t*>(p)[i], 0, 0, 0);
+    else return *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * (16 / V));
+}
+template <int DT, int V>
+__device__ __forceinline__ float held(const uint4& q, int j)
+{
+    const uint32_t w = DT == kF32 ? (j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w)
+                                  : (j / 2 == 0 ? q.x : j / 2 == 1 ? q.y : j / 2 == 2 ? q.z : q.w);
+    return DT == kF32 ? __uint_as_float(w) : __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
+}
+
+struct Two {
+    uint4 x, dy;
+};
+
+// take(load(p)) for a thread's pixels, AHEAD of them loaded before the first is taken
+template <int DT, int V, int AHEAD, class L, class F>
+__device__ __forceinline__ void each_vector(const Spot& s, uint32_t step, L load, F take)
+{
+    int64_t p = s.p;
+    for (; p + (AHEAD - 1) * (int64_t)step < s.end; p += AHEAD * (int64_t)step) {
+        decltype(load(p)) q[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) q[u] = load(p + u * (int64_t)step);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) take(q[u]);
+    }
+    for (; p < s.end; p += step) take(load(p));
+}
+
 // parts[image][slice][channel]: mean and sum of squares around it
 template <int DT, int V>
 __global__ __launch_bounds__(kThreads) void norm_fwd_sums_kernel(NormArgs a, Cut k, float2* parts)
@@ -129,18 +163,16 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_sums_kernel(NormArgs a, Cut
     float first[V], s1[V] = {}, s2[V] = {}, n = 0.0f;
     if (s.c >= 0 && s.p < s.end) {
         load_vec<DT, V>(a.x, s.base + s.p * a.C + s.c, first);
-#pragma unroll 4
-        for (int64_t p = s.p; p < s.end; p += k.ty) {
-            float v[V];
-            load_vec<DT, V>(a.x, s.base + p * a.C + s.c, v);
+        auto take = [&](const uint4& q) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = v[j] - first[j];
+                const float d = held<DT, V>(q, j) - first[j];
                 s1[j] += d;
                 s2[j] = fmaf(d, d, s2[j]);
             }
             n += 1.0f;
-        }
+        };
+        each_vector<DT, V, 8>(s, k.ty, [&](int64_t p) { return hold<DT, V>(a.x, s.base + p * a.C + s.c); }, take);
     }
     float mean[V], m2[V];
 #pragma unroll
@@ -255,20 +287,19 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(NormArgs a, Cut
     float s1[V] = {}, s2[V] = {};
     if (s.c >= 0 && s.p < s.end) {
         const Channel<V> ch(a, blockIdx.z, s.c);
-#pragma unroll 2
-        for (int64_t p = s.p; p < s.end; p += k.ty) {
-            const int64_t at = s.base + p * a.C + s.c;
-            float v[V], d[V];
-            load_vec<DT, V>(a.x, at, v);
-            load_vec<DT, V>(a.dy, at, d);
+        auto take = [&](const Two& q) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float xh = (v[j] - ch.mean[j]) * ch.rstd[j];
-                d[j] *= act_slope<ACT>(fmaf(xh, ch.w[j], ch.b[j]));
-                s1[j] += d[j];
-                s2[j] = fmaf(d[j], xh, s2[j]);
+                const float xh = (held<DT, V>(q.x, j) - ch.mean[j]) * ch.rstd[j];
+                const float d = held<DT, V>(q.dy, j) * act_slope<ACT>(fmaf(xh, ch.w[j], ch.b[j]));
+                s1[j] += d;
+                s2[j] = fmaf(d, xh, s2[j]);
             }
-        }
+        };
+        each_vector<DT, V, 4>(s, k.ty, [&](int64_t p) {
+            const int64_t at = s.base + p * a.C + s.c;
+            return Two{hold<DT, V>(a.x, at), hold<DT, V>(a.dy, at)};
+        }, take);
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) lds[j * kThreads + threadIdx.x] = make_float2(s1[j], s2[j]);
@@ -402,21 +433,6 @@ __device__ __forceinline__ bool slab_place(const Slab& k, uint32_t& image, uint3
     image = divide(idx, k.slabs);
     slab = idx - image * k.slabs.d;
     return idx < k.total;
-}
-
-// 16 bytes of a tensor, or one element in x
-template <int DT, int V>
-__device__ __forceinline__ uint4 hold(const void* p, int64_t i)
-{
-    if constexpr (V == 1) return make_uint4(DT == kBf16 ? static_cast<const uint16_t*>(p)[i] : static_cast<const uint32_t*>(p)[i], 0, 0, 0);
-    else return *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * (16 / V));
-}
-template <int DT, int V>
-__device__ __forceinline__ float held(const uint4& q, int j)
-{
-    const uint32_t w = DT == kF32 ? (j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w)
-                                  : (j / 2 == 0 ? q.x : j / 2 == 1 ? q.y : j / 2 == 2 ? q.z : q.w);
-    return DT == kF32 ? __uint_as_float(w) : __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16);
 }
 
 // Sums over the slab's pixels of S values a channel, v[k][j] of a thread's channel j: to sums[k][part][channel], of k.rows

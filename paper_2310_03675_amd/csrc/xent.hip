@@ -346,23 +346,12 @@ struct OutArgs {
     int64_t step;
     int dtype;
     const float *share, *dloss;         // factors of all, or null
-    float* slices;                      // parts of the contraction: [part][RA][RB], added up by another launch
-    float* sums;                        // several pieces: [RA][RB], what they have so far
+    float* slices;                      // [part of the contraction][RA][RB]: added up by another launch, and over the pieces kept
+    uint32_t parts;
     int first_piece, last_piece;
 };
 
 __device__ __forceinline__ float factor_of(const OutArgs& o) { return (o.share ? *o.share : 1.0f) * (o.dloss ? *o.dloss : 1.0f); }
-
-template <int DT>
-__device__ __forceinline__ void finish(const OutArgs& o, int64_t i, int64_t j, int64_t RB, float v, float factor)
-{
-    if (o.sums) {
-        float* s = o.sums + i * RB + j;
-        if (!o.first_piece) v += *s;
-        if (!o.last_piece) { *s = v; return; }
-    }
-    store_as<DT>(o.out, i * o.step + j, v * factor);
-}
 
 // sum <- f(sum, descriptor, element) for a wave's sums and where they belong in memory: `to` is its first line's and column's place,
 // lines are `step` apart.  A block of 32 lines has a descriptor of its own, which ends with the matrix: what lies behind the last
@@ -399,13 +388,13 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
     v16f acc[NA][NB] = {};
     bf16::multiply<P, MODE, MODE, TA, TB, WA, WB, S>(g, p, stages, wave, lane, acc);
     const int64_t i0 = (int64_t)p.at * TA + (wave / WB) * (TA / WA), j0 = (int64_t)p.bt * TB + (wave % WB) * (TB / WB);
-    const bool several = g.parts > 1;
-    float* part = several ? o.slices + (int64_t)p.part * g.RA * g.RB : o.sums;
-    if (!several && o.sums && !o.first_piece)
-        each_sum<NA, NB>(acc, g.RA - i0, g.RB - j0, lane, o.sums + i0 * g.RB + j0, g.RB, [](float v, __amdgpu_buffer_rsrc_t rs, uint32_t at) {
+    const bool several = o.parts > 1;
+    float* part = o.slices + (int64_t)p.part * g.RA * g.RB;
+    if (!o.first_piece)
+        each_sum<NA, NB>(acc, g.RA - i0, g.RB - j0, lane, part + i0 * g.RB + j0, g.RB, [](float v, __amdgpu_buffer_rsrc_t rs, uint32_t at) {
             return v + __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, 4 * at, 0, 0));
         });
-    if (several || (o.sums && !o.last_piece)) {
+    if (several || !o.last_piece) {
         each_sum<NA, NB>(acc, g.RA - i0, g.RB - j0, lane, part + i0 * g.RB + j0, g.RB, [](float v, __amdgpu_buffer_rsrc_t rs, uint32_t at) {
             __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rs, 4 * at, 0, 0);
             return v;
@@ -428,9 +417,9 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
                          });
 }
 
-// (four neighbours at a time where rows of both sides come in whole 16 bytes)
+// (four neighbours at a time where rows come in whole 16 bytes)
 template <int V>
-__global__ __launch_bounds__(kThreads) void xent_add_parts_kernel(OutArgs o, int64_t RA, int64_t RB, uint32_t parts)
+__global__ __launch_bounds__(kThreads) void xent_add_parts_kernel(OutArgs o, int64_t RA, int64_t RB)
 {
     const float factor = factor_of(o);
     const int64_t j = V * ((int64_t)blockIdx.x * kThreads + threadIdx.x), size = RA * RB;
@@ -439,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void xent_add_parts_kernel(OutArgs o, int
         const float* from = o.slices + i * RB + j;
         float v[V] = {};
 #pragma unroll 4
-        for (uint32_t k = 0; k < parts; ++k) {
+        for (uint32_t k = 0; k < o.parts; ++k) {
             if constexpr (V == 4) {
                 const float4 q = *reinterpret_cast<const float4*>(from + k * size);
                 v[0] += q.x; v[1] += q.y; v[2] += q.z; v[3] += q.w;
@@ -449,8 +438,8 @@ __global__ __launch_bounds__(kThreads) void xent_add_parts_kernel(OutArgs o, int
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            if (o.dtype == kBf16) finish<kBf16>(o, i, j + e, RB, v[e], factor);
-            else finish<kF32>(o, i, j + e, RB, v[e], factor);
+            if (o.dtype == kBf16) store_as<kBf16>(o.out, i * o.step + j + e, v[e] * factor);
+            else store_as<kF32>(o.out, i * o.step + j + e, v[e] * factor);
         }
     }
 }
@@ -851,8 +840,8 @@ __global__ __launch_bounds__(kThreads) void xent_small_add_kernel(XentArgs a, Sm
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
-// How a product is cut: large tiles of 256 x 256 (one plane) or 256 x 128 (three), or small ones of 128 x 128, and the
-// contraction in parts, which another launch adds up.
+// How a product is cut: large tiles of 256 x 256 (one plane) or 256 x 128 (three), one to a compute unit, or small ones of
+// 128 x 128 or 128 x 64, two to a compute unit; and the contraction in parts, which another launch adds up.
 struct Cut {
     int a, b;
     bool large;
@@ -860,24 +849,25 @@ struct Cut {
     double us;
 };
 
-// The cut that a simple model of the time likes best, microseconds: rounds of the workgroups that the chip holds (256; 512 of the
-// small tiles of one plane), each as many stages as a part has, at what a stage takes on a full chip; and for parts the
-// sums written, read again at 4 TB/s, and a launch; 5 to begin and end a round.  (Stages measured, large and small tiles: 8192 x 4096 x 8192 in bfloat16
-// 1.85 and 1.05, 0.75 where a compute unit has one; in fp32 2.8 and 1.35.  What the model chooses between, forward, both ways:
-// 2048 cubed in bfloat16 51 and 30 us, 8192 x 4096 x 8192 474 and 537; in fp32 137 and 94, 512 x 1024 x 32768 174 and 196.)
-Cut cut_of(int64_t RA, int64_t RB, int64_t D, int planes, bool may_split)
+// The cut that a simple model of the time likes best, microseconds: rounds of the workgroups that the chip holds (256, 512), each
+// as many stages as a part has, at what a stage takes on a full chip, and 5 to begin and end; for parts the sums written, read
+// again at 4 TB/s, and a launch, once for all pieces.  (Stages measured, large and small tiles: 8192 x 4096 x 8192 in bfloat16 1.85 and 1.05, in
+// fp32 2.8 and 1.4; 0.75 and 0.8 where a compute unit has one of the small.  What the model chooses between, forward, both
+// ways: 2048 cubed in bfloat16 51 and 30 us, 8192 x 4096 x 8192 474 and 537; in fp32 137 and 100, 512 x 1024 x 32768 174 and 196,
+// 10000 x 512 x 1000 100 and 71.  Small tiles of 128 x 128 in fp32, one to a compute unit and three stages in LDS: 93, 190, 82.)
+Cut cut_of(int64_t RA, int64_t RB, int64_t D, int planes, bool may_split, int64_t pieces = 1)
 {
     Cut best{};
     const int64_t stages = (D + bf16::stage_of(planes) - 1) / bf16::stage_of(planes);
     for (const bool large : {true, false}) {
-        Cut c{large ? 256 : 128, large && planes == 1 ? 256 : 128, large, 1, 0.0};
+        Cut c{large ? 256 : 128, large ? (planes == 1 ? 256 : 128) : planes == 1 ? 128 : 64, large, 1, 0.0};
         const int64_t tiles = ((RA + c.a - 1) / c.a) * ((RB + c.b - 1) / c.b);
         for (int64_t parts = 1; parts <= 64; ++parts) {
             if (parts > 1 && (!may_split || tiles * parts > 1024 || stages < 4 * parts)) break;
-            const int64_t groups = tiles * parts, slots = !large && planes == 1 ? 512 : 256;
-            const double stage = large ? (planes == 1 ? 1.85 : 2.8) : planes == 1 ? (groups > 256 ? 1.05 : 0.75) : 1.35;
+            const int64_t groups = tiles * parts, slots = large ? 256 : 512;
+            const double stage = large ? (planes == 1 ? 1.85 : 2.8) : groups > 256 ? (planes == 1 ? 1.05 : 1.4) : planes == 1 ? 0.75 : 0.8;
             double t = (double)((groups + slots - 1) / slots) * ((double)((stages + parts - 1) / parts) * stage + 5.0);
-            if (parts > 1) t += 6.0 + 4.0 * (double)(2 * parts + 1) * (double)RA * (double)RB / 4.0e6;
+            if (parts > 1) t += (6.0 + 4.0 * (double)(2 * parts + 1) * (double)RA * (double)RB / 4.0e6) / (double)pieces;
             if (best.a == 0 || t < best.us) { best = c; best.parts = (uint32_t)parts; best.us = t; }
         }
     }
@@ -893,7 +883,8 @@ struct Plan {
     int64_t x_step, w_step, dz_step;    // of packed rows, of dz
     size_t x, w;                        // bytes of X packed, of W or a piece of it packed
     size_t pairs, picked, rows;         // forward
-    size_t dz, sums, slices, column;    // backward
+    Cut dx;
+    size_t dz, dx_slices, slices, column;          // backward
     size_t z;                           // the logits, in front of those
 };
 
@@ -924,16 +915,16 @@ Plan plan_of(const XentArgs& a, bool sizes)
     p.pairs = up256(sizeof(float2) * ((a.N + 127) / 128 + (a.N + p.piece - 1) / p.piece) * a.M);
     p.picked = p.rows = up256(sizeof(float) * a.M);
     p.dz = up256(2 * (size_t)a.M * p.dz_step);
-    p.sums = p.piece < a.N ? up256(sizeof(float) * a.M * a.K) : 0;
+    // (dX is cut alike for all pieces: its parts' sums are kept from one to the next)
+    p.dx = cut_of(a.M, a.K, p.piece, p.planes, true, (a.N + p.piece - 1) / p.piece);
+    p.dx_slices = p.dx.parts > 1 || p.piece < a.N ? up256(sizeof(float) * p.dx.parts * a.M * a.K) : 0;
     p.column = up256(sizeof(float) * (size_t)((a.M + kRowsOfDz - 1) / kRowsOfDz) * p.piece);
     // in fp32, where the classes are one piece, a step keeps the logits: 4 bytes each, written and read, against six products
     if (p.planes == 3 && p.piece == a.N) p.z = up256(sizeof(float) * (size_t)a.M * up(a.N, 256));
     size_t most = 0;
-    for (const int64_t classes : {p.piece, a.N - (a.N - 1) / p.piece * p.piece}) {          // (the last piece may be cut another way)
-        const size_t px = cut_of(a.M, a.K, classes, p.planes, true).parts, pw = cut_of(a.K, classes, a.M, p.planes, true).parts;
-        const size_t sx = px > 1 ? px * a.M * a.K : 0, sw = pw > 1 ? pw * a.K * classes : 0;
-        if (sx > most) most = sx;
-        if (sw > most) most = sw;
+    for (const int64_t classes : {p.piece, a.N - (a.N - 1) / p.piece * p.piece}) {          // (the last piece's dW may be cut another way)
+        const size_t parts = cut_of(a.K, classes, a.M, p.planes, true).parts, bytes = parts > 1 ? parts * a.K * classes : 0;
+        if (bytes > most) most = bytes;
     }
     p.slices = up256(sizeof(float) * most);
     return p;
@@ -961,7 +952,7 @@ hipError_t launch_logits(int tag, const bf16::Args& g, const RowArgs& r, int pla
         else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 1, 128, 128, 2, 2, 2>), grid, dim3(256), 0, stream, g, r);
     } else {
         if (large) hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 256, 128, 4, 2, 2>), grid, dim3(512), 0, stream, g, r);
-        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 128, 128, 2, 4, 3>), grid, dim3(512), 0, stream, g, r);
+        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 128, 64, 2, 2, 2>), grid, dim3(256), 0, stream, g, r);
     }
     return hipGetLastError();
 }
@@ -977,18 +968,18 @@ hipError_t launch_gradient(int tag, const bf16::Args& g, const OutArgs& o, int p
             else hipLaunchKernelGGL((xent_gradient_kernel<1, MODE, 128, 128, 2, 2, 2>), grid, dim3(256), 0, stream, g, o);
         } else {
             if (large) hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 256, 128, 4, 2, 2>), grid, dim3(512), 0, stream, g, o);
-            else hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 128, 128, 2, 4, 3>), grid, dim3(512), 0, stream, g, o);
+            else hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 128, 64, 2, 2, 2>), grid, dim3(256), 0, stream, g, o);
         }
     }
-    if (g.parts > 1) {
+    if (o.parts > 1 && o.last_piece) {
         ProfileScope ps(K_XENT_ADD_PARTS, stream);
         const uint32_t down = (uint32_t)(g.RA < 65535 ? g.RA : 65535);
         if (g.RB % 4 == 0)
             hipLaunchKernelGGL(xent_add_parts_kernel<4>, dim3((uint32_t)((g.RB / 4 + kThreads - 1) / kThreads), down), dim3(kThreads), 0, stream,
-                               o, g.RA, g.RB, g.parts);
+                               o, g.RA, g.RB);
         else
             hipLaunchKernelGGL(xent_add_parts_kernel<1>, dim3((uint32_t)((g.RB + kThreads - 1) / kThreads), down), dim3(kThreads), 0, stream,
-                               o, g.RA, g.RB, g.parts);
+                               o, g.RA, g.RB);
     }
     return hipGetLastError();
 }
@@ -1176,7 +1167,7 @@ size_t xent_workspace(const XentArgs& a, bool forward, bool backward)
         return p.z + p.pairs + p.picked + p.rows + (backward ? p.x_slices + p.w_slices : 0);
     }
     const Plan p = plan_of(a, true);
-    const size_t f = forward ? p.pairs + p.picked + p.rows : 0, b = backward ? p.dz + p.sums + p.slices + p.column : 0;
+    const size_t f = forward ? p.pairs + p.picked + p.rows : 0, b = backward ? p.dz + p.dx_slices + p.slices + p.column : 0;
     return p.x + p.w + (backward ? p.z : 0) + (f > b ? f : b);
 }
 
@@ -1220,6 +1211,7 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
     const Plan p = plan_of(a, false);
     float* z = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.x + p.w);
     char* at = reinterpret_cast<char*>(z) + p.z;
+    uint32_t dx_parts = 1;
     for (int64_t first = 0; first < a.N; first += p.piece) {
         const int64_t classes = a.N - first < p.piece ? a.N - first : p.piece;
         Operands o;
@@ -1229,7 +1221,7 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
         r.saved = a.saved; r.dloss = a.dloss; r.each = a.reduction == kNone;
         r.dz = reinterpret_cast<uint16_t*>(at);
         r.step = p.dz_step;
-        if (a.dbias) r.column = reinterpret_cast<float*>(at + p.dz + p.sums + p.slices);
+        if (a.dbias) r.column = reinterpret_cast<float*>(at + p.dz + p.dx_slices + p.slices);
         Cut t = cut_of(classes, a.M, a.K, p.planes, false);
         bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, t.a, t.b, 1);
         uint32_t row_tiles = g.n_bt;
@@ -1249,22 +1241,24 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
         const bf16::Side dz{r.dz, r.step};
         OutArgs out{};
         out.dtype = a.dtype; out.share = a.saved + a.M; out.dloss = r.each ? nullptr : a.dloss;
-        out.slices = reinterpret_cast<float*>(at + p.dz + p.sums);
+        out.slices = reinterpret_cast<float*>(at + p.dz + p.dx_slices);
         out.first_piece = out.last_piece = 1;
         if (a.dX) {
             OutArgs x = out;
             x.out = a.dX; x.step = a.K;
-            x.sums = p.sums ? reinterpret_cast<float*>(at + p.dz) : nullptr;
+            x.slices = reinterpret_cast<float*>(at + p.dz);
             x.first_piece = first == 0; x.last_piece = first + classes == a.N;
-            t = cut_of(a.M, a.K, classes, p.planes, true);
-            g = bf16::plan(dz, o.w, a.M, a.K, classes, p.planes, t.a, t.b, t.parts);
-            if ((e = launch_gradient<kAlong>(K_XENT_DX, g, x, p.planes, t.large, stream)) != hipSuccess) return e;
+            g = bf16::plan(dz, o.w, a.M, a.K, classes, p.planes, p.dx.a, p.dx.b, p.dx.parts);
+            if (first == 0) dx_parts = g.parts;
+            x.parts = dx_parts;
+            if ((e = launch_gradient<kAlong>(K_XENT_DX, g, x, p.planes, p.dx.large, stream)) != hipSuccess) return e;
         }
         if (a.dW) {
             OutArgs w = out;
             w.out = static_cast<char*>(a.dW) + first * dtype_size(a.dtype); w.step = a.N;
             t = cut_of(a.K, classes, a.M, p.planes, true);
             g = bf16::plan(o.x, dz, a.K, classes, a.M, p.planes, t.a, t.b, t.parts);
+            w.parts = g.parts;
             if ((e = launch_gradient<kDown>(K_XENT_DW, g, w, p.planes, t.large, stream)) != hipSuccess) return e;
         }
         if (a.dbias) {

@@ -32,7 +32,7 @@ def _xent(name, **changes):
 def test_xent_refusals(name):
     for what in ("X", "W", "target", "saved"):
         assert _xent(name, **{what: None}) == NULL, what
-    for what, value in (("M", 0), ("K", 0), ("N", -1), ("M", 1 << 23), ("ldx", 63), ("ldw", 99), ("ldw", 1 << 50)):
+    for what, value in (("M", 0), ("K", 0), ("N", -1), ("M", 1 << 23), ("K", (1 << 21) + 1), ("ldx", 63), ("ldw", 99), ("ldw", 1 << 50)):
         assert _xent(name, **{what: value}) == DIM, (what, value)
     for what in ("X", "W", "bias", "target", "saved"):
         assert _xent(name, **{what: ODD}) == ALIGN, what
