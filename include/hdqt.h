@@ -522,23 +522,25 @@ typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
  * and its gradients, with g_i = dloss (a value for each row, or one) times the row's share in the loss:
  *     dz_ij = g_i (exp(z_ij - lse_i) - [j = target(i)]),   dX = dz W^T,   dW = X^T dz,   dbias_j = sum_i dz_ij
  * The logits are not kept: they are formed tile by tile, and in the backward pass again, in pieces of the
- * classes whose dz lies in the workspace (at most 256 MB of it, or 1024 classes).
+ * classes whose dz lies in the workspace (128 MB of it, or 1024 classes where those are more).
  *   X         [M, K], rows ldx >= K elements apart; W [K, N], rows ldw >= N apart (a head that has more
  *             classes than are in use); both of `dtype`
  *   bias      [N] of bias_dtype, or NULL.  Minus infinity takes a class out: probability and gradient zero
  *   target    int64 [M], a class or ignore_index (any value): such a row has loss and gradients zero and does
  *             not count.  Any other value makes the row's loss and gradients NaN.  A target that is taken out
  *             has loss plus infinity; a logit of plus infinity or NaN makes the row's loss and gradients NaN
+ *             (as an infinite feature or weight may in fp32, whatever the logit's sign)
  *   saved     hdqt_xent_saved_size(M) bytes, 4-byte aligned, written by the forward call, read by the
  *             backward call with the same arguments; private to the library
  *   dX, dW    [M, K] and [K, N], dense, of `dtype`; dbias [N] of bias_dtype; any may be NULL (one must not)
  *   dloss     fp32, M values for HDQT_REDUCE_NONE, else one; NULL: ones
- *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd,step}_workspace_size (0 for invalid arguments): besides the above, X
- *             and W (as a whole up to 256 MB, else a piece) in the form that the products take, where they are fp32 or
- *             their rows are no whole 16 bytes
+ *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd,step}_workspace_size (0 for invalid arguments): dz of a
+ *             piece, sums that are added up over pieces and parts of a product, and, for fp32 or rows that are no
+ *             whole 16 bytes, X and W (as a whole up to 256 MB, else a piece) in the form that the products take:
+ *             2 bytes an element, 6 in fp32
  * HDQT_EINVAL_DIM for K above 2^21, M or N above 4 194 240.
- * hdqt_xent_step is the forward and the backward call with dloss = 1.  Its backward half takes the logits from the
- * forward half where those fit the workspace's bounds (fp32, all classes one piece; and small problems).
+ * hdqt_xent_step is the forward and the backward call with dloss = 1.  Its backward half takes the logits from
+ * the forward half where those are few (small problems) or, in fp32, all classes are one piece.
  * bfloat16: products of bfloat16 with sums in 32 bits; dz is rounded to bfloat16 before its products.
  * fp32: as exact as products in 32 bits.
  */
@@ -587,7 +589,8 @@ int hdqt_groupnorm_bwd(const void *dy, const void *x, const void *weight, const 
  *     c = min(1, max_norm / (n + eps)),   dst = c src
  *   tensors   HOST memory, read before the call returns: the addresses travel with the launches, so a call can
  *             be captured.  Tensors of both types may be mixed, any number of them, empty ones too.  dst may
- *             be src; then nothing is written where c is 1.  hdqt_grad_norm does not look at dst
+ *             be src; then nothing is written where c is 1.  A dst overlaps no other tensor.  hdqt_grad_norm
+ *             does not look at dst
  *   norm      fp32, one value (device).  An infinite norm gives c = 0, a NaN among the elements c = NaN
  *   workspace 16-byte aligned, hdqt_clip_grad_norm_workspace_size (0 for invalid arguments) for both calls
  */

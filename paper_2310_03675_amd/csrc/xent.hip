@@ -310,7 +310,7 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
 constexpr int kRowsOfDz = 8;
 __global__ __launch_bounds__(kThreads) void xent_dz_kernel(RowArgs r)
 {
-    const int64_t c = 4 * ((int64_t)blockIdx.x * kThreads + threadIdx.x), row0 = (int64_t)blockIdx.y * kRowsOfDz;
+    const int64_t c = 4 * ((int64_t)blockIdx.y * kThreads + threadIdx.x), row0 = (int64_t)blockIdx.x * kRowsOfDz;
     if (c >= r.step / 3) return;
     float column[4] = {};
 #pragma unroll 4
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void xent_dz_kernel(RowArgs r)
     if (!r.column) return;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (c + e < r.classes) r.column[(int64_t)blockIdx.y * r.classes + c + e] = column[e];
+        if (c + e < r.classes) r.column[(int64_t)blockIdx.x * r.classes + c + e] = column[e];
 }
 
 // ---- gradients: dX (lines of A rows, of B features) and dW (lines of A features, of B classes) ----
@@ -761,10 +761,10 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
     });
 }
 
-// dW and db of few rows (up to MM): a thread has four classes' dz of all of them in registers and writes kOuterLines lines of
+// dW and db of few rows (up to MM), fp32: a thread has four classes' dz of all of them in registers and writes kOuterLines lines of
 // dW, so that only dW itself is moved (1 x 4096 x 128000 in fp32: 2 GB).
 constexpr int kOuterLines = 64, kOuterRows = 16;
-template <int DT, int MM>
+template <int MM>
 __global__ __launch_bounds__(kThreads) void xent_outer_kernel(XentArgs a, SmallArgs k)
 {
     __shared__ float x[MM][kOuterLines];
@@ -772,7 +772,7 @@ __global__ __launch_bounds__(kThreads) void xent_outer_kernel(XentArgs a, SmallA
     const float factor = (a.reduction == kNone ? 1.0f : (a.dloss ? *a.dloss : 1.0f)) * a.saved[a.M];
     for (int i = threadIdx.x; i < MM * kOuterLines; i += kThreads) {
         const int m = i / kOuterLines, f = i % kOuterLines;
-        x[m][f] = m < a.M && f0 + f < a.K ? load_as<DT>(a.X, m * a.ldx + f0 + f) : 0.0f;
+        x[m][f] = m < a.M && f0 + f < a.K ? load_as<kF32>(a.X, m * a.ldx + f0 + f) : 0.0f;
     }
     float d[MM][4];
 #pragma unroll
@@ -809,7 +809,7 @@ __global__ __launch_bounds__(kThreads) void xent_outer_kernel(XentArgs a, SmallA
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int64_t c = c0 + e * kThreads;
-            if (c < a.N) store_as<DT>(a.dW, (f0 + f) * a.N + c, s[e]);
+            if (c < a.N) store_as<kF32>(a.dW, (f0 + f) * a.N + c, s[e]);
         }
     }
 }
@@ -1132,15 +1132,14 @@ hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* a
     const uint32_t w_end = (uint32_t)((a.K + (a.dbias ? 1 : 0) + kSmallTile - 1) / kSmallTile);
     k.w_first = a.dW ? 0 : a.dbias ? w_end - 1 : w_end;
     k.w_tiles = (w_end - k.w_first) * k.w_across;
-    if (k.w_tiles && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20) {         // (of fewer outputs a launch more is not worth it)
+    // (of fewer outputs a launch more is not worth it; bfloat16 problems of so many are not small)
+    if (k.w_tiles && a.dtype == kF32 && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20) {
         k.w_tiles = 0;
         const dim3 grid((uint32_t)((a.N + 4 * kThreads - 1) / (4 * kThreads)), a.dW ? (uint32_t)((a.K + kOuterLines - 1) / kOuterLines) : 1);
         ProfileScope ps(K_XENT_DW, stream);
-        with_small(a, false, [&](auto dt, auto) {
-            if (a.M <= 2) hipLaunchKernelGGL((xent_outer_kernel<dt.value, 2>), grid, dim3(kThreads), 0, stream, a, k);
-            else if (a.M <= 8) hipLaunchKernelGGL((xent_outer_kernel<dt.value, 8>), grid, dim3(kThreads), 0, stream, a, k);
-            else hipLaunchKernelGGL((xent_outer_kernel<dt.value, kOuterRows>), grid, dim3(kThreads), 0, stream, a, k);
-        });
+        if (a.M <= 2) hipLaunchKernelGGL(xent_outer_kernel<2>, grid, dim3(kThreads), 0, stream, a, k);
+        else if (a.M <= 8) hipLaunchKernelGGL(xent_outer_kernel<8>, grid, dim3(kThreads), 0, stream, a, k);
+        else hipLaunchKernelGGL(xent_outer_kernel<kOuterRows>, grid, dim3(kThreads), 0, stream, a, k);
     }
     if (k.x_tiles || k.w_tiles) {
         ProfileScope ps(K_XENT_DX, stream);
@@ -1231,7 +1230,8 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
             if (!forward && (e = launch_logits<false>(K_XENT_LOGITS, g, r, p.planes, t.large, stream)) != hipSuccess) return e;
             row_tiles = (uint32_t)((a.M + kRowsOfDz - 1) / kRowsOfDz);
             ProfileScope ps(K_XENT_DLOGITS, stream);
-            hipLaunchKernelGGL(xent_dz_kernel, dim3((uint32_t)((p.dz_step / 3 + 4 * kThreads - 1) / (4 * kThreads)), row_tiles), dim3(kThreads), 0,
+            // (rows along x: they may be more than 65535 workgroups)
+            hipLaunchKernelGGL(xent_dz_kernel, dim3(row_tiles, (uint32_t)((p.dz_step / 3 + 4 * kThreads - 1) / (4 * kThreads))), dim3(kThreads), 0,
                                stream, r);
             e = hipGetLastError();
         } else {

@@ -132,3 +132,21 @@ def test_graph_and_streams():
         graph.replay()
         torch.cuda.synchronize()
         assert float(norm) == float(want) and all(torch.equal(a, b) for a, b in zip(out, eager))
+
+
+@pytest.mark.parametrize("kind", [2.0, math.inf])
+@pytest.mark.parametrize("lengths", [(1,), (7, 0, 100_003), (64,) * 300, (3_000_001, 5)])
+def test_the_workspace_is_enough_and_its_contents_are_not_used(lengths, kind):
+    """Filled with NaN before the call, and nothing behind its end is written.  Any iterable of tensors."""
+    g = torch.Generator().manual_seed(1)
+    grads = [torch.randn(n, generator=g).cuda() for n in lengths]
+    want = [v.clone() for v in grads]
+    norm = B.clip_grad_norm((v for v in want), 0.5, norm_type=kind)
+    rows, n, _ = B._tensors(grads, None)
+    need = B.load().hdqt_clip_grad_norm_workspace_size(rows, n)
+    whole = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    assert torch.equal(norm, B.grad_norm(iter(grads), kind, workspace=whole[:need]))
+    whole.fill_(0xFF)
+    assert torch.equal(norm, B.clip_grad_norm(grads, 0.5, norm_type=kind, workspace=whole[:need]))
+    assert all(torch.equal(p, q) for p, q in zip(grads, want)) and bool((whole[need:] == 0xFF).all())
+    assert all(bool(v.isfinite().all()) and float(v.abs().max()) <= 0.5 for v in grads if v.numel())

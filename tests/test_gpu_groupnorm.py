@@ -220,3 +220,23 @@ def test_graph_and_streams():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, y1) and all(torch.equal(p, q) for p, q in zip(grads, want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape,G", [((1, 1, 1), 1), ((1, 49, 96), 6), ((128, 16, 512), 32), ((3, 1025, 65), 5), ((2, 8192, 320), 32), ((5, 3000, 7), 7),
+                                     ((1, 20000, 1024), 1), ((300, 65, 40), 4)])
+def test_the_workspace_is_enough_and_its_contents_are_not_used(shape, G, dtype):
+    """Filled with NaN before each call, and nothing behind its end is written."""
+    x, dy, w, b = inputs(shape, dtype)
+    want, saved = B.groupnorm_fwd(x, G, w, b, act="silu")
+    grads = B.groupnorm_bwd(dy, x, saved, G, w, b, act="silu")
+    for backward in (False, True):
+        need = B.load().hdqt_groupnorm_workspace_size(*shape, G, B._DTYPES[dtype], int(backward))
+        whole = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+        if backward:
+            got = B.groupnorm_bwd(dy, x, saved, G, w, b, act="silu", workspace=whole[:need])
+            assert all(torch.equal(p, q) for p, q in zip(got, grads))
+        else:
+            got = B.groupnorm_fwd(x, G, w, b, act="silu", workspace=whole[:need])
+            assert torch.equal(got[0], want) and torch.equal(got[1], saved)
+        assert bool((whole[need:] == 0xFF).all())

@@ -29,17 +29,17 @@ def inputs(M, K, N, dtype, bias=True, ignored=0.0, spare=0, lead=0, seed=0, bdty
     return X, W, b, t.cuda()
 
 
-def reference(X, W, b, t, reduction="mean", dloss=None):
-    X, W, t = X.double().cpu(), W.double().cpu(), t.cpu()
-    z = X @ W + (0 if b is None else b.double().cpu())
+def reference(X, W, b, t, reduction="mean", dloss=None, where="cpu"):
+    X, W, t = X.double().to(where), W.double().to(where), t.to(where)
+    z = X @ W + (0 if b is None else b.double().to(where))
     lse = torch.logsumexp(z, 1)
     keep = t != IGNORE
     rows = torch.where(keep, lse - z.gather(1, t.clamp_min(0)[:, None])[:, 0], torch.zeros_like(lse))
     share = 1.0 / max(1, int(keep.sum())) if reduction == "mean" else 1.0
     loss = rows if reduction == "none" else rows.sum() * share
-    g = keep.double() * share * (1.0 if dloss is None else dloss.double().cpu())
+    g = keep.double() * share * (1.0 if dloss is None else dloss.double().to(where))
     dz = torch.exp(z - lse[:, None])
-    dz[torch.arange(len(t)), t.clamp_min(0)] -= 1
+    dz[torch.arange(len(t), device=where), t.clamp_min(0)] -= 1
     dz = dz * g[:, None]
     return loss, dz @ W.t(), X.t() @ dz, dz.sum(0), dz
 
@@ -49,7 +49,7 @@ def tolerance(dtype, K):
 
 
 def near(got, want, tol, floor=0.0):
-    d = float((got.double().cpu() - want).norm())
+    d = float((got.double().to(want.device) - want).norm())
     assert d <= tol * max(float(want.norm()), floor) + 1e-12, (d / (float(want.norm()) + 1e-300), tol)
 
 
@@ -126,6 +126,61 @@ def test_many_pieces_of_the_classes(dtype):
     near(dX, dX1, tol)
     near(dW, dW1, tol, float(dz.norm()))
     near(db, db1, tol, float(dz.norm()))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,K,N", [(1500, 520, 20011), (9001, 520, 6001), (4099, 1030, 5003), (24001, 72, 3001), (2600, 2056, 12011),
+                                   (13, 2048, 2100), (600_000, 8, 20), (2048, 2048, 2048)])
+def test_large_tiles_parts_and_pieces(dtype, M, K, N):
+    """Sizes at which the large tiles multiply, contractions come in parts, and dX is added up over pieces of which the
+    last is another size; more rows than a launch has workgroups in one direction.  The 64 bits on the GPU.  Tolerances as
+    above: sums of n <= 24001 terms in 32 bits add sqrt(n) 2^-25, 5e-6 (of 600000: 2.3e-5, to dW and dbias)."""
+    X, W, b, t = inputs(M, K, N, dtype, ignored=0.1)
+    loss, dX, dW, db = B.xent_step(X, W, t, bias=b, ignore_index=IGNORE)
+    want, dX1, dW1, db1, dz = reference(X, W, b, t, where="cuda")
+    tol = (4e-5 if dtype == F32 else 2.0 ** -7 + 4e-5)
+    near(loss, want, 4e-5)
+    near(dX, dX1, tol)
+    near(dW, dW1, tol, float(dz.norm()))
+    near(db, db1, tol, float(dz.norm()))
+    loss, saved = B.xent_fwd(X, W, t, bias=b, ignore_index=IGNORE)
+    apart = B.xent_bwd(None, X, W, t, saved, bias=b, ignore_index=IGNORE)
+    assert all(torch.equal(p, q) for p, q in zip(apart, (dX, dW, db)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,K,N,spare", [(40, 64, 96, 32), (300, 264, 1200, 8), (700, 512, 4096, 64), (300, 264, 1203, 5), (3, 2048, 2100, 4)])
+def test_what_lies_between_rows_is_not_read(dtype, M, K, N, spare):
+    X, W, b, t = inputs(M, K, N, dtype)
+    want = B.xent_step(X, W, t, bias=b)
+    wide, tall = (torch.full((r, c), math.nan, dtype=dtype, device="cuda") for r, c in ((K, N + spare), (M, K + 16)))
+    wide[:, :N], tall[:, 8:8 + K] = W, X
+    got = B.xent_step(tall[:, 8:8 + K], wide[:, :N], t, bias=b)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,K,N", [(1, 1, 1), (128, 512, 100), (65, 65, 65), (5, 2048, 4099), (2049, 24, 31), (777, 320, 1007), (1000, 40, 10007),
+                                   (512, 256, 2048), (9001, 40, 6001), (1500, 520, 20011)])
+def test_the_workspace_is_enough_and_its_contents_are_not_used(dtype, M, K, N):
+    """Filled with NaN before each call, and nothing behind its end is written."""
+    X, W, b, t = inputs(M, K, N, dtype, ignored=0.1)
+    lib, dt = B.load(), B._DTYPES[dtype]
+
+    def space(need):
+        whole = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+        return whole, whole[:need]
+
+    want = B.xent_step(X, W, t, bias=b)
+    whole, ws = space(lib.hdqt_xent_step_workspace_size(M, K, N, dt))
+    got = B.xent_step(X, W, t, bias=b, workspace=ws)
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and bool((whole[-4096:] == 0xFF).all())
+    whole, ws = space(lib.hdqt_xent_fwd_workspace_size(M, K, N, dt))
+    loss, saved = B.xent_fwd(X, W, t, bias=b, workspace=ws)
+    assert torch.equal(loss, want[0]) and bool((whole[-4096:] == 0xFF).all())
+    whole, ws = space(lib.hdqt_xent_bwd_workspace_size(M, K, N, dt))
+    got = B.xent_bwd(None, X, W, t, saved, bias=b, workspace=ws)
+    assert all(torch.equal(p, q) for p, q in zip(got, want[1:])) and bool((whole[-4096:] == 0xFF).all())
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
