@@ -41,10 +41,8 @@ __device__ __forceinline__ float exp_of(float t)
 // (largest, sum of exponentials relative to it) of two parts together
 __device__ __forceinline__ void join(float& m, float& l, float om, float ol)
 {
-    if (om == -INFINITY && ol == 0.0f) return;
-    if (m == -INFINITY && l == 0.0f) { m = om; l = ol; return; }
-    const float top = om > m ? om : m;
-    l = l * expf(m - top) + ol * expf(om - top);
+    const float top = fmaxf(m, om), base = top == -INFINITY ? 0.0f : top;
+    l = l * exp_of<true>(m - base) + ol * exp_of<true>(om - base);
     m = top;
 }
 
@@ -55,6 +53,7 @@ struct PackArgs {
     int64_t rows, cols, ld;
     uint16_t* dst;
     int64_t step;
+    uint32_t across, groups;            // workgroups side by side, and of this operand
 };
 
 __device__ __forceinline__ void split(float x, uint32_t (&part)[3])
@@ -67,34 +66,35 @@ __device__ __forceinline__ void split(float x, uint32_t (&part)[3])
     part[2] = to_bf16(rest - from_bf16(part[1]));
 }
 
-// A thread has two columns of kPackRows rows, all of whose loads are in flight.
+// A thread has two columns of kPackRows rows, all of whose loads are in flight.  Two operands in one launch, or one.
 constexpr int kPackRows = 8;
 template <int DT>
-__global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs a)
+__global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs one, PackArgs other)
 {
-    const int64_t c = 2 * ((int64_t)blockIdx.x * kThreads + threadIdx.x);
+    const bool second = blockIdx.x >= one.groups;
+    const PackArgs a = second ? other : one;
+    const uint32_t group = blockIdx.x - (second ? one.groups : 0), down = group / a.across;
+    const int64_t c = 2 * ((int64_t)(group - down * a.across) * kThreads + threadIdx.x), row0 = (int64_t)down * kPackRows;
     if (c >= (DT == kBf16 ? a.step : a.step / 3)) return;
-    for (int64_t row0 = (int64_t)blockIdx.y * kPackRows; row0 < a.rows; row0 += (int64_t)gridDim.y * kPackRows) {
-        float x[kPackRows], y[kPackRows];
+    float x[kPackRows], y[kPackRows];
 #pragma unroll
-        for (int i = 0; i < kPackRows; ++i) {
-            const int64_t from = (row0 + i) * a.ld + c;
-            x[i] = row0 + i < a.rows && c < a.cols ? load_as<DT>(a.src, from) : 0.0f;
-            y[i] = row0 + i < a.rows && c + 1 < a.cols ? load_as<DT>(a.src, from + 1) : 0.0f;
-        }
+    for (int i = 0; i < kPackRows; ++i) {
+        const int64_t from = (row0 + i) * a.ld + c;
+        x[i] = row0 + i < a.rows && c < a.cols ? load_as<DT>(a.src, from) : 0.0f;
+        y[i] = row0 + i < a.rows && c + 1 < a.cols ? load_as<DT>(a.src, from + 1) : 0.0f;
+    }
 #pragma unroll
-        for (int i = 0; i < kPackRows; ++i) {
-            if (row0 + i >= a.rows) break;
-            uint32_t* to = reinterpret_cast<uint32_t*>(a.dst + (row0 + i) * a.step + (DT == kBf16 ? c : c / 32 * 96 + c % 32));
-            if (DT == kBf16) {
-                *to = __float_as_uint(x[i]) >> 16 | (__float_as_uint(y[i]) & 0xFFFF0000u);
-            } else {
-                uint32_t p[3], q[3];
-                split(x[i], p);
-                split(y[i], q);
+    for (int i = 0; i < kPackRows; ++i) {
+        if (row0 + i >= a.rows) break;
+        uint32_t* to = reinterpret_cast<uint32_t*>(a.dst + (row0 + i) * a.step + (DT == kBf16 ? c : c / 32 * 96 + c % 32));
+        if (DT == kBf16) {
+            *to = __float_as_uint(x[i]) >> 16 | (__float_as_uint(y[i]) & 0xFFFF0000u);
+        } else {
+            uint32_t p[3], q[3];
+            split(x[i], p);
+            split(y[i], q);
 #pragma unroll
-                for (int k = 0; k < 3; ++k) to[16 * k] = p[k] | q[k] << 16;
-            }
+            for (int k = 0; k < 3; ++k) to[16 * k] = p[k] | q[k] << 16;
         }
     }
 }
@@ -446,76 +446,93 @@ __global__ __launch_bounds__(kThreads) void xent_add_parts_kernel(OutArgs o, int
 
 // ---- sums over rows ----
 
-// A row's pairs joined, by `lanes` threads to a row: its log of the sum of exponentials and its loss.  Where one workgroup has
-// all rows it adds them up as well.
-struct TotalArgs {
-    int lanes;
-    int alone;
+// A row's pairs joined, by `lanes` threads to a row: its log of the sum of exponentials and its loss, in the first of them.
+struct Row {
+    float lse, loss;
+    bool counted;
 };
-__device__ __forceinline__ void total_of(const XentArgs& a, double s, long long n)
+__device__ __forceinline__ Row row_of(const XentArgs& a, const float2* pairs, int64_t tiles, const float* picked, int64_t row, int lane,
+                                      int lanes)
+{
+    float m = -INFINITY, l = 0.0f, z = 0.0f;
+    int64_t target = 0;
+    if (row < a.M) {
+        target = a.target[row];         // (on their way at once; of a row whose target is no class no one has written z)
+        z = picked[row];
+#pragma unroll 4
+        for (int64_t i = lane; i < tiles; i += lanes) {
+            const float2 p = pairs[i * a.M + row];
+            join(m, l, p.x, p.y);
+        }
+    }
+    for (int k = 1; k < lanes; k <<= 1) {
+        const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
+        join(m, l, om, ol);
+    }
+    Row r{0.0f, 0.0f, false};
+    if (row >= a.M || lane) return r;
+    // (no class left: minus infinity; a logit of plus infinity: no probabilities)
+    r.lse = m == INFINITY ? NAN : l > 0.0f ? m + logf(l) : l != l ? l : m;
+    r.counted = target != a.ignore;
+    if (r.counted) {
+        const bool none = target < 0 || target >= a.N;          // (no class: seen in the loss and the gradients)
+        if (none) r.lse = z = NAN;
+        r.loss = z == -INFINITY && r.lse == r.lse ? INFINITY : r.lse - z;
+    }
+    return r;
+}
+
+// A row's share in the loss, in every thread, from each thread's sum and number of rows; `write`: that and the loss.
+__device__ __forceinline__ float total_of(const XentArgs& a, double s, int n, bool write)
 {
     __shared__ double sums[16];
-    __shared__ long long counts[16];
+    __shared__ int counts[16];
     s = wave_sum(s);
     n = wave_sum(n);
     if ((threadIdx.x & 63) == 0) { sums[threadIdx.x >> 6] = s; counts[threadIdx.x >> 6] = n; }
     __syncthreads();
-    if (threadIdx.x) return;
-    for (uint32_t w = 1; w < blockDim.x / kWave; ++w) { s += sums[w]; n += counts[w]; }
+    s = 0.0;
+    n = 0;
+    for (uint32_t w = 0; w < blockDim.x / kWave; ++w) { s += sums[w]; n += counts[w]; }
     const double share = a.reduction == kMean ? 1.0 / (double)(n > 0 ? n : 1) : 1.0;
-    a.saved[a.M] = (float)share;
-    if (a.reduction != kNone) a.loss[0] = (float)(s * share);
+    if (write && threadIdx.x == 0) {
+        a.saved[a.M] = (float)share;
+        if (a.reduction != kNone) a.loss[0] = (float)(s * share);
+    }
+    return (float)share;
 }
 
-__global__ __launch_bounds__(1024) void xent_rows_kernel(XentArgs a, const float2* pairs, int64_t tiles, const float* picked,
-                                                         float* rows, TotalArgs t)
+// Where one workgroup has all rows (alone) it adds them up as well.
+constexpr int kAlone = 512;
+__global__ __launch_bounds__(kAlone) void xent_rows_kernel(XentArgs a, const float2* pairs, int64_t tiles, const float* picked, float* rows,
+                                                           int lanes, int alone)
 {
-    const int lane = threadIdx.x & (t.lanes - 1), per = blockDim.x / t.lanes;
+    const int lane = threadIdx.x & (lanes - 1), per = blockDim.x / lanes;
     double sum = 0.0;
-    long long count = 0;
+    int count = 0;
     for (int64_t row0 = (int64_t)blockIdx.x * per; row0 < a.M; row0 += (int64_t)gridDim.x * per) {
-        const int64_t row = row0 + threadIdx.x / t.lanes;
-        const bool there = row < a.M;
-        float m = -INFINITY, l = 0.0f;
-        if (there)
-#pragma unroll 4
-            for (int64_t i = lane; i < tiles; i += t.lanes) {
-                const float2 p = pairs[i * a.M + row];
-                join(m, l, p.x, p.y);
-            }
-        for (int k = 1; k < t.lanes; k <<= 1) {
-            const float om = __shfl_xor(m, k), ol = __shfl_xor(l, k);
-            join(m, l, om, ol);
-        }
-        if (!there || lane) continue;
-        const int64_t target = a.target[row];
-        // (no class left: minus infinity; a logit of plus infinity: no probabilities)
-        float lse = m == INFINITY ? NAN : l > 0.0f ? m + logf(l) : l != l ? l : m, loss = 0.0f;
-        if (target != a.ignore) {
-            const bool none = target < 0 || target >= a.N;          // (no class: seen in the loss and the gradients)
-            if (none) lse = NAN;
-            const float z = none ? NAN : picked[row];
-            loss = z == -INFINITY && lse == lse ? INFINITY : lse - z;
-            ++count;
-        }
-        a.saved[row] = lse;
-        if (!t.alone || a.reduction == kNone) rows[row] = loss;
-        sum += (double)loss;
+        const int64_t row = row0 + threadIdx.x / lanes;
+        const Row r = row_of(a, pairs, tiles, picked, row, lane, lanes);
+        if (row >= a.M || lane) continue;
+        a.saved[row] = r.lse;
+        if (!alone || a.reduction == kNone) rows[row] = r.loss;
+        sum += (double)r.loss;
+        count += r.counted;
     }
-    if (t.alone) total_of(a, sum, count);
+    if (alone) total_of(a, sum, count, true);
 }
 
 // one workgroup: the loss over all rows and a row's share in it
 __global__ __launch_bounds__(1024) void xent_total_kernel(XentArgs a, const float* rows)
 {
     double s = 0.0;
-    long long n = 0;
+    int n = 0;
 #pragma unroll 4
     for (int64_t i = threadIdx.x; i < a.M; i += 1024) {
         s += (double)rows[i];
         n += a.target[i] != a.ignore;
     }
-    total_of(a, s, n);
+    total_of(a, s, n, true);
 }
 
 // db of a piece's classes: the tiles' sums of a class, sixteen threads to it
@@ -549,12 +566,16 @@ constexpr int kSmallWaves = 8, kSmallTile = 32;
 constexpr int kSmallAhead = 4;                      // steps of eight of the contraction, four to a half of a wave's lanes, in flight
 constexpr int kSmallSpan = 8 * kSmallAhead;         // of the contraction, side by side: a whole line of memory in fp32
 constexpr int kSmallRound = kSmallSpan * kSmallWaves;
+constexpr int kJoined = 2048;                       // rows, and pairs of them, that every workgroup of the gradients joins for itself
+static_assert(kAlone == 64 * kSmallWaves, "sums in the same order as the rows' own launch");
 
 struct SmallArgs {
     float* z;                           // [M][step], null: not wanted
     int64_t step;
     float2* pairs;                      // [tiles of classes][M]; null: not wanted
     float* picked;
+    float* rows;                        // gradients that join the pairs: the rows' losses, where they are wanted
+    int lanes;                          // and threads to a row
     uint32_t x_tiles, x_parts;          // gradients: tiles of dX, parts of its contraction; dW's tiles behind them
     uint32_t x_across, w_across;        // tiles side by side of dX (features), of the logits and dW (classes)
     uint32_t w_first;                   // first tile down of dW (where only db is wanted: the one with the line of ones)
@@ -583,7 +604,8 @@ __device__ __forceinline__ void load4(const void* p, int64_t at, int64_t left, f
     }
 }
 
-// The waves' sums of a 32 x 32 block added up: f(register, sum) for the registers of this wave, in order of the waves.
+// The waves' sums of a 32 x 32 block added up: f(register, its number in this wave, sum) for the registers of this wave, in order
+// of the waves.
 template <class F>
 __device__ __forceinline__ void join_waves(const v16f& acc, float (*lds)[16][64], int wave, int lane, F f)
 {
@@ -596,7 +618,7 @@ __device__ __forceinline__ void join_waves(const v16f& acc, float (*lds)[16][64]
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < kSmallWaves; ++w) s += lds[w][e][lane];
-        f(e, s);
+        f(e, k, s);
     }
 }
 
@@ -611,6 +633,14 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_logits_kernel(Xen
     const int64_t class0 = (int64_t)across * kSmallTile, row0 = (int64_t)down * kSmallTile;
     const int64_t c = class0 + line, row = row0 + line;
     const bool class_there = c < a.N, row_there = row < a.M;
+    const int64_t target = row_there ? a.target[row] : -1;
+    float bias[16 / kSmallWaves];           // of the sums that this wave joins
+#pragma unroll
+    for (int q = 0; q < 16 / kSmallWaves; ++q) {
+        const int e = wave * (16 / kSmallWaves) + q;
+        const int64_t of = class0 + 8 * (e >> 2) + 4 * half + (e & 3);
+        bias[q] = a.bias && of < a.N ? any_load(a.bias, a.bias_dtype, of) : 0.0f;
+    }
     v16f acc = {};
     for (int64_t base = kSmallSpan * wave; base < a.K; base += kSmallRound) {
         float x[kSmallAhead][4], w[kSmallAhead][4];
@@ -626,13 +656,12 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_logits_kernel(Xen
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(w[u][e], x[u][e], acc, 0, 0, 0);
     }
-    join_waves(acc, lds, wave, lane, [&](int e, float s) {
+    join_waves(acc, lds, wave, lane, [&](int e, int q, float s) {
         const int64_t of = class0 + 8 * (e >> 2) + 4 * half + (e & 3);
-        z[e][lane] = of >= a.N ? -INFINITY : a.bias ? s + any_load(a.bias, a.bias_dtype, of) : s;
+        z[e][lane] = of >= a.N ? -INFINITY : s + bias[q];
     });
     __syncthreads();
     if (wave) return;
-    const int64_t target = row_there ? a.target[row] : -1;
     float v[16], top = -INFINITY, sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -677,13 +706,39 @@ __device__ __forceinline__ float row_factor(const XentArgs& a, int64_t row)
 
 // dX: lines of A are rows, of B features.  dW: lines of A features, and one of ones behind them, whose products are db; of B
 // classes.
-template <int DT, bool VEC>
+// JOIN: the forward pass has left the rows' pairs as they are.  Every workgroup joins all rows' for itself, and the first one
+// writes what the forward pass owes: a launch less (1 x 561 x 11 16.8 us in three launches, 14.1 in two; 128 x 512 x 100 17.6 and
+// 14.4).  Kernels this short wait for their own instructions: with the next round's loads in flight beside the products
+// (half as much code again) they take 16.4 and 16.7, and large ones no less (32 x 256 x 64000 in fp32 405 us, here 217).
+template <int DT, bool VEC, bool JOIN>
 __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(XentArgs a, SmallArgs k)
 {
     __shared__ float lds[kSmallWaves][16][64];
+    __shared__ float joined[JOIN ? kJoined : 1];
+    float factor = a.reduction == kNone || !a.dloss ? 1.0f : *a.dloss;
+    if constexpr (JOIN) {
+        const int at = threadIdx.x & (k.lanes - 1), per = kAlone / k.lanes;
+        double sum = 0.0;
+        int count = 0;
+        for (int64_t row0 = 0; row0 < a.M; row0 += per) {
+            const int64_t row = row0 + threadIdx.x / k.lanes;
+            const Row r = row_of(a, k.pairs, k.w_across, k.picked, row, at, k.lanes);
+            if (row >= a.M || at) continue;
+            joined[row] = r.lse;
+            if (blockIdx.x == 0) {
+                a.saved[row] = r.lse;
+                if (a.reduction == kNone) k.rows[row] = r.loss;
+            }
+            sum += (double)r.loss;
+            count += r.counted;
+        }
+        factor *= total_of(a, sum, count, blockIdx.x == 0);             // (its barrier stands before the first reader)
+    } else {
+        factor *= a.saved[a.M];
+    }
+    auto lse_of = [&](int64_t row) { return JOIN ? joined[row] : a.saved[row]; };
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = lane & 31, half = lane >> 5;
     v16f acc = {};
-    const float factor = (a.reduction == kNone ? 1.0f : (a.dloss ? *a.dloss : 1.0f)) * a.saved[a.M];
     if (blockIdx.x < k.x_tiles * k.x_parts) {
         const uint32_t part = blockIdx.x / k.x_tiles, tile = blockIdx.x - part * k.x_tiles, down = tile / k.x_across;
         const int64_t row0 = (int64_t)down * kSmallTile, f0 = (int64_t)(tile - down * k.x_across) * kSmallTile;
@@ -691,7 +746,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
         const bool row_there = row < a.M, f_there = f < a.K;
         const int64_t target = row_there ? a.target[row] : -1;
         const bool counted = row_there && target != a.ignore;
-        const float lse = row_there ? a.saved[row] : 0.0f, each = counted ? row_factor(a, row) : 0.0f;
+        const float lse = row_there ? lse_of(row) : 0.0f, each = counted ? row_factor(a, row) : 0.0f;
         const Share share = share_of(a.N, part, k.x_parts);
         for (int64_t base = share.begin + kSmallSpan * wave; base < share.end; base += kSmallRound) {
             float z[kSmallAhead][4], w[kSmallAhead][4];
@@ -710,7 +765,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
                     acc = __builtin_amdgcn_mfma_f32_32x32x2f32(d, w[u][e], acc, 0, 0, 0);
                 }
         }
-        join_waves(acc, lds, wave, lane, [&](int e, float s) {
+        join_waves(acc, lds, wave, lane, [&](int e, int, float s) {
             const int64_t i = row0 + 8 * (e >> 2) + 4 * half + (e & 3);
             if (i >= a.M || !f_there) return;
             if (k.x_parts > 1) k.slices[((int64_t)part * a.M + i) * a.K + f] = s;
@@ -735,7 +790,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
                 x[u][e] = row >= share.end ? 0.0f : f < a.K ? load_as<DT>(a.X, row * a.ldx + f) : f == a.K ? 1.0f : 0.0f;
                 z[u][e] = row < share.end && c_there ? k.z[row * k.step + c] : 0.0f;
                 target[u][e] = row < share.end ? a.target[r] : a.ignore;
-                lse[u][e] = a.saved[r];
+                lse[u][e] = lse_of(r);
                 g[u][e] = each ? a.dloss[r] : 1.0f;
             }
 #pragma unroll
@@ -746,7 +801,7 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
                 acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[u][e], d, acc, 0, 0, 0);
             }
     }
-    join_waves(acc, lds, wave, lane, [&](int e, float s) {
+    join_waves(acc, lds, wave, lane, [&](int e, int, float s) {
         const int64_t i = f0 + 8 * (e >> 2) + 4 * half + (e & 3);
         if (!c_there) return;
         if (k.w_parts > 1) {
@@ -930,15 +985,21 @@ Plan plan_of(const XentArgs& a, bool sizes)
     return p;
 }
 
-hipError_t launch_pack(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint16_t* dst, int64_t step, hipStream_t stream)
+PackArgs pack_of(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint16_t* dst, int64_t step)
 {
-    const PackArgs a{src, rows, cols, ld, dst, step};
     const int64_t pairs = (dtype == kBf16 ? step : step / 3) / 2;
-    const int64_t down = (rows + kPackRows - 1) / kPackRows;
-    const dim3 grid((uint32_t)((pairs + kThreads - 1) / kThreads), (uint32_t)(down < 65535 ? down : 65535));
+    PackArgs a{src, rows, cols, ld, dst, step, (uint32_t)((pairs + kThreads - 1) / kThreads), 0};
+    a.groups = a.across * (uint32_t)((rows + kPackRows - 1) / kPackRows);
+    return a;
+}
+// (either may be empty)
+hipError_t launch_pack(const PackArgs& one, const PackArgs& other, int dtype, hipStream_t stream)
+{
+    const dim3 grid(one.groups + other.groups);
+    if (grid.x == 0) return hipSuccess;
     ProfileScope ps(K_XENT_PACK, stream);
-    if (dtype == kBf16) hipLaunchKernelGGL(xent_pack_kernel<kBf16>, grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL(xent_pack_kernel<kF32>, grid, dim3(kThreads), 0, stream, a);
+    if (dtype == kBf16) hipLaunchKernelGGL(xent_pack_kernel<kBf16>, grid, dim3(kThreads), 0, stream, one, other);
+    else hipLaunchKernelGGL(xent_pack_kernel<kF32>, grid, dim3(kThreads), 0, stream, one, other);
     return hipGetLastError();
 }
 
@@ -996,26 +1057,33 @@ hipError_t operands_of(const XentArgs& a, const Plan& p, char* workspace, int64_
     uint16_t *px = reinterpret_cast<uint16_t*>(workspace), *pw = reinterpret_cast<uint16_t*>(workspace + p.x);
     o->x = p.pack_x ? bf16::Side{px, p.x_step} : bf16::Side{static_cast<const uint16_t*>(a.X), a.ldx};
     o->w = p.pack_w ? bf16::Side{pw + (p.whole_w ? p.planes * first : 0), p.w_step} : bf16::Side{reinterpret_cast<const uint16_t*>(w), a.ldw};
-    hipError_t e = hipSuccess;
-    if (p.pack_x && !have && first == 0) e = launch_pack(a.X, a.dtype, a.M, a.K, a.ldx, px, p.x_step, stream);
-    if (!p.pack_w || e != hipSuccess) return e;
-    if (!p.whole_w) return have && p.piece == a.N ? e : launch_pack(w, a.dtype, a.K, classes, a.ldw, pw, p.w_step, stream);
-    return have || first ? e : launch_pack(a.W, a.dtype, a.K, a.N, a.ldw, pw, p.w_step, stream);
+    PackArgs x{}, of_w{};
+    if (p.pack_x && !have && first == 0) x = pack_of(a.X, a.dtype, a.M, a.K, a.ldx, px, p.x_step);
+    if (p.pack_w && p.whole_w && !have && first == 0) of_w = pack_of(a.W, a.dtype, a.K, a.N, a.ldw, pw, p.w_step);
+    if (p.pack_w && !p.whole_w && !(have && p.piece == a.N)) of_w = pack_of(w, a.dtype, a.K, classes, a.ldw, pw, p.w_step);
+    return launch_pack(x, of_w, a.dtype, stream);
 }
+
+int lanes_of(int64_t tiles)
+{
+    int lanes = 1;
+    while (lanes < 64 && 4 * lanes < tiles) lanes *= 2;
+    return lanes;
+}
+// (four rounds of a workgroup at most: less than another launch)
+bool rows_alone(const XentArgs& a, int64_t tiles) { return a.M * lanes_of(tiles) <= 4 * kAlone; }
 
 // from the tiles' pairs to the loss
 hipError_t launch_rows(const XentArgs& a, const float2* pairs, int64_t tiles, const float* picked, float* rows, hipStream_t stream)
 {
     ProfileScope ps(K_XENT_LOSS, stream);
-    TotalArgs t{1, 0};
-    while (t.lanes < 64 && 4 * t.lanes < tiles) t.lanes *= 2;
-    t.alone = a.M * t.lanes <= 2048;            // (two rounds of a workgroup at most: less than another launch)
-    if (t.alone) {
-        hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(1024), 0, stream, a, pairs, tiles, picked, rows, t);
+    const int lanes = lanes_of(tiles);
+    if (rows_alone(a, tiles)) {
+        hipLaunchKernelGGL(xent_rows_kernel, dim3(1), dim3(kAlone), 0, stream, a, pairs, tiles, picked, rows, lanes, 1);
         return hipGetLastError();
     }
-    const int64_t per = kThreads / t.lanes;
-    hipLaunchKernelGGL(xent_rows_kernel, dim3((uint32_t)((a.M + per - 1) / per)), dim3(kThreads), 0, stream, a, pairs, tiles, picked, rows, t);
+    const int64_t per = kThreads / lanes;
+    hipLaunchKernelGGL(xent_rows_kernel, dim3((uint32_t)((a.M + per - 1) / per)), dim3(kThreads), 0, stream, a, pairs, tiles, picked, rows, lanes, 0);
     hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, stream, a, rows);
     return hipGetLastError();
 }
@@ -1092,7 +1160,15 @@ bool fours(const void* p, int64_t ld, int64_t cols, int dtype)
     return reinterpret_cast<uintptr_t>(p) % (size_t)(4 * dtype_size(dtype)) == 0 && ld % 4 == 0 && cols % 4 == 0;
 }
 
-// forward: the loss; keep: the logits for the gradients
+bool outer_problem(const XentArgs& a)
+{
+    // (of fewer outputs a launch more is not worth it; bfloat16 problems of so many are not small)
+    return (a.dW || a.dbias) && a.dtype == kF32 && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20;
+}
+// whether a step's gradients join the rows' pairs for themselves: few of them
+bool joins(const XentArgs& a, const SmallPlan& p) { return !outer_problem(a) && rows_alone(a, p.class_tiles) && p.class_tiles * a.M <= kJoined; }
+
+// forward: the loss; keep: the logits for the gradients, which may follow
 hipError_t launch_small_logits(const XentArgs& a, const SmallPlan& p, char* at, bool forward, bool keep, hipStream_t stream)
 {
     SmallArgs k{};
@@ -1111,14 +1187,19 @@ hipError_t launch_small_logits(const XentArgs& a, const SmallPlan& p, char* at, 
         });
     }
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !forward) return e;
+    if (e != hipSuccess || !forward || (keep && joins(a, p))) return e;
     float* rows = a.reduction == kNone ? a.loss : reinterpret_cast<float*>(at + p.z + p.pairs + p.picked);
     return launch_rows(a, k.pairs, p.class_tiles, k.picked, rows, stream);
 }
 
-hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* at, hipStream_t stream)
+hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* at, bool forward, hipStream_t stream)
 {
     SmallArgs k{};
+    const bool join = forward && joins(a, p);
+    k.pairs = reinterpret_cast<float2*>(at + p.z);
+    k.picked = reinterpret_cast<float*>(at + p.z + p.pairs);
+    k.rows = a.loss;
+    k.lanes = lanes_of(p.class_tiles);
     k.z = reinterpret_cast<float*>(at);
     k.step = p.step;
     k.x_across = (uint32_t)((a.K + kSmallTile - 1) / kSmallTile);
@@ -1132,8 +1213,7 @@ hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* a
     const uint32_t w_end = (uint32_t)((a.K + (a.dbias ? 1 : 0) + kSmallTile - 1) / kSmallTile);
     k.w_first = a.dW ? 0 : a.dbias ? w_end - 1 : w_end;
     k.w_tiles = (w_end - k.w_first) * k.w_across;
-    // (of fewer outputs a launch more is not worth it; bfloat16 problems of so many are not small)
-    if (k.w_tiles && a.dtype == kF32 && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20) {
+    if (outer_problem(a)) {
         k.w_tiles = 0;
         const dim3 grid((uint32_t)((a.N + 4 * kThreads - 1) / (4 * kThreads)), a.dW ? (uint32_t)((a.K + kOuterLines - 1) / kOuterLines) : 1);
         ProfileScope ps(K_XENT_DW, stream);
@@ -1144,8 +1224,9 @@ hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* a
     if (k.x_tiles || k.w_tiles) {
         ProfileScope ps(K_XENT_DX, stream);
         with_small(a, fours(a.W, a.ldw, a.N, a.dtype), [&](auto dt, auto vec) {
-            hipLaunchKernelGGL((xent_small_gradients_kernel<dt.value, vec.value>), dim3(k.x_tiles * k.x_parts + k.w_tiles * k.w_parts), dim3(64 * kSmallWaves),
-                               0, stream, a, k);
+            const dim3 grid(k.x_tiles * k.x_parts + k.w_tiles * k.w_parts), block(64 * kSmallWaves);
+            if (join) hipLaunchKernelGGL((xent_small_gradients_kernel<dt.value, vec.value, true>), grid, block, 0, stream, a, k);
+            else hipLaunchKernelGGL((xent_small_gradients_kernel<dt.value, vec.value, false>), grid, block, 0, stream, a, k);
         });
     }
     const int64_t of_x = a.dX && p.x_parts > 1 ? a.M * a.K : 0, of_w = k.w_tiles && p.w_parts > 1 ? (a.K + 1) * a.N : 0;
@@ -1205,7 +1286,7 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
     if (small_problem(a)) {
         const SmallPlan s = small_plan(a);
         if (!forward && (e = launch_small_logits(a, s, static_cast<char*>(workspace), false, true, stream)) != hipSuccess) return e;
-        return launch_small_gradients(a, s, static_cast<char*>(workspace), stream);
+        return launch_small_gradients(a, s, static_cast<char*>(workspace), forward, stream);
     }
     const Plan p = plan_of(a, false);
     float* z = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.x + p.w);
