@@ -13,6 +13,7 @@ namespace hdqt {
 namespace {
 
 constexpr int kThreads = kClipThreads, kLoads = kClipLoads;
+constexpr int64_t kClipStream = (int64_t)128 << 20;         // bytes of all pieces above which the product goes past the caches
 
 // the tensor that piece `p` of the launch belongs to
 __device__ __forceinline__ int tensor_of(const ClipTable& t, uint32_t p)
@@ -147,7 +148,23 @@ __global__ __launch_bounds__(kFinish) void clip_finish_kernel(const double* part
     *scale = f.scale;
 }
 
-template <int DT>
+// sixteen bytes, and where they are not to stay in the caches
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+template <bool STREAM>
+__device__ __forceinline__ uint4 take(const uint4* p)
+{
+    if constexpr (!STREAM) return *p;
+    const v4u q = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
+    return make_uint4(q.x, q.y, q.z, q.w);
+}
+template <bool STREAM>
+__device__ __forceinline__ void put(uint4* p, uint4 v)
+{
+    if constexpr (!STREAM) *p = v;
+    else __builtin_nontemporal_store(v4u{v.x, v.y, v.z, v.w}, reinterpret_cast<v4u*>(p));
+}
+
+template <bool STREAM, int DT>
 __device__ __forceinline__ void piece_scale(const ClipTensor& t, int64_t begin, int64_t end, bool wide, float c)
 {
     constexpr int V = DT == kBf16 ? 8 : 4;
@@ -162,7 +179,7 @@ __device__ __forceinline__ void piece_scale(const ClipTensor& t, int64_t begin, 
         uint4 v[kLoads];
 #pragma unroll
         for (int k = 0; k < kLoads; ++k)
-            if (at + k * kThreads < whole / V) v[k] = src[at + k * kThreads];
+            if (at + k * kThreads < whole / V) v[k] = take<STREAM>(src + at + k * kThreads);
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
@@ -173,7 +190,7 @@ __device__ __forceinline__ void piece_scale(const ClipTensor& t, int64_t begin, 
                 else
                     w[j] = __float_as_uint(c * __uint_as_float(w[j]));
             }
-            if (at + k * kThreads < whole / V) dst[at + k * kThreads] = make_uint4(w[0], w[1], w[2], w[3]);
+            if (at + k * kThreads < whole / V) put<STREAM>(dst + at + k * kThreads, make_uint4(w[0], w[1], w[2], w[3]));
         }
     }
     const int64_t i = whole + threadIdx.x;
@@ -183,7 +200,9 @@ __device__ __forceinline__ void piece_scale(const ClipTensor& t, int64_t begin, 
 // Of few pieces every workgroup adds up the sums itself, one after a launch of a single workgroup would (ResNet-18's 62
 // gradients, 1400 pieces: a launch less); of many it reads what that launch has left.  (From the last piece to the first, which
 // the memory-side cache may still hold, is no faster: 453 us either way for 2.4 GB, 18.6 against 17.4 for ResNet-18's.)
-template <bool LARGEST, bool OWN>
+// STREAM: past the caches.  With a pass over the results behind it, out of place, of 100 MB 112 us, 104 through the caches; of 150
+// MB 152 and 168, 300 MB 304 and 333, 1 GB 1014 and 1055.
+template <bool LARGEST, bool OWN, bool STREAM>
 __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, const double* parts, uint32_t pieces, float max_norm, float eps,
                                                               float* norm, const float* scale)
 {
@@ -200,8 +219,8 @@ __global__ __launch_bounds__(kThreads) void clip_scale_kernel(ClipTable t, const
     }
     if (c == 1.0f && x.src == x.dst) return;
     const Piece p = piece_of(t, x, piece);
-    if (x.dtype == kBf16) piece_scale<kBf16>(x, p.begin, p.end, p.wide, c);
-    else piece_scale<kF32>(x, p.begin, p.end, p.wide, c);
+    if (x.dtype == kBf16) piece_scale<STREAM, kBf16>(x, p.begin, p.end, p.wide, c);
+    else piece_scale<STREAM, kF32>(x, p.begin, p.end, p.wide, c);
 }
 
 } // namespace
@@ -228,9 +247,10 @@ hipError_t launch_clip_scale(const ClipTable& t, const double* parts, uint32_t p
 {
     ProfileScope ps(K_CLIP_SCALE, stream);
     const dim3 grid(t.pieces), block(kThreads);
-    if (!clip_scales_alone(pieces)) hipLaunchKernelGGL((clip_scale_kernel<false, false>), grid, block, 0, stream, t, parts, pieces, max_norm, eps, norm, scale);
-    else if (largest) hipLaunchKernelGGL((clip_scale_kernel<true, true>), grid, block, 0, stream, t, parts, pieces, max_norm, eps, norm, scale);
-    else hipLaunchKernelGGL((clip_scale_kernel<false, true>), grid, block, 0, stream, t, parts, pieces, max_norm, eps, norm, scale);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, t, parts, pieces, max_norm, eps, norm, scale); };
+    const bool large = (int64_t)pieces * t.loads * kThreads * 16 > kClipStream;
+    if (!clip_scales_alone(pieces)) launch(large ? clip_scale_kernel<false, false, true> : clip_scale_kernel<false, false, false>);
+    else launch(largest ? clip_scale_kernel<true, true, false> : clip_scale_kernel<false, true, false>);
     return hipGetLastError();
 }
 
