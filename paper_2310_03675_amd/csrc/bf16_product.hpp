@@ -6,6 +6,12 @@
 // the transposing LDS reads of this chip.  fp32 operands (P = 3) are three bfloat16 matrices, planes, that add up to them, 8
 // bits each, and the product is the six products of planes that are not below 2^-24 of the whole, smallest first; a stage
 // holds all planes, so that six products share the loads and the LDS reads of six planes.
+//
+// What bounds it: 8192 x 4096 x 16384 in tiles of 256 x 256, eight waves, the matrix pipe is busy 57 to 64 % of the time at
+// the 1.7 to 1.85 GHz that the chip holds under it, LDS 22 %, without conflicts; a stage of 64 takes 1.85 us, of which the
+// products are 1.1.  A step of the classifier's loss over 128000 classes takes 28.2 ms, with one set of fragments 29.8; with the matrix
+// instructions at a higher wave priority, or without the fences around the reads, 28.7 and 29.6; with four waves of 128 x 128,
+// one to a SIMD, 31.8.
 #pragma once
 #include "train.hpp"
 

