@@ -3,7 +3,7 @@
 // contract of every function.
 
 #include "../../include/hdqt.h"
-#include "common.hpp"
+#include "train.hpp"
 
 #include <limits.h>
 #include <mutex>

@@ -234,9 +234,6 @@ enum KernelId {
     K_DUAL_ABSMAX_X, K_DUAL_ABSMAX_W, K_DUAL_ABSMAX_G, K_DUAL_QUANT_X, K_DUAL_QUANT_W, K_DUAL_QUANT_G,
     K_DUAL_ABSMAX_BATCH, K_DUAL_QUANT_BATCH, K_REQUANT_TILES, K_REQUANT_SUM, K_IM2COL, K_RELU_MASK,
     K_GEMM_RAGGED, K_GEMM_SMALL, K_COL2IM, K_TRANSPOSE, K_EXPAND,
-    K_CLIP_NORM, K_CLIP_FINISH, K_CLIP_SCALE, K_NORM_FWD_SUMS, K_NORM_FWD_FINISH, K_NORM_FWD, K_NORM_BWD_SUMS,
-    K_NORM_BWD_FINISH, K_NORM_BWD, K_XENT_LOGITS, K_XENT_LOSS, K_XENT_DLOGITS, K_XENT_DX, K_XENT_DW, K_XENT_DBIAS,
-    K_XENT_PACK, K_XENT_ADD_PARTS, K_NORM_PARAMS,
     K_COUNT
 };
 bool quantize_fast_eligible(const QuantArgs& q);
@@ -264,7 +261,6 @@ bool gemm_packed_eligible(const GemmArgs& g);
 hipError_t launch_gemm_packed(const GemmArgs& g, hipStream_t stream);
 hipError_t launch_gemm_fast(const GemmArgs& g, hipStream_t stream);
 const char* kernel_name(int id);
-int hip_fail(hipError_t e);          // notes the error for hdqt_last_hip_error (api.hip); HDQT_EHIP
 bool profiling_enabled();
 void profile_begin(int id, hipStream_t stream);
 void profile_end(int id, hipStream_t stream);

@@ -10,7 +10,7 @@
 // one thread controls; the events of two threads' launches are not kept apart.
 
 #include "../../include/hdqt.h"
-#include "common.hpp"
+#include "train.hpp"
 
 #include <atomic>
 #include <mutex>
@@ -29,7 +29,7 @@ std::vector<Pending> g_open;     // begun, not yet ended (per launch, LIFO)
 
 const char* kernel_name(int id)
 {
-    static const char* names[K_COUNT] = {
+    static const char* names[K_ALL_COUNT] = {
         "zero", "fwht_row_absmax", "fwht_row_quant", "fwht_col_absmax", "fwht_col_quant",
         "fwht_any_absmax", "fwht_any_quant", "gemm_tiled_aligned", "gemm_tiled_generic", "reduce_splits",
         "gemm_i4", "fwht_dual_absmax", "fwht_dual_quant", "gemm_i4_fwd", "gemm_i4_bwd_input",
@@ -40,7 +40,7 @@ const char* kernel_name(int id)
         "clip_norm", "clip_finish", "clip_scale", "groupnorm_fwd_sums", "groupnorm_fwd_finish", "groupnorm_fwd",
         "groupnorm_bwd_sums", "groupnorm_bwd_finish", "groupnorm_bwd", "xent_logits", "xent_loss", "xent_dlogits",
         "xent_dx", "xent_dw", "xent_dbias", "xent_pack", "xent_add_parts", "groupnorm_params"};
-    return (id >= 0 && id < K_COUNT) ? names[id] : "?";
+    return (id >= 0 && id < K_ALL_COUNT) ? names[id] : "?";
 }
 
 bool profiling_enabled() { return g_enabled.load(std::memory_order_relaxed); }
@@ -83,8 +83,8 @@ int hdqt_profile_enable(int on)
 int hdqt_profile_collect(hdqt_kernel_time_t* rows, int max_rows)
 {
     std::lock_guard<std::mutex> lock(hdqt::g_mu);
-    double total[hdqt::K_COUNT] = {0};
-    long launches[hdqt::K_COUNT] = {0};
+    double total[hdqt::K_ALL_COUNT] = {0};
+    long launches[hdqt::K_ALL_COUNT] = {0};
     for (const hdqt::Pending& p : hdqt::g_pending) {
         float ms = 0.0f;
         if (hipEventSynchronize(p.stop) == hipSuccess &&
@@ -97,7 +97,7 @@ int hdqt_profile_collect(hdqt_kernel_time_t* rows, int max_rows)
     }
     hdqt::g_pending.clear();
     int n = 0;
-    for (int id = 0; id < hdqt::K_COUNT; ++id) {
+    for (int id = 0; id < hdqt::K_ALL_COUNT; ++id) {
         if (!launches[id]) continue;
         if (rows && n < max_rows) {
             strncpy(rows[n].name, hdqt::kernel_name(id), sizeof(rows[n].name) - 1);

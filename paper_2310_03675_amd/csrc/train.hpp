@@ -6,6 +6,15 @@
 
 namespace hdqt {
 
+// these operators' kernels, behind the others' (common.hpp is left as it is: the benchmark's counters are tied to it)
+enum TrainKernelId {
+    K_CLIP_NORM = K_COUNT, K_CLIP_FINISH, K_CLIP_SCALE, K_NORM_FWD_SUMS, K_NORM_FWD_FINISH, K_NORM_FWD, K_NORM_BWD_SUMS,
+    K_NORM_BWD_FINISH, K_NORM_BWD, K_XENT_LOGITS, K_XENT_LOSS, K_XENT_DLOGITS, K_XENT_DX, K_XENT_DW, K_XENT_DBIAS,
+    K_XENT_PACK, K_XENT_ADD_PARTS, K_NORM_PARAMS,
+    K_ALL_COUNT
+};
+int hip_fail(hipError_t e);          // notes the error for hdqt_last_hip_error (api.hip); HDQT_EHIP
+
 enum Dtype { kF32 = 0, kBf16 = 1 };
 inline int64_t dtype_size(int d) { return d == kBf16 ? 2 : 4; }
 
