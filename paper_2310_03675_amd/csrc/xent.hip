@@ -1,5 +1,5 @@
-// Softmax cross entropy of a linear classifier over N classes, in pieces of the classes, without the logits in memory
-// (gfx950):
+// Softmax cross entropy of a linear classifier over N classes, in pieces of the classes, of which large problems keep no
+// logits (gfx950):
 //   z = X W + b,  lse_i = log sum_j exp z_ij,  loss_i = lse_i - z_i,target(i)  (0 where the target is to be ignored)
 //   dz_ij = g_i (exp(z_ij - lse_i) - [j = target(i)]),  dX = dz W^T,  dW = X^T dz,  db = sum_i dz_ij
 // Forward, every tile of the product leaves the largest logit of a row and the sum of exponentials relative to it; a
@@ -8,9 +8,9 @@
 //
 // The matrix pipe bounds large problems: four products of 2 M K N operations forward and backward, of which three are what the
 // gradients need and one is what not keeping the logits costs.  8192 x 4096 x 128000 in bfloat16: 28.2 ms, the products 6.9 to
-// 7.3 each, 1180 to 1250 TFLOP/s, where a large library product reaches 1160 to 1525 by orientation; 4096 x 2048 x 50257 3.1 ms,
+// 7.4 each, 1170 to 1240 TFLOP/s, where a large library product reaches 1160 to 1525 by orientation; 4096 x 2048 x 50257 3.1 ms,
 // 1110, of it 0.11 for W, whose rows are no whole 16 bytes.  fp32 (six products of planes; the logits kept where the classes are one
-// piece): 777 x 320 x 10007 158 us of which the three products take 115, 130 TFLOP/s of 32 bits, and the library's large one 154.
+// piece): 777 x 320 x 10007 160 us of which the three products take 124, 120 TFLOP/s of 32 bits; the library's large one has 154.
 // dz is rounded to bfloat16 where the problem is: its error, 2^-9 of each term, is of the size of the operands' own; db is
 // summed in front of that rounding.  Small problems (below) wait for launches and memory, not for the matrix pipe.
 #include "bf16_product.hpp"
