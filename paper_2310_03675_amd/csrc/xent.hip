@@ -719,7 +719,7 @@ __device__ __forceinline__ float row_factor(const XentArgs& a, int64_t row)
 // JOIN: the forward pass has left the rows' pairs as they are.  Every workgroup joins all rows' for itself, and the first one
 // writes what the forward pass owes: a launch less (1 x 561 x 11 16.8 us in three launches, 14.1 in two; 128 x 512 x 100 17.6 and
 // 14.4).  Kernels this short wait for their own instructions: with the next round's loads in flight beside the products
-// (half as much code again) they take 16.4 and 16.7, and large ones no less (32 x 256 x 64000 in fp32 405 us, here 217).
+// (half as much code again) they take 16.4 and 16.7, and large ones no less (32 x 256 x 64000 in fp32 by these kernels 405 us, without 217).
 template <int DT, bool VEC, bool JOIN>
 __global__ __launch_bounds__(64 * kSmallWaves) void xent_small_gradients_kernel(XentArgs a, SmallArgs k)
 {
@@ -1112,21 +1112,8 @@ RowArgs rows_of(const XentArgs& a, int64_t first, int64_t classes)
 
 constexpr int64_t kSmallLogits = (int64_t)8 << 20;          // of 4 bytes
 
-// Whether a problem is small.  bfloat16: the large products' seven launches are what they take (128 x 512 x 1000 44 us, here 35;
-// 512 x 512 x 100 49 and 32; 2048 x 512 x 100 52 and 53), unless W is large, whose single elements are read here (1 x 512 x 33000
-// 72 and 118).  fp32: by the time of a step, microseconds, here three products at 50 TFLOP/s on whole tiles and a fifth
-// more, there the cuts' and what the packing and the logits move at 4 TB/s (512 x 2048 x 1000 152 us, the large products
-// 178; 2048 x 512 x 1000 175 and 136; 8192 x 2048 x 100 412 and 240; 1 x 4096 x 128000 1543 and 4763).
-bool small_problem(const XentArgs& a)
-{
-    if (a.M * a.N > kSmallLogits) return false;
-    if (a.dtype == kBf16) return a.K * a.N <= ((int64_t)3 << 19) && a.M * a.N <= ((int64_t)1 << 26) / a.K;
-    const double kn = (double)a.K * (double)a.N, mk = (double)a.M * (double)a.K, mn = (double)a.M * (double)a.N;
-    const double here = 18.0 + 3.6 * (double)up(a.M, kSmallTile) * (double)up(a.N, kSmallTile) * (double)a.K / 25.0e6;
-    const double large = 60.0 + cut_of(a.N, a.M, a.K, 3, false).us + cut_of(a.M, a.K, a.N, 3, true).us + cut_of(a.K, a.N, a.M, 3, true).us +
-                         (10.0 * (kn + mk) + 14.0 * mn) / 4.0e6;
-    return here <= large;
-}
+// (of fewer outputs a launch more is not worth it; bfloat16 problems of so many are not small)
+bool few_rows(const XentArgs& a) { return a.dtype == kF32 && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20; }
 
 struct SmallPlan {
     int64_t class_tiles, row_tiles, step;
@@ -1154,6 +1141,34 @@ SmallPlan small_plan(const XentArgs& a)
     return p;
 }
 
+// Whether a problem is small.  bfloat16: the large products' seven launches are what they take (128 x 512 x 1000 44 us, here 34;
+// 512 x 512 x 100 49 and 30; 2048 x 512 x 100 51 and 52), unless W is large, whose single elements are read here (1 x 512 x 33000
+// 74 and 298).  fp32: by models of a step's time, microseconds.  Here 512 workgroups at a time, 2 to begin and 3 for every
+// round of the contraction, dW's 1 and 4, and a third for each round of the longest chain; of few rows dW at 4 TB/s.  There
+// the cuts', what the packing and the logits move at 3.5 TB/s, and 14.  (Fitted to 29 problems, of which both choose the faster
+// way, here and there: 128 x 512 x 1000 30 and 59, 512 x 512 x 1000 56 and 72, 32 x 2048 x 4000 101 and 113, 512 x 2048 x 1000 148 and
+// 119, 128 x 512 x 10000 119 and 84, 8192 x 512 x 100 102 and 84, 8192 x 64 x 100 39 and 65, 1 x 4096 x 128000 1508 and 4702.)
+bool small_problem(const XentArgs& a)
+{
+    if (a.M * a.N > kSmallLogits) return false;
+    if (a.dtype == kBf16) return a.K * a.N <= ((int64_t)3 << 19) && a.M * a.N <= ((int64_t)1 << 26) / a.K;
+    const SmallPlan p = small_plan(a);
+    const double kn = (double)a.K * (double)a.N, mk = (double)a.M * (double)a.K, mn = (double)a.M * (double)a.N;
+    auto rounds = [](int64_t length, int64_t of, uint32_t parts) {
+        const int64_t n = (length + of - 1) / of;
+        return (double)((n + parts - 1) / parts);
+    };
+    const double z = rounds(a.K, kSmallRound, 1), x = rounds(a.N, kSmallRound, p.x_parts), w = rounds(a.M, kSmallRound / 2, p.w_parts);
+    const double k_tiles = (double)((a.K + kSmallTile - 1) / kSmallTile), with_ones = (double)(a.K / kSmallTile + 1);
+    double here = 14.0 + 0.35 * (z + (x > w ? x : w));
+    here += (double)(p.row_tiles * p.class_tiles) / 512.0 * (2.0 + 3.0 * z) + (double)p.row_tiles * k_tiles * p.x_parts / 512.0 * (2.0 + 3.0 * x);
+    if (few_rows(a)) here += 4.0 + 4.0 * kn / 4.0e6;
+    else here += (double)p.class_tiles * with_ones * p.w_parts / 512.0 * (1.0 + 4.2 * w);
+    const double large = 14.0 + cut_of(a.N, a.M, a.K, 3, false).us + cut_of(a.M, a.K, a.N, 3, true).us + cut_of(a.K, a.N, a.M, 3, true).us +
+                         (10.0 * (kn + mk) + 14.0 * mn) / 3.5e6;
+    return here <= large;
+}
+
 // f(type, whole sixteen or eight bytes)
 template <class F>
 void with_small(const XentArgs& a, bool vec, F f)
@@ -1172,11 +1187,7 @@ bool fours(const void* p, int64_t ld, int64_t cols, int dtype)
     return reinterpret_cast<uintptr_t>(p) % (size_t)(4 * dtype_size(dtype)) == 0 && ld % 4 == 0 && cols % 4 == 0;
 }
 
-bool outer_problem(const XentArgs& a)
-{
-    // (of fewer outputs a launch more is not worth it; bfloat16 problems of so many are not small)
-    return (a.dW || a.dbias) && a.dtype == kF32 && a.M <= kOuterRows && a.K * a.N >= (int64_t)4 << 20;
-}
+bool outer_problem(const XentArgs& a) { return (a.dW || a.dbias) && few_rows(a); }
 // whether a step's gradients join the rows' pairs for themselves: few of them
 bool joins(const XentArgs& a, const SmallPlan& p)
 {
