@@ -716,7 +716,8 @@ bool slab_of(const NormArgs& a, int V, bool backward, SlabPlan* plan)
     k.slabs = make_divisor(C / channels);
     k.total = C / channels * (uint32_t)a.B;
     k.per_xcd = (k.total + 7) / 8;
-    return true;
+    // (a launch has fewer than 2^32 threads along an axis; the slices' grid is spread over three)
+    return (uint64_t)8 * k.per_xcd * plan->threads < (uint64_t)1 << 32;
 }
 
 // f(threads, vectors as types): no more vectors than the threads' number asks for
