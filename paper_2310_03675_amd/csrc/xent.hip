@@ -999,19 +999,35 @@ Plan plan_of(const XentArgs& a, bool sizes)
 PackArgs pack_of(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint16_t* dst, int64_t step)
 {
     const int64_t pairs = (dtype == kBf16 ? step : step / 3) / 2;
-    PackArgs a{src, rows, cols, ld, dst, step, (uint32_t)((pairs + kThreads - 1) / kThreads), 0};
-    a.groups = a.across * (uint32_t)((rows + kPackRows - 1) / kPackRows);
-    return a;
+    return {src, rows, cols, ld, dst, step, (uint32_t)((pairs + kThreads - 1) / kThreads), 0};
+}
+// its first rows, as many as kPackGroups workgroups have (a launch has fewer than 2^32 threads: of both operands 2^31 at most)
+constexpr int64_t kPackGroups = (int64_t)1 << 22;
+PackArgs take_rows(PackArgs* a, int64_t size)
+{
+    PackArgs first = *a;
+    if (!a->rows) return first;
+    const int64_t most = kPackGroups / a->across * kPackRows;
+    if (first.rows > most) first.rows = most;
+    first.groups = a->across * (uint32_t)((first.rows + kPackRows - 1) / kPackRows);
+    a->rows -= first.rows;
+    a->src = static_cast<const char*>(a->src) + first.rows * a->ld * size;
+    a->dst += first.rows * a->step;
+    return first;
 }
 // (either may be empty)
-hipError_t launch_pack(const PackArgs& one, const PackArgs& other, int dtype, hipStream_t stream)
+hipError_t launch_pack(PackArgs one, PackArgs other, int dtype, hipStream_t stream)
 {
-    const dim3 grid(one.groups + other.groups);
-    if (grid.x == 0) return hipSuccess;
-    ProfileScope ps(K_XENT_PACK, stream);
-    if (dtype == kBf16) hipLaunchKernelGGL(xent_pack_kernel<kBf16>, grid, dim3(kThreads), 0, stream, one, other);
-    else hipLaunchKernelGGL(xent_pack_kernel<kF32>, grid, dim3(kThreads), 0, stream, one, other);
-    return hipGetLastError();
+    while (one.rows || other.rows) {
+        const PackArgs p = take_rows(&one, dtype_size(dtype)), q = take_rows(&other, dtype_size(dtype));
+        const dim3 grid(p.groups + q.groups);
+        ProfileScope ps(K_XENT_PACK, stream);
+        if (dtype == kBf16) hipLaunchKernelGGL(xent_pack_kernel<kBf16>, grid, dim3(kThreads), 0, stream, p, q);
+        else hipLaunchKernelGGL(xent_pack_kernel<kF32>, grid, dim3(kThreads), 0, stream, p, q);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <bool GRAD>

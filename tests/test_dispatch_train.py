@@ -1,4 +1,7 @@
 """What the operators around the products launch, at the edges of their rules (host code: nothing is launched)."""
+import math
+import random
+
 import pytest
 
 from dispatch_train import dispatch
@@ -13,3 +16,46 @@ def test_normalisations_of_many_groups_are_launched(B, P, C, G, dtype, off):
     registers each."""
     for call in dispatch([(kind, B, P, C, G, dtype, off, act) for kind in ("norm_fwd", "norm_bwd") for act in range(3)]):
         assert call.rc == 0, call
+
+
+@pytest.mark.parametrize("M,K,N", [(4194240, 16536, 3), (11, 2097112, 32663), (4194145, 16637, 1), (1, 2097152, 33327)])
+@pytest.mark.parametrize("off", [0, 1])
+def test_operands_of_any_size_are_packed(M, K, N, off):
+    """More features and rows, or classes, than a launch has threads for at eight rows and two columns each."""
+    for call in dispatch([("xent_fwd", M, K, N, off, BF16, 1), ("xent_step", M, K, N, off, BF16, 1, 6)]):
+        assert call.rc == 0, call
+
+
+def _size(rng, lo, hi):
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    return rng.choice((lo, hi, hi - rng.randint(0, 99), max(lo, min(hi, round(v))), max(lo, min(hi, round(v)))))
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_what_the_memory_holds_is_launched(seed):
+    """Sizes at random, up to the largest that are taken, of which tensors and workspace are at most 288 GB."""
+    rng, calls, held = random.Random(seed), [], []
+    while len(calls) < 2000:
+        dtype, off = rng.randint(0, 1), rng.randint(0, 1)
+        size = 2 if dtype else 4
+        if rng.random() < 0.5:
+            C = _size(rng, 100, 65536)
+            G = rng.choice([d for d in (1, 2, 3, 4, 5, 8, 10, 16, 32, 50, 64, 100, 128, 256, 1024, C) if C % d == 0])
+            images, P = _size(rng, 100, 65535), _size(rng, 100, (1 << 31) - 1) // 100
+            if images * G > 1 << 23:
+                continue
+            calls.append((rng.choice(("norm_fwd", "norm_bwd")), images, P, C, G, dtype, off, rng.randint(0, 2)))
+            held.append(2 * images * P * C * size)
+        else:
+            M, K, N = _size(rng, 100, 4194240) // rng.choice((1, 100)), _size(rng, 100, 1 << 21), _size(rng, 100, 4194240) // rng.choice((1, 100))
+            need = rng.randint(1, 7)
+            kind = rng.choice(("xent_fwd", "xent_bwd", "xent_step"))
+            calls.append((kind, M, K, N, off, dtype, rng.randint(0, 2), need))
+            grads = 0 if kind == "xent_fwd" else (need & 1) * M * K + (need >> 1 & 1) * K * N
+            held.append((M * K + K * N + grads) * size)
+    fit = 0
+    for call, tensors, got in zip(calls, held, dispatch(calls)):
+        if tensors + got.workspace <= 288e9:
+            fit += 1
+            assert got.rc == 0, (call, got)
+    assert fit > 400
