@@ -764,10 +764,16 @@ void with_types(const NormArgs& a, int V, F f)
 
 size_t norm_workspace(const NormArgs& a, bool backward)
 {
-    // (whatever the tensors' alignment turns out to be: the larger of both ways)
-    const Cut one = cut_of(a, 1), wide = cut_of(a, a.dtype == kBf16 ? (a.C % 8 ? 1 : 8) : (a.C % 4 ? 1 : 4));
-    const size_t p = parts_bytes(a, one), q = parts_bytes(a, wide);
-    return (p > q ? p : q) + (backward ? images_bytes(a) + (size_t)a.B * a.G * sizeof(float2) : 0);
+    // (whatever the tensors' alignment turns out to be: the larger of both ways; slices' sums only where a way has slices)
+    size_t most = 0;
+    for (const int V : {1, a.dtype == kBf16 ? (a.C % 8 ? 1 : 8) : (a.C % 4 ? 1 : 4)}) {
+        SlabPlan slab;
+        if (slab_of(a, V, backward, &slab)) continue;
+        const size_t need = (backward ? (size_t)a.B * a.G * sizeof(float2) : 0) + parts_bytes(a, cut_of(a, V));
+        if (need > most) most = need;
+    }
+    most += backward ? images_bytes(a) : 0;
+    return most ? most : 256;           // (none is what invalid arguments have)
 }
 
 hipError_t launch_norm_fwd(const NormArgs& a, void* workspace, hipStream_t stream)

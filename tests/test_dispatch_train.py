@@ -59,3 +59,12 @@ def test_what_the_memory_holds_is_launched(seed):
             fit += 1
             assert got.rc == 0, (call, got)
     assert fit > 400
+
+
+def test_normalisations_without_slices_hold_no_sums_of_slices():
+    """A workspace is for what a call writes into it: with an image's channels in registers nothing forward, and the images'
+    sums of their channels backward."""
+    sizes = [(128, 1024, 64, 32, F32), (128, 16, 512, 32, F32), (65535, 1, 256, 8, BF16), (4096, 1, 8192, 64, F32), (1, 49, 96, 3, BF16)]
+    for (images, P, C, G, dtype), fwd, bwd in zip(sizes, dispatch([("norm_fwd",) + s for s in sizes]), dispatch([("norm_bwd",) + s for s in sizes])):
+        assert all("sums" not in k for k in fwd.kernels + bwd.kernels)
+        assert 0 < fwd.workspace <= 256 and 0 < bwd.workspace <= 8 * images * C + 256, (fwd, bwd)
