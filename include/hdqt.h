@@ -521,8 +521,9 @@ typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
  *     loss = l (HDQT_REDUCE_NONE, M values), sum_i l_i, or sum_i l_i / max(1, rows that count)
  * and its gradients, with g_i = dloss (a value for each row, or one) times the row's share in the loss:
  *     dz_ij = g_i (exp(z_ij - lse_i) - [j = target(i)]),   dX = dz W^T,   dW = X^T dz,   dbias_j = sum_i dz_ij
- * The logits are not kept: they are formed tile by tile, and in the backward pass again, in pieces of the
- * classes whose dz lies in the workspace (128 MB of it, or 1024 classes where those are more).
+ * The logits are formed in pieces of the classes, and in the backward pass again; neither call keeps them but for
+ * small problems.  dz of a piece lies in the workspace: 128 MB of it, or 1024 classes where those are more (which may
+ * be all of them).
  *   X         [M, K], rows ldx >= K elements apart; W [K, N], rows ldw >= N apart (a head that has more
  *             classes than are in use); both of `dtype`
  *   bias      [N] of bias_dtype, or NULL.  Minus infinity takes a class out: probability and gradient zero
@@ -535,12 +536,14 @@ typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
  *   dX, dW    [M, K] and [K, N], dense, of `dtype`; dbias [N] of bias_dtype; any may be NULL (one must not)
  *   dloss     fp32, M values for HDQT_REDUCE_NONE, else one; NULL: ones
  *   workspace 256-byte aligned, hdqt_xent_{fwd,bwd,step}_workspace_size (0 for invalid arguments): dz of a
- *             piece, sums that are added up over pieces and parts of a product, and, for fp32 or rows that are no
- *             whole 16 bytes, X and W (as a whole up to 256 MB, else a piece) in the form that the products take:
- *             2 bytes an element, 6 in fp32
+ *             piece (2 bytes an element, 6 in fp32), sums that are added up over rows, over pieces and over parts of a
+ *             product, for fp32 or rows that are no whole 16 bytes X and W (as a whole up to 256 MB, else a piece) in
+ *             the form that the products take (2 bytes an element, 6 in fp32), and the logits (4 bytes) of small
+ *             problems (8 M at most) and of a step that keeps them
  * HDQT_EINVAL_DIM for K above 2^21, M or N above 4 194 240.
- * hdqt_xent_step is the forward and the backward call with dloss = 1.  Its backward half takes the logits from
- * the forward half where those are few (small problems) or, in fp32, all classes are one piece.
+ * hdqt_xent_step is the forward and the backward call with dloss = 1, and gives the same bits.  Its backward half takes
+ * the logits from the forward half where the problem is small or, in fp32, all classes are one piece and their logits at
+ * most 128 MB.
  * bfloat16: products of bfloat16 with sums in 32 bits; dz is rounded to bfloat16 before its products.
  * fp32: as exact as products in 32 bits.
  */

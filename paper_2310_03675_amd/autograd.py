@@ -253,7 +253,7 @@ class Unfold(torch.autograd.Function):
 
 class CrossEntropy(torch.autograd.Function):
     """Softmax cross entropy of the classifier X W + bias (hdqt_xent_fwd / hdqt_xent_bwd): the logits are not kept
-    between the passes, nor formed as a whole.  X [M, K], W [K, N], both fp32 or bfloat16, target int64 [M]."""
+    between the passes, and formed in pieces of the classes (of 128 MB, or 1024 classes).  X [M, K], W [K, N], both fp32 or bfloat16, target int64 [M]."""
 
     @staticmethod
     def forward(ctx, X, W, bias, target, ignore_index: int, reduction: str):

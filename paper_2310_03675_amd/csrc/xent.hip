@@ -1,5 +1,4 @@
-// Softmax cross entropy of a linear classifier over N classes, in pieces of the classes, of which large problems keep no
-// logits (gfx950):
+// Softmax cross entropy of a linear classifier over N classes, in pieces of the classes (gfx950):
 //   z = X W + b,  lse_i = log sum_j exp z_ij,  loss_i = lse_i - z_i,target(i)  (0 where the target is to be ignored)
 //   dz_ij = g_i (exp(z_ij - lse_i) - [j = target(i)]),  dX = dz W^T,  dW = X^T dz,  db = sum_i dz_ij
 // Forward, every tile of the product leaves the largest logit of a row and the sum of exponentials relative to it; a
@@ -9,8 +8,8 @@
 // The matrix pipe bounds large problems: four products of 2 M K N operations forward and backward, of which three are what the
 // gradients need and one is what not keeping the logits costs.  8192 x 4096 x 128000 in bfloat16: 28.2 ms, the products 6.9 to
 // 7.4 each, 1170 to 1240 TFLOP/s, where a large library product reaches 1160 to 1525 by orientation; 4096 x 2048 x 50257 3.1 ms,
-// 1110, of it 0.11 for W, whose rows are no whole 16 bytes.  fp32 (six products of planes; the logits kept where the classes are one
-// piece): 777 x 320 x 10007 160 us of which the three products take 124, 120 TFLOP/s of 32 bits; the library's large one has 154.
+// 1110, of it 0.11 for W, whose rows are no whole 16 bytes.  fp32 (six products of planes; a step keeps the logits where the classes are
+// one piece): 777 x 320 x 10007 160 us of which the three products take 124, 120 TFLOP/s of 32 bits; the library's large one has 154.
 // dz is rounded to bfloat16 where the problem is: its error, 2^-9 of each term, is of the size of the operands' own; db is
 // summed in front of that rounding.  Small problems (below) wait for launches and memory, not for the matrix pipe.
 #include "bf16_product.hpp"
@@ -118,8 +117,9 @@ struct RowArgs {
     int each;                           // rows have a factor of their own
     uint16_t* dz;                       // [M][step], zeros behind the classes
     int64_t step;
-    float* column;                      // [tiles of rows][classes]: dz's sums over a tile's rows; null: not wanted
-    float* z;                           // [M][z_step]: the logits, where the gradients that follow can have them; null: not kept
+    float* column;                      // [tiles of rows][classes]: dz's sums over a tile's rows, or over kRowsOfDz; null: not wanted
+    int eights;                         // the latter
+    float* z;                           // [M][z_step]: the logits, for a step's gradients; null: not kept
     int64_t z_step;
 };
 
@@ -134,12 +134,17 @@ __device__ __forceinline__ float sum_halves(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// over lanes 0 .. 31 and over lanes 32 .. 63, in every one of them
-__device__ __forceinline__ float sum_of_32(float v)
+// over eight lanes side by side, and over lanes 0 .. 31 and lanes 32 .. 63, in every one of them
+__device__ __forceinline__ float sum_of_8(float v)
 {
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, true));        // lane ^ 1
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, true));        // lane ^ 2
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, true));       // the other four of eight
+    return v;
+}
+__device__ __forceinline__ float sum_of_32(float v)
+{
+    v = sum_of_8(v);
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, true));       // the other eight of sixteen
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
@@ -155,6 +160,11 @@ __device__ __forceinline__ float sum_of_32(float v)
     bf16::Stages<S> stages;                                                                                  \
     stages.a[0] = a0; stages.a[1] = a1; stages.b[0] = b0; stages.b[1] = b1;                                  \
     if constexpr (S > 2) { stages.a[S - 1] = a2; stages.b[S - 1] = b2; }
+
+// Rows whose dz is added up for dbias first where a step keeps the logits: the same, to the bit, when a backward call of that size
+// multiplies them again.  (Where no step does, a tile's rows: a sum for eight rows is 0.5 bytes a logit, 40000 x 32 x 4321 backward
+// 1117 us and 1323.)
+constexpr int kRowsOfDz = 8;
 
 // Lines of A are classes (W, read down), lines of B rows (X): a lane then holds sums of one row of the logits, and the
 // maximum and the sum over classes stay inside it but for one exchange between the wave's halves.
@@ -202,7 +212,7 @@ HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
                 }
             }
         if constexpr (!GRAD) {
-            if (any && r.pairs) {
+            if (any) {
 #pragma unroll
                 for (int i = 0; i < NA; ++i)
 #pragma unroll
@@ -218,7 +228,6 @@ HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
                         *reinterpret_cast<float4*>(to + 32 * i + 8 * q) =
                             make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
             }
-            if (!r.pairs) return;
             top = larger_half(top);
             const float base = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
@@ -277,8 +286,31 @@ HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
     if constexpr (NB > 2) column(std::integral_constant<int, 2>{});
     if constexpr (NB > 3) column(std::integral_constant<int, 3>{});
     static_assert(NB <= 4, "a call for each");
+    if constexpr (P == 3 && GRAD) {
+        if (r.column && r.eights) {
+            // a class's sums over eight rows, where a stage was; lines eight words longer, so that the four of a block lie in other banks
+            constexpr int kLine = TA + 8;
+            static_assert(TB / kRowsOfDz * kLine * sizeof(float) <= sizeof a0, "room for them");
+            float* eights = reinterpret_cast<float*>(a0);
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int i = 0; i < NA; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float s = sum_of_8(acc[i][j][e]);
+                        if ((lane & 7) == 0)
+                            eights[((row0 + 32 * j + (lane & 31)) >> 3) * kLine + class0 + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)] = s;
+                    }
+            __syncthreads();
+            for (int t = threadIdx.x; t < TB / kRowsOfDz * TA; t += 64 * WA * WB) {
+                const int64_t c = (int64_t)p.at * TA + t % TA, eight = (int64_t)p.bt * (TB / kRowsOfDz) + t / TA;
+                if (c < r.classes && eight * kRowsOfDz < r.M) r.column[eight * r.classes + c] = eights[t / TA * kLine + t % TA];
+            }
+            return;
+        }
+    }
     if constexpr (!GRAD) {
-        if (!r.pairs) return;           // (only the logits are wanted)
         __syncthreads();
         for (int t = threadIdx.x; t < TB; t += 64 * WA * WB) {
             const int64_t row = (int64_t)p.bt * TB + t;
@@ -310,34 +342,41 @@ HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
     }
 }
 
-// dz in planes from the logits, where the forward pass has kept them: a workgroup has kRowsOfDz rows of 1024 classes, a thread
-// four classes.  Memory bounds it: 4 bytes read and 6 written for a logit, 777 x 10007 in 15 us (5.2 TB/s, out of the
-// memory-side cache), where the logits' product takes 45.
-constexpr int kRowsOfDz = 8;
+// dz in planes from the logits that a step has kept: a workgroup has kRowsOfDz rows of 1024 classes, a thread four classes.  Memory
+// bounds it: 4 bytes read and 6 written for a logit, 777 x 10007 in 15 us (5.2 TB/s, out of the memory-side cache), where the
+// logits' product takes 45.
 __global__ __launch_bounds__(kThreads) void xent_dz_kernel(RowArgs r)
 {
     const int64_t c = 4 * ((int64_t)blockIdx.y * kThreads + threadIdx.x), row0 = (int64_t)blockIdx.x * kRowsOfDz;
     if (c >= r.step / 3) return;
     float column[4] = {};
-#pragma unroll 4
-    for (int64_t row = row0; row < row0 + kRowsOfDz && row < r.M; ++row) {
-        const int64_t target = r.target[row], at = target - r.first_class - c;
-        const bool counted = target != r.ignore;
-        const float lse = r.saved[row], base = lse == -INFINITY ? 0.0f : lse;
-        const float each = r.each && counted ? (r.dloss ? r.dloss[row] : 1.0f) : 1.0f;
-        // (behind the last class there is no logit in memory that anyone has written)
-        const float4 q = c < r.z_step ? *reinterpret_cast<const float4*>(r.z + row * r.z_step + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const float z[4] = {q.x, q.y, q.z, q.w};
-        uint32_t s[4][3];
+#pragma unroll 1
+    for (int half = 0; half < kRowsOfDz; half += 4) {
+        float v[4][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float d = exp_of<true>(z[e] - base) - (at == e ? 1.0f : 0.0f), v = counted && c + e < r.classes ? d * each : 0.0f;
-            column[e] += v;
-            split(v, s[e]);
+        for (int k = 0; k < 4; ++k) {
+            const int64_t row = row0 + half + k, at_row = row < r.M ? row : r.M - 1;
+            const int64_t target = r.target[at_row], at = target - r.first_class - c;
+            const bool counted = row < r.M && target != r.ignore;
+            const float lse = r.saved[at_row], base = lse == -INFINITY ? 0.0f : lse;
+            const float each = r.each && counted ? (r.dloss ? r.dloss[at_row] : 1.0f) : 1.0f;
+            // (behind the last class there is no logit in memory that anyone has written)
+            const float4 q = c < r.z_step ? *reinterpret_cast<const float4*>(r.z + at_row * r.z_step + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            const float z[4] = {q.x, q.y, q.z, q.w};
+            uint32_t s[4][3];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float d = exp_of<true>(z[e] - base) - (at == e ? 1.0f : 0.0f);
+                v[k][e] = counted && c + e < r.classes ? d * each : 0.0f;
+                split(v[k][e], s[e]);
+            }
+            if (row >= r.M) continue;
+            uint16_t* to = r.dz + row * r.step + c / 32 * 96 + c % 32;
+#pragma unroll
+            for (int p = 0; p < 3; ++p) *reinterpret_cast<uint2*>(to + 32 * p) = make_uint2(s[0][p] | s[1][p] << 16, s[2][p] | s[3][p] << 16);
         }
-        uint16_t* to = r.dz + row * r.step + c / 32 * 96 + c % 32;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(to + 32 * k) = make_uint2(s[0][k] | s[1][k] << 16, s[2][k] | s[3][k] << 16);
+        for (int e = 0; e < 4; ++e) column[e] += (v[0][e] + v[1][e]) + (v[2][e] + v[3][e]);      // (in pairs, as lanes add them)
     }
     if (!r.column) return;
 #pragma unroll
@@ -940,6 +979,9 @@ Cut cut_of(int64_t RA, int64_t RB, int64_t D, int planes, bool may_split, int64_
     return best;
 }
 
+// dz of a piece, and logits that a step keeps, stay within what the memory-side cache holds between their writer and their readers
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;
+
 // How a call is cut, and where its pieces of the workspace lie.
 struct Plan {
     int planes;                         // 3: fp32
@@ -951,7 +993,8 @@ struct Plan {
     size_t pairs, picked, rows;         // forward
     Cut dx;
     size_t dz, dx_slices, slices, column;          // backward
-    size_t z;                           // the logits, in front of those
+    bool keeps;                         // a step of this size keeps the logits,
+    size_t z;                           // in front of those; 0: this call does not
 };
 
 bool whole_rows(const void* p, int64_t ld, int64_t cols, int dtype)
@@ -959,15 +1002,14 @@ bool whole_rows(const void* p, int64_t ld, int64_t cols, int dtype)
     return dtype == kBf16 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld < (int64_t)1 << 21;
 }
 
-// (sizes: for any alignment of the operands)
-Plan plan_of(const XentArgs& a, bool sizes)
+// (sizes: for any alignment of the operands; step: the forward and the backward pass in one call)
+Plan plan_of(const XentArgs& a, bool sizes, bool step)
 {
     Plan p{};
     p.planes = a.dtype == kF32 ? 3 : 1;
     p.pack_x = sizes || !whole_rows(a.X, a.ldx, a.K, a.dtype);
     p.pack_w = sizes || !whole_rows(a.W, a.ldw, a.N, a.dtype);
-    // dz of a piece stays within 128 MB, which the memory-side cache holds between its writer and its readers
-    p.piece = ((int64_t)128 << 20) / (2 * p.planes * a.M) / 256 * 256;
+    p.piece = kPieceBytes / (2 * p.planes * a.M) / 256 * 256;
     if (p.piece < 1024) p.piece = 1024;
     if (p.piece > 65536) p.piece = 65536;
     if (p.piece > a.N) p.piece = a.N;
@@ -984,9 +1026,14 @@ Plan plan_of(const XentArgs& a, bool sizes)
     // (dX is cut alike for all pieces: its parts' sums are kept from one to the next)
     p.dx = cut_of(a.M, a.K, p.piece, p.planes, true, (a.N + p.piece - 1) / p.piece);
     p.dx_slices = p.dx.parts > 1 || p.piece < a.N ? up256(sizeof(float) * p.dx.parts * a.M * a.K) : 0;
-    p.column = up256(sizeof(float) * (size_t)((a.M + kRowsOfDz - 1) / kRowsOfDz) * p.piece);
-    // in fp32, where the classes are one piece, a step keeps the logits: 4 bytes each, written and read, against six products
-    if (p.planes == 3 && p.piece == a.N) p.z = up256(sizeof(float) * (size_t)a.M * up(a.N, 256));
+    // in fp32, where the classes are one piece, a step keeps the logits: 4 bytes each, written and read, against six products.  (A backward
+    // call of its own multiplies them in the launch that makes dz: 777 x 320 x 10007 154.5 us, by way of the logits 155.2; 512 x 2048 x
+    // 1000 105 and 111, 128 x 512 x 10000 68 and 75.  What a step loses by the bound: 50000 x 512 x 1000 1164 us, 1392 without its 205 MB.)
+    const int64_t z = (int64_t)sizeof(float) * a.M * up(a.N, 256);
+    p.keeps = p.planes == 3 && p.piece == a.N && z <= kPieceBytes;
+    p.z = step && p.keeps ? up256((size_t)z) : 0;
+    const int64_t rows = p.keeps ? kRowsOfDz : p.planes == 3 ? 64 : 128;        // (the smaller tiles')
+    p.column = up256(sizeof(float) * (size_t)((a.M + rows - 1) / rows) * p.piece);
     size_t most = 0;
     for (const int64_t classes : {p.piece, a.N - (a.N - 1) / p.piece * p.piece}) {          // (the last piece's dW may be cut another way)
         const size_t parts = cut_of(a.K, classes, a.M, p.planes, true).parts, bytes = parts > 1 ? parts * a.K * classes : 0;
@@ -1288,17 +1335,17 @@ size_t xent_workspace(const XentArgs& a, bool forward, bool backward)
         const SmallPlan p = small_plan(a);
         return p.z + p.pairs + p.picked + p.rows + (backward ? p.x_slices + p.w_slices : 0);
     }
-    const Plan p = plan_of(a, true);
+    const Plan p = plan_of(a, true, forward && backward);
     const size_t f = forward ? p.pairs + p.picked + p.rows : 0, b = backward ? p.dz + p.dx_slices + p.slices + p.column : 0;
-    return p.x + p.w + (backward ? p.z : 0) + (f > b ? f : b);
+    return p.x + p.w + p.z + (f > b ? f : b);
 }
 
 hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hipStream_t stream)
 {
     if (small_problem(a)) return launch_small_logits(a, small_plan(a), static_cast<char*>(workspace), true, backward, stream);
-    const Plan p = plan_of(a, false);
+    const Plan p = plan_of(a, false, backward);
     char* at = static_cast<char*>(workspace) + p.x + p.w;
-    char* rest = at + (backward ? p.z : 0);
+    char* rest = at + p.z;
     float2* pairs = reinterpret_cast<float2*>(rest);
     float* picked = reinterpret_cast<float*>(rest + p.pairs);
     float* rows = a.reduction == kNone ? a.loss : reinterpret_cast<float*>(rest + p.pairs + p.picked);
@@ -1311,7 +1358,7 @@ hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hi
         RowArgs r = rows_of(a, first, classes);
         r.pairs = pairs + tiles * a.M;
         r.picked = picked;
-        if (backward && p.z) r.z = reinterpret_cast<float*>(at);
+        if (p.z) r.z = reinterpret_cast<float*>(at);
         r.z_step = up(a.N, 256);
         const Cut t = cut_of(classes, a.M, a.K, p.planes, false);
         const bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, t.a, t.b, 1);
@@ -1330,7 +1377,7 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
         if (!forward && (e = launch_small_logits(a, s, static_cast<char*>(workspace), false, true, stream)) != hipSuccess) return e;
         return launch_small_gradients(a, s, static_cast<char*>(workspace), forward, stream);
     }
-    const Plan p = plan_of(a, false);
+    const Plan p = plan_of(a, false, forward);
     float* z = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.x + p.w);
     char* at = reinterpret_cast<char*>(z) + p.z;
     uint32_t dx_parts = 1;
@@ -1346,12 +1393,11 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
         if (a.dbias) r.column = reinterpret_cast<float*>(at + p.dz + p.dx_slices + p.slices);
         Cut t = cut_of(classes, a.M, a.K, p.planes, false);
         bf16::Args g = bf16::plan(o.w, o.x, classes, a.M, a.K, p.planes, t.a, t.b, 1);
-        uint32_t row_tiles = g.n_bt;
+        r.eights = p.keeps;
+        const uint32_t row_tiles = p.keeps ? (uint32_t)((a.M + kRowsOfDz - 1) / kRowsOfDz) : g.n_bt;
         if (p.z) {
             r.z = z;
             r.z_step = up(a.N, 256);
-            if (!forward && (e = launch_logits<false>(K_XENT_LOGITS, g, r, p.planes, t.large, stream)) != hipSuccess) return e;
-            row_tiles = (uint32_t)((a.M + kRowsOfDz - 1) / kRowsOfDz);
             ProfileScope ps(K_XENT_DLOGITS, stream);
             // (rows along x: they may be more than 65535 workgroups)
             hipLaunchKernelGGL(xent_dz_kernel, dim3(row_tiles, (uint32_t)((p.dz_step / 3 + 4 * kThreads - 1) / (4 * kThreads))), dim3(kThreads), 0,

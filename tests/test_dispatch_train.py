@@ -68,3 +68,23 @@ def test_normalisations_without_slices_hold_no_sums_of_slices():
     for (images, P, C, G, dtype), fwd, bwd in zip(sizes, dispatch([("norm_fwd",) + s for s in sizes]), dispatch([("norm_bwd",) + s for s in sizes])):
         assert all("sums" not in k for k in fwd.kernels + bwd.kernels)
         assert 0 < fwd.workspace <= 256 and 0 < bwd.workspace <= 8 * images * C + 256, (fwd, bwd)
+
+
+def _cdiv(a, b):
+    return -(-a // b)
+
+
+@pytest.mark.parametrize("M,K,N", [(777, 320, 10007), (512, 2048, 1000), (10000, 512, 1000), (1000000, 512, 1000), (200000, 32, 1024), (3000000, 8, 20),
+                                   (40000, 32, 4321), (9001, 520, 6001)])
+def test_backward_calls_keep_no_logits(M, K, N):
+    """In fp32, where a step may keep them: a workspace of X and W in planes, dz of a piece in planes (128 MB, or 1024
+    classes), sums over rows for dbias, and sums of parts.  A step's logits are 128 MB at most."""
+    bwd, step = dispatch([("xent_bwd", M, K, N, 0, F32, 1, 7), ("xent_step", M, K, N, 0, F32, 1, 7)])
+    assert bwd.rc == step.rc == 0 and not any("dz_kernel" in k for k in bwd.kernels)
+    piece = min(N, max(1024, (128 << 20) // (6 * M) // 256 * 256))
+    planes = 6 * (M * _cdiv(K, 32) * 32 + K * _cdiv(N, 32) * 32)
+    dz, eights = 6 * M * _cdiv(piece, 256) * 256, 4 * _cdiv(M, 8 if piece == N and 4 * M * _cdiv(N, 256) * 256 <= 128 << 20 else 64) * piece
+    parts = 4 * 64 * max(M * K if M * K <= 1 << 24 else 0, K * N)          # (few outputs come in parts)
+    sums = 4 * M * K if piece < N or M * K <= 1 << 24 else 0
+    assert bwd.workspace <= planes + dz + eights + parts + sums + 4096
+    assert step.workspace - bwd.workspace <= (128 << 20) + 16 * M * _cdiv(N, 128)
