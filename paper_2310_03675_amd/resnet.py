@@ -16,17 +16,14 @@ from .autograd import ClassifierLoss, GroupNormAct, HdqtConv2d, HdqtLinear, Laye
 from .workloads import resnet18_layer_table
 
 
-class BatchNormRelu(torch.nn.BatchNorm2d):
-    """Batch normalisation and the rectifier behind it."""
-
-    def forward(self, x):
-        return torch.relu(super().forward(x))
-
-
 def _norm(kind: str, channels: int, act: str, groups: int):
-    if kind == "group":
-        return GroupNormAct(min(groups, channels), channels, act=act)
-    return BatchNormRelu(channels) if act == "relu" else torch.nn.BatchNorm2d(channels)
+    """PyTorch's batch normalisation, without the activation, or the library's group normalisation with it."""
+    return GroupNormAct(min(groups, channels), channels, act=act) if kind == "group" else torch.nn.BatchNorm2d(channels)
+
+
+def _rectified(norm, x):
+    """The rectifier behind a normalisation, outside of PyTorch's: whatever takes its place (torch.nn.SyncBatchNorm) keeps it."""
+    return norm(x) if isinstance(norm, GroupNormAct) else torch.relu(norm(x))
 
 
 class _Block(torch.nn.Module):
@@ -37,7 +34,7 @@ class _Block(torch.nn.Module):
         self.bn_p = _norm(norm, cout, "none", groups) if proj is not None else None
 
     def forward(self, x):
-        h = self.bn_a(self.conv_a(x))
+        h = _rectified(self.bn_a, self.conv_a(x))
         h = self.bn_b(self.conv_b(h))
         sc = x if self.proj is None else self.bn_p(self.proj(x))
         return torch.relu(h + sc)
@@ -91,7 +88,7 @@ class ResNet18(torch.nn.Module):
             self.to(device)
 
     def forward(self, x, target=None):
-        h = self.bn0(self.stem(x))
+        h = _rectified(self.bn0, self.stem(x))
         h = self.blocks(h).mean(dim=(2, 3))
         if hasattr(self, "fc"):
             return self.fc(h)
