@@ -88,6 +88,8 @@ class ResNet18(torch.nn.Module):
             self.to(device)
 
     def forward(self, x, target=None):
+        if target is not None and hasattr(self, "fc"):
+            raise ValueError('a target is for head="loss": the quantized classifier returns logits')
         h = _rectified(self.bn0, self.stem(x))
         h = self.blocks(h).mean(dim=(2, 3))
         if hasattr(self, "fc"):

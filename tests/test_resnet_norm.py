@@ -48,3 +48,10 @@ def test_the_rectifier_stays_when_the_normalisation_is_replaced(convert):
         assert float(seen[name].min()) == 0.0, name
     for name in ["bn0"] + [f"bn{i}a" for i in range(8)]:          # (a hook sees the normalisation alone)
         assert float(seen[name].min()) < 0.0, name
+
+
+def test_a_target_needs_the_loss_head():
+    """Refused before anything runs: the quantized classifier has no loss, and logits are not what a caller with targets
+    asks for."""
+    with pytest.raises(ValueError):
+        resnet.ResNet18()(torch.zeros(1, 3, 32, 32), torch.zeros(1, dtype=torch.int64))
