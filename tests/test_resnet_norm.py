@@ -9,7 +9,7 @@ from paper_2310_03675_amd.autograd import HdqtConv2d
 
 def _network(**options):
     torch.manual_seed(0)
-    net = resnet.ResNet18(head="loss", **options)
+    net = resnet.ResNet18(**options)
     for m in list(net.modules()):
         for name, conv in list(m.named_children()):
             if isinstance(conv, HdqtConv2d):
@@ -34,7 +34,7 @@ def _rectified(net, x):
 
 @pytest.mark.parametrize("convert", [False, True])
 def test_the_rectifier_stays_when_the_normalisation_is_replaced(convert):
-    net = _network()
+    net = _network(head="loss")
     x = torch.randn(4, 3, 32, 32)
     net.train()
     net(x)                                        # (running statistics)
@@ -53,5 +53,9 @@ def test_the_rectifier_stays_when_the_normalisation_is_replaced(convert):
 def test_a_target_needs_the_loss_head():
     """Refused before anything runs: the quantized classifier has no loss, and logits are not what a caller with targets
     asks for."""
+    net = _network()
+    net.fc = torch.nn.Linear(512, 100)
+    x = torch.zeros(2, 3, 32, 32)
+    assert tuple(net(x).shape) == (2, 100)
     with pytest.raises(ValueError):
-        resnet.ResNet18()(torch.zeros(1, 3, 32, 32), torch.zeros(1, dtype=torch.int64))
+        net(x, torch.zeros(2, dtype=torch.int64))
