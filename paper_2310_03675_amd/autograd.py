@@ -341,7 +341,7 @@ class ClassifierLoss(torch.nn.Module):
 def clip_gradients(parameters, max_norm: float, norm_type: float = 2.0, eps: float = 1e-6) -> torch.Tensor:
     """The norm of the parameters' gradients together, which are multiplied in place by min(1, max_norm / (norm + eps))
     (hdqt_clip_grad_norm).  The norm stays on the device: nothing waits for it."""
-    parameters = list(parameters)
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
     grads = [p.grad for p in parameters if p.grad is not None]
     if not grads:
         return torch.zeros((), device=parameters[0].device if parameters else None)

@@ -11,3 +11,13 @@ def test_without_gradients_the_norm_is_on_the_parameters_device():
         norm = A.clip_gradients(parameters, 1.0)
         assert norm.device.type == "meta" and norm.shape == () and norm.dtype == torch.float32
     assert float(A.clip_gradients([], 1.0)) == 0.0
+
+
+def test_a_single_tensor(monkeypatch):
+    """A parameter is its own list: its rows have no gradients, and nothing was clipped."""
+    got = []
+    monkeypatch.setattr(A.B, "clip_grad_norm", lambda grads, *how: got.append((grads, how)) or torch.ones(()))
+    p = torch.nn.Parameter(torch.zeros(4, 3))
+    p.grad = torch.ones(4, 3)
+    assert float(A.clip_gradients(p, 0.5, 2.0, 1e-6)) == 1.0
+    assert len(got) == 1 and got[0][0][0] is p.grad and len(got[0][0]) == 1 and got[0][1] == (0.5, 2.0, 1e-6)
