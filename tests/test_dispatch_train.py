@@ -88,3 +88,26 @@ def test_backward_calls_keep_no_logits(M, K, N):
     sums = 4 * M * K if piece < N or M * K <= 1 << 24 else 0
     assert bwd.workspace <= planes + dz + eights + parts + sums + 4096
     assert step.workspace - bwd.workspace <= (128 << 20) + 16 * M * _cdiv(N, 128)
+
+
+def test_the_tests_of_values_reach_the_large_kernels():
+    """Both tiles of either type, the launch that makes dz from logits that a step has kept, and dX over several pieces."""
+    import torch
+    from test_gpu_xent_edges import LARGE
+
+    seen = set()
+    for dtype, code in ((torch.float32, F32), (torch.bfloat16, BF16)):
+        for size in LARGE[dtype]:
+            for what in ("xent_step", "xent_bwd"):
+                call = dispatch([(what, *size, 0, code, 1, 7)])[0]
+                assert call.rc == 0 and not any("small" in k for k in call.kernels), call
+                seen.update(call.kernels)
+                if sum(k.startswith("xent_gradient_kernel") for k in call.kernels) > 2:
+                    seen.add(f"pieces {code}")
+    for planes, tiles in ((1, ("256, 256", "128, 128")), (3, ("256, 128", "128, 64"))):
+        for tile in tiles:
+            for grad in ("false", "true"):
+                assert any(k.startswith(f"xent_logits_kernel<{grad}, {planes}, {tile}") for k in seen), (grad, planes, tile)
+            for mode in (0, 1):
+                assert any(k.startswith(f"xent_gradient_kernel<{planes}, {mode}, {tile}") for k in seen), (mode, planes, tile)
+    assert "xent_dz_kernel" in seen and {"pieces 0", "pieces 1"} <= seen
