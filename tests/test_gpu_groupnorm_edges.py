@@ -39,3 +39,51 @@ def test_more_groups_than_a_launch_has_threads_for():
     near(dx[some], dwant, 2.0 ** -8 + 2e-6, norm=terms)
     for c in (0, 519, C - 1):                # sums of 65535 terms, added up in 64 bits
         near(db[c], dy[:, 0, c].double().sum().cpu(), 1.0, norm=2e-6 * dy[:, 0, c].double().norm().cpu() + 2.0 ** -23 * db[c].abs().cpu())
+
+
+@pytest.mark.parametrize("shape,G", [((4, 100, 48), 4), ((2, 9000, 320), 32)])
+def test_calls_on_a_side_stream(shape, G):
+    """Both calls, images in registers and in slices: the results of the default stream's, and of what was written there before."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, dy = (torch.randn(*shape, generator=g, device="cuda") for _ in range(2))
+    w, b = (torch.randn(shape[-1], generator=g, device="cuda") for _ in range(2))
+    want, saved0 = B.groupnorm_fwd(x, G, w, b, act="silu")
+    grads = B.groupnorm_bwd(dy, x, saved0, G, w, b, act="silu")
+    x2, dy2 = torch.zeros_like(x), torch.zeros_like(dy)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        x2.copy_(x)
+        dy2.copy_(dy)
+    y, saved = B.groupnorm_fwd(x2, G, w, b, act="silu", stream=side)
+    got = B.groupnorm_bwd(dy2, x2, saved, G, w, b, act="silu", stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(y, want) and torch.equal(saved, saved0) and all(torch.equal(p, q) for p, q in zip(got, grads))
+    torch.cuda.synchronize()
+
+
+def test_input_gradient_beyond_32_bits():
+    """2.4 G elements: the last rows of dx are written, and are those of a gradient that x does not explain."""
+    P, C, G = 1 << 24, 72, 3
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.empty(2, P, C, dtype=BF16, device="cuda").normal_(generator=g)
+    dy = torch.empty_like(x).normal_(generator=g)
+    _, saved = B.groupnorm_fwd(x, G)
+    out = torch.full_like(x, float("nan"))
+    dx, _, _ = B.groupnorm_bwd(dy, x, saved, G, out=out)
+    assert dx is out
+    # the means over 400 M elements in 64 bits, in parts of the pixels
+    s1, s2, n = torch.zeros(2, G, dtype=torch.float64), torch.zeros(2, G, dtype=torch.float64), P * (C // G)
+    mean, rstd = (saved[..., k].double().reshape(2, 1, G, 1) for k in (0, 1))
+    for at in range(0, P, 1 << 20):
+        v, d = (t[:, at:at + (1 << 20)].double().reshape(2, -1, G, C // G) for t in (x, dy))
+        s1 += d.sum((1, 3)).cpu()
+        s2 += (d * (v - mean) * rstd).sum((1, 3)).cpu()
+    m1, m2 = ((s / n).reshape(2, 1, G, 1) for s in (s1, s2))
+    at = (1 << 31) // C - P                     # (of the second image: 2^31 elements from the start)
+    for rows in (slice(0, 100), slice(at - 50, at + 50), slice(P - 100, P)):
+        v, d = (t[:, rows].double().cpu().reshape(2, -1, G, C // G) for t in (x, dy))
+        xh = (v - mean.cpu()) * rstd.cpu()
+        want = (rstd.cpu() * (d - m1 - xh * m2)).reshape(2, -1, C)
+        near(dx[:, rows], want, 2.0 ** -8 + 2e-6, norm=(rstd.cpu() * d).norm())
+        assert bool(dx[:, rows].any(2).all())
