@@ -507,8 +507,9 @@ int hdqt_layer_bwd(const float *G, const float *W, const void *saved, float *dX,
  * floating point.  Differences from the conventions above: tensors are fp32 or bfloat16
  * (hdqt_dtype_t), a pointer needs the alignment of its elements only (16 bytes are faster), and
  * infinities and NaN are taken as the formulas take them.  Products, sums, softmax statistics, means and
- * variances are held in 32 bits or more; a bfloat16 output is rounded once, to nearest even.  Results do
- * not depend on the order in which workgroups finish.
+ * variances are held in 32 bits or more; bfloat16 outputs are rounded to nearest even, and the one value between
+ * inputs and outputs that is held in fewer bits is the loss's dz in bfloat16 (below).  Results do not depend on the
+ * order in which workgroups finish.
  */
 typedef enum { HDQT_F32 = 0, HDQT_BF16 = 1 } hdqt_dtype_t;
 typedef enum { HDQT_REDUCE_NONE = 0, HDQT_REDUCE_MEAN = 1, HDQT_REDUCE_SUM = 2 } hdqt_reduction_t;
@@ -544,8 +545,9 @@ typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
  * hdqt_xent_step is the forward and the backward call with dloss = 1, and gives the same bits.  Its backward half takes
  * the logits from the forward half where the problem is small or, in fp32, all classes are one piece and their logits at
  * most 128 MB.
- * bfloat16: products of bfloat16 with sums in 32 bits; dz is rounded to bfloat16 before its products.
- * fp32: as exact as products in 32 bits.
+ * bfloat16: products of bfloat16 with sums in 32 bits; dz is rounded to bfloat16 before its products (but in small
+ * problems), each by 2^-8 of itself at most, so that dX and dW are rounded twice, dbias once; an exponential is off by
+ * |z - lse| 2^-24 of itself.  fp32: as exact as products in 32 bits.
  */
 size_t hdqt_xent_saved_size(int64_t M);
 size_t hdqt_xent_fwd_workspace_size(int64_t M, int64_t K, int64_t N, int dtype);
@@ -572,7 +574,8 @@ int hdqt_xent_step(const void *X, int64_t ldx, const void *W, int64_t ldw, const
  *     dx = (weight d - mean(weight d) - xh mean(weight d xh)) / sqrt(var + eps)
  *   x, y, dy, dx   of `dtype`, dense; y may be x, dx may be dy.  weight, bias, dweight, dbias [C] of
  *                  param_dtype; weight NULL: ones, bias NULL: zeros
- *   act            max(pre, 0) has the derivative 0 at 0; pre / (1 + exp(-pre)) for HDQT_ACT_SILU
+ *   act            max(pre, 0) has the derivative 0 at 0; pre / (1 + exp(-pre)) for HDQT_ACT_SILU, the exponential off
+ *                  by (|pre| + 1) 2^-24 of itself, the quotient by 2^-23
  *   saved          fp32 [B, G, 2], 8-byte aligned: mean and 1 / sqrt(var + eps), written by the forward call
  *   dx, dweight, dbias   any may be NULL (one must not)
  *   workspace      16-byte aligned, hdqt_groupnorm_workspace_size (0 for invalid arguments)

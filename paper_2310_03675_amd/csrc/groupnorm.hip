@@ -73,7 +73,9 @@ __device__ __forceinline__ float param(const void* p, int dtype, int c, float ot
 }
 
 // 1 / (1 + exp(-pre)) by the chip's reciprocal (one unit in the last place): a division's ten instructions would be most of
-// what an element of the backward pass costs (8 x 65536 x 320 in bfloat16, the sums: 178 us with it)
+// what an element of the backward pass costs (8 x 65536 x 320 in bfloat16, the sums: 178 us with it).  The exponential is the chip's
+// power of two of the rounded product with log2 e: |pre| 2^-24 of it, in fp32 too, where pre is behind a normalisation and seldom beyond
+// 10 (128 x 1024 x 64: outputs off by 1.88e-7 in the 2-norm, by exact functions 1.78e-7).
 __device__ __forceinline__ float logistic(float pre) { return __builtin_amdgcn_rcpf(1.0f + __expf(-pre)); }
 
 template <int ACT>

@@ -10,8 +10,9 @@
 // 7.4 each, 1170 to 1240 TFLOP/s, where a large library product reaches 1160 to 1525 by orientation; 4096 x 2048 x 50257 3.1 ms,
 // 1110, of it 0.11 for W, whose rows are no whole 16 bytes.  fp32 (six products of planes; a step keeps the logits where the classes are
 // one piece): 777 x 320 x 10007 160 us of which the three products take 124, 120 TFLOP/s of 32 bits; the library's large one has 154.
-// dz is rounded to bfloat16 where the problem is: its error, 2^-9 of each term, is of the size of the operands' own; db is
-// summed in front of that rounding.  Small problems (below) wait for launches and memory, not for the matrix pipe.
+// dz is rounded to bfloat16 where the problem is, by 2^-8 of each at most: the matrix cores' bfloat16 products take it, at sixteen times
+// the rate of 32-bit ones and a third of the memory of planes, and the error is of the size of the operands' own; db is summed in
+// front of that rounding.  Small problems (below) wait for launches and memory, not for the matrix pipe.
 #include "bf16_product.hpp"
 
 namespace hdqt {
@@ -30,7 +31,8 @@ __device__ __forceinline__ float any_load(const void* p, int dtype, int64_t i)
 }
 
 // exp(t) for t <= 0 up to rounding.  EXACT: the product with log2 e in two parts, for results in 32 bits; else its rounding
-// is |t| 2^-24 of the result.
+// is |t| 2^-24 of the result, at most 2^-25 of the row's largest one: far below dz's own rounding to bfloat16, and as much as any
+// rounding in a row's sum.
 template <bool EXACT>
 __device__ __forceinline__ float exp_of(float t)
 {
