@@ -101,18 +101,17 @@ struct Panel {
     static constexpr int kStage = 64, kRowBytes = MODE == kAlong ? 2 * kStage : 2 * T, kPieces = kRowBytes / 16;
     static constexpr int kBytes = 2 * kStage * T;
     static constexpr int kLoads = kBytes / (1024 * WAVES);          // of a wave, 1 KB each
-    static_assert(P == 1 && kLoads >= 1 && kPieces >= 8 && 1024 % kRowBytes == 0, "a load is whole rows");
+    static_assert(P == 1 && kLoads > 1 && (MODE == kAlong || kPieces >= 16) && 1024 % kRowBytes == 0, "a load is whole rows");
 
     static __device__ __forceinline__ int turn(int row)
     {
-        if (MODE == kAlong) return (row >> 1) & 7;
-        return kPieces >= 16 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+        return MODE == kAlong ? (row >> 1) & 7 : 4 * (row & 3);
     }
 
     uint32_t off[kLoads];           // of a lane's piece, from the stage's first byte
     int64_t lines_left, d, step;
     const uint16_t* base;
-    int col[kLoads > 1 ? 2 : 1];    // kAlong: first code of a lane's piece in even and odd loads
+    int col[2];                     // kAlong: first code of a lane's piece in even and odd loads
 
     __device__ __forceinline__ Panel(const Side& s, int64_t lines, int64_t line0, int64_t D, int wave, int lane)
     {
@@ -124,7 +123,7 @@ struct Panel {
             const int row = (wave * kLoads + j) * (1024 / kRowBytes) + lane / kPieces;
             const int piece = (lane % kPieces) ^ turn(row);
             off[j] = (uint32_t)row * (uint32_t)step * 2 + 16 * piece;
-            if (MODE == kAlong) col[j & (kLoads > 1)] = 8 * piece;          // (turns repeat every 16 rows: two loads)
+            if (MODE == kAlong) col[j & 1] = 8 * piece;          // (turns repeat every 16 rows: two loads)
             else if (8 * piece >= lines_left) off[j] = kOutside;
         }
     }
@@ -137,7 +136,7 @@ struct Panel {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             uint32_t o = off[j];
-            if (MODE == kAlong) o = at + col[j & (kLoads > 1)] < d ? o : kOutside;
+            if (MODE == kAlong) o = at + col[j & 1] < d ? o : kOutside;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rs, (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + j) * 1024), 16, o, 0, 0, 0);
         }
@@ -243,34 +242,31 @@ struct Fragments<3, MODE, T, N> {
     }
 };
 
-// A wave's loads but the last FLYING have arrived, and all it reads from LDS; then every wave's.  (The wait is one that the
-// compiler's own bookkeeping takes in.)
-template <int FLYING>
+// A wave's loads have arrived, and all it reads from LDS; then every wave's.  (The wait is one that the compiler's own
+// bookkeeping takes in.)
 __device__ __forceinline__ void wait_and_meet()
 {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070 | (FLYING & 15) | (FLYING >> 4) << 14);
+    __builtin_amdgcn_s_waitcnt(0x0070);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-template <int S>
 struct Stages {
-    uint8_t *a[S], *b[S];
+    uint8_t *a[2], *b[2];
 };
 
-// The part's sums: acc[i][j], block i of the wave's lines of A and j of B.  S stages in LDS, objects of their own, so that the
+// The part's sums: acc[i][j], block i of the wave's lines of A and j of B.  Two stages in LDS, objects of their own, so that the
 // compiler knows which loads a read must wait for.  A wave waits for its own part of a stage, and for its own reads of the
 // buffer that is brought next, in front of the barrier.
-template <int P, int MA, int MB, int TA, int TB, int WA, int WB, int S, int NA, int NB>
-__device__ __forceinline__ void multiply(const Args& g, const Place& p, const Stages<S>& lds, int wave, int lane,
+template <int P, int MA, int MB, int TA, int TB, int WA, int WB, int NA, int NB>
+__device__ __forceinline__ void multiply(const Args& g, const Place& p, const Stages& lds, int wave, int lane,
                                          v16f (&acc)[NA][NB])
 {
 #ifdef __HIP_DEVICE_COMPILE__       // (the host's pass has no use for the body, nor all of its builtins)
     static_assert(NA == TA / WA / 32 && NB == TB / WB / 32, "a wave's blocks");
     typedef Panel<P, MA, TA, WA * WB> PanelA;
     typedef Panel<P, MB, TB, WA * WB> PanelB;
-    constexpr int kLoads = PanelA::kLoads + PanelB::kLoads;
     const PanelA pa(g.A, g.RA, (int64_t)p.at * TA, g.D, wave, lane);
     const PanelB pb(g.B, g.RB, (int64_t)p.bt * TB, g.D, wave, lane);
     const Fragments<P, MA, TA, NA> fa((wave / WB) * (TA / WA), lane);
@@ -312,28 +308,27 @@ __device__ __forceinline__ void multiply(const Args& g, const Place& p, const St
     };
     constexpr int kSteps = stage_of(P) / 16;
     static_assert(kSteps % 2 == 0, "the sets take turns");
-    // (stages behind the last are zeros: whole rounds of S, and the same waits everywhere)
-#pragma unroll
-    for (int u = 0; u + 1 < S; ++u) bring(u, lds.a[u], lds.b[u]);
-    wait_and_meet<(S - 2) * kLoads>();
-    bring(S - 1, lds.a[S - 1], lds.b[S - 1]);
+    // (stages behind the last are zeros: whole rounds of two, and the same waits everywhere)
+    bring(0, lds.a[0], lds.b[0]);
+    wait_and_meet();
+    bring(1, lds.a[1], lds.b[1]);
     read(set[0], 0, 0);
-    for (uint32_t s = 0; s < p.n; s += S) {
+    for (uint32_t s = 0; s < p.n; s += 2) {
 #pragma unroll
-        for (int u = 0; u < S; ++u) {
+        for (int u = 0; u < 2; ++u) {
 #pragma unroll
             for (int q = 0; q + 1 < kSteps; ++q) {
                 read(set[(q + 1) & 1], u, q + 1);
                 products(set[q & 1]);
             }
             // the stage has been read: what is brought next goes into its place, while the last sixteen are multiplied
-            wait_and_meet<(S - 2) * kLoads>();
-            bring(s + u + S, lds.a[u], lds.b[u]);
-            read(set[0], (u + 1) % S, 0);
+            wait_and_meet();
+            bring(s + u + 2, lds.a[u], lds.b[u]);
+            read(set[0], 1 - u, 0);
             products(set[1]);
         }
     }
-    wait_and_meet<0>();             // (what follows may write where a stage lies)
+    wait_and_meet();                // (what follows may write where a stage lies)
 #endif
 }
 

@@ -147,7 +147,7 @@ struct Two {
 };
 
 // take(load(p)) for a thread's pixels, AHEAD of them loaded before the first is taken
-template <int DT, int V, int AHEAD, class L, class F>
+template <int AHEAD, class L, class F>
 __device__ __forceinline__ void each_vector(const Spot& s, uint32_t step, L load, F take)
 {
     int64_t p = s.p;
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void norm_fwd_sums_kernel(NormArgs a, Cut
             }
             n += 1.0f;
         };
-        each_vector<DT, V, 8>(s, k.ty, [&](int64_t p) { return hold<DT, V>(a.x, s.base + p * a.C + s.c); }, take);
+        each_vector<8>(s, k.ty, [&](int64_t p) { return hold<DT, V>(a.x, s.base + p * a.C + s.c); }, take);
     }
     float mean[V], m2[V];
 #pragma unroll
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sums_kernel(NormArgs a, Cut
                 s2[j] = fmaf(d, xh, s2[j]);
             }
         };
-        each_vector<DT, V, 4>(s, k.ty, [&](int64_t p) {
+        each_vector<4>(s, k.ty, [&](int64_t p) {
             const int64_t at = s.base + p * a.C + s.c;
             return Two{hold<DT, V>(a.x, at), hold<DT, V>(a.dy, at)};
         }, take);

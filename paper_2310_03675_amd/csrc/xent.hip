@@ -155,13 +155,11 @@ __device__ __forceinline__ float sum_of_32(float v)
 // A large tile's workgroup has a compute unit to itself, a small one's shares it with another: two waves to a SIMD either way.
 #define HDQT_TILE_KERNEL(WA, WB) __global__ __launch_bounds__(64 * WA * WB) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 
-// S stages of P planes' operands in LDS, each an object of its own
-#define HDQT_STAGES(P, S, TA, TB)                                                                            \
-    constexpr int kA = (P == 1 ? 128 : 192) * TA, kB = (P == 1 ? 128 : 192) * TB;                            \
-    __shared__ __align__(1024) uint8_t a0[kA], a1[kA], a2[S > 2 ? kA : 16], b0[kB], b1[kB], b2[S > 2 ? kB : 16]; \
-    bf16::Stages<S> stages;                                                                                  \
-    stages.a[0] = a0; stages.a[1] = a1; stages.b[0] = b0; stages.b[1] = b1;                                  \
-    if constexpr (S > 2) { stages.a[S - 1] = a2; stages.b[S - 1] = b2; }
+// two stages of P planes' operands in LDS, each an object of its own
+#define HDQT_STAGES(P, TA, TB)                                                    \
+    constexpr int kA = (P == 1 ? 128 : 192) * TA, kB = (P == 1 ? 128 : 192) * TB; \
+    __shared__ __align__(1024) uint8_t a0[kA], a1[kA], b0[kB], b1[kB];            \
+    const bf16::Stages stages{{a0, a1}, {b0, b1}};
 
 // Rows whose dz is added up for dbias first where a step keeps the logits: the same, to the bit, when a backward call of that size
 // multiplies them again.  (Where no step does, a tile's rows: a sum for eight rows is 0.5 bytes a logit, 40000 x 32 x 4321 backward
@@ -170,12 +168,12 @@ constexpr int kRowsOfDz = 8;
 
 // Lines of A are classes (W, read down), lines of B rows (X): a lane then holds sums of one row of the logits, and the
 // maximum and the sum over classes stay inside it but for one exchange between the wave's halves.
-template <bool GRAD, int P, int TA, int TB, int WA, int WB, int S>
+template <bool GRAD, int P, int TA, int TB, int WA, int WB>
 HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
     constexpr bool kExact = P == 3;
-    HDQT_STAGES(P, S, TA, TB);
+    HDQT_STAGES(P, TA, TB);
     __shared__ __align__(16) float bias[TA];
     __shared__ float2 halves[GRAD ? 1 : WA][GRAD ? 1 : TB];
     __shared__ float columns[GRAD ? WB : 1][GRAD ? TA : 1];
@@ -187,7 +185,7 @@ HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
         bias[t] = c >= r.classes ? -INFINITY : r.bias ? any_load(r.bias, r.bias_dtype, c) : 0.0f;
     }
     v16f acc[NA][NB] = {};
-    bf16::multiply<P, kDown, kAlong, TA, TB, WA, WB, S>(g, p, stages, wave, lane, acc);
+    bf16::multiply<P, kDown, kAlong, TA, TB, WA, WB>(g, p, stages, wave, lane, acc);
 
     const int class0 = (wave / WB) * (TA / WA), row0 = (wave % WB) * (TB / WB);
     auto column = [&](auto jj) {
@@ -285,9 +283,7 @@ HDQT_TILE_KERNEL(WA, WB) xent_logits_kernel(bf16::Args g, RowArgs r)
     };
     column(std::integral_constant<int, 0>{});
     if constexpr (NB > 1) column(std::integral_constant<int, 1>{});
-    if constexpr (NB > 2) column(std::integral_constant<int, 2>{});
-    if constexpr (NB > 3) column(std::integral_constant<int, 3>{});
-    static_assert(NB <= 4, "a call for each");
+    static_assert(NB <= 2, "a call for each");
     if constexpr (P == 3 && GRAD) {
         if (r.column && r.eights) {
             // a class's sums over eight rows, where a stage was; lines eight words longer, so that the four of a block lie in other banks
@@ -427,16 +423,16 @@ __device__ __forceinline__ void each_sum(v16f (&acc)[NA][NB], int64_t lines, int
     }
 }
 
-template <int P, int MODE, int TA, int TB, int WA, int WB, int S>
+template <int P, int MODE, int TA, int TB, int WA, int WB>
 HDQT_TILE_KERNEL(WA, WB) xent_gradient_kernel(bf16::Args g, OutArgs o)
 {
     constexpr int NA = TA / WA / 32, NB = TB / WB / 32;
-    HDQT_STAGES(P, S, TA, TB);
+    HDQT_STAGES(P, TA, TB);
     const bf16::Place p = bf16::place_of(g);
     if (!p.there) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     v16f acc[NA][NB] = {};
-    bf16::multiply<P, MODE, MODE, TA, TB, WA, WB, S>(g, p, stages, wave, lane, acc);
+    bf16::multiply<P, MODE, MODE, TA, TB, WA, WB>(g, p, stages, wave, lane, acc);
     const int64_t i0 = (int64_t)p.at * TA + (wave / WB) * (TA / WA), j0 = (int64_t)p.bt * TB + (wave % WB) * (TB / WB);
     const bool several = o.parts > 1;
     float* part = o.slices + (int64_t)p.part * g.RA * g.RB;
@@ -1085,11 +1081,11 @@ hipError_t launch_logits(int tag, const bf16::Args& g, const RowArgs& r, int pla
     ProfileScope ps(tag, stream);
     const dim3 grid(8 * g.per_xcd);
     if (planes == 1) {
-        if (large) hipLaunchKernelGGL((xent_logits_kernel<GRAD, 1, 256, 256, 2, 4, 2>), grid, dim3(512), 0, stream, g, r);
-        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 1, 128, 128, 2, 2, 2>), grid, dim3(256), 0, stream, g, r);
+        if (large) hipLaunchKernelGGL((xent_logits_kernel<GRAD, 1, 256, 256, 2, 4>), grid, dim3(512), 0, stream, g, r);
+        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 1, 128, 128, 2, 2>), grid, dim3(256), 0, stream, g, r);
     } else {
-        if (large) hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 256, 128, 4, 2, 2>), grid, dim3(512), 0, stream, g, r);
-        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 128, 64, 2, 2, 2>), grid, dim3(256), 0, stream, g, r);
+        if (large) hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 256, 128, 4, 2>), grid, dim3(512), 0, stream, g, r);
+        else hipLaunchKernelGGL((xent_logits_kernel<GRAD, 3, 128, 64, 2, 2>), grid, dim3(256), 0, stream, g, r);
     }
     return hipGetLastError();
 }
@@ -1101,11 +1097,11 @@ hipError_t launch_gradient(int tag, const bf16::Args& g, const OutArgs& o, int p
         ProfileScope ps(tag, stream);
         const dim3 grid(8 * g.per_xcd);
         if (planes == 1) {
-            if (large) hipLaunchKernelGGL((xent_gradient_kernel<1, MODE, 256, 256, 2, 4, 2>), grid, dim3(512), 0, stream, g, o);
-            else hipLaunchKernelGGL((xent_gradient_kernel<1, MODE, 128, 128, 2, 2, 2>), grid, dim3(256), 0, stream, g, o);
+            if (large) hipLaunchKernelGGL((xent_gradient_kernel<1, MODE, 256, 256, 2, 4>), grid, dim3(512), 0, stream, g, o);
+            else hipLaunchKernelGGL((xent_gradient_kernel<1, MODE, 128, 128, 2, 2>), grid, dim3(256), 0, stream, g, o);
         } else {
-            if (large) hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 256, 128, 4, 2, 2>), grid, dim3(512), 0, stream, g, o);
-            else hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 128, 64, 2, 2, 2>), grid, dim3(256), 0, stream, g, o);
+            if (large) hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 256, 128, 4, 2>), grid, dim3(512), 0, stream, g, o);
+            else hipLaunchKernelGGL((xent_gradient_kernel<3, MODE, 128, 64, 2, 2>), grid, dim3(256), 0, stream, g, o);
         }
     }
     if (o.parts > 1 && o.last_piece) {
