@@ -10,8 +10,8 @@
 // slices of the pixels, their joining, and the result, and are read twice; the last launch walks from the end to the start,
 // where what it begins with is still in the memory-side cache.
 //
-// 128 x 1024 x 64 in fp32, an image's slab in registers: 20 us forward (67 MB, 3.4 TB/s), 34 backward (101 MB, 3.0), 134 in
-// three launches each way and 60 so, all of it; 8 x 65536 x 320 in bfloat16, which the chip's registers do not hold (336 MB): sums
+// 128 x 1024 x 64 in fp32, an image's slab in registers: 20 us forward (67 MB, 3.4 TB/s; the 512 workgroups all at once), 34 backward (101
+// MB, 3.0; 70 registers, one workgroup to a compute unit, two rounds), 134 in three launches each way and 60 so, all of it; 8 x 65536 x 320 in bfloat16, which the chip's registers do not hold (336 MB): sums
 // 77 and 146 us (4.4 and 4.6 TB/s), results 129 and 193 (5.2, some of it from that cache), 570 in all, where a copy moves 4.8.
 // 1 x 49 x 96: 5 us, a launch; 128 x 16 x 512: 18, three launches.
 //
@@ -641,7 +641,8 @@ __global__ __launch_bounds__(T) void norm_bwd_slab_kernel(NormArgs a, Slab k, fl
         }
 }
 
-// 16 bytes at a time where every pixel starts at a multiple of them
+// 16 bytes at a time where every pixel starts at a multiple of them, else an element (both ways, 128 x 1024 x 65 in fp32 109 us, of 64
+// channels 56; 8 x 65536 x 321 in bfloat16 1008, of 320 560)
 int vector_of(const NormArgs& a)
 {
     const int v = a.dtype == kBf16 ? 8 : 4;
@@ -676,8 +677,9 @@ Cut cut_of(const NormArgs& a, int V)
 constexpr uint32_t kSlabThreads = 1024;
 
 // The slab for an image's channels, and how many threads and vectors each; false where no slab fits.
-// Slabs are 64 bytes of a pixel and more (whole sectors), wider where that still leaves two workgroups to a compute
-// unit, and threads as few as hold the slab with four vectors each, 1024 with up to sixteen (backward, of x and dy both, eight).
+// Slabs are 64 bytes of a pixel and more (whole sectors), wider where there still are two for every compute unit, and threads as few as
+// hold the slab with four vectors each, 1024 with up to sixteen (backward, of x and dy both, eight).  Two of 1024 are on a compute
+// unit at once where a thread has 64 registers at most (forward with four vectors, single elements), else one.
 struct SlabPlan {
     Slab k;
     uint32_t threads, vectors;

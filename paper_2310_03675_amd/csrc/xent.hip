@@ -9,7 +9,8 @@
 // gradients need and one is what not keeping the logits costs.  8192 x 4096 x 128000 in bfloat16: 28.2 ms, the products 6.9 to
 // 7.4 each, 1170 to 1240 TFLOP/s, where a large library product reaches 1160 to 1525 by orientation; 4096 x 2048 x 50257 3.1 ms,
 // 1110, of it 0.11 for W, whose rows are no whole 16 bytes.  fp32 (six products of planes; a step keeps the logits where the classes are
-// one piece): 777 x 320 x 10007 160 us of which the three products take 124, 120 TFLOP/s of 32 bits; the library's large one has 154.
+// one piece): 777 x 320 x 10007 155 us of which the three products take 124, 120 TFLOP/s of 32 bits, 720 of bfloat16; the library's
+// large fp32 product has 154.
 // dz is rounded to bfloat16 where the problem is, by 2^-8 of each at most: the matrix cores' bfloat16 products take it, at sixteen times
 // the rate of 32-bit ones and a third of the memory of planes, and the error is of the size of the operands' own; db is summed in
 // front of that rounding.  Small problems (below) wait for launches and memory, not for the matrix pipe.
