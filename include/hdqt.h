@@ -522,9 +522,9 @@ typedef enum { HDQT_NORM_2 = 0, HDQT_NORM_MAX = 1 } hdqt_norm_t;
  *     loss = l (HDQT_REDUCE_NONE, M values), sum_i l_i, or sum_i l_i / max(1, rows that count)
  * and its gradients, with g_i = dloss (a value for each row, or one) times the row's share in the loss:
  *     dz_ij = g_i (exp(z_ij - lse_i) - [j = target(i)]),   dX = dz W^T,   dW = X^T dz,   dbias_j = sum_i dz_ij
- * The logits are formed in pieces of the classes, and in the backward pass again; neither call keeps them but for
- * small problems.  dz of a piece lies in the workspace: 128 MB of it, or 1024 classes where those are more (which may
- * be all of them).
+ * The logits are formed in pieces of the classes, and in the backward pass again, where those of small problems lie
+ * in the workspace as a whole.  dz of a piece lies there too: 128 MB of it, or 1024 classes where those are more
+ * (which may be all of them).
  *   X         [M, K], rows ldx >= K elements apart; W [K, N], rows ldw >= N apart (a head that has more
  *             classes than are in use); both of `dtype`
  *   bias      [N] of bias_dtype, or NULL.  Minus infinity takes a class out: probability and gradient zero

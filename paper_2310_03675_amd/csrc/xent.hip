@@ -1182,7 +1182,8 @@ struct SmallPlan {
     uint32_t x_parts, w_parts;              // of dX's and dW's contractions
     size_t z, pairs, picked, rows, x_slices, w_slices;
 };
-SmallPlan small_plan(const XentArgs& a)
+// (gradients: they will be asked for, and read the logits)
+SmallPlan small_plan(const XentArgs& a, bool gradients)
 {
     SmallPlan p{};
     p.class_tiles = (a.N + kSmallTile - 1) / kSmallTile;
@@ -1195,7 +1196,7 @@ SmallPlan small_plan(const XentArgs& a)
     };
     p.x_parts = parts(p.row_tiles * ((a.K + kSmallTile - 1) / kSmallTile), a.N);
     p.w_parts = parts(p.class_tiles * (a.K / kSmallTile + 1), a.M);
-    p.z = up256(sizeof(float) * a.M * p.step);
+    p.z = gradients ? up256(sizeof(float) * a.M * p.step) : 0;
     p.pairs = up256(sizeof(float2) * p.class_tiles * a.M);
     p.picked = p.rows = up256(sizeof(float) * a.M);
     p.x_slices = p.x_parts > 1 ? up256(sizeof(float) * p.x_parts * a.M * a.K) : 0;
@@ -1214,7 +1215,7 @@ bool small_problem(const XentArgs& a)
 {
     if (a.M * a.N > kSmallLogits) return false;
     if (a.dtype == kBf16) return a.K * a.N <= ((int64_t)3 << 19) && a.M * a.N <= ((int64_t)1 << 26) / a.K;
-    const SmallPlan p = small_plan(a);
+    const SmallPlan p = small_plan(a, true);
     const double kn = (double)a.K * (double)a.N, mk = (double)a.M * (double)a.K, mn = (double)a.M * (double)a.N;
     auto rounds = [](int64_t length, int64_t of, uint32_t parts) {
         const int64_t n = (length + of - 1) / of;
@@ -1331,7 +1332,7 @@ hipError_t launch_small_gradients(const XentArgs& a, const SmallPlan& p, char* a
 size_t xent_workspace(const XentArgs& a, bool forward, bool backward)
 {
     if (small_problem(a)) {
-        const SmallPlan p = small_plan(a);
+        const SmallPlan p = small_plan(a, backward);
         return p.z + p.pairs + p.picked + p.rows + (backward ? p.x_slices + p.w_slices : 0);
     }
     const Plan p = plan_of(a, true, forward && backward);
@@ -1341,7 +1342,7 @@ size_t xent_workspace(const XentArgs& a, bool forward, bool backward)
 
 hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hipStream_t stream)
 {
-    if (small_problem(a)) return launch_small_logits(a, small_plan(a), static_cast<char*>(workspace), true, backward, stream);
+    if (small_problem(a)) return launch_small_logits(a, small_plan(a, backward), static_cast<char*>(workspace), true, backward, stream);
     const Plan p = plan_of(a, false, backward);
     char* at = static_cast<char*>(workspace) + p.x + p.w;
     char* rest = at + p.z;
@@ -1372,7 +1373,7 @@ hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hip
 {
     hipError_t e;
     if (small_problem(a)) {
-        const SmallPlan s = small_plan(a);
+        const SmallPlan s = small_plan(a, true);
         if (!forward && (e = launch_small_logits(a, s, static_cast<char*>(workspace), false, true, stream)) != hipSuccess) return e;
         return launch_small_gradients(a, s, static_cast<char*>(workspace), forward, stream);
     }

@@ -111,3 +111,11 @@ def test_the_tests_of_values_reach_the_large_kernels():
             for mode in (0, 1):
                 assert any(k.startswith(f"xent_gradient_kernel<{planes}, {mode}, {tile}") for k in seen), (mode, planes, tile)
     assert "xent_dz_kernel" in seen and {"pieces 0", "pieces 1"} <= seen
+
+
+@pytest.mark.parametrize("M,K,N,dtype", [(512, 512, 1000, F32), (8192, 64, 100, F32), (1, 256, 4000, BF16), (2048, 32, 700, BF16)])
+def test_forward_calls_of_small_problems_hold_no_logits(M, K, N, dtype):
+    """Only gradients read them: a forward call's workspace is the rows' pairs, eight bytes for each 32 classes, and two words a row."""
+    fwd, bwd = dispatch([(what, M, K, N, 0, dtype, 1, 7) for what in ("xent_fwd", "xent_bwd")])
+    assert fwd.rc == bwd.rc == 0 and any("small_logits" in k for k in fwd.kernels)
+    assert fwd.workspace <= 8 * M * _cdiv(N, 32) + 8 * M + 768 and bwd.workspace >= 4 * M * N
