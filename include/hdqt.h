@@ -614,6 +614,58 @@ int hdqt_clip_grad_norm(const hdqt_tensor_t *tensors, int64_t count, float max_n
                         void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Dropout: y = residual + (dropped ? 0 : x / (1 - p)), element by element, with a mask that is never stored.
+ * Element e of the tensor has a draw u(e) of 32 bits and is dropped where u(e) < round(p 2^32); what is kept is multiplied by
+ * 2^32 / (2^32 - round(p 2^32)), rounded to fp32.  u(e)'s upper half is field e mod 8 (16 bits, lowest first) of
+ * Philox4x32-10 with the counter (e / 8 mod 2^32, e / 2^35, tensor_id, 1) under the key seed + *step, its lower half the same
+ * field with 2 for the counter's last word (the stochastic rounding has 0 there: one seed and id may serve both).  The gradient
+ * of x is hdqt_dropout of y's gradient, without a residual, under the same description.
+ *   hdqt_dropout_t  HOST memory, read before the call returns.  step: device, int64, 8-byte aligned, read when the kernel runs
+ *                   (a captured call takes another mask at every replay whose step differs); NULL: 0.  p from 0 to 1
+ *   x, residual, y  of `dtype`, dense; residual may be NULL; y may be x or residual.  A dropped element of x is not looked at
+ *                   (it may be NaN)
+ * HDQT_EINVAL_DIM for more than 2^40 elements.  No workspace.
+ */
+typedef struct {
+    double p;
+    uint64_t seed;
+    const int64_t *step;
+    uint32_t tensor_id;
+    uint32_t reserved;
+} hdqt_dropout_t;
+int hdqt_dropout(const void *x, const void *residual, void *y, int64_t elements, int dtype, const hdqt_dropout_t *dropout,
+                 void *stream);
+
+/*
+ * Layer normalisation of M rows of C values, with a residual block's sum in front of it:
+ *     s = x, or residual + dropout(x), rounded to `dtype`;  mean and variance over a row of s
+ *     xh = (s - mean) / sqrt(var + eps),   y = xh weight + bias
+ * and its gradients, xh formed again from s, d = weight dy, means over a row:
+ *     ds = (d - mean(d) - xh mean(d xh)) / sqrt(var + eps) + dsum,   dresidual = ds,   dx = dropout(ds)
+ *     dweight = sum dy xh,   dbias = sum dy (over rows)
+ *   x, residual, sum, y, s, dy, dsum, dx, dresidual   [M, C] of `dtype`, dense.  weight, bias, dweight, dbias [C] of
+ *                param_dtype; weight NULL: ones, bias NULL: zeros
+ *   residual, dropout   either may be NULL: x itself, not dropped
+ *   sum          where s is left for the backward pass and for what goes past the normalisation; NULL: it is not wanted.
+ *                Without residual and dropout s is x, and sum is not written.  sum may be x or residual, y may be x
+ *   saved        fp32 [M, 2], 8-byte aligned: mean and 1 / sqrt(var + eps), written by the forward call; NULL there: not wanted
+ *   s            what the forward call left in sum, or its x
+ *   dsum         the gradient that reaches s from elsewhere, or NULL
+ *   dx, dresidual, dweight, dbias   any may be NULL (one must not); dx may be dy, dresidual may be dsum.  Without dropout
+ *                dx and dresidual are the same values
+ *   workspace    of the backward call, 16-byte aligned, hdqt_layernorm_bwd_workspace_size (0 for invalid arguments); it may be
+ *                NULL where neither dweight nor dbias is asked for
+ * HDQT_EINVAL_DIM for C above 32768, M of 2^31 or more.
+ */
+int hdqt_layernorm_fwd(const void *x, const void *residual, const hdqt_dropout_t *dropout, const void *weight, const void *bias,
+                       void *sum, void *y, float *saved, int64_t M, int64_t C, float eps, int dtype, int param_dtype,
+                       void *stream);
+size_t hdqt_layernorm_bwd_workspace_size(int64_t M, int64_t C, int dtype);
+int hdqt_layernorm_bwd(const void *dy, const void *dsum, const void *s, const hdqt_dropout_t *dropout, const void *weight,
+                       const float *saved, void *dx, void *dresidual, void *dweight, void *dbias, int64_t M, int64_t C,
+                       int dtype, int param_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Optional per-kernel timing, for benchmarks.  While enabled, every kernel the
  * library launches is bracketed by two HIP events on its stream (this is the
  * only state the library keeps, and events are the only thing it creates).

@@ -62,6 +62,7 @@ EXPORTED = [
     "hdqt_xent_saved_size", "hdqt_xent_fwd_workspace_size", "hdqt_xent_bwd_workspace_size", "hdqt_xent_step_workspace_size", "hdqt_xent_fwd",
     "hdqt_xent_bwd", "hdqt_xent_step", "hdqt_groupnorm_workspace_size", "hdqt_groupnorm_fwd", "hdqt_groupnorm_bwd",
     "hdqt_clip_grad_norm_workspace_size", "hdqt_grad_norm", "hdqt_clip_grad_norm",
+    "hdqt_dropout", "hdqt_layernorm_fwd", "hdqt_layernorm_bwd_workspace_size", "hdqt_layernorm_bwd",
 ]
 
 
@@ -101,6 +102,11 @@ class CTensor(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class CDropout(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_void_p), ("tensor_id", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
 @dataclass
 class Operand:
     b: int = 4
@@ -123,6 +129,20 @@ class Params:
 
     def c(self) -> CParams:
         return CParams(self.had_block, self.acc_bits, self.s, self.seed, self.A.c(), self.B.c())
+
+
+@dataclass
+class Dropout:
+    """Which elements of a tensor are dropped: a share p of them, by the generator of the stochastic rounding under the key
+    seed + step (an int64 tensor of one element on the device, read when the kernel runs: a captured call takes another mask at
+    every replay whose step differs) and this tensor id."""
+    p: float = 0.0
+    seed: int = 0
+    tensor_id: int = 0
+    step: Optional[torch.Tensor] = None
+
+    def c(self) -> CDropout:
+        return CDropout(self.p, self.seed, None if self.step is None else self.step.data_ptr(), self.tensor_id, 0)
 
 
 _lib = None
@@ -255,6 +275,15 @@ def load() -> C.CDLL:
     lib.hdqt_grad_norm.argtypes = [C.POINTER(CTensor), i64, i32, vp, vp, sz, vp]
     lib.hdqt_clip_grad_norm.restype = i32
     lib.hdqt_clip_grad_norm.argtypes = [C.POINTER(CTensor), i64, f32, f32, i32, vp, vp, sz, vp]
+    drop = C.POINTER(CDropout)
+    lib.hdqt_dropout.restype = i32
+    lib.hdqt_dropout.argtypes = [vp, vp, vp, i64, i32, drop, vp]
+    lib.hdqt_layernorm_fwd.restype = i32
+    lib.hdqt_layernorm_fwd.argtypes = [vp, vp, drop] + [vp] * 5 + [i64, i64, f32, i32, i32, vp]
+    lib.hdqt_layernorm_bwd_workspace_size.restype = sz
+    lib.hdqt_layernorm_bwd_workspace_size.argtypes = [i64, i64, i32]
+    lib.hdqt_layernorm_bwd.restype = i32
+    lib.hdqt_layernorm_bwd.argtypes = [vp, vp, vp, drop] + [vp] * 6 + [i64, i64, i32, i32, vp, sz, vp]
     lib.hdqt_strerror.restype = C.c_char_p
     lib.hdqt_strerror.argtypes = [i32]
     lib.hdqt_last_hip_error.restype = i32
@@ -1113,3 +1142,105 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, eps: float = 
         if rc:
             raise HdqtError(rc, "hdqt_clip_grad_norm")
         return norm
+
+
+# ---- a residual block: dropout, layer normalisation, low-rank adapters --------------------------
+
+def _dropout(d: Optional[Dropout], device):
+    """The description as the library takes it, or None."""
+    if d is None:
+        return None
+    if d.step is not None:
+        _check_out("a dropout's step", d.step, d.step.shape, torch.int64, device)
+        if d.step.numel() != 1:
+            raise ValueError("a dropout's step is one number")
+    return C.byref(d.c())
+
+
+def dropout(x: torch.Tensor, d: Dropout, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """hdqt_dropout -> residual + dropout(x), or dropout(x): x fp32 or bfloat16, contiguous, of any shape.  The gradient of x is
+    dropout(dy, d) with the same d.  out may be x or residual."""
+    if not x.is_cuda or not x.is_contiguous():
+        raise ValueError("x must be a contiguous device tensor")
+    if x.numel() == 0:
+        raise HdqtError(-2, "hdqt_dropout")
+    if residual is not None:
+        _check_out("residual", residual, x.shape, x.dtype, x.device)
+    with _place(x.device, stream):
+        if out is None:
+            out = torch.empty_like(x)
+        _check_out("out", out, x.shape, x.dtype, x.device)
+        rc = load().hdqt_dropout(_ptr(x), _ptr(residual), _ptr(out), x.numel(), _dtype(x), _dropout(d, x.device), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_dropout")
+        return out
+
+
+def _layer_sizes(x, weight, bias):
+    if x.dim() < 1 or not x.is_cuda or not x.is_contiguous():
+        raise ValueError("x must be a contiguous device tensor [..., columns]")
+    if x.numel() == 0:
+        raise HdqtError(-2, "hdqt_layernorm")
+    C_ = x.shape[-1]
+    given = [t for t in (weight, bias) if t is not None]
+    for t in given:
+        if t.dtype not in (torch.float32, x.dtype) or t.dtype != given[0].dtype:
+            raise ValueError(f"weight and bias must be float32 or {x.dtype}, both the same")
+        _check_out("weight and bias", t, (C_,), t.dtype, x.device)
+    return x.numel() // C_, C_, given[0].dtype if given else torch.float32
+
+
+def layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                  residual: Optional[torch.Tensor] = None, dropout: Optional[Dropout] = None, need=(True, True),
+                  out: Optional[torch.Tensor] = None, out_sum: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_layernorm_fwd -> (y, sum, saved fp32 [..., 2]): the rows of x [..., columns] (fp32 or bfloat16), or of
+    sum = residual + dropout(x), normalised.  Without residual and dropout sum is x itself.  need: whether sum and saved, which the
+    backward pass takes, are wanted (None in their place).  out may be x, out_sum x or residual."""
+    M, C_, pdt = _layer_sizes(x, weight, bias)
+    if residual is not None:
+        _check_out("residual", residual, x.shape, x.dtype, x.device)
+    with _place(x.device, stream):
+        if out is None:
+            out = torch.empty_like(x)
+        _check_out("out", out, x.shape, x.dtype, x.device)
+        total = x
+        if residual is not None or dropout is not None:
+            total = out_sum if out_sum is not None or not need[0] else torch.empty_like(x)
+            if total is not None:
+                _check_out("out_sum", total, x.shape, x.dtype, x.device)
+        saved = torch.empty(x.shape[:-1] + (2,), dtype=torch.float32, device=x.device) if need[1] else None
+        rc = load().hdqt_layernorm_fwd(_ptr(x), _ptr(residual), _dropout(dropout, x.device), _ptr(weight), _ptr(bias), _ptr(total),
+                                       _ptr(out), _ptr(saved), M, C_, eps, _dtype(x), _DTYPES[pdt], _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_layernorm_fwd")
+        return out, total, saved
+
+
+def layernorm_bwd(dy: torch.Tensor, s: torch.Tensor, saved: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                  dsum: Optional[torch.Tensor] = None, dropout: Optional[Dropout] = None, need=(True, True, True, True),
+                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_layernorm_bwd -> (dx, dresidual, dweight, dbias), those that `need` asks for.  s and saved: of layernorm_fwd (its sum);
+    dsum: the gradient that reaches the sum past the normalisation.  Without dropout dx and dresidual are one tensor.  dweight
+    and dbias are of the weight's type (fp32 without)."""
+    M, C_, pdt = _layer_sizes(s, weight, None)
+    _check_dev(workspace)
+    _check_out("dy", dy, s.shape, s.dtype, s.device)
+    _check_out("saved", saved, s.shape[:-1] + (2,), torch.float32, s.device)
+    if dsum is not None:
+        _check_out("dsum", dsum, s.shape, s.dtype, s.device)
+    with _place(s.device, stream):
+        dx = torch.empty_like(s) if need[0] or (need[1] and dropout is None) else None
+        dres = None if dropout is None or not need[1] else torch.empty_like(s)
+        dw, db = (torch.empty(C_, dtype=pdt, device=s.device) if want else None for want in need[2:])
+        if workspace is None and (need[2] or need[3]):
+            workspace = _bytes(load().hdqt_layernorm_bwd_workspace_size(M, C_, _dtype(s)), s.device)
+        rc = load().hdqt_layernorm_bwd(_ptr(dy), _ptr(dsum), _ptr(s), _dropout(dropout, s.device), _ptr(weight), _ptr(saved), _ptr(dx),
+                                       _ptr(dres), _ptr(dw), _ptr(db), M, C_, _dtype(s), _DTYPES[pdt], _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_layernorm_bwd")
+        if dropout is None:
+            dx, dres = (dx if want else None for want in need[:2])
+        return dx, dres, dw, db

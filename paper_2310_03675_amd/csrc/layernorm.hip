@@ -1,0 +1,403 @@
+// Layer normalisation of rows, with the residual sum and the dropout in front of it (gfx950):
+//   s = x, or residual + dropout(x), rounded to the tensors' type;  mu, var over a row's C values;
+//   xh = (s - mu) / sqrt(var + eps);  y = xh w + b
+// and its gradients, d = w dy:
+//   ds = (d - mean(d) - xh mean(d xh)) / sqrt(var + eps) + dsum;  dresidual = ds, dx = dropout(ds);  dw = sum dy xh, db = sum dy
+// (over rows; dsum: the gradient that reaches s past the normalisation).  Memory bounds it.
+//
+// A row stays in registers: R vectors of eight to each of a power of two of threads, 64 at most where that holds it, so that
+// its sums stay inside a wave, else several waves' through LDS.  Variances are sums of squares around the mean.  Backward, a
+// workgroup keeps the parameters' gradients of the columns that its threads have over all its rows, and leaves one part of them,
+// which a second launch adds up in 64 bits: no atomics, results do not depend on what finishes first.
+#include "dropout.hpp"
+#include "lane_ops.hpp"
+
+#include <type_traits>
+
+namespace hdqt {
+
+namespace {
+
+// How rows lie on threads.
+struct Rows {
+    uint32_t width;                 // threads to a row
+    uint32_t R;                     // vectors to a thread
+    uint32_t at_once;               // rows of a workgroup
+    uint32_t groups;                // workgroups
+};
+
+// sum over the `width` (a power of two up to 64) neighbouring lanes of a lane, the same in each
+__device__ __forceinline__ float lanes_sum(float v, uint32_t width)
+{
+    auto half = [&](uint32_t m) { return width > m; };
+    if (half(1)) v += lanes::lane_xor<1>(v);
+    if (half(2)) v += lanes::lane_xor<2>(v);
+    if (half(4)) v += lanes::lane_xor<4>(v);
+    if (half(8)) v += lanes::lane_xor<8>(v);
+#ifdef __HIP_DEVICE_COMPILE__
+    if (half(16)) {
+        const lanes::v2u r = __builtin_amdgcn_permlane16_swap(lanes::as_u(v), lanes::as_u(v), false, false);
+        v = lanes::as_f(r[0]) + lanes::as_f(r[1]);
+    }
+    if (half(32)) {
+        const lanes::v2u r = __builtin_amdgcn_permlane32_swap(lanes::as_u(v), lanes::as_u(v), false, false);
+        v = lanes::as_f(r[0]) + lanes::as_f(r[1]);
+    }
+#endif
+    return v;
+}
+
+// Sums of N values over a row's threads, in each of them.  Every thread of the workgroup comes here.  lds: N values a wave; two
+// calls in turn have one each.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], uint32_t width, float* lds)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i], width < 64 ? width : 64);
+    if (width <= 64) return;
+    const uint32_t wave = threadIdx.x >> 6, waves = width >> 6, first = wave & ~(waves - 1);
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) lds[N * wave + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float s = 0.0f;
+        for (uint32_t w = 0; w < waves; ++w) s += lds[N * (first + w) + i];
+        v[i] = s;
+    }
+}
+
+// A thread's vector of a row: columns c + lo to c + hi of it.  The last of a row that is no whole vectors begins eight before the
+// row's end, and what it has of the one before is left out.
+template <bool WHOLE>
+struct Span {
+    int c, lo, hi;
+    bool there;
+    __device__ __forceinline__ Span(uint32_t vector, int C, bool row)
+    {
+        const int first = 8 * (int)vector;
+        there = row && first < C;
+        c = WHOLE || first + 8 <= C || C < 8 ? first : C - 8;
+        lo = WHOLE ? 0 : first - c;
+        hi = WHOLE || C >= 8 ? 8 : C;
+    }
+    __device__ __forceinline__ bool has(int j) const { return WHOLE || (j >= lo && j < hi); }
+    template <int DT>
+    __device__ __forceinline__ Eight<DT> load(const void* p, int64_t base) const
+    {
+        if (WHOLE || hi == 8) return load_eight<DT>(p, base + c);
+        return load_some<DT>(p, base + c, lo, hi);
+    }
+    template <int DT>
+    __device__ __forceinline__ void store(void* p, int64_t base, const Eight<DT>& q) const
+    {
+        if (WHOLE || (lo == 0 && hi == 8)) store_eight<DT>(p, base + c, q);
+        else store_some<DT>(p, base + c, lo, hi, q);
+    }
+    // of the parameters, or `otherwise`
+    __device__ __forceinline__ void params(const void* p, int dtype, float otherwise, float (&v)[8]) const
+    {
+        if (!p) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = otherwise;
+        } else if (dtype == kBf16) {
+            const Eight<kBf16> q = load<kBf16>(p, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = q.get(j);
+        } else {
+            const Eight<kF32> q = load<kF32>(p, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = q.get(j);
+        }
+    }
+};
+
+template <int DT, int R, bool WHOLE, int T>
+__global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows k)
+{
+    __shared__ float lds[2][T / 64];
+    const uint32_t group = threadIdx.x / k.width, t = threadIdx.x & (k.width - 1);
+    const bool drops = a.drop.on, changed = drops || a.residual;
+    const uint64_t key = drops ? drop_key(a.drop) : 0;
+    const float count = (float)a.C;
+    // (as often for every thread: they meet)
+    for (int64_t first = (int64_t)blockIdx.x * k.at_once; first < a.M; first += (int64_t)k.groups * k.at_once) {
+        const int64_t row = first + group, base = row * a.C;
+        const bool there = row < a.M;
+        Eight<DT> q[R], res[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            q[r] = res[r] = Eight<DT>{};
+            if (at.there) q[r] = at.template load<DT>(a.x, base);
+            if (at.there && a.residual) res[r] = at.template load<DT>(a.residual, base);
+        }
+        float sum[1] = {0.0f}, squares[1] = {0.0f};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            if (!at.there) continue;
+            if (changed) {
+                const uint32_t keep = drops ? kept_eight(a.drop, key, base + at.c) : 0;
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float x = q[r].get(j), of = res[r].get(j);
+                    if (drops) v[j] = keep >> j & 1 ? (a.residual ? fmaf(x, a.drop.rate, of) : x * a.drop.rate) : of;
+                    else v[j] = of + x;
+                }
+                q[r].set(v);
+                if (a.sum) at.store(a.sum, base, q[r]);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[0] += at.has(j) ? q[r].get(j) : 0.0f;
+        }
+        row_sums(sum, k.width, lds[0]);
+        const float mean = sum[0] / count;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            q[r].renew();
+            if (!at.there) continue;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = at.has(j) ? q[r].get(j) - mean : 0.0f;
+                squares[0] = fmaf(d, d, squares[0]);
+            }
+        }
+        row_sums(squares, k.width, lds[1]);
+        const float rstd = 1.0f / sqrtf(squares[0] / count + a.eps);
+        if (a.saved && there && t == 0) reinterpret_cast<float2*>(a.saved)[row] = make_float2(mean, rstd);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            q[r].renew();
+            if (!at.there) continue;
+            float w[8], b[8], v[8];
+            at.params(a.weight, a.param_dtype, 1.0f, w);
+            at.params(a.bias, a.param_dtype, 0.0f, b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = fmaf((q[r].get(j) - mean) * rstd, w[j], b[j]);
+            q[r].set(v);
+            at.store(a.y, base, q[r]);
+        }
+    }
+}
+
+// parts[workgroup][2][C]: sums over its rows of dy xh and of dy
+template <int DT, int R, bool WHOLE, int T>
+__global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows k, float* parts)
+{
+    __shared__ float lds[2][2 * (T / 64)];
+    extern __shared__ float columns[];          // [2][C], where a workgroup has several rows at once
+    const uint32_t group = threadIdx.x / k.width, t = threadIdx.x & (k.width - 1);
+    const bool drops = a.drop.on && a.dx;
+    const uint64_t key = drops ? drop_key(a.drop) : 0;
+    const float count = (float)a.C;
+    float dw[R][8] = {}, db[R][8] = {};
+    uint32_t turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * k.at_once; first < a.M; first += (int64_t)k.groups * k.at_once) {
+        const int64_t row = first + group, base = row * a.C;
+        const bool there = row < a.M;
+        Eight<DT> s[R], dy[R], more[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            s[r] = dy[r] = more[r] = Eight<DT>{};
+            if (at.there) s[r] = at.template load<DT>(a.s, base);
+            if (at.there) dy[r] = at.template load<DT>(a.dy, base);
+            if (at.there && a.dsum) more[r] = at.template load<DT>(a.dsum, base);
+        }
+        const float2 stats = there ? reinterpret_cast<const float2*>(a.saved)[row] : make_float2(0.0f, 0.0f);
+        float sums[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            if (!at.there) continue;
+            float w[8];
+            at.params(a.weight, a.param_dtype, 1.0f, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xh = (s[r].get(j) - stats.x) * stats.y, g = dy[r].get(j), d = g * w[j];
+                if (!at.has(j)) continue;
+                dw[r][j] = fmaf(g, xh, dw[r][j]);
+                db[r][j] += g;
+                sums[0] += d;
+                sums[1] = fmaf(d, xh, sums[1]);
+            }
+        }
+        if (!a.dx && !a.dresidual) continue;            // (all of the workgroup: it does not meet)
+        row_sums(sums, k.width, lds[turn]);
+        turn ^= 1;
+        const float m1 = sums[0] / count, m2 = sums[1] / count;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            s[r].renew();
+            dy[r].renew();
+            if (!at.there) continue;
+            float w[8], v[8];
+            at.params(a.weight, a.param_dtype, 1.0f, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xh = (s[r].get(j) - stats.x) * stats.y, d = dy[r].get(j) * w[j], g = d - m1 - xh * m2;
+                v[j] = fmaf(stats.y, g, more[r].get(j));
+            }
+            Eight<DT> q;
+            if (a.dresidual || !drops) {
+                q.set(v);
+                if (a.dresidual) at.store(a.dresidual, base, q);
+                if (a.dx && !drops) at.store(a.dx, base, q);
+            }
+            if (drops) {
+                const uint32_t keep = kept_eight(a.drop, key, base + at.c);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = keep >> j & 1 ? v[j] * a.drop.rate : 0.0f;
+                q.set(v);
+                at.store(a.dx, base, q);
+            }
+        }
+    }
+    if (!a.dweight && !a.dbias) return;
+    // one group of rows after the other
+    float* const to = parts + (int64_t)blockIdx.x * 2 * a.C;
+    for (uint32_t g = 0; g < k.at_once; ++g) {
+        if (group == g) {
+            const bool last = g + 1 == k.at_once;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const Span<WHOLE> at(t + r * k.width, a.C, true);
+                if (!at.there) continue;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int c = at.c + j;
+                    if (!at.has(j)) continue;
+                    if (g) {
+                        dw[r][j] += columns[c];
+                        db[r][j] += columns[a.C + c];
+                    }
+                    (last ? to : columns)[c] = dw[r][j];
+                    (last ? to : columns)[a.C + c] = db[r][j];
+                }
+            }
+        }
+        if (g + 1 < k.at_once) __syncthreads();
+    }
+}
+
+// dw and db: the parts' sums of 32 columns
+constexpr int kParamThreads = 512;
+__global__ __launch_bounds__(kParamThreads) void layernorm_params_kernel(LayerNormArgs a, const float* parts, uint32_t groups)
+{
+    __shared__ double lds[kParamThreads / 32][33];
+    const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x, of = blockIdx.y;
+    double s = 0.0;
+    if (c < (uint32_t)a.C)
+#pragma unroll 8
+        for (uint32_t g = y; g < groups; g += kParamThreads / 32) s += (double)parts[((int64_t)g * 2 + of) * a.C + c];
+    lds[y][x] = s;
+    __syncthreads();
+    void* to = of ? a.dbias : a.dweight;
+    if (y || c >= (uint32_t)a.C || !to) return;
+    for (int i = 1; i < kParamThreads / 32; ++i) s += lds[i][x];
+    if (a.param_dtype == kBf16) store_as<kBf16>(to, c, (float)s);
+    else store_as<kF32>(to, c, (float)s);
+}
+
+uint32_t power_from(uint32_t n)
+{
+    uint32_t p = 1;
+    while (p < n) p *= 2;
+    return p;
+}
+
+// As many threads to a row as it has vectors, half of them and again while that leaves enough waves for the chip and `most` vectors
+// hold the row.
+Rows rows_of(const LayerNormArgs& a, uint32_t most, uint32_t threads, int64_t waves)
+{
+    Rows k{};
+    const uint32_t vectors = (uint32_t)((a.C + 7) / 8);
+    k.width = power_from(vectors) < 1024 ? power_from(vectors) : 1024;
+    auto need = [&](uint32_t width) { return power_from((vectors + width - 1) / width); };
+    while (k.width > 64 && need(k.width / 2) <= most && a.M * (k.width / 2) >= waves * 64) k.width /= 2;
+    k.R = need(k.width);
+    if (threads < k.width) threads = k.width;
+    k.at_once = threads / k.width;
+    return k;
+}
+
+constexpr uint32_t kFwdThreads = 256, kBwdThreads = 512;
+
+Rows fwd_rows(const LayerNormArgs& a)
+{
+    Rows k = rows_of(a, 2, kFwdThreads, 4096);
+    const int64_t groups = (a.M + k.at_once - 1) / k.at_once;
+    k.groups = (uint32_t)(groups < (1 << 20) ? groups : 1 << 20);
+    return k;
+}
+Rows bwd_rows(const LayerNormArgs& a)
+{
+    Rows k = rows_of(a, 2, kBwdThreads, 2048);
+    const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.R > 2 ? 1 : k.R > 1 ? 2 : 4);
+    k.groups = (uint32_t)(groups < most ? groups : most);
+    return k;
+}
+
+// f(type, R, whether rows are whole vectors, whether a workgroup has 1024 threads)
+template <class F>
+void with_rows(const LayerNormArgs& a, const Rows& k, F f)
+{
+    using std::integral_constant;
+    auto of = [&](auto dt) {
+        auto whole = [&](auto r, auto w) {
+            if (k.width * k.at_once > 512) f(dt, r, w, integral_constant<int, 1024>{});
+            else f(dt, r, w, integral_constant<int, 512>{});
+        };
+        auto held = [&](auto r) {
+            if (a.C % 8) whole(r, std::false_type{});
+            else whole(r, std::true_type{});
+        };
+        if (k.R == 1) held(integral_constant<int, 1>{});
+        else if (k.R == 2) held(integral_constant<int, 2>{});
+        else held(integral_constant<int, 4>{});
+    };
+    if (a.dtype == kBf16) of(integral_constant<int, kBf16>{});
+    else of(integral_constant<int, kF32>{});
+}
+
+} // namespace
+
+size_t layernorm_workspace(const LayerNormArgs& a) { return (size_t)bwd_rows(a).groups * 2 * a.C * sizeof(float); }
+
+hipError_t launch_layernorm_fwd(const LayerNormArgs& a, hipStream_t stream)
+{
+    const Rows k = fwd_rows(a);
+    ProfileScope ps(K_LAYERNORM_FWD, stream);
+    with_rows(a, k, [&](auto dt, auto r, auto whole, auto t) {
+        hipLaunchKernelGGL((layernorm_fwd_kernel<dt.value, r.value, whole.value, t.value>), dim3(k.groups), dim3(k.width * k.at_once), 0, stream,
+                           a, k);
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStream_t stream)
+{
+    const Rows k = bwd_rows(a);
+    float* parts = static_cast<float*>(workspace);
+    {
+        ProfileScope ps(K_LAYERNORM_BWD, stream);
+        const size_t lds = k.at_once > 1 ? 2 * (size_t)a.C * sizeof(float) : 0;
+        with_rows(a, k, [&](auto dt, auto r, auto whole, auto t) {
+            hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, r.value, whole.value, t.value>), dim3(k.groups), dim3(k.width * k.at_once), lds,
+                               stream, a, k, parts);
+        });
+    }
+    if (a.dweight || a.dbias) {
+        ProfileScope ps(K_LAYERNORM_PARAMS, stream);
+        hipLaunchKernelGGL(layernorm_params_kernel, dim3((uint32_t)((a.C + 31) / 32), 2), dim3(kParamThreads), 0, stream, a, parts, k.groups);
+    }
+    return hipGetLastError();
+}
+
+} // namespace hdqt

@@ -1,6 +1,6 @@
-// Declarations of the operators around the integer products of a training step (api_train.hip is their C ABI):
-// clipping of gradients by their global norm (clip.hip), group normalisation (groupnorm.hip), the classifier's
-// loss (xent.hip).
+// Declarations of the operators around the integer products of a training step (api_train.hip and api_block.hip are their C
+// ABI): clipping of gradients by their global norm (clip.hip), group normalisation (groupnorm.hip), the classifier's
+// loss (xent.hip), dropout (dropout.hip), layer normalisation (layernorm.hip), low-rank adapters (adapters.hip).
 #pragma once
 #include "common.hpp"
 
@@ -10,7 +10,8 @@ namespace hdqt {
 enum TrainKernelId {
     K_CLIP_NORM = K_COUNT, K_CLIP_FINISH, K_CLIP_SCALE, K_NORM_FWD_SUMS, K_NORM_FWD_FINISH, K_NORM_FWD, K_NORM_BWD_SUMS,
     K_NORM_BWD_FINISH, K_NORM_BWD, K_XENT_LOGITS, K_XENT_LOSS, K_XENT_DLOGITS, K_XENT_DX, K_XENT_DW, K_XENT_DBIAS,
-    K_XENT_PACK, K_XENT_ADD_PARTS, K_NORM_PARAMS,
+    K_XENT_PACK, K_XENT_ADD_PARTS, K_NORM_PARAMS, K_DROPOUT, K_LAYERNORM_FWD, K_LAYERNORM_BWD, K_LAYERNORM_PARAMS,
+    K_ADAPT_PLAN, K_ADAPT_DOWN, K_ADAPT_UP, K_ADAPT_WEIGHTS,
     K_ALL_COUNT
 };
 int hip_fail(hipError_t e);          // notes the error for hdqt_last_hip_error (api.hip); HDQT_EHIP
@@ -139,5 +140,38 @@ size_t xent_workspace(const XentArgs& a, bool forward, bool backward);        //
 hipError_t launch_xent_fwd(const XentArgs& a, void* workspace, bool backward, hipStream_t stream);
 // forward: the forward pass has just run in the same workspace
 hipError_t launch_xent_bwd(const XentArgs& a, void* workspace, bool forward, hipStream_t stream);
+
+// ---- dropout.hip ----
+
+struct DropArgs {
+    uint64_t seed;
+    const int64_t* step;                // device: added to the seed; or null
+    uint32_t hi, lo;                    // round(p 2^32): what is above its 16 lowest bits (2^16: nothing is kept), and those
+    uint32_t tensor_id;
+    float rate;                         // what is kept is multiplied by: 1 / (1 - p)
+    int on;                             // 0: there is no dropout
+};
+hipError_t launch_dropout(const void* x, const void* residual, void* y, int64_t n, int dtype, const DropArgs& d, hipStream_t stream);
+
+// ---- layernorm.hip ----
+
+constexpr int64_t kLayerNormColumns = 32768;        // what 1024 threads hold in registers, forward and backward
+struct LayerNormArgs {
+    const void *x, *residual;           // [M, C]; residual may be null
+    void *sum, *y;                      // sum may be null
+    const void *s, *dy, *dsum;          // backward: what was normalised; dsum may be null
+    void *dx, *dresidual;               // either may be null
+    const void *weight, *bias;          // [C] or null (ones, zeros)
+    void *dweight, *dbias;              // or null
+    float* saved;                       // [M] pairs: mean, 1 / standard deviation; forward may be null
+    DropArgs drop;
+    int64_t M;
+    int C;
+    float eps;
+    int dtype, param_dtype;
+};
+size_t layernorm_workspace(const LayerNormArgs& a);         // of the backward pass
+hipError_t launch_layernorm_fwd(const LayerNormArgs& a, hipStream_t stream);
+hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStream_t stream);
 
 } // namespace hdqt
