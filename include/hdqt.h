@@ -666,6 +666,37 @@ int hdqt_layernorm_bwd(const void *dy, const void *dsum, const void *s, const hd
                        int dtype, int param_dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Low-rank adapters beside a shared projection of K features to N, n of them of rank r; each of M rows has one of its own, or none:
+ *     h_i = x_i A_a,   out_i = base_i + scale_a h_i B_a,   a = ids[i]
+ * and its gradients:
+ *     g_i = scale_a dy_i B_a^T,   dx_i = base_i + g_i A_a^T,   dA_a = sum x_i^T g_i,   dB_a = sum scale_a h_i^T dy_i
+ * (sums over the rows that have a; base's own gradient is dy).
+ *   x, base, out, dy   [M, K], [M, N], [M, N], [M, N]; A [n, K, r], B [n, r, N] and their gradients; all of `dtype`, dense.  An
+ *             adapter of a smaller rank has zeros behind it
+ *   ids       int64 [M].  Below 0: no adapter, out_i = base_i, dx_i = base_i, no part in dA and dB.  n or above: out_i and dx_i
+ *             are NaN, no part in dA and dB.  Rows need not stand in any order
+ *   scale     fp32 [n], or NULL: ones
+ *   base      what the shared projection left, or NULL: zeros; out may be base.  Backward, the same for dx: the gradient of
+ *             x by the shared projection
+ *   saved     hdqt_adapters_saved_size bytes (0 for invalid arguments), 16-byte aligned, written by the forward call, read by the
+ *             backward call with the same x, A, ids and sizes; private to the library
+ *   dx, dA, dB   any may be NULL (one must not).  An adapter that no row has gets zeros
+ *   workspace of the backward call, 16-byte aligned, hdqt_adapters_bwd_workspace_size (0 for invalid arguments)
+ * h and g are held in fp32.  fp32: as exact as products in 32 bits.  bfloat16: products of bfloat16 with sums in 32 bits, h and g in
+ * the second product as two bfloat16 values each, off by 2^-16 of themselves at most; an infinity among A or B may give NaN
+ * where the formula has an infinity.
+ * HDQT_EINVAL_DIM for M above 4 194 240, K or N above 2^21, r above 128, n above 1024.
+ */
+size_t hdqt_adapters_saved_size(int64_t M, int64_t K, int64_t N, int r, int n, int dtype);
+size_t hdqt_adapters_bwd_workspace_size(int64_t M, int64_t K, int64_t N, int r, int n, int dtype);
+int hdqt_adapters_fwd(const void *x, const void *A, const void *B, const int64_t *ids, const float *scale, const void *base,
+                      void *out, void *saved, size_t saved_bytes, int64_t M, int64_t K, int64_t N, int r, int n, int dtype,
+                      void *stream);
+int hdqt_adapters_bwd(const void *dy, const void *x, const void *A, const void *B, const int64_t *ids, const float *scale,
+                      const void *saved, size_t saved_bytes, const void *base, void *dx, void *dA, void *dB, int64_t M,
+                      int64_t K, int64_t N, int r, int n, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Optional per-kernel timing, for benchmarks.  While enabled, every kernel the
  * library launches is bracketed by two HIP events on its stream (this is the
  * only state the library keeps, and events are the only thing it creates).

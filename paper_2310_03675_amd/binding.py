@@ -63,6 +63,7 @@ EXPORTED = [
     "hdqt_xent_bwd", "hdqt_xent_step", "hdqt_groupnorm_workspace_size", "hdqt_groupnorm_fwd", "hdqt_groupnorm_bwd",
     "hdqt_clip_grad_norm_workspace_size", "hdqt_grad_norm", "hdqt_clip_grad_norm",
     "hdqt_dropout", "hdqt_layernorm_fwd", "hdqt_layernorm_bwd_workspace_size", "hdqt_layernorm_bwd",
+    "hdqt_adapters_saved_size", "hdqt_adapters_bwd_workspace_size", "hdqt_adapters_fwd", "hdqt_adapters_bwd",
 ]
 
 
@@ -284,6 +285,13 @@ def load() -> C.CDLL:
     lib.hdqt_layernorm_bwd_workspace_size.argtypes = [i64, i64, i32]
     lib.hdqt_layernorm_bwd.restype = i32
     lib.hdqt_layernorm_bwd.argtypes = [vp, vp, vp, drop] + [vp] * 6 + [i64, i64, i32, i32, vp, sz, vp]
+    for name in ("hdqt_adapters_saved_size", "hdqt_adapters_bwd_workspace_size"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [i64, i64, i64, i32, i32, i32]
+    lib.hdqt_adapters_fwd.restype = i32
+    lib.hdqt_adapters_fwd.argtypes = [vp] * 8 + [sz, i64, i64, i64, i32, i32, i32, vp]
+    lib.hdqt_adapters_bwd.restype = i32
+    lib.hdqt_adapters_bwd.argtypes = [vp] * 7 + [sz] + [vp] * 4 + [i64, i64, i64, i32, i32, i32, vp, sz, vp]
     lib.hdqt_strerror.restype = C.c_char_p
     lib.hdqt_strerror.argtypes = [i32]
     lib.hdqt_last_hip_error.restype = i32
@@ -1244,3 +1252,64 @@ def layernorm_bwd(dy: torch.Tensor, s: torch.Tensor, saved: torch.Tensor, weight
         if dropout is None:
             dx, dres = (dx if want else None for want in need[:2])
         return dx, dres, dw, db
+
+
+def _adapter_sizes(x, A, B, ids, scale):
+    """M, K, N, r, n of a call, whose tensors are as they should be."""
+    if x.dim() != 2 or A.dim() != 3 or B.dim() != 3 or not x.is_cuda or not x.is_contiguous():
+        raise ValueError("x must be a contiguous device matrix [rows, features], A [adapters, features, rank], B [adapters, rank, outputs]")
+    if x.numel() == 0 or A.numel() == 0 or B.numel() == 0:
+        raise HdqtError(-2, "hdqt_adapters")
+    (M, K), (n, _, r), N = x.shape, A.shape, B.shape[2]
+    _check_out("A", A, (n, K, r), x.dtype, x.device)
+    _check_out("B", B, (n, r, N), x.dtype, x.device)
+    _check_out("ids", ids, (M,), torch.int64, x.device)
+    if scale is not None:
+        _check_out("scale", scale, (n,), torch.float32, x.device)
+    return M, K, N, r, n
+
+
+def adapters_fwd(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, ids: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                 base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_adapters_fwd -> (out [M, N], saved): out_i = base_i + scale_a x_i A_a B_a with a = ids[i], none where that is negative.
+    x [M, K], A [n, K, r], B [n, r, N] (fp32 or bfloat16), ids int64 [M], scale fp32 [n].  out may be base."""
+    sizes = M, K, N, r, n = _adapter_sizes(x, A, B, ids, scale)
+    if base is not None:
+        _check_out("base", base, (M, N), x.dtype, x.device)
+    with _place(x.device, stream):
+        if out is None:
+            out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        _check_out("out", out, (M, N), x.dtype, x.device)
+        saved = _bytes(load().hdqt_adapters_saved_size(*sizes, _dtype(x)), x.device)
+        rc = load().hdqt_adapters_fwd(_ptr(x), _ptr(A), _ptr(B), _ptr(ids), _ptr(scale), _ptr(base), _ptr(out), _ptr(saved), saved.numel(),
+                                      *sizes, _dtype(x), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_adapters_fwd")
+        return out, saved
+
+
+def adapters_bwd(dy: torch.Tensor, x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, ids: torch.Tensor, saved: torch.Tensor,
+                 scale: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None, need=(True, True, True),
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None):
+    """hdqt_adapters_bwd -> (dx, dA, dB), those that `need` asks for.  saved: of adapters_fwd with the same x, A and ids; base: the
+    gradient of x by the shared projection, which dx is added to; out, for dx, may be base."""
+    sizes = M, K, N, r, n = _adapter_sizes(x, A, B, ids, scale)
+    _check_dev(saved, workspace)
+    _check_out("dy", dy, (M, N), x.dtype, x.device)
+    if base is not None:
+        _check_out("base", base, (M, K), x.dtype, x.device)
+    with _place(x.device, stream):
+        dx = None
+        if need[0]:
+            dx = torch.empty_like(x) if out is None else out
+            _check_out("out", dx, x.shape, x.dtype, x.device)
+        dA, dB = (torch.empty_like(t) if want else None for t, want in zip((A, B), need[1:]))
+        if workspace is None:
+            workspace = _bytes(load().hdqt_adapters_bwd_workspace_size(*sizes, _dtype(x)), x.device)
+        rc = load().hdqt_adapters_bwd(_ptr(dy), _ptr(x), _ptr(A), _ptr(B), _ptr(ids), _ptr(scale), _ptr(saved), saved.numel(), _ptr(base),
+                                      _ptr(dx), _ptr(dA), _ptr(dB), *sizes, _dtype(x), _ptr(workspace), workspace.numel(), _stream(None))
+        if rc:
+            raise HdqtError(rc, "hdqt_adapters_bwd")
+        return dx, dA, dB

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhdqt.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "quantize.hip", "quantize_fast.hip", "quantize_dual.hip", "gemm.hip", "gemm_fast.hip", "gemm_small.hip", "gemm_six.hip", "gemm_bytes.hip", "gemm_packed.hip", "gemm_fold.hip", "im2col.hip", "profile.hip", "probe.hip",
-           "api_train.hip", "clip.hip", "groupnorm.hip", "xent.hip", "api_block.hip", "dropout.hip", "layernorm.hip"]
+           "api_train.hip", "clip.hip", "groupnorm.hip", "xent.hip", "api_block.hip", "dropout.hip", "layernorm.hip", "adapters.hip"]
 
 # -ffp-contract=off: every binary32 operation of the quantizer rounds on its own,
 # as in the definition the results are checked against.

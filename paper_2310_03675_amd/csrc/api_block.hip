@@ -47,6 +47,34 @@ int check_layernorm(const hdqt::LayerNormArgs& a)
     return off(a.saved, 8) ? HDQT_EALIGN : HDQT_OK;
 }
 
+// (as for the products; a classifier's features)
+constexpr int64_t kMaxTokens = (int64_t)65535 * 64, kMaxFeatures = (int64_t)1 << 21;
+
+bool sized(const hdqt::AdapterArgs& a)
+{
+    return a.M >= 1 && a.M <= kMaxTokens && a.K >= 1 && a.K <= kMaxFeatures && a.N >= 1 && a.N <= kMaxFeatures && a.r >= 1 &&
+           a.r <= hdqt::kRankMost && a.n >= 1 && a.n <= hdqt::kAdaptersMost && known_dtype(a.dtype);
+}
+
+hdqt::AdapterArgs sizes_of(int64_t M, int64_t K, int64_t N, int r, int n, int dtype)
+{
+    hdqt::AdapterArgs a{};
+    a.M = M; a.K = K; a.N = N; a.r = r; a.n = n; a.dtype = dtype;
+    return a;
+}
+
+int check_adapters(const hdqt::AdapterArgs& a, size_t saved_bytes)
+{
+    if (!a.x || !a.A || !a.B || !a.ids || !a.saved) return HDQT_EINVAL_NULL;
+    if (!known_dtype(a.dtype)) return HDQT_EINVAL_DTYPE;
+    if (!sized(a)) return HDQT_EINVAL_DIM;
+    const int64_t size = hdqt::dtype_size(a.dtype);
+    for (const void* p : {a.x, a.A, a.B, a.base, (const void*)a.out, a.dy, (const void*)a.dA, (const void*)a.dB})
+        if (off(p, size)) return HDQT_EALIGN;
+    if (off(a.ids, 8) || off(a.scale, 4) || off(a.saved, 16)) return HDQT_EALIGN;
+    return saved_bytes < hdqt::adapters_saved(a) ? HDQT_EWORKSPACE : HDQT_OK;
+}
+
 } // namespace
 
 extern "C" {
@@ -106,6 +134,46 @@ int hdqt_layernorm_bwd(const void* dy, const void* dsum, const void* s, const hd
         if (off(workspace, 16)) return HDQT_EALIGN;
     }
     const hipError_t e = hdqt::launch_layernorm_bwd(a, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? HDQT_OK : hip_fail(e);
+}
+
+size_t hdqt_adapters_saved_size(int64_t M, int64_t K, int64_t N, int r, int n, int dtype)
+{
+    const hdqt::AdapterArgs a = sizes_of(M, K, N, r, n, dtype);
+    return sized(a) ? hdqt::adapters_saved(a) : 0;
+}
+
+size_t hdqt_adapters_bwd_workspace_size(int64_t M, int64_t K, int64_t N, int r, int n, int dtype)
+{
+    const hdqt::AdapterArgs a = sizes_of(M, K, N, r, n, dtype);
+    return sized(a) ? hdqt::adapters_workspace(a) : 0;
+}
+
+int hdqt_adapters_fwd(const void* x, const void* A, const void* B, const int64_t* ids, const float* scale, const void* base, void* out,
+                      void* saved, size_t saved_bytes, int64_t M, int64_t K, int64_t N, int r, int n, int dtype, void* stream)
+{
+    if (!out) return HDQT_EINVAL_NULL;
+    hdqt::AdapterArgs a = sizes_of(M, K, N, r, n, dtype);
+    a.x = x; a.A = A; a.B = B; a.ids = ids; a.scale = scale; a.base = base; a.out = out; a.saved = saved;
+    const int rc = check_adapters(a, saved_bytes);
+    if (rc) return rc;
+    const hipError_t e = hdqt::launch_adapters_fwd(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? HDQT_OK : hip_fail(e);
+}
+
+int hdqt_adapters_bwd(const void* dy, const void* x, const void* A, const void* B, const int64_t* ids, const float* scale,
+                      const void* saved, size_t saved_bytes, const void* base, void* dx, void* dA, void* dB, int64_t M, int64_t K, int64_t N,
+                      int r, int n, int dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!dy || (!dx && !dA && !dB)) return HDQT_EINVAL_NULL;
+    hdqt::AdapterArgs a = sizes_of(M, K, N, r, n, dtype);
+    a.dy = dy; a.x = x; a.A = A; a.B = B; a.ids = ids; a.scale = scale; a.base = base; a.out = dx; a.dA = dA; a.dB = dB;
+    a.saved = const_cast<void*>(saved);
+    const int rc = check_adapters(a, saved_bytes);
+    if (rc) return rc;
+    if (short_of(workspace, workspace_bytes, hdqt::adapters_workspace(a))) return HDQT_EWORKSPACE;
+    if (off(workspace, 16)) return HDQT_EALIGN;
+    const hipError_t e = hdqt::launch_adapters_bwd(a, workspace, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? HDQT_OK : hip_fail(e);
 }
 

@@ -174,4 +174,24 @@ size_t layernorm_workspace(const LayerNormArgs& a);         // of the backward p
 hipError_t launch_layernorm_fwd(const LayerNormArgs& a, hipStream_t stream);
 hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStream_t stream);
 
+// ---- adapters.hip ----
+
+constexpr int kAdaptersMost = 1024, kRankMost = 128;
+struct AdapterArgs {
+    const void *x, *A, *B;              // [M, K], [n, K, r], [n, r, N]
+    const int64_t* ids;                 // [M]
+    const float* scale;                 // [n] or null
+    const void* base;                   // [M, N] (backward: of dx, [M, K]) or null
+    void* out;                          // [M, N]; backward: dx [M, K] or null
+    const void* dy;                     // [M, N]
+    void *dA, *dB;                      // as A and B, or null
+    void* saved;
+    int64_t M, K, N;
+    int r, n, dtype;
+};
+size_t adapters_saved(const AdapterArgs& a);
+size_t adapters_workspace(const AdapterArgs& a);            // of the backward pass
+hipError_t launch_adapters_fwd(const AdapterArgs& a, hipStream_t stream);
+hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_t stream);
+
 } // namespace hdqt
