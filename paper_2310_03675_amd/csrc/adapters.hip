@@ -35,42 +35,65 @@ constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kMostGroups =
 enum Mode { kAlong, kDown };        // memory runs along the contraction, or across it
 
 // 16 bytes of a line: eight bfloat16 values or four of 32 bits
-struct Piece {
+struct __attribute__((aligned(16))) Piece {
     uint32_t w[4];
 };
 template <int DT>
 constexpr int lane_of() { return DT == kF32 ? 4 : 8; }
 
-// (n: how many of them there are; the others are zero)
-template <int DT>
-__device__ __forceinline__ Piece load_piece(const void* p, int64_t at, int n)
+// N neighbouring elements of a line, in the first places of a piece.  WHOLE: all are there.  Else the first `n` of them are, and the
+// others zero: element by element, at addresses that are inside (`at` is), so that no branch comes between one load and the next.
+template <int DT, int N, bool WHOLE>
+__device__ __forceinline__ Piece load_few(const void* p, int64_t at, int n)
 {
-    constexpr int L = lane_of<DT>();
     Piece q{};
-    const char* from = static_cast<const char*>(p) + at * (16 / L);
-    if (n >= L) {
-        __builtin_memcpy(q.w, from, 16);
+    if constexpr (WHOLE) {
+        __builtin_memcpy(q.w, static_cast<const char*>(p) + at * (DT == kF32 ? 4 : 2), N * (DT == kF32 ? 4 : 2));
     } else {
 #pragma unroll
-        for (int j = 0; j < L - 1; ++j)
-            if (j < n) {
-                if (DT == kF32) q.w[j & 3] = static_cast<const uint32_t*>(p)[at + j];
-                else q.w[j / 2] |= (uint32_t)static_cast<const uint16_t*>(p)[at + j] << 16 * (j & 1);
+        for (int j = 0; j < N; ++j) {
+            const int64_t i = at + (j < n ? j : 0);
+            if (DT == kF32) {
+                const uint32_t v = static_cast<const uint32_t*>(p)[i];
+                q.w[j & 3] = j < n ? v : 0u;
+            } else {
+                const uint32_t v = static_cast<const uint16_t*>(p)[i];
+                q.w[j / 2] |= (j < n ? v : 0u) << 16 * (j & 1);
             }
+        }
     }
     return q;
 }
+template <int DT, bool WHOLE>
+__device__ __forceinline__ Piece load_piece(const void* p, int64_t at, int n)
+{
+    return load_few<DT, lane_of<DT>(), WHOLE>(p, at, n);
+}
+__device__ __forceinline__ Piece only_if(bool there, const Piece& q) { return there ? q : Piece{}; }
+// zeros for the first n elements
 template <int DT>
-__device__ __forceinline__ void store_piece(void* p, int64_t at, int n, const Piece& q)
+__device__ __forceinline__ Piece without(Piece q, int n)
+{
+#pragma unroll
+    for (int j = 0; j < lane_of<DT>(); ++j) {
+        if (DT == kF32) q.w[j & 3] = j < n ? 0u : q.w[j & 3];
+        else q.w[j / 2] &= j < n ? 0xFFFFu << 16 * (1 - (j & 1)) : 0xFFFFFFFFu;
+    }
+    return q;
+}
+
+// elements lo to hi - 1
+template <int DT>
+__device__ __forceinline__ void store_piece(void* p, int64_t at, int lo, int hi, const Piece& q)
 {
     constexpr int L = lane_of<DT>();
-    if (n >= L) {
+    if (lo <= 0 && hi >= L) {
         __builtin_memcpy(static_cast<char*>(p) + at * (16 / L), q.w, 16);
         return;
     }
 #pragma unroll
-    for (int j = 0; j < L - 1; ++j)
-        if (j < n) {
+    for (int j = 0; j < L; ++j)
+        if (j >= lo && j < hi) {
             if (DT == kF32) static_cast<uint32_t*>(p)[at + j] = q.w[j & 3];
             else static_cast<uint16_t*>(p)[at + j] = (uint16_t)(q.w[j / 2] >> 16 * (j & 1));
         }
@@ -89,26 +112,6 @@ __device__ __forceinline__ Piece piece_of(const float (&v)[lane_of<DT>()])
     for (int j = 0; j < 4; ++j) {
         if constexpr (DT == kF32) q.w[j] = __float_as_uint(v[j]);
         else q.w[j] = to_bf16(v[2 * j]) | to_bf16(v[2 * j + 1]) << 16;
-    }
-    return q;
-}
-
-// N neighbouring elements of a line, in the first places of a piece
-template <int DT, int N>
-__device__ __forceinline__ Piece load_few(const void* p, int64_t at, int n)
-{
-    if constexpr (N == lane_of<DT>()) return load_piece<DT>(p, at, n);
-    Piece q{};
-    const char* from = static_cast<const char*>(p) + at * (DT == kF32 ? 4 : 2);
-    if (n >= N) {
-        __builtin_memcpy(q.w, from, N * (DT == kF32 ? 4 : 2));
-    } else {
-#pragma unroll
-        for (int j = 0; j < N - 1; ++j)
-            if (j < n) {
-                if (DT == kF32) q.w[j & 3] = static_cast<const uint32_t*>(p)[at + j];
-                else q.w[j / 2] |= (uint32_t)static_cast<const uint16_t*>(p)[at + j] << 16 * (j & 1);
-            }
     }
     return q;
 }
@@ -208,8 +211,28 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
     const int64_t rows = (M + 64 * kPlanWaves - 1) / (64 * kPlanWaves) * 64, first = wave * rows, end = first + rows < M ? first + rows : M;
     for (uint32_t i = threadIdx.x; i < kPlanWaves * kMostGroups; i += kPlanThreads) (&counts[0][0])[i] = 0;
     __syncthreads();
-#pragma unroll 4
-    for (int64_t i = first + lane; i < end; i += 64) atomicAdd(&counts[wave][group_of(ids[i], n)], 1u);
+    // f(a row, its group, lanes with the same) for a wave's rows, 64 at a time, kAhead of those loaded before the first is taken
+    constexpr int kAhead = 8;
+    auto each = [&](auto f) {
+        for (int64_t i = first; i < end; i += 64 * kAhead) {
+            int64_t id[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t at = i + 64 * u + lane;
+                id[u] = ids[at < end ? at : end - 1];
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t at = i + 64 * u + lane;
+                const bool there = at < end;
+                const uint32_t g = group_of(id[u], n);
+                f(at, g, there, same_lanes(g, bits, __ballot(there)));
+            }
+        }
+    };
+    each([&](int64_t, uint32_t g, bool there, uint64_t same) {
+        if (there && (same & ((1ull << lane) - 1)) == 0) counts[wave][g] += (uint32_t)__popcll(same);
+    });
     __syncthreads();
     // a thread's two groups: their rows and tiles, and the sums of those of the groups before
     uint32_t have[2] = {0, 0}, cut[2];
@@ -262,16 +285,13 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
         }
         const_cast<uint2*>(p.tile)[i] = make_uint2(lo, starts[lo] + kTile * (i - tiles[lo]));
     }
-    for (int64_t i = first; i < end; i += 64) {
-        const bool there = i + lane < end;
-        const uint32_t g = there ? group_of(ids[i + lane], n) : 0;
-        const uint64_t same = same_lanes(g, bits, __ballot(there));
+    each([&](int64_t row, uint32_t g, bool there, uint64_t same) {
         const int leader = __ffsll((unsigned long long)same) - 1;
         uint32_t at = 0;
         if (there && lane == leader) at = atomicAdd(&counts[wave][g], (uint32_t)__popcll(same));
         at = __shfl(at, leader & 63);
-        if (there) order[starts[g] + at + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (uint32_t)(i + lane);
-    }
+        if (there) order[starts[g] + at + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (uint32_t)row;
+    });
 }
 
 // Rows of one group, for a wave: `count` of them, place p's row by row(p).
@@ -302,6 +322,25 @@ struct RowArgs {
     int64_t M;
     int n;
 };
+
+// A launch of `inner` x `outer` workgroups.  They go to the eight XCDs in turn: each gets a run of its own, inner after inner, so
+// that tiles of one adapter, which read the same part of its matrix, share an L2.
+struct Grid {
+    Divisor inner;
+    uint32_t total, per_xcd;
+};
+Grid grid_of(uint32_t inner, uint32_t outer)
+{
+    const uint32_t total = inner * outer;
+    return {make_divisor(inner), total, (total + 7) / 8};
+}
+__device__ __forceinline__ bool place_of(const Grid& k, uint32_t& inner, uint32_t& outer)
+{
+    const uint32_t idx = (blockIdx.x & 7) * k.per_xcd + (blockIdx.x >> 3);
+    outer = divide(idx, k.inner);
+    inner = idx - outer * k.inner.d;
+    return idx < k.total;
+}
 
 // The rows of workgroup `tile`: none where there is no such tile, or where an earlier row of the few has them.
 __device__ __forceinline__ Group tile_rows(const RowArgs& a, uint32_t tile)
@@ -337,24 +376,36 @@ __device__ __forceinline__ Group adapter_rows(const RowArgs& a, uint32_t adapter
 
 struct DownArgs {
     RowArgs rows;
+    Grid grid;                      // tiles, parts
     const void *x, *W;              // [M, D]; of an adapter [D, r] (kDown) or [r, D] (kAlong)
     float* h;                       // [parts][M][16 RT]
     int64_t D;
     int r;
-    uint32_t parts, chunks;         // of the contraction: parts, and how many times 4 kLane a part has
+    uint32_t chunks;                // of the contraction: how many times 4 kLane a part has
 };
 
-template <int DT, int RT, int MODE>
+// SHORT: the contraction is shorter than a chunk, and loaded element by element.  Else its last chunk, where it is no whole number of
+// them, begins a chunk before the end, and what it has of the one before is taken for zeros.
+template <int DT, int RT, int MODE, bool SHORT>
 __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(DownArgs a)
 {
-    constexpr int L = lane_of<DT>(), kChunk = 4 * L, RL = RT < L ? RT : L, RQ = RT / RL;
-    // tile t + RL q of the ranks: a lane's is 16 RL q + RL (l % 16) + t
+    constexpr int L = lane_of<DT>(), kChunk = 4 * L, RL = RT < L ? RT : L, RQ = RT / RL, kAhead = RT <= 4 ? 4 : 2;
     __shared__ v4f sums[kDownWaves / 2][kSubs][RT][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-    const Group rows = tile_rows(a.rows, blockIdx.x);
+    uint32_t tile, part;
+    if (!place_of(a.grid, tile, part)) return;
+    const Group rows = tile_rows(a.rows, tile);
     if (!rows.count || rows.group >= (uint32_t)a.rows.n) return;
     const char* W = static_cast<const char*>(a.W) + (int64_t)rows.group * a.D * a.r * (16 / L);
-    const int64_t first = (int64_t)blockIdx.y * a.chunks, all = (a.D + kChunk - 1) / kChunk;
+    // tile t + RL q of the ranks: a lane's is rank[q] + t.  (16 RL q + RL (l % 16); the last lanes' begin RL before the last rank's end,
+    // and have ranks of the lanes before again: r is above RL, where that is more than one)
+    int rank[RQ];
+#pragma unroll
+    for (int q = 0; q < RQ; ++q) {
+        const int c = 16 * RL * q + RL * j;
+        rank[q] = c + RL <= a.r ? c : a.r - RL;
+    }
+    const int64_t first = (int64_t)part * a.chunks, all = (a.D + kChunk - 1) / kChunk;
     const int64_t last = first + a.chunks < all ? first + a.chunks : all;
     for (uint32_t place = 0; place < rows.count; place += kTile) {
         int64_t line[kSubs];
@@ -364,42 +415,62 @@ __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(DownArgs a)
             line[s] = (int64_t)rows.row(p < rows.count ? p : place) * a.D;
         }
         v4f acc[kSubs][RT] = {};
-        auto chunk = [&](int64_t c, auto whole) {
-            const int64_t k = c * kChunk + L * g;
-            const int n = whole.value || k + L <= a.D ? L : k < a.D ? (int)(a.D - k) : 0;
-            Piece x[kSubs], w[RT];
+        // N chunks, one of every wave's after the other; `skip` elements of each line of the one are not its
+        auto chunks = [&](int64_t from, auto number, int skip) {
+            constexpr int N = number.value, LINES = MODE == kDown ? L : RL;
+            Piece x[N][kSubs], w[N][RQ * LINES];
 #pragma unroll
-            for (int s = 0; s < kSubs; ++s) x[s] = load_piece<DT>(a.x, line[s] + k, whole.value ? L : n);
+            for (int u = 0; u < N; ++u) {
+                const int64_t k = from + (int64_t)u * kDownWaves * kChunk + L * g;
+                const int n = SHORT ? (int)(a.D - k) : L;
+                const int64_t in = SHORT && n <= 0 ? 0 : k;
 #pragma unroll
-            for (int q = 0; q < RQ; ++q) {
-                const int c0 = 16 * RL * q + RL * j;
-                if constexpr (MODE == kDown) {
-                    Piece lines[L];
+                for (int s = 0; s < kSubs; ++s) x[u][s] = load_piece<DT, !SHORT>(a.x, line[s] + in, n);
 #pragma unroll
-                    for (int e = 0; e < L; ++e) {
-                        lines[e] = Piece{};
-                        if (whole.value || e < n) lines[e] = load_few<DT, RL>(W, (k + e) * a.r + c0, a.r - c0);
+                for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                    for (int e = 0; e < LINES; ++e) {
+                        if constexpr (MODE == kDown)
+                            w[u][L * q + e] = only_if(!SHORT || e < n, load_few<DT, RL, true>(W, (SHORT && e >= n ? 0 : k + e) * a.r + rank[q], RL));
+                        else
+                            w[u][RL * q + e] = load_piece<DT, !SHORT>(W, (int64_t)(rank[q] + e) * a.D + in, n);
                     }
+            }
+            if (N == 1 && !SHORT && skip) {
+                const int own = skip - L * g;               // elements of a lane's that are not
 #pragma unroll
-                    for (int t = 0; t < RL; ++t) w[RL * q + t] = turned<DT>(lines, t);
-                } else {
+                for (int s = 0; s < kSubs; ++s) x[0][s] = without<DT>(x[0][s], own);
 #pragma unroll
-                    for (int t = 0; t < RL; ++t) {
-                        w[RL * q + t] = Piece{};
-                        if (c0 + t < a.r) w[RL * q + t] = load_piece<DT>(W, (c0 + t) * a.D + k, whole.value ? L : n);
-                    }
-                }
+                for (int i = 0; i < RQ * LINES; ++i) w[0][i] = MODE == kDown ? only_if(i % L >= own, w[0][i]) : without<DT>(w[0][i], own);
             }
 #pragma unroll
-            for (int s = 0; s < kSubs; ++s)
+            for (int u = 0; u < N; ++u)
 #pragma unroll
-                for (int t = 0; t < RT; ++t) acc[s][t] = multiply<DT>(x[s], w[t], acc[s][t]);
+                for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                    for (int t = 0; t < RL; ++t) {
+                        Piece b;
+                        if constexpr (MODE == kDown) {
+                            Piece lines[L];
+#pragma unroll
+                            for (int e = 0; e < L; ++e) lines[e] = w[u][L * q + e];
+                            b = turned<DT>(lines, t);
+                        } else {
+                            b = w[u][RL * q + t];
+                        }
+#pragma unroll
+                        for (int s = 0; s < kSubs; ++s) acc[s][RL * q + t] = multiply<DT>(x[u][s], b, acc[s][RL * q + t]);
+                    }
         };
-        const int64_t full = a.D / kChunk < last ? a.D / kChunk : last;
+        using std::integral_constant;
+        const int64_t full = SHORT ? last : a.D / kChunk < last ? a.D / kChunk : last;
         int64_t c = first + wave;
-#pragma unroll 4
-        for (; c < full; c += kDownWaves) chunk(c, std::true_type{});
-        if (c < last) chunk(c, std::false_type{});
+        if (!SHORT)
+            for (; c + (kAhead - 1) * kDownWaves < full; c += kAhead * kDownWaves) chunks(c * kChunk, integral_constant<int, kAhead>{}, 0);
+        for (; c < last; c += kDownWaves) {
+            const bool cut = c >= full;
+            chunks(cut ? a.D - kChunk : c * kChunk, integral_constant<int, 1>{}, cut ? (int)(c * kChunk - (a.D - kChunk)) : 0);
+        }
 #pragma unroll
         for (int half = kDownWaves / 2; half; half /= 2) {
             __syncthreads();
@@ -423,13 +494,14 @@ __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(DownArgs a)
                     const uint32_t p = place + 16 * s + 4 * g + i;
                     const uint32_t row = rows.row(p < rows.count ? p : place);
                     if (p >= rows.count) continue;
-                    float* to = a.h + ((int64_t)blockIdx.y * a.rows.M + row) * (16 * RT);
+                    float* to = a.h + ((int64_t)part * a.rows.M + row) * (16 * RT);
 #pragma unroll
                     for (int q = 0; q < RQ; ++q)
 #pragma unroll
                         for (int t = 0; t < RL; ++t) {
-                            const int c0 = 16 * RL * q + RL * j + t;
-                            to[c0] = c0 < a.r ? acc[s][RL * q + t][i] : 0.0f;       // (0 x infinity behind the last rank)
+                            const int c = 16 * RL * q + RL * j + t;
+                            to[rank[q] + t] = acc[s][RL * q + t][i];
+                            if (c >= a.r) to[c] = 0.0f;     // (behind the last rank)
                         }
                 }
     }
@@ -439,6 +511,8 @@ __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(DownArgs a)
 
 struct UpArgs {
     RowArgs rows;
+    Grid grid;                      // tiles, and workgroups over the columns
+    uint32_t across;                // of those
     const float* h;                 // [parts][M][16 RT]
     const float* scale;             // [n] or null
     const void* W;                  // of an adapter [r, N] (kDown) or [N, r] (kAlong)
@@ -468,96 +542,111 @@ __device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t pa
     for (int j = 0; j < N; ++j) v[j] *= scale;
 }
 
-template <int DT, int RT, int MODE>
+// SHORT: there are fewer columns than a wave has, or (kAlong) fewer ranks than a load, and W and base are loaded element by element.
+// Else the last columns, and the last ranks of a line along them, begin so far before the end that loads are whole; what others have
+// already is not written, and zero in h.
+template <int DT, int RT, int MODE, bool SHORT>
 __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
 {
     constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L;
     // bfloat16, one tile of ranks: both planes are one chunk, the second beside the same lines of W again
     constexpr bool kFolded = DT == kBf16 && RT == 1;
     constexpr int P = kFolded ? 1 : planes_of<DT>(), C = 16 * RT < kChunk ? 1 : 16 * RT / kChunk, kRanks = 16 * RT;
+    __shared__ Piece h[kSubs * C][P][64];
+    __shared__ __attribute__((aligned(16))) uint32_t lines[kTile];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-    const Group rows = tile_rows(a.rows, blockIdx.x);
+    uint32_t tile, over;
+    if (!place_of(a.grid, tile, over)) return;
+    const Group rows = tile_rows(a.rows, tile);
     if (!rows.count) return;
     const bool none = rows.group == (uint32_t)a.rows.n, wrong = rows.group > (uint32_t)a.rows.n;
     if (none && a.base == a.out) return;
     const char* W = static_cast<const char*>(a.W) + (none || wrong ? 0 : (int64_t)rows.group * a.N * a.r * (16 / L));
     const float scale = a.scale && !none && !wrong ? a.scale[rows.group] : 1.0f;
-    const int at = L * (kFolded ? g & 1 : g);              // a lane's first rank of a chunk
+    // a lane's ranks of a chunk: from first(c) on, those before own(c) another lane's
+    auto own = [&](int c) { return kChunk * c + L * (kFolded ? g & 1 : g); };
+    auto first = [&](int c) { return MODE == kDown || SHORT || own(c) + L <= a.r ? own(c) : a.r - L; };
     for (uint32_t place = 0; place < rows.count; place += kTile) {
-        Piece h[kSubs][C][P];
-        int64_t line[kSubs][4];
-        bool there[kSubs][4];
+        // the tile's h, split, and its rows, for all waves
+        if (place) __syncthreads();
+        for (int f = wave; f < kSubs * C; f += kUpWaves) {
+            const int s = f / C, c = f % C;
+            const uint32_t p = place + 16 * s + j, row = rows.row(p < rows.count ? p : place);       // (behind the last: any that there is)
+            float v[L] = {};
+            if (!none && !wrong) load_h<L>(a.h + (int64_t)row * kRanks + first(c), a.rows.M * kRanks, a.parts, scale, v);
+            if (MODE == kAlong && !SHORT)
 #pragma unroll
-        for (int s = 0; s < kSubs; ++s) {
-            const uint32_t p = place + 16 * s + j;
-            const uint32_t row = rows.row(p < rows.count ? p : place);
+                for (int e = 0; e < L; ++e) v[e] = first(c) + e >= own(c) ? v[e] : 0.0f;
+            Piece two[planes_of<DT>()];
+            split<DT>(v, two);
+            if constexpr (kFolded) h[f][0][lane] = g < 2 ? two[0] : two[1];
+            else
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float v[L] = {};
-                if (!none && !wrong) load_h<L>(a.h + (int64_t)row * kRanks + kChunk * c + at, a.rows.M * kRanks, a.parts, scale, v);
-                Piece two[planes_of<DT>()];
-                split<DT>(v, two);
-                if constexpr (kFolded) h[s][c][0] = g < 2 ? two[0] : two[1];
-                else
-#pragma unroll
-                    for (int k = 0; k < P; ++k) h[s][c][k] = two[k];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t q = place + 16 * s + 4 * g + i;
-                there[s][i] = q < rows.count;
-                line[s][i] = (int64_t)rows.row(there[s][i] ? q : place) * a.N;
-            }
+                for (int k = 0; k < P; ++k) h[f][k][lane] = two[k];
+            if (c == 0 && g == 0) lines[16 * s + j] = row;
         }
-        for (int64_t c0 = ((int64_t)blockIdx.y * kUpWaves + wave) * kColumns; c0 < a.N; c0 += (int64_t)gridDim.y * kUpWaves * kColumns) {
-            const int64_t col = c0 + L * j;
-            const int n = col + L <= a.N ? L : col < a.N ? (int)(a.N - col) : 0;
-            Piece base[kSubs][4];
-#pragma unroll
-            for (int s = 0; s < kSubs; ++s)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    base[s][i] = Piece{};
-                    if (a.base && there[s][i]) base[s][i] = load_piece<DT>(a.base, line[s][i] + col, n);
-                }
-            v4f acc[kSubs][L] = {};
+        __syncthreads();
+        for (int64_t c0 = ((int64_t)over * kUpWaves + wave) * kColumns; c0 < a.N; c0 += (int64_t)a.across * kUpWaves * kColumns) {
+            // a lane's columns: from col on, those from lo to hi its own
+            const int64_t from = SHORT || c0 + kColumns <= a.N ? c0 : a.N - kColumns;
+            const int lo = (int)(c0 - from) - L * j, hi = SHORT ? (int)(a.N - c0) - L * j : L;
+            const int64_t col = SHORT && hi <= 0 ? c0 : from + L * j;
+            Piece w[C][L];
             if (!none && !wrong)
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
-                    const int rank = kChunk * c + at;
-                    Piece w[L];
-                    if constexpr (MODE == kDown) {
-                        Piece lines[L];
 #pragma unroll
-                        for (int e = 0; e < L; ++e) {
-                            lines[e] = Piece{};
-                            if (rank + e < a.r) lines[e] = load_piece<DT>(W, (rank + e) * a.N + col, n);
-                        }
-#pragma unroll
-                        for (int t = 0; t < L; ++t) w[t] = turned<DT>(lines, t);
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < L; ++t) {
-                            w[t] = Piece{};
-                            if (t < n) w[t] = load_piece<DT>(W, (col + t) * a.r + rank, a.r - rank);
+                    for (int e = 0; e < L; ++e) {
+                        if constexpr (MODE == kDown) {     // line own(c) + e
+                            const int rank = own(c) + e < a.r ? own(c) + e : 0;
+                            w[c][e] = load_piece<DT, !SHORT>(W, rank * a.N + col, hi);
+                        } else {                           // column col + e
+                            const int rank = first(c) < a.r ? first(c) : 0;
+                            w[c][e] = load_piece<DT, !SHORT>(W, (col + (SHORT && e >= hi ? 0 : e)) * a.r + rank, a.r - first(c));
                         }
                     }
+                    if (a.r != kRanks)                     // (h is zero there, but W may be infinite)
 #pragma unroll
-                    for (int k = P - 1; k >= 0; --k)
+                        for (int e = 0; e < L; ++e) w[c][e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[c][e]);
+                    if constexpr (MODE == kDown) {
+                        Piece t[L];
 #pragma unroll
-                        for (int s = 0; s < kSubs; ++s)
+                        for (int e = 0; e < L; ++e) t[e] = turned<DT>(w[c], e);
 #pragma unroll
-                            for (int t = 0; t < L; ++t) acc[s][t] = multiply<DT>(h[s][c][k], w[t], acc[s][t]);
+                        for (int e = 0; e < L; ++e) w[c][e] = t[e];
+                    }
                 }
+#pragma unroll 1
+            for (int s = 0; s < kSubs; ++s) {
+                const uint32_t at = place + 16 * s + 4 * g;
+                if (place + 16 * s >= rows.count) break;
+                const uint4 row = *reinterpret_cast<const uint4*>(lines + 16 * s + 4 * g);
+                const int64_t line[4] = {row.x * a.N + col, row.y * a.N + col, row.z * a.N + col, row.w * a.N + col};
+                Piece base[4];
+                if (a.base)
 #pragma unroll
-            for (int s = 0; s < kSubs; ++s)
+                    for (int i = 0; i < 4; ++i) base[i] = load_piece<DT, !SHORT>(a.base, line[i], hi);
+                v4f acc[L] = {};
+                if (!none && !wrong)
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+#pragma unroll
+                        for (int k = P - 1; k >= 0; --k) {
+                            const Piece x = h[s * C + c][k][lane];
+#pragma unroll
+                            for (int t = 0; t < L; ++t) acc[t] = multiply<DT>(x, w[c][t], acc[t]);
+                        }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v[L];
 #pragma unroll
-                    for (int t = 0; t < L; ++t) v[t] = wrong ? __builtin_nanf("") : value<DT>(base[s][i], t) + acc[s][t][i];
-                    if (there[s][i]) store_piece<DT>(a.out, line[s][i] + col, n, piece_of<DT>(v));
+                    for (int t = 0; t < L; ++t) {
+                        v[t] = wrong ? __builtin_nanf("") : acc[t][i];
+                        if (a.base) v[t] += value<DT>(base[i], t);
+                    }
+                    if (at + i < rows.count && hi > 0) store_piece<DT>(a.out, line[i], lo, hi, piece_of<DT>(v));
                 }
+            }
         }
     }
 }
@@ -567,115 +656,131 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
 // an adapter's gradient: W[j][c] = sum over its rows of scale h[row][j] v[row][c]
 struct WeightArgs {
     RowArgs rows;
+    Grid grid;                      // blocks of columns of both, and adapters times parts of the rows
     const float* h[2];              // dA: g; dB: h.  [parts][M][16 RT]
     const void* v[2];               // dA: x; dB: dy
     void* out[2];                   // [n][K][r]; [n][r][N]; either may be null
-    float* sums;                    // where a gradient is added up over parts of the rows, [split][n][r][K + N], else null
+    float* sums;                    // where a gradient is added up over parts of the rows, [split][n K r + n r N], else null
     const float* scale;
     int64_t N[2];
     int r;
-    uint32_t parts[2], blocks[2], split;        // blocks of columns
+    uint32_t parts[2], blocks, split;           // blocks: of dA's columns
+    Divisor by_r, by_split;
+    // elements of a part's sums, and of those dA's
+    __device__ __forceinline__ int64_t of_a_part() const { return (int64_t)rows.n * r * (N[0] + N[1]); }
+    __device__ __forceinline__ int64_t of_dA() const { return (int64_t)rows.n * r * N[0]; }
 };
 
+// A workgroup has 128 columns (64 in fp32) and all ranks of one gradient: a wave two tiles of ranks at most, and of the rows what the
+// waves with the same ranks share.
 template <int DT, int RT>
 __global__ __launch_bounds__(64 * kWeightWaves) void weights_kernel(WeightArgs a)
 {
     constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L, RW = RT < 2 ? RT : 2, P = planes_of<DT>();
-    __shared__ v4f sums[kWeightWaves / 2][RW][L][64];
+    constexpr int kShares = kWeightWaves / (RT / RW), kAcross = kColumns + 4;
+    // dB: [rank][column]; dA: [column][rank]; rows of one more than they hold, for the banks
+    __shared__ float tile[kAcross * (16 * RT + 1)];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-    const int of = blockIdx.x >= a.blocks[0];
+    uint32_t block, which;
+    if (!place_of(a.grid, block, which)) return;
+    const int of = block >= a.blocks;
     if (!a.out[of]) return;
-    const int64_t N = a.N[of], c0 = (int64_t)(blockIdx.x - (of ? a.blocks[0] : 0)) * kColumns, col = c0 + L * j;
-    const uint32_t adapter = blockIdx.y, rank0 = blockIdx.z / a.split * (16 * RW), part = blockIdx.z % a.split;
+    const int64_t N = a.N[of], c0 = (int64_t)(block - (of ? a.blocks : 0)) * kColumns, col = c0 + L * j;
+    const uint32_t adapter = divide(which, a.by_split), part = which - adapter * a.split;
+    const int rank0 = wave / kShares * (16 * RW), share = wave % kShares;
     const Group rows = adapter_rows(a.rows, adapter);
     const float* h = a.h[of] + rank0 + j;
-    const int n = col + L <= N ? L : col < N ? (int)(N - col) : 0;
+    const int n = col + L <= N ? L : col < N ? (int)(N - col) : 0, there = N - c0 < kColumns ? (int)(N - c0) : kColumns;
     v4f acc[RW][L] = {};
-    // (as often for every lane of a wave: the rows of a few are handed from lane to lane)
-    const uint32_t step = kChunk * kWeightWaves * a.split;
-    for (uint32_t first = kChunk * (part * kWeightWaves + wave); first < rows.count; first += step) {
-        Piece lines[L];
-        float u[RW][L];
+    auto sum = [&](auto whole) {
+        constexpr bool WHOLE = whole.value;
+        // (as often for every lane of a wave: the rows of a few are handed from lane to lane)
+        const uint32_t step = kChunk * kShares * a.split;
+        for (uint32_t first = kChunk * (part * kShares + share); first < rows.count; first += step) {
+            Piece lines[L];
+            float u[RW][L];
+#pragma unroll
+            for (int e = 0; e < L; ++e) {
+                const uint32_t p = first + L * g + e;
+                const bool has = p < rows.count;           // (the others: a row that there is, taken for zeros)
+                const int64_t row = rows.row(has ? p : first);
+                lines[e] = load_piece<DT, WHOLE>(a.v[of], row * N + (WHOLE || n > 0 ? col : 0), n);
+                lines[e] = only_if(has, lines[e]);
+#pragma unroll
+                for (int t = 0; t < RW; ++t) {
+                    u[t][e] = h[row * (16 * RT) + 16 * t];
+                    for (uint32_t s = 1; s < a.parts[of]; ++s) u[t][e] += h[(s * a.rows.M + row) * (16 * RT) + 16 * t];
+                    u[t][e] = has ? u[t][e] : 0.0f;
+                }
+            }
+            Piece up[RW][P];
+#pragma unroll
+            for (int t = 0; t < RW; ++t) split<DT>(u[t], up[t]);
+#pragma unroll
+            for (int c = 0; c < L; ++c) {
+                const Piece w = turned<DT>(lines, c);
+#pragma unroll
+                for (int t = 0; t < RW; ++t)
+#pragma unroll
+                    for (int k = P - 1; k >= 0; --k) acc[t][c] = multiply<DT>(up[t][k], w, acc[t][c]);
+            }
+        }
+    };
+    if (c0 + kColumns <= N) sum(std::true_type{});
+    else sum(std::false_type{});
+    const float scale = a.scale ? a.scale[adapter] : 1.0f;
+    // the shares one after the other; a lane has ranks rank0 + 16 t + 4 g + i of columns col + c
+    const int line = a.r | 1;
+#pragma unroll
+    for (int s = 0; s < kShares; ++s) {
+        if (share == s)
+#pragma unroll
+            for (int t = 0; t < RW; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int rank = rank0 + 16 * t + 4 * g + i;
+                    if (rank >= a.r) continue;
+#pragma unroll
+                    for (int c = 0; c < L; ++c) {
+                        float* to = tile + (of ? rank * kAcross + L * j + c : (L * j + c) * line + rank);
+                        *to = s ? *to + acc[t][c][i] : acc[t][c][i];
+                    }
+                }
+        __syncthreads();
+    }
+    // dA's part is one run of memory, dB's one of every rank
+    const int64_t to = of ? (int64_t)adapter * a.r * N + c0 : ((int64_t)adapter * N + c0) * a.r;
+    float* sums = a.sums ? a.sums + (int64_t)part * a.of_a_part() + (of ? a.of_dA() : 0) : nullptr;
+    const int runs = of ? a.r : 1, length = of ? there : there * a.r, pieces = (length + L - 1) / L;
+    for (int i = threadIdx.x; i < runs * pieces; i += 64 * kWeightWaves) {
+        const int run = of ? i / pieces : 0, e0 = (i - run * pieces) * L, left = length - e0 < L ? length - e0 : L;
+        float v[L];
 #pragma unroll
         for (int e = 0; e < L; ++e) {
-            const uint32_t p = first + L * g + e;
-            const bool there = p < rows.count;
-            const int64_t row = rows.row(there ? p : first);
-            lines[e] = Piece{};
-            if (there) lines[e] = load_piece<DT>(a.v[of], row * N + col, n);
-#pragma unroll
-            for (int t = 0; t < RW; ++t) {
-                u[t][e] = 0.0f;
-                if (there)
-                    for (uint32_t s = 0; s < a.parts[of]; ++s) u[t][e] += h[(s * a.rows.M + row) * (16 * RT) + 16 * t];
-            }
+            const int in = e < left ? e0 + e : e0, c = of ? in : (int)divide((uint32_t)in, a.by_r);
+            v[e] = scale * (of ? tile[run * kAcross + in] : tile[c * line + in - c * a.r]);
         }
-        Piece up[RW][P];
+        const int64_t dest = to + (int64_t)run * N + e0;
+        if (sums) {
 #pragma unroll
-        for (int t = 0; t < RW; ++t) split<DT>(u[t], up[t]);
-#pragma unroll
-        for (int c = 0; c < L; ++c) {
-            const Piece w = turned<DT>(lines, c);
-#pragma unroll
-            for (int t = 0; t < RW; ++t)
-#pragma unroll
-                for (int k = P - 1; k >= 0; --k) acc[t][c] = multiply<DT>(up[t][k], w, acc[t][c]);
+            for (int e = 0; e < L; ++e)
+                if (e < left) sums[dest + e] = v[e];
+        } else {
+            store_piece<DT>(a.out[of], dest, 0, left, piece_of<DT>(v));
         }
     }
-#pragma unroll
-    for (int half = kWeightWaves / 2; half; half /= 2) {
-        __syncthreads();
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int t = 0; t < RW; ++t)
-#pragma unroll
-                for (int c = 0; c < L; ++c) sums[wave - half][t][c][lane] = acc[t][c];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int t = 0; t < RW; ++t)
-#pragma unroll
-                for (int c = 0; c < L; ++c) acc[t][c] += sums[wave][t][c][lane];
-    }
-    if (wave) return;
-    const float scale = a.scale ? a.scale[adapter] : 1.0f;
-    // a lane has ranks rank0 + 16 t + 4 g to + 3 of columns col to col + kLane - 1
-#pragma unroll
-    for (int t = 0; t < RW; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int rank = (int)rank0 + 16 * t + 4 * g + i;
-            if (rank >= a.r) continue;
-            float v[L];
-#pragma unroll
-            for (int c = 0; c < L; ++c) v[c] = acc[t][c][i] * scale;
-            if (a.sums) {
-                float* to = a.sums + ((int64_t)(part * gridDim.y + adapter) * a.r) * (a.N[0] + a.N[1]) + (of ? (int64_t)a.r * a.N[0] : 0) + rank * N + col;
-                for (int c = 0; c < n; ++c) to[c] = v[c];
-            } else if (of) {
-                store_piece<DT>(a.out[1], ((int64_t)adapter * a.r + rank) * N + col, n, piece_of<DT>(v));
-            } else {
-                for (int c = 0; c < n; ++c) store_as<DT>(a.out[0], ((int64_t)adapter * N + col + c) * a.r + rank, v[c]);
-            }
-        }
 }
 
 // the gradients where their rows are in parts
 template <int DT>
-__global__ __launch_bounds__(256) void add_parts_kernel(WeightArgs a, uint32_t n)
+__global__ __launch_bounds__(256) void add_parts_kernel(WeightArgs a)
 {
-    const int64_t one = (int64_t)a.r * (a.N[0] + a.N[1]), all = one * n;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= all) return;
+    const int64_t all = a.of_a_part(), dA = a.of_dA(), i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int of = i >= dA;
+    if (i >= all || !a.out[of]) return;
     float s = 0.0f;
     for (uint32_t part = 0; part < a.split; ++part) s += a.sums[part * all + i];
-    const int64_t adapter = i / one, in = i - adapter * one, dA = (int64_t)a.r * a.N[0];
-    if (in < dA) {
-        const int64_t rank = in / a.N[0], c = in - rank * a.N[0];
-        if (a.out[0]) store_as<DT>(a.out[0], (adapter * a.N[0] + c) * a.r + rank, s);
-    } else if (a.out[1]) {
-        store_as<DT>(a.out[1], adapter * a.r * a.N[1] + in - dA, s);
-    }
+    store_as<DT>(a.out[of], of ? i - dA : i, s);
 }
 
 int tiles_of_rank(int r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }
@@ -713,8 +818,8 @@ size_t h_bytes(const AdapterArgs& a, int64_t D)
 // of them, none of fewer than 128 rows to an adapter.
 uint32_t split_of(const AdapterArgs& a)
 {
-    const int64_t columns = a.dtype == kBf16 ? 128 : 64, RT = tiles_of_rank(a.r);
-    const int64_t groups = ((a.K + columns - 1) / columns + (a.N + columns - 1) / columns) * a.n * (RT < 2 ? 1 : RT / 2);
+    const int64_t columns = a.dtype == kBf16 ? 128 : 64;
+    const int64_t groups = ((a.K + columns - 1) / columns + (a.N + columns - 1) / columns) * a.n;
     int64_t split = 1024 / groups;
     const int64_t most = a.M / (128 * (int64_t)a.n);
     if (split > most) split = most;
@@ -748,22 +853,28 @@ void launch_down(const AdapterArgs& a, const void* x, const void* W, float* h, i
 {
     ProfileScope ps(K_ADAPT_DOWN, stream);
     const Parts p = parts_of(a, D);
-    const DownArgs d{rows, x, W, h, D, a.r, p.parts, p.chunks};
+    const DownArgs d{rows, grid_of(grid_tiles(a), p.parts), x, W, h, D, a.r, p.chunks};
     with_types(a, [&](auto dt, auto rt) {
-        hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE>), dim3(grid_tiles(a), p.parts), dim3(64 * kDownWaves), 0, stream, d);
+        const dim3 grid(8 * d.grid.per_xcd), block(64 * kDownWaves);
+        if (D < 4 * lane_of<dt.value>()) hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, d);
+        else hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, false>), grid, block, 0, stream, d);
     });
 }
+
+// (a workgroup has a tile's columns in so many parts: as few as make 2048 workgroups)
 template <int MODE>
 void launch_up(const AdapterArgs& a, const float* h, const void* W, const void* base, void* out, int64_t N, int64_t D, const RowArgs& rows,
                hipStream_t stream)
 {
     ProfileScope ps(K_ADAPT_UP, stream);
-    const UpArgs u{rows, h, a.scale, W, base, out, N, a.r, parts_of(a, D).parts};
-    const int64_t columns = (a.dtype == kBf16 ? 128 : 64) * kUpWaves;
-    int64_t across = (N + columns - 1) / columns;
-    if (across > 32768) across = 32768;
+    const int64_t columns = (a.dtype == kBf16 ? 128 : 64) * kUpWaves, most = (N + columns - 1) / columns, want = 2048 / grid_tiles(a) + 1;
+    const uint32_t across = (uint32_t)(most < want ? most : want);
+    const UpArgs u{rows, grid_of(grid_tiles(a), across), across, h, a.scale, W, base, out, N, a.r, parts_of(a, D).parts};
     with_types(a, [&](auto dt, auto rt) {
-        hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE>), dim3(grid_tiles(a), (uint32_t)across), dim3(64 * kUpWaves), 0, stream, u);
+        const dim3 grid(8 * u.grid.per_xcd), block(64 * kUpWaves);
+        constexpr int L = lane_of<dt.value>();
+        if (N < 16 * L || (MODE == kAlong && a.r < L)) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, u);
+        else hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, false>), grid, block, 0, stream, u);
     });
 }
 
@@ -796,7 +907,7 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
     if (a.out) launch_up<kAlong>(a, g, a.A, a.base, a.out, a.K, a.N, rows, stream);
     if (a.dA || a.dB) {
         ProfileScope ps(K_ADAPT_WEIGHTS, stream);
-        const int64_t columns = a.dtype == kBf16 ? 128 : 64, RT = tiles_of_rank(a.r);
+        const int64_t columns = a.dtype == kBf16 ? 128 : 64;
         WeightArgs w{};
         w.rows = rows;
         w.h[0] = g; w.h[1] = h;
@@ -806,15 +917,17 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
         w.N[0] = a.K; w.N[1] = a.N;
         w.r = a.r;
         w.parts[0] = parts_of(a, a.N).parts; w.parts[1] = parts_of(a, a.K).parts;
-        w.blocks[0] = (uint32_t)((a.K + columns - 1) / columns); w.blocks[1] = (uint32_t)((a.N + columns - 1) / columns);
         w.split = split_of(a);
+        w.by_r = make_divisor((uint32_t)a.r);
+        w.by_split = make_divisor(w.split);
+        w.blocks = (uint32_t)((a.K + columns - 1) / columns);
+        w.grid = grid_of(w.blocks + (uint32_t)((a.N + columns - 1) / columns), (uint32_t)a.n * w.split);
         if (w.split > 1) w.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + h_bytes(a, a.N));
         with_types(a, [&](auto dt, auto rt) {
-            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(w.blocks[0] + w.blocks[1], (uint32_t)a.n, (uint32_t)(RT < 2 ? 1 : RT / 2) * w.split),
-                               dim3(64 * kWeightWaves), 0, stream, w);
+            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(8 * w.grid.per_xcd), dim3(64 * kWeightWaves), 0, stream, w);
             if (w.split > 1) {
                 const int64_t all = (int64_t)a.n * a.r * (a.K + a.N);
-                hipLaunchKernelGGL((add_parts_kernel<dt.value>), dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, stream, w, (uint32_t)a.n);
+                hipLaunchKernelGGL((add_parts_kernel<dt.value>), dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, stream, w);
             }
         });
     }
