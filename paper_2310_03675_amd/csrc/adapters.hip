@@ -209,21 +209,27 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
     const uint32_t groups = (uint32_t)n + 2;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t rows = (M + 64 * kPlanWaves - 1) / (64 * kPlanWaves) * 64, first = wave * rows, end = first + rows < M ? first + rows : M;
-    for (uint32_t i = threadIdx.x; i < kPlanWaves * kMostGroups; i += kPlanThreads) (&counts[0][0])[i] = 0;
-    __syncthreads();
-    // f(a row, its group, lanes with the same) for a wave's rows, 64 at a time, kAhead of those loaded before the first is taken
+    // f(a row, its group, lanes with the same) for a wave's rows, 64 at a time, kAhead of those loaded before the first is taken; where
+    // that is all of them, they are loaded once
     constexpr int kAhead = 8;
+    int64_t id[kAhead];
+    auto load = [&](int64_t i) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t at = i + 64 * u + lane;
+            id[u] = at < end ? ids[at] : 0;
+        }
+    };
+    if (first < end) load(first);
+    for (uint32_t i = lane; i < groups; i += 64) counts[wave][i] = 0;
+    __syncthreads();
     auto each = [&](auto f) {
         for (int64_t i = first; i < end; i += 64 * kAhead) {
-            int64_t id[kAhead];
+            if (rows > 64 * kAhead) load(i);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int64_t at = i + 64 * u + lane;
-                id[u] = ids[at < end ? at : end - 1];
-            }
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int64_t at = i + 64 * u + lane;
+                if (i + 64 * u >= end) break;
                 const bool there = at < end;
                 const uint32_t g = group_of(id[u], n);
                 f(at, g, there, same_lanes(g, bits, __ballot(there)));
@@ -387,9 +393,9 @@ struct DownArgs {
 // SHORT: the contraction is shorter than a chunk, and loaded element by element.  Else its last chunk, where it is no whole number of
 // them, begins a chunk before the end, and what it has of the one before is taken for zeros.
 template <int DT, int RT, int MODE, bool SHORT>
-__global__ __launch_bounds__(64 * kDownWaves) void down_kernel(DownArgs a)
+__global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
 {
-    constexpr int L = lane_of<DT>(), kChunk = 4 * L, RL = RT < L ? RT : L, RQ = RT / RL, kAhead = RT <= 4 ? 4 : 2;
+    constexpr int L = lane_of<DT>(), kChunk = 4 * L, RL = RT < L ? RT : L, RQ = RT / RL, kAhead = RT < 4 ? 4 : 2;
     __shared__ v4f sums[kDownWaves / 2][kSubs][RT][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     uint32_t tile, part;
@@ -415,13 +421,13 @@ __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(DownArgs a)
             line[s] = (int64_t)rows.row(p < rows.count ? p : place) * a.D;
         }
         v4f acc[kSubs][RT] = {};
-        // N chunks, one of every wave's after the other; `skip` elements of each line of the one are not its
+        // N chunks side by side (four are 256 bytes of a row: whole lines of memory); `skip` elements of each line of the one are not its
         auto chunks = [&](int64_t from, auto number, int skip) {
             constexpr int N = number.value, LINES = MODE == kDown ? L : RL;
             Piece x[N][kSubs], w[N][RQ * LINES];
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int64_t k = from + (int64_t)u * kDownWaves * kChunk + L * g;
+                const int64_t k = from + u * kChunk + L * g;
                 const int n = SHORT ? (int)(a.D - k) : L;
                 const int64_t in = SHORT && n <= 0 ? 0 : k;
 #pragma unroll
@@ -464,10 +470,10 @@ __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(DownArgs a)
         };
         using std::integral_constant;
         const int64_t full = SHORT ? last : a.D / kChunk < last ? a.D / kChunk : last;
-        int64_t c = first + wave;
+        int64_t c = first;
         if (!SHORT)
-            for (; c + (kAhead - 1) * kDownWaves < full; c += kAhead * kDownWaves) chunks(c * kChunk, integral_constant<int, kAhead>{}, 0);
-        for (; c < last; c += kDownWaves) {
+            for (; c + kDownWaves * kAhead <= full; c += kDownWaves * kAhead) chunks((c + wave * kAhead) * kChunk, integral_constant<int, kAhead>{}, 0);
+        for (c += wave; c < last; c += kDownWaves) {
             const bool cut = c >= full;
             chunks(cut ? a.D - kChunk : c * kChunk, integral_constant<int, 1>{}, cut ? (int)(c * kChunk - (a.D - kChunk)) : 0);
         }
@@ -523,21 +529,30 @@ struct UpArgs {
     uint32_t parts;
 };
 
-// a row's values from `rank` on, all parts together, times `scale`
+// a row's values, all parts together, times `scale`
 template <int N>
 __device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t parts, float scale, float (&v)[N])
 {
+    auto add = [&](uint32_t s) {
+        float4 q[N / 4];
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) q[j] = reinterpret_cast<const float4*>(h + s * part)[j];
+#pragma unroll
+        for (int j = 0; j < N / 4; ++j) {
+            v[4 * j] += q[j].x;
+            v[4 * j + 1] += q[j].y;
+            v[4 * j + 2] += q[j].z;
+            v[4 * j + 3] += q[j].w;
+        }
+    };
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] = 0.0f;
-    for (uint32_t s = 0; s < parts; ++s)
+    uint32_t s = 0;
+    for (; s + 4 <= parts; s += 4) {
 #pragma unroll
-        for (int j = 0; j < N; j += 4) {
-            const float4 q = *reinterpret_cast<const float4*>(h + s * part + j);
-            v[j] += q.x;
-            v[j + 1] += q.y;
-            v[j + 2] += q.z;
-            v[j + 3] += q.w;
-        }
+        for (int u = 0; u < 4; ++u) add(s + u);
+    }
+    for (; s < parts; ++s) add(s);
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] *= scale;
 }
@@ -591,7 +606,18 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
             const int64_t from = SHORT || c0 + kColumns <= a.N ? c0 : a.N - kColumns;
             const int lo = (int)(c0 - from) - L * j, hi = SHORT ? (int)(a.N - c0) - L * j : L;
             const int64_t col = SHORT && hi <= 0 ? c0 : from + L * j;
-            Piece w[C][L];
+            int64_t line[kSubs][4];
+            Piece base[kSubs][4], w[C][L];
+#pragma unroll
+            for (int s = 0; s < kSubs; ++s) {
+                const uint4 row = *reinterpret_cast<const uint4*>(lines + 16 * s + 4 * g);
+                const uint32_t of[4] = {row.x, row.y, row.z, row.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) line[s][i] = of[i] * a.N + col;
+                if (a.base)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) base[s][i] = load_piece<DT, !SHORT>(a.base, line[s][i], hi);
+            }
             if (!none && !wrong)
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
@@ -616,16 +642,12 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
                         for (int e = 0; e < L; ++e) w[c][e] = t[e];
                     }
                 }
-#pragma unroll 1
+#pragma unroll
             for (int s = 0; s < kSubs; ++s) {
+                // (one block of rows after the other: the sums of one are in registers)
+                __builtin_amdgcn_sched_barrier(0);
                 const uint32_t at = place + 16 * s + 4 * g;
                 if (place + 16 * s >= rows.count) break;
-                const uint4 row = *reinterpret_cast<const uint4*>(lines + 16 * s + 4 * g);
-                const int64_t line[4] = {row.x * a.N + col, row.y * a.N + col, row.z * a.N + col, row.w * a.N + col};
-                Piece base[4];
-                if (a.base)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) base[i] = load_piece<DT, !SHORT>(a.base, line[i], hi);
                 v4f acc[L] = {};
                 if (!none && !wrong)
 #pragma unroll
@@ -642,9 +664,9 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
 #pragma unroll
                     for (int t = 0; t < L; ++t) {
                         v[t] = wrong ? __builtin_nanf("") : acc[t][i];
-                        if (a.base) v[t] += value<DT>(base[i], t);
+                        if (a.base) v[t] += value<DT>(base[s][i], t);
                     }
-                    if (at + i < rows.count && hi > 0) store_piece<DT>(a.out, line[i], lo, hi, piece_of<DT>(v));
+                    if (at + i < rows.count && hi > 0) store_piece<DT>(a.out, line[s][i], lo, hi, piece_of<DT>(v));
                 }
             }
         }
@@ -665,7 +687,7 @@ struct WeightArgs {
     int64_t N[2];
     int r;
     uint32_t parts[2], blocks, split;           // blocks: of dA's columns
-    Divisor by_r, by_split;
+    Divisor by_split;
     // elements of a part's sums, and of those dA's
     __device__ __forceinline__ int64_t of_a_part() const { return (int64_t)rows.n * r * (N[0] + N[1]); }
     __device__ __forceinline__ int64_t of_dA() const { return (int64_t)rows.n * r * N[0]; }
@@ -677,9 +699,8 @@ template <int DT, int RT>
 __global__ __launch_bounds__(64 * kWeightWaves) void weights_kernel(WeightArgs a)
 {
     constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L, RW = RT < 2 ? RT : 2, P = planes_of<DT>();
-    constexpr int kShares = kWeightWaves / (RT / RW), kAcross = kColumns + 4;
-    // dB: [rank][column]; dA: [column][rank]; rows of one more than they hold, for the banks
-    __shared__ float tile[kAcross * (16 * RT + 1)];
+    constexpr int kShares = kWeightWaves / (RT / RW);
+    __shared__ v4f sums[kWeightWaves / 2][RW][L][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     uint32_t block, which;
     if (!place_of(a.grid, block, which)) return;
@@ -690,28 +711,43 @@ __global__ __launch_bounds__(64 * kWeightWaves) void weights_kernel(WeightArgs a
     const int rank0 = wave / kShares * (16 * RW), share = wave % kShares;
     const Group rows = adapter_rows(a.rows, adapter);
     const float* h = a.h[of] + rank0 + j;
-    const int n = col + L <= N ? L : col < N ? (int)(N - col) : 0, there = N - c0 < kColumns ? (int)(N - c0) : kColumns;
+    const int n = col + L <= N ? L : col < N ? (int)(N - col) : 0;
     v4f acc[RW][L] = {};
     auto sum = [&](auto whole) {
         constexpr bool WHOLE = whole.value;
         // (as often for every lane of a wave: the rows of a few are handed from lane to lane)
         const uint32_t step = kChunk * kShares * a.split;
-        for (uint32_t first = kChunk * (part * kShares + share); first < rows.count; first += step) {
+        uint32_t next[L];
+        auto look = [&](uint32_t first) {
+#pragma unroll
+            for (int e = 0; e < L; ++e) {
+                const uint32_t p = first + L * g + e;
+                next[e] = rows.row(p < rows.count ? p : first);            // (behind the last: one that there is, taken for zeros)
+            }
+        };
+        uint32_t first = kChunk * (part * kShares + share);
+        if (first < rows.count) look(first);
+        for (; first < rows.count; first += step) {
             Piece lines[L];
             float u[RW][L];
 #pragma unroll
             for (int e = 0; e < L; ++e) {
-                const uint32_t p = first + L * g + e;
-                const bool has = p < rows.count;           // (the others: a row that there is, taken for zeros)
-                const int64_t row = rows.row(has ? p : first);
+                const int64_t row = next[e];
                 lines[e] = load_piece<DT, WHOLE>(a.v[of], row * N + (WHOLE || n > 0 ? col : 0), n);
-                lines[e] = only_if(has, lines[e]);
 #pragma unroll
                 for (int t = 0; t < RW; ++t) {
                     u[t][e] = h[row * (16 * RT) + 16 * t];
                     for (uint32_t s = 1; s < a.parts[of]; ++s) u[t][e] += h[(s * a.rows.M + row) * (16 * RT) + 16 * t];
-                    u[t][e] = has ? u[t][e] : 0.0f;
                 }
+            }
+            const uint32_t ahead = first + step;
+            if (ahead < rows.count) look(ahead);
+#pragma unroll
+            for (int e = 0; e < L; ++e) {
+                const bool has = first + L * g + e < rows.count;
+                lines[e] = only_if(has, lines[e]);
+#pragma unroll
+                for (int t = 0; t < RW; ++t) u[t][e] = has ? u[t][e] : 0.0f;
             }
             Piece up[RW][P];
 #pragma unroll
@@ -728,45 +764,70 @@ __global__ __launch_bounds__(64 * kWeightWaves) void weights_kernel(WeightArgs a
     };
     if (c0 + kColumns <= N) sum(std::true_type{});
     else sum(std::false_type{});
-    const float scale = a.scale ? a.scale[adapter] : 1.0f;
-    // the shares one after the other; a lane has ranks rank0 + 16 t + 4 g + i of columns col + c
-    const int line = a.r | 1;
+    // the waves with the same ranks together, as far as there were rows for them
+    const uint32_t begun = part * kShares * kChunk;
 #pragma unroll
-    for (int s = 0; s < kShares; ++s) {
-        if (share == s)
+    for (int half = kShares / 2; half; half /= 2) {
+        if (rows.count <= begun + half * kChunk) continue;
+        __syncthreads();
+        if (share >= half && share < 2 * half)
 #pragma unroll
             for (int t = 0; t < RW; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int rank = rank0 + 16 * t + 4 * g + i;
-                    if (rank >= a.r) continue;
-#pragma unroll
-                    for (int c = 0; c < L; ++c) {
-                        float* to = tile + (of ? rank * kAcross + L * j + c : (L * j + c) * line + rank);
-                        *to = s ? *to + acc[t][c][i] : acc[t][c][i];
-                    }
-                }
+                for (int c = 0; c < L; ++c) sums[(rank0 / (16 * RW)) * (kShares / 2) + share - half][t][c][lane] = acc[t][c];
         __syncthreads();
+        if (share < half)
+#pragma unroll
+            for (int t = 0; t < RW; ++t)
+#pragma unroll
+                for (int c = 0; c < L; ++c) acc[t][c] += sums[(rank0 / (16 * RW)) * (kShares / 2) + share][t][c][lane];
     }
-    // dA's part is one run of memory, dB's one of every rank
-    const int64_t to = of ? (int64_t)adapter * a.r * N + c0 : ((int64_t)adapter * N + c0) * a.r;
-    float* sums = a.sums ? a.sums + (int64_t)part * a.of_a_part() + (of ? a.of_dA() : 0) : nullptr;
-    const int runs = of ? a.r : 1, length = of ? there : there * a.r, pieces = (length + L - 1) / L;
-    for (int i = threadIdx.x; i < runs * pieces; i += 64 * kWeightWaves) {
-        const int run = of ? i / pieces : 0, e0 = (i - run * pieces) * L, left = length - e0 < L ? length - e0 : L;
-        float v[L];
+    if (share || n <= 0) return;
+    const float scale = a.scale ? a.scale[adapter] : 1.0f;
+    float* parts = a.sums ? a.sums + (int64_t)part * a.of_a_part() + (of ? a.of_dA() : 0) : nullptr;
+    // a lane has ranks rank0 + 16 t + 4 g + i of columns col + c: of a rank's run in dB kLane elements, of a column's in dA four
+    if (of) {
 #pragma unroll
-        for (int e = 0; e < L; ++e) {
-            const int in = e < left ? e0 + e : e0, c = of ? in : (int)divide((uint32_t)in, a.by_r);
-            v[e] = scale * (of ? tile[run * kAcross + in] : tile[c * line + in - c * a.r]);
-        }
-        const int64_t dest = to + (int64_t)run * N + e0;
-        if (sums) {
+        for (int t = 0; t < RW; ++t)
 #pragma unroll
-            for (int e = 0; e < L; ++e)
-                if (e < left) sums[dest + e] = v[e];
-        } else {
-            store_piece<DT>(a.out[of], dest, 0, left, piece_of<DT>(v));
+            for (int i = 0; i < 4; ++i) {
+                const int rank = rank0 + 16 * t + 4 * g + i;
+                if (rank >= a.r) continue;
+                const int64_t to = ((int64_t)adapter * a.r + rank) * N + col;
+                float v[L];
+#pragma unroll
+                for (int c = 0; c < L; ++c) v[c] = scale * acc[t][c][i];
+                if (parts) {
+#pragma unroll
+                    for (int c = 0; c < L; ++c)
+                        if (c < n) parts[to + c] = v[c];
+                } else {
+                    store_piece<DT>(a.out[1], to, 0, n, piece_of<DT>(v));
+                }
+            }
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < L; ++c) {
+        if (c >= n) continue;
+#pragma unroll
+        for (int t = 0; t < RW; ++t) {
+            const int rank = rank0 + 16 * t + 4 * g, left = a.r - rank < 4 ? a.r - rank : 4;
+            const int64_t to = ((int64_t)adapter * N + col + c) * a.r + rank;
+            const v4f v = scale * acc[t][c];
+            if (left == 4 && !parts && DT == kBf16) {
+                const uint32_t two[2] = {to_bf16(v[0]) | to_bf16(v[1]) << 16, to_bf16(v[2]) | to_bf16(v[3]) << 16};
+                __builtin_memcpy(static_cast<uint16_t*>(a.out[0]) + to, two, 8);
+            } else if (left == 4) {
+                __builtin_memcpy((parts ? parts : static_cast<float*>(a.out[0])) + to, &v, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (i < left) {
+                        if (parts) parts[to + i] = v[i];
+                        else store_as<DT>(a.out[0], to + i, v[i]);
+                    }
+            }
         }
     }
 }
@@ -918,7 +979,6 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
         w.r = a.r;
         w.parts[0] = parts_of(a, a.N).parts; w.parts[1] = parts_of(a, a.K).parts;
         w.split = split_of(a);
-        w.by_r = make_divisor((uint32_t)a.r);
         w.by_split = make_divisor(w.split);
         w.blocks = (uint32_t)((a.K + columns - 1) / columns);
         w.grid = grid_of(w.blocks + (uint32_t)((a.N + columns - 1) / columns), (uint32_t)a.n * w.split);
