@@ -1169,6 +1169,10 @@ def dropout(x: torch.Tensor, d: Dropout, residual: Optional[torch.Tensor] = None
             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """hdqt_dropout -> residual + dropout(x), or dropout(x): x fp32 or bfloat16, contiguous, of any shape.  The gradient of x is
     dropout(dy, d) with the same d.  out may be x or residual."""
+    if stream is None:
+        r = _native(_host.dropout(x, d, residual, out), "hdqt_dropout")
+        if r is not None:
+            return r
     if not x.is_cuda or not x.is_contiguous():
         raise ValueError("x must be a contiguous device tensor")
     if x.numel() == 0:
@@ -1206,6 +1210,10 @@ def layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: 
     """hdqt_layernorm_fwd -> (y, sum, saved fp32 [..., 2]): the rows of x [..., columns] (fp32 or bfloat16), or of
     sum = residual + dropout(x), normalised.  Without residual and dropout sum is x itself.  need: whether sum and saved, which the
     backward pass takes, are wanted (None in their place).  out may be x, out_sum x or residual."""
+    if out is None and out_sum is None and stream is None:
+        r = _native(_host.layernorm_fwd(x, weight, bias, eps, residual, dropout, need), "hdqt_layernorm_fwd")
+        if r is not None:
+            return r
     M, C_, pdt = _layer_sizes(x, weight, bias)
     if residual is not None:
         _check_out("residual", residual, x.shape, x.dtype, x.device)
@@ -1232,6 +1240,10 @@ def layernorm_bwd(dy: torch.Tensor, s: torch.Tensor, saved: torch.Tensor, weight
     """hdqt_layernorm_bwd -> (dx, dresidual, dweight, dbias), those that `need` asks for.  s and saved: of layernorm_fwd (its sum);
     dsum: the gradient that reaches the sum past the normalisation.  Without dropout dx and dresidual are one tensor.  dweight
     and dbias are of the weight's type (fp32 without)."""
+    if workspace is None and stream is None:
+        r = _native(_host.layernorm_bwd(dy, s, saved, weight, dsum, dropout, need), "hdqt_layernorm_bwd")
+        if r is not None:
+            return r
     M, C_, pdt = _layer_sizes(s, weight, None)
     _check_dev(workspace)
     _check_out("dy", dy, s.shape, s.dtype, s.device)
@@ -1274,6 +1286,10 @@ def adapters_fwd(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, ids: torch.T
                  stream: Optional[torch.cuda.Stream] = None):
     """hdqt_adapters_fwd -> (out [M, N], saved): out_i = base_i + scale_a x_i A_a B_a with a = ids[i], none where that is negative.
     x [M, K], A [n, K, r], B [n, r, N] (fp32 or bfloat16), ids int64 [M], scale fp32 [n].  out may be base."""
+    if stream is None:
+        got = _native(_host.adapters_fwd(x, A, B, ids, scale, base, out), "hdqt_adapters_fwd")
+        if got is not None:
+            return got
     sizes = M, K, N, r, n = _adapter_sizes(x, A, B, ids, scale)
     if base is not None:
         _check_out("base", base, (M, N), x.dtype, x.device)
@@ -1295,8 +1311,13 @@ def adapters_bwd(dy: torch.Tensor, x: torch.Tensor, A: torch.Tensor, B: torch.Te
                  stream: Optional[torch.cuda.Stream] = None):
     """hdqt_adapters_bwd -> (dx, dA, dB), those that `need` asks for.  saved: of adapters_fwd with the same x, A and ids; base: the
     gradient of x by the shared projection, which dx is added to; out, for dx, may be base."""
+    if out is None and workspace is None and stream is None:
+        got = _native(_host.adapters_bwd(x, A, B, ids, scale, dy, saved, base, need), "hdqt_adapters_bwd")
+        if got is not None:
+            return got
     sizes = M, K, N, r, n = _adapter_sizes(x, A, B, ids, scale)
-    _check_dev(saved, workspace)
+    _check_dev(workspace)
+    _check_out("saved", saved, saved.shape, torch.uint8, x.device)
     _check_out("dy", dy, (M, N), x.dtype, x.device)
     if base is not None:
         _check_out("base", base, (M, K), x.dtype, x.device)

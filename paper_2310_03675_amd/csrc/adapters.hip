@@ -17,7 +17,7 @@
 //
 // bfloat16: h, g and their sums are held in 32 bits.  Where they are multiplied again each is taken as two bfloat16 values, the first
 // cut off and the second rounded: off by 2^-16 of itself at most.  fp32: products in 32 bits.
-#include "train.hpp"
+#include "dropout.hpp"
 
 #include <type_traits>
 
@@ -29,7 +29,8 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int kSubs = 2, kTile = 16 * kSubs;        // rows of a tile, in blocks of the matrix instruction
-constexpr int kDownWaves = 8, kUpWaves = 4, kWeightWaves = 4;
+constexpr int kDownWaves = 8, kUpWaves = 4;
+constexpr int weight_waves(int RT) { return RT < 4 ? 4 : RT; }
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kMostGroups = kAdaptersMost + 2;
 
 enum Mode { kAlong, kDown };        // memory runs along the contraction, or across it
@@ -111,7 +112,7 @@ __device__ __forceinline__ Piece piece_of(const float (&v)[lane_of<DT>()])
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         if constexpr (DT == kF32) q.w[j] = __float_as_uint(v[j]);
-        else q.w[j] = to_bf16(v[2 * j]) | to_bf16(v[2 * j + 1]) << 16;
+        else q.w[j] = two_bf16(v[2 * j], v[2 * j + 1]);
     }
     return q;
 }
@@ -155,17 +156,16 @@ __device__ __forceinline__ void split(const float (&v)[lane_of<DT>()], Piece (&t
 #pragma unroll
         for (int j = 0; j < 4; ++j) to[0].w[j] = __float_as_uint(v[j]);
     } else {
-        uint32_t first[8], second[8];
+        float rest[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            first[j] = __float_as_uint(v[j]) >> 16;
-            const float cut = from_bf16(first[j]);
-            second[j] = v[j] == cut ? 0u : to_bf16(v[j] - cut);         // (equal: an infinity has no rest)
+            const float cut = __uint_as_float(__float_as_uint(v[j]) & 0xFFFF0000u);
+            rest[j] = v[j] == cut ? 0.0f : v[j] - cut;                  // (equal: an infinity has no rest)
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            to[0].w[j] = first[2 * j] | first[2 * j + 1] << 16;
-            to[1].w[j] = second[2 * j] | second[2 * j + 1] << 16;
+            to[0].w[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]), 0x07060302u);
+            to[1].w[j] = two_bf16(rest[2 * j], rest[2 * j + 1]);
         }
     }
 }
@@ -471,8 +471,17 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
         using std::integral_constant;
         const int64_t full = SHORT ? last : a.D / kChunk < last ? a.D / kChunk : last;
         int64_t c = first;
-        if (!SHORT)
-            for (; c + kDownWaves * kAhead <= full; c += kDownWaves * kAhead) chunks((c + wave * kAhead) * kChunk, integral_constant<int, kAhead>{}, 0);
+        if (!SHORT && full > first) {
+            // (tiles begin at different places, so that they do not all ask the same channels of the memory: rows are often a power of
+            // two apart)
+            const uint32_t turns = (uint32_t)(full - first) / (kDownWaves * kAhead);
+            uint32_t turn = turns ? (tile * 5) % turns : 0;
+            for (uint32_t i = 0; i < turns; ++i) {
+                chunks((first + (turn * kDownWaves + wave) * kAhead) * kChunk, integral_constant<int, kAhead>{}, 0);
+                if (++turn == turns) turn = 0;
+            }
+            c += (int64_t)turns * kDownWaves * kAhead;
+        }
         for (c += wave; c < last; c += kDownWaves) {
             const bool cut = c >= full;
             chunks(cut ? a.D - kChunk : c * kChunk, integral_constant<int, 1>{}, cut ? (int)(c * kChunk - (a.D - kChunk)) : 0);
@@ -517,8 +526,8 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
 
 struct UpArgs {
     RowArgs rows;
-    Grid grid;                      // tiles, and workgroups over the columns
-    uint32_t across;                // of those
+    Grid grid;                      // workgroups over the columns, tiles
+    uint32_t across;                // of the former
     const float* h;                 // [parts][M][16 RT]
     const float* scale;             // [n] or null
     const void* W;                  // of an adapter [r, N] (kDown) or [N, r] (kAlong)
@@ -571,7 +580,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
     __shared__ __attribute__((aligned(16))) uint32_t lines[kTile];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     uint32_t tile, over;
-    if (!place_of(a.grid, tile, over)) return;
+    if (!place_of(a.grid, over, tile)) return;
     const Group rows = tile_rows(a.rows, tile);
     if (!rows.count) return;
     const bool none = rows.group == (uint32_t)a.rows.n, wrong = rows.group > (uint32_t)a.rows.n;
@@ -696,11 +705,11 @@ struct WeightArgs {
 // A workgroup has 128 columns (64 in fp32) and all ranks of one gradient: a wave two tiles of ranks at most, and of the rows what the
 // waves with the same ranks share.
 template <int DT, int RT>
-__global__ __launch_bounds__(64 * kWeightWaves) void weights_kernel(WeightArgs a)
+__global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightArgs a)
 {
-    constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L, RW = RT < 2 ? RT : 2, P = planes_of<DT>();
-    constexpr int kShares = kWeightWaves / (RT / RW);
-    __shared__ v4f sums[kWeightWaves / 2][RW][L][64];
+    constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L, P = planes_of<DT>(), RW = 1;
+    constexpr int kWaves = weight_waves(RT), kShares = kWaves / RT;
+    __shared__ v4f sums[kShares > 1 ? kWaves / 2 : 1][RW][L][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     uint32_t block, which;
     if (!place_of(a.grid, block, which)) return;
@@ -816,7 +825,7 @@ __global__ __launch_bounds__(64 * kWeightWaves) void weights_kernel(WeightArgs a
             const int64_t to = ((int64_t)adapter * N + col + c) * a.r + rank;
             const v4f v = scale * acc[t][c];
             if (left == 4 && !parts && DT == kBf16) {
-                const uint32_t two[2] = {to_bf16(v[0]) | to_bf16(v[1]) << 16, to_bf16(v[2]) | to_bf16(v[3]) << 16};
+                const uint32_t two[2] = {two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
                 __builtin_memcpy(static_cast<uint16_t*>(a.out[0]) + to, two, 8);
             } else if (left == 4) {
                 __builtin_memcpy((parts ? parts : static_cast<float*>(a.out[0])) + to, &v, 16);
@@ -930,7 +939,7 @@ void launch_up(const AdapterArgs& a, const float* h, const void* W, const void* 
     ProfileScope ps(K_ADAPT_UP, stream);
     const int64_t columns = (a.dtype == kBf16 ? 128 : 64) * kUpWaves, most = (N + columns - 1) / columns, want = 2048 / grid_tiles(a) + 1;
     const uint32_t across = (uint32_t)(most < want ? most : want);
-    const UpArgs u{rows, grid_of(grid_tiles(a), across), across, h, a.scale, W, base, out, N, a.r, parts_of(a, D).parts};
+    const UpArgs u{rows, grid_of(across, grid_tiles(a)), across, h, a.scale, W, base, out, N, a.r, parts_of(a, D).parts};
     with_types(a, [&](auto dt, auto rt) {
         const dim3 grid(8 * u.grid.per_xcd), block(64 * kUpWaves);
         constexpr int L = lane_of<dt.value>();
@@ -984,7 +993,7 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
         w.grid = grid_of(w.blocks + (uint32_t)((a.N + columns - 1) / columns), (uint32_t)a.n * w.split);
         if (w.split > 1) w.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + h_bytes(a, a.N));
         with_types(a, [&](auto dt, auto rt) {
-            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(8 * w.grid.per_xcd), dim3(64 * kWeightWaves), 0, stream, w);
+            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(8 * w.grid.per_xcd), dim3(64 * weight_waves(rt.value)), 0, stream, w);
             if (w.split > 1) {
                 const int64_t all = (int64_t)a.n * a.r * (a.K + a.N);
                 hipLaunchKernelGGL((add_parts_kernel<dt.value>), dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, stream, w);

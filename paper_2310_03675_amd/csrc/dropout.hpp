@@ -12,6 +12,14 @@
 
 namespace hdqt {
 
+// Two values as bfloat16, rounded to nearest even, in one instruction of this chip (a NaN stays one).
+__device__ __forceinline__ uint32_t two_bf16(float a, float b)
+{
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{a, b}), v2b));
+}
+
 // Eight neighbouring elements, wherever they start.
 template <int DT>
 struct Eight {
@@ -25,7 +33,7 @@ struct Eight {
     __device__ __forceinline__ void set(const float (&v)[8])
     {
 #pragma unroll
-        for (int j = 0; j < kWords; ++j) w[j] = DT == kF32 ? __float_as_uint(v[j]) : to_bf16(v[2 * j % 8]) | to_bf16(v[(2 * j + 1) % 8]) << 16;
+        for (int j = 0; j < kWords; ++j) w[j] = DT == kF32 ? __float_as_uint(v[j]) : two_bf16(v[2 * j % 8], v[(2 * j + 1) % 8]);
     }
     // The compiler takes the values for new ones: what it made of them before is not kept in registers, twice as wide, but made again.
     __device__ __forceinline__ void renew()

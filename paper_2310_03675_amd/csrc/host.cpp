@@ -53,11 +53,19 @@ struct Library {
     decltype(&hdqt_clip_grad_norm_workspace_size) clip_workspace_size;
     decltype(&hdqt_grad_norm) grad_norm;
     decltype(&hdqt_clip_grad_norm) clip;
+    decltype(&hdqt_dropout) dropout;
+    decltype(&hdqt_layernorm_fwd) layernorm_fwd;
+    decltype(&hdqt_layernorm_bwd_workspace_size) layernorm_workspace_size;
+    decltype(&hdqt_layernorm_bwd) layernorm_bwd;
+    decltype(&hdqt_adapters_saved_size) adapters_saved_size;
+    decltype(&hdqt_adapters_bwd_workspace_size) adapters_workspace_size;
+    decltype(&hdqt_adapters_fwd) adapters_fwd;
+    decltype(&hdqt_adapters_bwd) adapters_bwd;
 } lib;
 PyObject *get_device, *get_stream;           // torch's: the current device, its current stream's handle
 
 struct Names {
-    PyObject *had_block, *acc_bits, *s, *seed, *A, *B, *b, *round, *clip, *tensor_id, *cuda_stream;
+    PyObject *had_block, *acc_bits, *s, *seed, *A, *B, *b, *round, *clip, *tensor_id, *cuda_stream, *p, *step;
 } names;
 
 // Not the ordinary form of a call.
@@ -432,19 +440,21 @@ const at::Tensor& like(PyObject* o, at::ScalarType type, at::IntArrayRef shape, 
     return t;
 }
 
-// which of three results are asked for
-struct Need {
-    bool k[3];
-    explicit Need(PyObject* o)
+// which of N results are asked for
+template <int N>
+struct NeedOf {
+    bool k[N];
+    explicit NeedOf(PyObject* o)
     {
-        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) throw Other();
-        for (int i = 0; i < 3; ++i) {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != N) throw Other();
+        for (int i = 0; i < N; ++i) {
             PyObject* b = PyTuple_GET_ITEM(o, i);
             if (!PyBool_Check(b)) throw Other();
             k[i] = b == Py_True;
         }
     }
 };
+using Need = NeedOf<3>;
 
 double number(PyObject* o)
 {
@@ -657,6 +667,181 @@ PyObject* clip_grad_norm(PyObject* const* a)
     return norm_of(Gradients(a[0], a[1]), integer(a[4]), true, (float)number(a[2]), (float)number(a[3]));
 }
 
+// ---- a residual block: dropout, layer normalisation, low-rank adapters ----
+
+// a binding.Dropout, or None
+struct Dropped {
+    hdqt_dropout_t value{};
+    const hdqt_dropout_t* d = nullptr;
+    Dropped(PyObject* o, const at::Tensor& beside)
+    {
+        if (o == Py_None) return;
+        const Member p(o, names.p), step(o, names.step);
+        value.p = number(p.o);
+        value.seed = bits_of(o, names.seed);
+        value.tensor_id = (uint32_t)bits_of(o, names.tensor_id);
+        if (step.o != Py_None) {
+            const at::Tensor& t = tensor(step.o, at::kLong);
+            if (t.numel() != 1 || t.device() != beside.device()) throw Other();
+            value.step = (const int64_t*)address(t);
+        }
+        d = &value;
+    }
+};
+
+const at::Tensor* maybe_like(PyObject* o, const at::Tensor& x) { return o == Py_None ? nullptr : &like(o, x.scalar_type(), x.sizes(), x); }
+
+// dropout(x, d, residual | None, out | None) -> y
+PyObject* dropout(PyObject* const* a)
+{
+    const at::Tensor& x = on_device(a[0]);
+    const int dtype = type_of(x);
+    if (!x.is_contiguous() || x.numel() == 0) throw Other();
+    const Dropped d(a[1], x);
+    const at::Tensor *residual = maybe_like(a[2], x), *given = maybe_like(a[3], x);
+    void* stream = stream_of(x);
+    at::Tensor y;
+    if (!given) y = fresh(x.sizes(), x.scalar_type(), x);
+    const int rc = unlocked([&] { return lib.dropout(address(x), address(residual), given ? address(given) : address(y), x.numel(), dtype, d.d, stream); });
+    if (rc) return PyLong_FromLong(rc);
+    return (given ? Result(a[3]) : Result(std::move(y))).o;
+}
+
+// x [..., columns], weight | None, bias | None
+struct Layered {
+    const at::Tensor& x;
+    const at::Tensor *weight, *bias;
+    int64_t M, C;
+    int dtype, param_dtype;
+    at::ScalarType param_type;
+    std::vector<int64_t> saved_shape;
+    void* stream;
+    Layered(PyObject* px, PyObject* w, PyObject* b) : x(on_device(px))
+    {
+        dtype = type_of(x);
+        if (x.dim() < 1 || x.numel() == 0 || !x.is_contiguous()) throw Other();
+        C = x.size(-1); M = x.numel() / C;
+        weight = w == Py_None ? nullptr : &on_device(w);
+        bias = b == Py_None ? nullptr : &on_device(b);
+        const at::Tensor* one = weight ? weight : bias;
+        param_dtype = one ? type_of(*one) : HDQT_F32;
+        param_type = one ? one->scalar_type() : at::kFloat;
+        if (param_dtype == HDQT_BF16 && dtype != HDQT_BF16) throw Other();
+        if (weight) like(w, param_type, {C}, x);
+        if (bias) like(b, param_type, {C}, x);
+        saved_shape.assign(x.sizes().begin(), x.sizes().end());
+        saved_shape.back() = 2;
+        stream = stream_of(x);
+    }
+    at::Tensor as_x() const { return fresh(x.sizes(), x.scalar_type(), x); }
+};
+
+void* address_of(const at::Tensor& t) { return t.defined() ? address(t) : nullptr; }
+
+// layernorm_fwd(x, weight, bias, eps, residual, dropout, need) -> (y, sum | None, saved | None)
+PyObject* layernorm_fwd(PyObject* const* a)
+{
+    const Layered n(a[0], a[1], a[2]);
+    const float eps = (float)number(a[3]);
+    const at::Tensor* residual = maybe_like(a[4], n.x);
+    const Dropped d(a[5], n.x);
+    const NeedOf<2> need(a[6]);
+    const bool summed = residual || d.d;
+    at::Tensor y = n.as_x(), sum, saved;
+    if (summed && need.k[0]) sum = n.as_x();
+    if (need.k[1]) saved = fresh(n.saved_shape, at::kFloat, n.x);
+    const int rc = unlocked([&] {
+        return lib.layernorm_fwd(address(n.x), address(residual), d.d, address(n.weight), address(n.bias), address_of(sum), address(y),
+                                 (float*)address_of(saved), n.M, n.C, eps, n.dtype, n.param_dtype, n.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(Result(std::move(y)), summed ? Result(std::move(sum)) : Result(a[0]), Result(std::move(saved)));
+}
+
+// layernorm_bwd(dy, s, saved, weight, dsum, dropout, need) -> (dx, dresidual, dweight, dbias)
+PyObject* layernorm_bwd(PyObject* const* a)
+{
+    const Layered n(a[1], a[3], Py_None);
+    const at::Tensor &dy = like(a[0], n.x.scalar_type(), n.x.sizes(), n.x), &saved = like(a[2], at::kFloat, n.saved_shape, n.x);
+    const at::Tensor* dsum = maybe_like(a[4], n.x);
+    const Dropped d(a[5], n.x);
+    const NeedOf<4> need(a[6]);
+    at::Tensor dx, dres, dw, db, ws;
+    if (need.k[0] || (need.k[1] && !d.d)) dx = n.as_x();
+    if (need.k[1] && d.d) dres = n.as_x();
+    if (need.k[2]) dw = fresh({n.C}, n.param_type, n.x);
+    if (need.k[3]) db = fresh({n.C}, n.param_type, n.x);
+    if (need.k[2] || need.k[3]) ws = bytes(lib.layernorm_workspace_size(n.M, n.C, n.dtype), n.x);
+    const int rc = unlocked([&] {
+        return lib.layernorm_bwd(address(dy), address(dsum), address(n.x), d.d, address(n.weight), (const float*)address(saved), address_of(dx),
+                                 address_of(dres), address_of(dw), address_of(db), n.M, n.C, n.dtype, n.param_dtype, address_of(ws),
+                                 ws.defined() ? (size_t)ws.numel() : 0, n.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    if (!d.d && need.k[1]) dres = dx;
+    if (!need.k[0]) dx = at::Tensor();
+    return tuple(Result(std::move(dx)), Result(std::move(dres)), Result(std::move(dw)), Result(std::move(db)));
+}
+
+// x, A, B, ids, scale | None
+struct Adapted {
+    const at::Tensor &x, &A, &B, &ids;
+    const at::Tensor* scale;
+    int64_t M, K, N;
+    int r, n, dtype;
+    void* stream;
+    explicit Adapted(PyObject* const* a) : x(on_device(a[0])), A(on_device(a[1])), B(on_device(a[2])), ids(on_device(a[3]))
+    {
+        dtype = type_of(x);
+        if (x.dim() != 2 || A.dim() != 3 || B.dim() != 3 || !x.is_contiguous()) throw Other();
+        if (x.numel() == 0 || A.numel() == 0 || B.numel() == 0 || A.size(0) > INT32_MAX || A.size(2) > INT32_MAX) throw Other();
+        M = x.size(0); K = x.size(1); N = B.size(2); n = (int)A.size(0); r = (int)A.size(2);
+        like(a[1], x.scalar_type(), {n, K, r}, x);
+        like(a[2], x.scalar_type(), {n, r, N}, x);
+        like(a[3], at::kLong, {M}, x);
+        scale = a[4] == Py_None ? nullptr : &like(a[4], at::kFloat, {n}, x);
+        stream = stream_of(x);
+    }
+};
+
+// adapters_fwd(x, A, B, ids, scale, base | None, out | None) -> (out, saved)
+PyObject* adapters_fwd(PyObject* const* a)
+{
+    const Adapted p(a);
+    const at::Tensor* base = a[5] == Py_None ? nullptr : &like(a[5], p.x.scalar_type(), {p.M, p.N}, p.x);
+    const at::Tensor* given = a[6] == Py_None ? nullptr : &like(a[6], p.x.scalar_type(), {p.M, p.N}, p.x);
+    at::Tensor out, saved = bytes(lib.adapters_saved_size(p.M, p.K, p.N, p.r, p.n, p.dtype), p.x);
+    if (!given) out = fresh({p.M, p.N}, p.x.scalar_type(), p.x);
+    const int rc = unlocked([&] {
+        return lib.adapters_fwd(address(p.x), address(p.A), address(p.B), (const int64_t*)address(p.ids), (const float*)address(p.scale),
+                                address(base), given ? address(given) : address(out), address(saved), (size_t)saved.numel(), p.M, p.K, p.N, p.r,
+                                p.n, p.dtype, p.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(given ? Result(a[6]) : Result(std::move(out)), Result(std::move(saved)));
+}
+
+// adapters_bwd(x, A, B, ids, scale, dy, saved, base | None, need) -> (dx, dA, dB)
+PyObject* adapters_bwd(PyObject* const* a)
+{
+    const Adapted p(a);
+    const at::Tensor &dy = like(a[5], p.x.scalar_type(), {p.M, p.N}, p.x), &saved = tensor(a[6], at::kByte, 1);
+    if (saved.device() != p.x.device()) throw Other();
+    const at::Tensor* base = maybe_like(a[7], p.x);
+    const Need need(a[8]);
+    at::Tensor dx, dA, dB, ws = bytes(lib.adapters_workspace_size(p.M, p.K, p.N, p.r, p.n, p.dtype), p.x);
+    if (need.k[0]) dx = fresh(p.x.sizes(), p.x.scalar_type(), p.x);
+    if (need.k[1]) dA = fresh(p.A.sizes(), p.x.scalar_type(), p.x);
+    if (need.k[2]) dB = fresh(p.B.sizes(), p.x.scalar_type(), p.x);
+    const int rc = unlocked([&] {
+        return lib.adapters_bwd(address(dy), address(p.x), address(p.A), address(p.B), (const int64_t*)address(p.ids),
+                                (const float*)address(p.scale), address(saved), (size_t)saved.numel(), address(base), address_of(dx), address_of(dA),
+                                address_of(dB), p.M, p.K, p.N, p.r, p.n, p.dtype, address(ws), (size_t)ws.numel(), p.stream);
+    });
+    if (rc) return PyLong_FromLong(rc);
+    return tuple(Result(std::move(dx)), Result(std::move(dA)), Result(std::move(dB)));
+}
+
 // What a function may throw (a call of another form; whatever an allocation or a tensor without
 // memory of its own raises, which the other way raises again) ends here.  So do the interpreter's errors that
 // only say that a member is missing or no number; any other (an interrupt or a time limit's exception out of
@@ -724,6 +909,14 @@ PyObject* bind(PyObject*, PyObject* args)
     find(l.clip_workspace_size, "hdqt_clip_grad_norm_workspace_size");
     find(l.grad_norm, "hdqt_grad_norm");
     find(l.clip, "hdqt_clip_grad_norm");
+    find(l.dropout, "hdqt_dropout");
+    find(l.layernorm_fwd, "hdqt_layernorm_fwd");
+    find(l.layernorm_workspace_size, "hdqt_layernorm_bwd_workspace_size");
+    find(l.layernorm_bwd, "hdqt_layernorm_bwd");
+    find(l.adapters_saved_size, "hdqt_adapters_saved_size");
+    find(l.adapters_workspace_size, "hdqt_adapters_bwd_workspace_size");
+    find(l.adapters_fwd, "hdqt_adapters_fwd");
+    find(l.adapters_bwd, "hdqt_adapters_bwd");
     if (!all) return PyErr_Format(PyExc_ImportError, "%s lacks functions of include/hdqt.h", path);
     Py_INCREF(device);
     Py_INCREF(stream);
@@ -739,7 +932,8 @@ PyMethodDef methods[] = {
     HDQT_ENTRY(quantize, 6), HDQT_ENTRY(gemm, 14), HDQT_ENTRY(layer_step, 9), HDQT_ENTRY(layer_fwd, 8),
     HDQT_ENTRY(layer_bwd, 10), HDQT_ENTRY(conv_fwd, 7), HDQT_ENTRY(conv_bwd, 10), HDQT_ENTRY(xent_fwd, 6), HDQT_ENTRY(xent_step, 7),
     HDQT_ENTRY(xent_bwd, 9), HDQT_ENTRY(groupnorm_fwd, 6), HDQT_ENTRY(groupnorm_bwd, 8), HDQT_ENTRY(grad_norm, 2),
-    HDQT_ENTRY(clip_grad_norm, 5),
+    HDQT_ENTRY(clip_grad_norm, 5), HDQT_ENTRY(dropout, 4), HDQT_ENTRY(layernorm_fwd, 7), HDQT_ENTRY(layernorm_bwd, 7),
+    HDQT_ENTRY(adapters_fwd, 7), HDQT_ENTRY(adapters_bwd, 9),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -749,7 +943,7 @@ PyMODINIT_FUNC PyInit__host()
 {
 #define HDQT_NAME(x) names.x = PyUnicode_InternFromString(#x)
     HDQT_NAME(had_block); HDQT_NAME(acc_bits); HDQT_NAME(s); HDQT_NAME(seed); HDQT_NAME(A); HDQT_NAME(B);
-    HDQT_NAME(b); HDQT_NAME(round); HDQT_NAME(clip); HDQT_NAME(tensor_id); HDQT_NAME(cuda_stream);
+    HDQT_NAME(b); HDQT_NAME(round); HDQT_NAME(clip); HDQT_NAME(tensor_id); HDQT_NAME(cuda_stream); HDQT_NAME(p); HDQT_NAME(step);
 #undef HDQT_NAME
     return PyModule_Create(&module);
 }
