@@ -29,7 +29,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int kSubs = 2, kTile = 16 * kSubs;        // rows of a tile, in blocks of the matrix instruction
-constexpr int kDownWaves = 8, kUpWaves = 4;
+constexpr int kDownWaves = 8, kUpWaves = 4, kMostParts = 4;
 constexpr int weight_waves(int RT) { return RT < 4 ? 4 : RT; }
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kMostGroups = kAdaptersMost + 2;
 
@@ -305,8 +305,10 @@ struct Group {
     uint32_t group, count;
     const uint32_t* order;          // the plan's, from the group's or the tile's first place on, or null:
     uint32_t listed;                // of up to 64 rows, lane p has place p's
-    __device__ __forceinline__ uint32_t row(uint32_t place) const
+    // lane l's: the row at place `from` + l, the last one's behind it
+    __device__ __forceinline__ uint32_t rows(uint32_t from) const
     {
+        const uint32_t at = from + (threadIdx.x & 63), place = at < count ? at : count - 1;
         return order ? order[place] : __shfl(listed, (int)place);
     }
 };
@@ -414,12 +416,10 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
     const int64_t first = (int64_t)part * a.chunks, all = (a.D + kChunk - 1) / kChunk;
     const int64_t last = first + a.chunks < all ? first + a.chunks : all;
     for (uint32_t place = 0; place < rows.count; place += kTile) {
+        const uint32_t row = rows.rows(place);
         int64_t line[kSubs];
 #pragma unroll
-        for (int s = 0; s < kSubs; ++s) {
-            const uint32_t p = place + 16 * s + j;          // (rows behind the last: any that there is)
-            line[s] = (int64_t)rows.row(p < rows.count ? p : place) * a.D;
-        }
+        for (int s = 0; s < kSubs; ++s) line[s] = (int64_t)__shfl(row, 16 * s + j) * a.D;
         v4f acc[kSubs][RT] = {};
         // N chunks side by side (four are 256 bytes of a row: whole lines of memory); `skip` elements of each line of the one are not its
         auto chunks = [&](int64_t from, auto number, int skip) {
@@ -506,10 +506,9 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
             for (int s = 0; s < kSubs; ++s)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t p = place + 16 * s + 4 * g + i;
-                    const uint32_t row = rows.row(p < rows.count ? p : place);
-                    if (p >= rows.count) continue;
-                    float* to = a.h + ((int64_t)part * a.rows.M + row) * (16 * RT);
+                    const uint32_t of = __shfl(row, 16 * s + 4 * g + i);
+                    if (place + 16 * s + 4 * g + i >= rows.count) continue;
+                    float* to = a.h + ((int64_t)part * a.rows.M + of) * (16 * RT);
 #pragma unroll
                     for (int q = 0; q < RQ; ++q)
 #pragma unroll
@@ -538,46 +537,41 @@ struct UpArgs {
     uint32_t parts;
 };
 
-// a row's values, all parts together, times `scale`
+// a row's values, all parts together (four are asked for at once), times `scale`
 template <int N>
 __device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t parts, float scale, float (&v)[N])
 {
-    auto add = [&](uint32_t s) {
-        float4 q[N / 4];
+    constexpr int B = kMostParts, V = N / 4;
+    v4f q[B][V];
 #pragma unroll
-        for (int j = 0; j < N / 4; ++j) q[j] = reinterpret_cast<const float4*>(h + s * part)[j];
+    for (int u = 0; u < B; ++u)
+        if (u == 0 || parts > 1)
 #pragma unroll
-        for (int j = 0; j < N / 4; ++j) {
-            v[4 * j] += q[j].x;
-            v[4 * j + 1] += q[j].y;
-            v[4 * j + 2] += q[j].z;
-            v[4 * j + 3] += q[j].w;
-        }
-    };
+            for (int j = 0; j < V; ++j) q[u][j] = reinterpret_cast<const v4f*>(h + (u < (int)parts ? u : 0) * part)[j];
+        else
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = 0.0f;
-    uint32_t s = 0;
-    for (; s + 4 <= parts; s += 4) {
+            for (int j = 0; j < V; ++j) q[u][j] = v4f{};
 #pragma unroll
-        for (int u = 0; u < 4; ++u) add(s + u);
-    }
-    for (; s < parts; ++s) add(s);
+    for (int u = 1; u < B; ++u)
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] *= scale;
+        for (int j = 0; j < V; ++j) q[0][j] += u < (int)parts ? q[u][j] : v4f{};
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = q[0][j / 4][j % 4] * scale;
 }
 
-// SHORT: there are fewer columns than a wave has, or (kAlong) fewer ranks than a load, and W and base are loaded element by element.
-// Else the last columns, and the last ranks of a line along them, begin so far before the end that loads are whole; what others have
-// already is not written, and zero in h.
-template <int DT, int RT, int MODE, bool SHORT>
+// How columns end.  kShort: there are fewer than a wave has, or (kAlong) fewer ranks than a load, and W and base are loaded element by
+// element.  Else the last columns, and the last ranks of a line along them, begin so far before the end that loads are whole; what
+// others have already is not written, and zero in h.  kEven: columns are whole loads, so that a lane writes all of its own or none.
+enum End { kEven, kOdd, kShort };
+template <int DT, int RT, int MODE, int END>
 __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
 {
+    constexpr bool SHORT = END == kShort;
     constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L;
     // bfloat16, one tile of ranks: both planes are one chunk, the second beside the same lines of W again
     constexpr bool kFolded = DT == kBf16 && RT == 1;
     constexpr int P = kFolded ? 1 : planes_of<DT>(), C = 16 * RT < kChunk ? 1 : 16 * RT / kChunk, kRanks = 16 * RT;
     __shared__ Piece h[kSubs * C][P][64];
-    __shared__ __attribute__((aligned(16))) uint32_t lines[kTile];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     uint32_t tile, over;
     if (!place_of(a.grid, over, tile)) return;
@@ -591,71 +585,86 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
     auto own = [&](int c) { return kChunk * c + L * (kFolded ? g & 1 : g); };
     auto first = [&](int c) { return MODE == kDown || SHORT || own(c) + L <= a.r ? own(c) : a.r - L; };
     for (uint32_t place = 0; place < rows.count; place += kTile) {
-        // the tile's h, split, and its rows, for all waves
+        const uint32_t all = rows.rows(place);
+        uint32_t row[kSubs][4];
+#pragma unroll
+        for (int s = 0; s < kSubs; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) row[s][i] = __shfl(all, 16 * s + 4 * g + i);
+        // a lane's columns from c0 on: from col, those from lo to hi its own
+        int64_t col;
+        int lo, hi;
+        Piece base[kSubs][4], w[C][L];
+        auto fetch = [&](int64_t c0) {
+            const int64_t from = SHORT || c0 + kColumns <= a.N ? c0 : a.N - kColumns;
+            lo = (int)(c0 - from) - L * j;
+            hi = SHORT ? (int)(a.N - c0) - L * j : L;
+            col = SHORT && hi <= 0 ? c0 : from + L * j;
+            if (a.base)
+#pragma unroll
+                for (int s = 0; s < kSubs; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) base[s][i] = load_piece<DT, !SHORT>(a.base, row[s][i] * a.N + col, hi);
+            if (none || wrong) return;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < L; ++e) {
+                    if constexpr (MODE == kDown) {         // line own(c) + e
+                        const int rank = own(c) + e < a.r ? own(c) + e : 0;
+                        w[c][e] = load_piece<DT, !SHORT>(W, rank * a.N + col, hi);
+                    } else {                               // column col + e
+                        const int rank = first(c) < a.r ? first(c) : 0;
+                        w[c][e] = load_piece<DT, !SHORT>(W, (col + (SHORT && e >= hi ? 0 : e)) * a.r + rank, a.r - first(c));
+                    }
+                }
+        };
+        // the first columns are on their way while the tile's h is split, for all waves
+        int64_t c0 = ((int64_t)over * kUpWaves + wave) * kColumns;
+        const int64_t step = (int64_t)a.across * kUpWaves * kColumns;
+        if (c0 < a.N) fetch(c0);
         if (place) __syncthreads();
         for (int f = wave; f < kSubs * C; f += kUpWaves) {
             const int s = f / C, c = f % C;
-            const uint32_t p = place + 16 * s + j, row = rows.row(p < rows.count ? p : place);       // (behind the last: any that there is)
+            const uint32_t of = __shfl(all, 16 * s + j);
             float v[L] = {};
-            if (!none && !wrong) load_h<L>(a.h + (int64_t)row * kRanks + first(c), a.rows.M * kRanks, a.parts, scale, v);
+            if (!none && !wrong) load_h<L>(a.h + (int64_t)of * kRanks + first(c), a.rows.M * kRanks, a.parts, scale, v);
             if (MODE == kAlong && !SHORT)
 #pragma unroll
                 for (int e = 0; e < L; ++e) v[e] = first(c) + e >= own(c) ? v[e] : 0.0f;
             Piece two[planes_of<DT>()];
             split<DT>(v, two);
-            if constexpr (kFolded) h[f][0][lane] = g < 2 ? two[0] : two[1];
-            else
+            if constexpr (kFolded) {
+                // (word by word: a choice between the two in memory would put them into LDS, at an address that a load from the
+                // host's queue decides: 10 us)
+                Piece of_lane;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) of_lane.w[k] = g < 2 ? two[0].w[k] : two[1].w[k];
+                h[f][0][lane] = of_lane;
+            } else {
 #pragma unroll
                 for (int k = 0; k < P; ++k) h[f][k][lane] = two[k];
-            if (c == 0 && g == 0) lines[16 * s + j] = row;
+            }
         }
         __syncthreads();
-        for (int64_t c0 = ((int64_t)over * kUpWaves + wave) * kColumns; c0 < a.N; c0 += (int64_t)a.across * kUpWaves * kColumns) {
-            // a lane's columns: from col on, those from lo to hi its own
-            const int64_t from = SHORT || c0 + kColumns <= a.N ? c0 : a.N - kColumns;
-            const int lo = (int)(c0 - from) - L * j, hi = SHORT ? (int)(a.N - c0) - L * j : L;
-            const int64_t col = SHORT && hi <= 0 ? c0 : from + L * j;
-            int64_t line[kSubs][4];
-            Piece base[kSubs][4], w[C][L];
+        for (; c0 < a.N; c0 += step) {
 #pragma unroll
-            for (int s = 0; s < kSubs; ++s) {
-                const uint4 row = *reinterpret_cast<const uint4*>(lines + 16 * s + 4 * g);
-                const uint32_t of[4] = {row.x, row.y, row.z, row.w};
+            for (int c = 0; c < C; ++c) {
+                if (a.r != kRanks)                         // (h is zero there, but W may be infinite)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) line[s][i] = of[i] * a.N + col;
-                if (a.base)
+                    for (int e = 0; e < L; ++e) w[c][e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[c][e]);
+                if constexpr (MODE == kDown) {
+                    Piece t[L];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) base[s][i] = load_piece<DT, !SHORT>(a.base, line[s][i], hi);
-            }
-            if (!none && !wrong)
+                    for (int e = 0; e < L; ++e) t[e] = turned<DT>(w[c], e);
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-#pragma unroll
-                    for (int e = 0; e < L; ++e) {
-                        if constexpr (MODE == kDown) {     // line own(c) + e
-                            const int rank = own(c) + e < a.r ? own(c) + e : 0;
-                            w[c][e] = load_piece<DT, !SHORT>(W, rank * a.N + col, hi);
-                        } else {                           // column col + e
-                            const int rank = first(c) < a.r ? first(c) : 0;
-                            w[c][e] = load_piece<DT, !SHORT>(W, (col + (SHORT && e >= hi ? 0 : e)) * a.r + rank, a.r - first(c));
-                        }
-                    }
-                    if (a.r != kRanks)                     // (h is zero there, but W may be infinite)
-#pragma unroll
-                        for (int e = 0; e < L; ++e) w[c][e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[c][e]);
-                    if constexpr (MODE == kDown) {
-                        Piece t[L];
-#pragma unroll
-                        for (int e = 0; e < L; ++e) t[e] = turned<DT>(w[c], e);
-#pragma unroll
-                        for (int e = 0; e < L; ++e) w[c][e] = t[e];
-                    }
+                    for (int e = 0; e < L; ++e) w[c][e] = t[e];
                 }
+            }
 #pragma unroll
             for (int s = 0; s < kSubs; ++s) {
                 // (one block of rows after the other: the sums of one are in registers)
                 __builtin_amdgcn_sched_barrier(0);
-                const uint32_t at = place + 16 * s + 4 * g;
                 if (place + 16 * s >= rows.count) break;
                 v4f acc[L] = {};
                 if (!none && !wrong)
@@ -675,9 +684,12 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
                         v[t] = wrong ? __builtin_nanf("") : acc[t][i];
                         if (a.base) v[t] += value<DT>(base[s][i], t);
                     }
-                    if (at + i < rows.count && hi > 0) store_piece<DT>(a.out, line[s][i], lo, hi, piece_of<DT>(v));
+                    if (place + 16 * s + 4 * g + i >= rows.count || hi <= 0 || lo >= L) continue;
+                    if constexpr (END == kEven) store_piece<DT>(a.out, row[s][i] * a.N + col, 0, L, piece_of<DT>(v));
+                    else store_piece<DT>(a.out, row[s][i] * a.N + col, lo, hi, piece_of<DT>(v));
                 }
             }
+            if (c0 + step < a.N) fetch(c0 + step);
         }
     }
 }
@@ -726,22 +738,14 @@ __global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightAr
         constexpr bool WHOLE = whole.value;
         // (as often for every lane of a wave: the rows of a few are handed from lane to lane)
         const uint32_t step = kChunk * kShares * a.split;
-        uint32_t next[L];
-        auto look = [&](uint32_t first) {
-#pragma unroll
-            for (int e = 0; e < L; ++e) {
-                const uint32_t p = first + L * g + e;
-                next[e] = rows.row(p < rows.count ? p : first);            // (behind the last: one that there is, taken for zeros)
-            }
-        };
-        uint32_t first = kChunk * (part * kShares + share);
-        if (first < rows.count) look(first);
+        uint32_t first = kChunk * (part * kShares + share), next = 0;
+        if (first < rows.count) next = rows.rows(first);
         for (; first < rows.count; first += step) {
             Piece lines[L];
             float u[RW][L];
 #pragma unroll
             for (int e = 0; e < L; ++e) {
-                const int64_t row = next[e];
+                const int64_t row = __shfl(next, L * g + e);               // (behind the last: one that there is, taken for zeros)
                 lines[e] = load_piece<DT, WHOLE>(a.v[of], row * N + (WHOLE || n > 0 ? col : 0), n);
 #pragma unroll
                 for (int t = 0; t < RW; ++t) {
@@ -750,7 +754,7 @@ __global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightAr
                 }
             }
             const uint32_t ahead = first + step;
-            if (ahead < rows.count) look(ahead);
+            if (ahead < rows.count) next = rows.rows(ahead);
 #pragma unroll
             for (int e = 0; e < L; ++e) {
                 const bool has = first + L * g + e < rows.count;
@@ -867,7 +871,7 @@ Parts parts_of(const AdapterArgs& a, int64_t D)
     const int64_t chunk = a.dtype == kBf16 ? 32 : 16, chunks = (D + chunk - 1) / chunk;
     const int64_t tiles = a.M <= kDirect ? (a.M < a.n ? a.M : a.n) : a.M / kTile + (a.n < a.M / kTile ? a.n : a.M / kTile);
     int64_t parts = 512 / (tiles > 0 ? tiles : 1);
-    if (parts > 8) parts = 8;
+    if (parts > kMostParts) parts = kMostParts;
     while (parts > 1 && chunks < parts * kDownWaves) --parts;
     if (parts < 1) parts = 1;
     const int64_t each = (chunks + parts - 1) / parts;
@@ -943,8 +947,9 @@ void launch_up(const AdapterArgs& a, const float* h, const void* W, const void* 
     with_types(a, [&](auto dt, auto rt) {
         const dim3 grid(8 * u.grid.per_xcd), block(64 * kUpWaves);
         constexpr int L = lane_of<dt.value>();
-        if (N < 16 * L || (MODE == kAlong && a.r < L)) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, u);
-        else hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, false>), grid, block, 0, stream, u);
+        if (N < 16 * L || (MODE == kAlong && a.r < L)) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kShort>), grid, block, 0, stream, u);
+        else if (N % L) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kOdd>), grid, block, 0, stream, u);
+        else hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kEven>), grid, block, 0, stream, u);
     });
 }
 

@@ -260,11 +260,20 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
         }
     }
     if (!a.dweight && !a.dbias) return;
-    // one group of rows after the other
+    // the rows that a wave has side by side, then one wave's, or one row's several waves, after the other
+    for (uint32_t m = k.width; m < 64; m <<= 1)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                dw[r][j] += __shfl_xor(dw[r][j], (int)m);
+                db[r][j] += __shfl_xor(db[r][j], (int)m);
+            }
+    const uint32_t wide = k.width < 64 ? 64 : k.width, turns = blockDim.x / wide, mine = threadIdx.x / wide;
     float* const to = parts + (int64_t)blockIdx.x * 2 * a.C;
-    for (uint32_t g = 0; g < k.at_once; ++g) {
-        if (group == g) {
-            const bool last = g + 1 == k.at_once;
+    for (uint32_t g = 0; g < turns; ++g) {
+        if (mine == g && threadIdx.x - mine * wide < k.width) {
+            float* const into = g + 1 == turns ? to : columns;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const Span<WHOLE> at(t + r * k.width, a.C, true);
@@ -277,12 +286,12 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
                         dw[r][j] += columns[c];
                         db[r][j] += columns[a.C + c];
                     }
-                    (last ? to : columns)[c] = dw[r][j];
-                    (last ? to : columns)[a.C + c] = db[r][j];
+                    into[c] = dw[r][j];
+                    into[a.C + c] = db[r][j];
                 }
             }
         }
-        if (g + 1 < k.at_once) __syncthreads();
+        if (g + 1 < turns) __syncthreads();
     }
 }
 
@@ -339,7 +348,7 @@ Rows fwd_rows(const LayerNormArgs& a)
 Rows bwd_rows(const LayerNormArgs& a)
 {
     Rows k = rows_of(a, 2, kBwdThreads, 2048);
-    const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.R > 2 ? 1 : k.R > 1 ? 2 : 4);
+    const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.R > 2 ? 1 : k.R > 1 ? 2 : 3);
     k.groups = (uint32_t)(groups < most ? groups : most);
     return k;
 }
