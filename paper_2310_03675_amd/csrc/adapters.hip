@@ -564,7 +564,7 @@ __device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t pa
 // others have already is not written, and zero in h.  kEven: columns are whole loads, so that a lane writes all of its own or none.
 enum End { kEven, kOdd, kShort };
 template <int DT, int RT, int MODE, int END>
-__global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
+__global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
 {
     constexpr bool SHORT = END == kShort;
     constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L;
@@ -594,7 +594,19 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
         // a lane's columns from c0 on: from col, those from lo to hi its own
         int64_t col;
         int lo, hi;
-        Piece base[kSubs][4], w[C][L];
+        Piece base[kSubs][4], w[L];
+        auto lines = [&](int c) {
+#pragma unroll
+            for (int e = 0; e < L; ++e) {
+                if constexpr (MODE == kDown) {             // line own(c) + e
+                    const int rank = own(c) + e < a.r ? own(c) + e : 0;
+                    w[e] = load_piece<DT, !SHORT>(W, rank * a.N + col, hi);
+                } else {                                   // column col + e
+                    const int rank = first(c) < a.r ? first(c) : 0;
+                    w[e] = load_piece<DT, !SHORT>(W, (col + (SHORT && e >= hi ? 0 : e)) * a.r + rank, a.r - first(c));
+                }
+            }
+        };
         auto fetch = [&](int64_t c0) {
             const int64_t from = SHORT || c0 + kColumns <= a.N ? c0 : a.N - kColumns;
             lo = (int)(c0 - from) - L * j;
@@ -605,19 +617,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
                 for (int s = 0; s < kSubs; ++s)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) base[s][i] = load_piece<DT, !SHORT>(a.base, row[s][i] * a.N + col, hi);
-            if (none || wrong) return;
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int e = 0; e < L; ++e) {
-                    if constexpr (MODE == kDown) {         // line own(c) + e
-                        const int rank = own(c) + e < a.r ? own(c) + e : 0;
-                        w[c][e] = load_piece<DT, !SHORT>(W, rank * a.N + col, hi);
-                    } else {                               // column col + e
-                        const int rank = first(c) < a.r ? first(c) : 0;
-                        w[c][e] = load_piece<DT, !SHORT>(W, (col + (SHORT && e >= hi ? 0 : e)) * a.r + rank, a.r - first(c));
-                    }
-                }
+            if (!none && !wrong) lines(0);
         };
         // the first columns are on their way while the tile's h is split, for all waves
         int64_t c0 = ((int64_t)over * kUpWaves + wave) * kColumns;
@@ -648,40 +648,32 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(UpArgs a)
         }
         __syncthreads();
         for (; c0 < a.N; c0 += step) {
+            v4f acc[kSubs][L] = {};
+            if (!none && !wrong)
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                if (a.r != kRanks)                         // (h is zero there, but W may be infinite)
+                for (int c = 0; c < C; ++c) {
+                    if (c) lines(c);
+                    if (a.r != kRanks)                     // (h is zero there, but W may be infinite)
 #pragma unroll
-                    for (int e = 0; e < L; ++e) w[c][e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[c][e]);
-                if constexpr (MODE == kDown) {
-                    Piece t[L];
+                        for (int e = 0; e < L; ++e) w[e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[e]);
 #pragma unroll
-                    for (int e = 0; e < L; ++e) t[e] = turned<DT>(w[c], e);
+                    for (int t = 0; t < L; ++t) {
+                        const Piece b = MODE == kDown ? turned<DT>(w, t) : w[t];
 #pragma unroll
-                    for (int e = 0; e < L; ++e) w[c][e] = t[e];
+                        for (int k = P - 1; k >= 0; --k)
+#pragma unroll
+                            for (int s = 0; s < kSubs; ++s) acc[s][t] = multiply<DT>(h[s * C + c][k][lane], b, acc[s][t]);
+                    }
                 }
-            }
 #pragma unroll
             for (int s = 0; s < kSubs; ++s) {
-                // (one block of rows after the other: the sums of one are in registers)
-                __builtin_amdgcn_sched_barrier(0);
                 if (place + 16 * s >= rows.count) break;
-                v4f acc[L] = {};
-                if (!none && !wrong)
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-#pragma unroll
-                        for (int k = P - 1; k >= 0; --k) {
-                            const Piece x = h[s * C + c][k][lane];
-#pragma unroll
-                            for (int t = 0; t < L; ++t) acc[t] = multiply<DT>(x, w[c][t], acc[t]);
-                        }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v[L];
 #pragma unroll
                     for (int t = 0; t < L; ++t) {
-                        v[t] = wrong ? __builtin_nanf("") : acc[t][i];
+                        v[t] = wrong ? __builtin_nanf("") : acc[s][t][i];
                         if (a.base) v[t] += value<DT>(base[s][i], t);
                     }
                     if (place + 16 * s + 4 * g + i >= rows.count || hi <= 0 || lo >= L) continue;
