@@ -389,16 +389,44 @@ struct DownArgs {
     float* h;                       // [parts][M][16 RT]
     int64_t D;
     int r;
-    uint32_t chunks;                // of the contraction: how many times 4 kLane a part has
+    uint32_t steps;                 // of the contraction: how many times 8 kLane a part has
 };
 
-// SHORT: the contraction is shorter than a chunk, and loaded element by element.  Else its last chunk, where it is no whole number of
-// them, begins a chunk before the end, and what it has of the one before is taken for zeros.
+// The sums of a workgroup's waves, in the first one's
+template <int RT>
+__device__ __forceinline__ void join_waves(v4f (&acc)[kSubs][RT], v4f* lds, int wave, int lane)
+{
+#pragma unroll
+    for (int half = kDownWaves / 2; half; half /= 2) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int s = 0; s < kSubs; ++s)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) lds[(((wave - half) * kSubs + s) * RT + t) * 64 + lane] = acc[s][t];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int s = 0; s < kSubs; ++s)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) acc[s][t] += lds[((wave * kSubs + s) * RT + t) * 64 + lane];
+    }
+}
+
+// A wave's step: 128 bytes of every row, two chunks.  x (and W, where it runs along the contraction) is loaded as memory lies, eight
+// lanes to a row, into registers, while the step before is multiplied, and handed to the lanes that multiply it through LDS that is
+// the wave's own: asked for as the fragments lie, sixteen rows side by side, every lane's 16 bytes are an access of the cache of their
+// own, four times as many (a tile of 8192 x 16384 in bfloat16 against rank 64: 284 us).  A row's pieces are turned by the row's
+// number, so that eight lanes' reads lie in different banks.
+// SHORT: the contraction is shorter than a step; element by element.  Else the last step, where it is no whole one, begins a step
+// before the end, and what it has of the one before is taken for zeros.
 template <int DT, int RT, int MODE, bool SHORT>
 __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
 {
-    constexpr int L = lane_of<DT>(), kChunk = 4 * L, RL = RT < L ? RT : L, RQ = RT / RL, kAhead = RT < 4 ? 4 : 2;
-    __shared__ v4f sums[kDownWaves / 2][kSubs][RT][64];
+    constexpr int L = lane_of<DT>(), kChunk = 4 * L, kStep = 2 * kChunk, RL = RT < L ? RT : L, RQ = RT / RL;
+    constexpr int kRows = kTile + (MODE == kAlong ? 16 * RT : 0), kLoads = kRows / 8;           // of a step, that go through LDS
+    constexpr int kBytes = SHORT ? 0 : 128 * kRows * kDownWaves, kSums = kDownWaves / 2 * kSubs * RT * 64 * (int)sizeof(v4f);
+    __shared__ __attribute__((aligned(16))) char lds[kBytes > kSums ? kBytes : kSums];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     uint32_t tile, part;
     if (!place_of(a.grid, tile, part)) return;
@@ -413,94 +441,114 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
         const int c = 16 * RL * q + RL * j;
         rank[q] = c + RL <= a.r ? c : a.r - RL;
     }
-    const int64_t first = (int64_t)part * a.chunks, all = (a.D + kChunk - 1) / kChunk;
-    const int64_t last = first + a.chunks < all ? first + a.chunks : all;
+    const int64_t first = (int64_t)part * a.steps, all = (a.D + kStep - 1) / kStep;
+    const int64_t last = first + a.steps < all ? first + a.steps : all;
     for (uint32_t place = 0; place < rows.count; place += kTile) {
         const uint32_t row = rows.rows(place);
-        int64_t line[kSubs];
-#pragma unroll
-        for (int s = 0; s < kSubs; ++s) line[s] = (int64_t)__shfl(row, 16 * s + j) * a.D;
         v4f acc[kSubs][RT] = {};
-        // N chunks side by side (four are 256 bytes of a row: whole lines of memory); `skip` elements of each line of the one are not its
-        auto chunks = [&](int64_t from, auto number, int skip) {
-            constexpr int N = number.value, LINES = MODE == kDown ? L : RL;
-            Piece x[N][kSubs], w[N][RQ * LINES];
+        // the chunk's products: x's fragments, and W's lines across the contraction or fragments along it
+        auto products = [&](const Piece (&x)[kSubs], const Piece (&w)[RQ][MODE == kDown ? L : RL]) {
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const int64_t k = from + u * kChunk + L * g;
-                const int n = SHORT ? (int)(a.D - k) : L;
-                const int64_t in = SHORT && n <= 0 ? 0 : k;
+            for (int q = 0; q < RQ; ++q)
 #pragma unroll
-                for (int s = 0; s < kSubs; ++s) x[u][s] = load_piece<DT, !SHORT>(a.x, line[s] + in, n);
+                for (int t = 0; t < RL; ++t) {
+                    Piece b;
+                    if constexpr (MODE == kDown) b = turned<DT>(w[q], t);
+                    else b = w[q][t];
 #pragma unroll
-                for (int q = 0; q < RQ; ++q)
-#pragma unroll
-                    for (int e = 0; e < LINES; ++e) {
-                        if constexpr (MODE == kDown)
-                            w[u][L * q + e] = only_if(!SHORT || e < n, load_few<DT, RL, true>(W, (SHORT && e >= n ? 0 : k + e) * a.r + rank[q], RL));
-                        else
-                            w[u][RL * q + e] = load_piece<DT, !SHORT>(W, (int64_t)(rank[q] + e) * a.D + in, n);
-                    }
-            }
-            if (N == 1 && !SHORT && skip) {
-                const int own = skip - L * g;               // elements of a lane's that are not
-#pragma unroll
-                for (int s = 0; s < kSubs; ++s) x[0][s] = without<DT>(x[0][s], own);
-#pragma unroll
-                for (int i = 0; i < RQ * LINES; ++i) w[0][i] = MODE == kDown ? only_if(i % L >= own, w[0][i]) : without<DT>(w[0][i], own);
-            }
-#pragma unroll
-            for (int u = 0; u < N; ++u)
-#pragma unroll
-                for (int q = 0; q < RQ; ++q)
-#pragma unroll
-                    for (int t = 0; t < RL; ++t) {
-                        Piece b;
-                        if constexpr (MODE == kDown) {
-                            Piece lines[L];
-#pragma unroll
-                            for (int e = 0; e < L; ++e) lines[e] = w[u][L * q + e];
-                            b = turned<DT>(lines, t);
-                        } else {
-                            b = w[u][RL * q + t];
-                        }
-#pragma unroll
-                        for (int s = 0; s < kSubs; ++s) acc[s][RL * q + t] = multiply<DT>(x[u][s], b, acc[s][RL * q + t]);
-                    }
+                    for (int s = 0; s < kSubs; ++s) acc[s][RL * q + t] = multiply<DT>(x[s], b, acc[s][RL * q + t]);
+                }
         };
-        using std::integral_constant;
-        const int64_t full = SHORT ? last : a.D / kChunk < last ? a.D / kChunk : last;
-        int64_t c = first;
-        if (!SHORT && full > first) {
-            // (tiles begin at different places, so that they do not all ask the same channels of the memory: rows are often a power of
-            // two apart)
-            const uint32_t turns = (uint32_t)(full - first) / (kDownWaves * kAhead);
-            uint32_t turn = turns ? (tile * 5) % turns : 0;
-            for (uint32_t i = 0; i < turns; ++i) {
-                chunks((first + (turn * kDownWaves + wave) * kAhead) * kChunk, integral_constant<int, kAhead>{}, 0);
-                if (++turn == turns) turn = 0;
+        if constexpr (SHORT) {
+            for (int64_t k0 = (first + wave) * kStep; k0 < a.D && first + wave < last; k0 += kChunk) {
+                const int64_t k = k0 + L * g;
+                const int n = (int)(a.D - k);
+                const int64_t in = n <= 0 ? 0 : k;
+                Piece x[kSubs], w[RQ][MODE == kDown ? L : RL];
+#pragma unroll
+                for (int s = 0; s < kSubs; ++s) x[s] = load_piece<DT, false>(a.x, (int64_t)__shfl(row, 16 * s + j) * a.D + in, n);
+#pragma unroll
+                for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                    for (int e = 0; e < (MODE == kDown ? L : RL); ++e) {
+                        if constexpr (MODE == kDown) w[q][e] = only_if(e < n, load_few<DT, RL, true>(W, (e < n ? k + e : 0) * a.r + rank[q], RL));
+                        else w[q][e] = load_piece<DT, false>(W, (int64_t)(rank[q] + e) * a.D + in, n);
+                    }
+                products(x, w);
             }
-            c += (int64_t)turns * kDownWaves * kAhead;
+        } else {
+            char* const mine = lds + 128 * kRows * wave;
+            // a lane's pieces: piece l % 8 of rows l / 8, 8 + l / 8, ..: the tile's rows, then the ranks in the fragments' order
+            const char* from[kLoads];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int at = 8 * i + lane / 8;
+                if (8 * i < kTile) {
+                    from[i] = static_cast<const char*>(a.x) + (int64_t)__shfl(row, at) * a.D * (16 / L);
+                } else {
+                    const int f = at - kTile, c = 16 * RL * (f / (16 * RL)) + RL * (f % 16);        // fragment f / 16 - RL q, line f % 16
+                    from[i] = W + (int64_t)((c + RL <= a.r ? c : a.r - RL) + f / 16 % RL) * a.D * (16 / L);
+                }
+                from[i] += 16 * (lane % 8);
+            }
+            Piece next[kLoads], lines[2][MODE == kDown ? RQ : 1][MODE == kDown ? L : 1];
+            auto load = [&](int64_t step) {
+                const int64_t k = (step + 1) * kStep <= a.D ? step * kStep : a.D - kStep;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) __builtin_memcpy(next[i].w, from[i] + k * (16 / L), 16);
+                if constexpr (MODE == kDown)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                            for (int e = 0; e < L; ++e) lines[c][q][e] = load_few<DT, RL, true>(W, (k + kChunk * c + L * g + e) * a.r + rank[q], RL);
+            };
+            int64_t step = first + wave;
+            if (step < last) load(step);
+            for (; step < last; step += kDownWaves) {
+                const int skip = (step + 1) * kStep <= a.D ? 0 : (int)((step + 1) * kStep - a.D);
+                if (skip) {
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) next[i] = without<DT>(next[i], skip - L * (lane % 8));
+                    if constexpr (MODE == kDown)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                                for (int e = 0; e < L; ++e) lines[c][q][e] = only_if(kChunk * c + L * g + e >= skip, lines[c][q][e]);
+                }
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+                    *reinterpret_cast<Piece*>(mine + 1024 * i + 128 * (lane / 8) + 16 * ((lane ^ lane / 8) % 8)) = next[i];
+                Piece w[2][RQ][MODE == kDown ? L : RL];
+                if constexpr (MODE == kDown)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                            for (int e = 0; e < L; ++e) w[c][q][e] = lines[c][q][e];
+                if (step + kDownWaves < last) load(step + kDownWaves);
+                auto fragment = [&](int f, int c) {         // 16 rows from 16 f on
+                    return *reinterpret_cast<const Piece*>(mine + 2048 * f + 128 * j + 16 * ((4 * c + g) ^ (j & 7)));
+                };
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    Piece x[kSubs];
+#pragma unroll
+                    for (int s = 0; s < kSubs; ++s) x[s] = fragment(s, c);
+                    if constexpr (MODE == kAlong)
+#pragma unroll
+                        for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                            for (int t = 0; t < RL; ++t) w[c][q][t] = fragment(kSubs + RL * q + t, c);
+                    products(x, w[c]);
+                }
+            }
         }
-        for (c += wave; c < last; c += kDownWaves) {
-            const bool cut = c >= full;
-            chunks(cut ? a.D - kChunk : c * kChunk, integral_constant<int, 1>{}, cut ? (int)(c * kChunk - (a.D - kChunk)) : 0);
-        }
-#pragma unroll
-        for (int half = kDownWaves / 2; half; half /= 2) {
-            __syncthreads();
-            if (wave >= half && wave < 2 * half)
-#pragma unroll
-                for (int s = 0; s < kSubs; ++s)
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) sums[wave - half][s][t][lane] = acc[s][t];
-            __syncthreads();
-            if (wave < half)
-#pragma unroll
-                for (int s = 0; s < kSubs; ++s)
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) acc[s][t] += sums[wave][s][t][lane];
-        }
+        join_waves<RT>(acc, reinterpret_cast<v4f*>(lds), wave, lane);
         if (wave == 0)
 #pragma unroll
             for (int s = 0; s < kSubs; ++s)
@@ -518,6 +566,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
                             if (c >= a.r) to[c] = 0.0f;     // (behind the last rank)
                         }
                 }
+        if (place + kTile < rows.count) __syncthreads();
     }
 }
 
@@ -854,20 +903,20 @@ int tiles_of_rank(int r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }
 // (what a grid has: tiles that may be)
 uint32_t grid_tiles(const AdapterArgs& a) { return (uint32_t)(a.M <= kDirect ? a.M : most_tiles(a.M, a.n)); }
 
-// Parts of a contraction over D: as many as make 512 workgroups, none of fewer than eight waves' chunks.
+// Parts of a contraction over D: as many as make 512 workgroups, none of fewer than a step for each of the eight waves.
 struct Parts {
-    uint32_t parts, chunks;
+    uint32_t parts, steps;
 };
 Parts parts_of(const AdapterArgs& a, int64_t D)
 {
-    const int64_t chunk = a.dtype == kBf16 ? 32 : 16, chunks = (D + chunk - 1) / chunk;
+    const int64_t step = a.dtype == kBf16 ? 64 : 32, steps = (D + step - 1) / step;
     const int64_t tiles = a.M <= kDirect ? (a.M < a.n ? a.M : a.n) : a.M / kTile + (a.n < a.M / kTile ? a.n : a.M / kTile);
     int64_t parts = 512 / (tiles > 0 ? tiles : 1);
     if (parts > kMostParts) parts = kMostParts;
-    while (parts > 1 && chunks < parts * kDownWaves) --parts;
+    while (parts > 1 && steps < parts * kDownWaves) --parts;
     if (parts < 1) parts = 1;
-    const int64_t each = (chunks + parts - 1) / parts;
-    return {(uint32_t)((chunks + each - 1) / each), (uint32_t)each};
+    const int64_t each = (steps + parts - 1) / parts;
+    return {(uint32_t)((steps + each - 1) / each), (uint32_t)each};
 }
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -919,10 +968,10 @@ void launch_down(const AdapterArgs& a, const void* x, const void* W, float* h, i
 {
     ProfileScope ps(K_ADAPT_DOWN, stream);
     const Parts p = parts_of(a, D);
-    const DownArgs d{rows, grid_of(grid_tiles(a), p.parts), x, W, h, D, a.r, p.chunks};
+    const DownArgs d{rows, grid_of(grid_tiles(a), p.parts), x, W, h, D, a.r, p.steps};
     with_types(a, [&](auto dt, auto rt) {
         const dim3 grid(8 * d.grid.per_xcd), block(64 * kDownWaves);
-        if (D < 4 * lane_of<dt.value>()) hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, d);
+        if (D < 8 * lane_of<dt.value>()) hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, d);
         else hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, false>), grid, block, 0, stream, d);
     });
 }
