@@ -348,13 +348,149 @@ def clip_gradients(parameters, max_norm: float, norm_type: float = 2.0, eps: flo
     return B.clip_grad_norm(grads, max_norm, norm_type, eps)
 
 
+class Dropout(torch.autograd.Function):
+    """residual + dropout(x) (hdqt_dropout): no mask is kept, the backward pass forms it again.  x contiguous, residual of its
+    shape or None, `how` a binding.Dropout."""
+
+    @staticmethod
+    def forward(ctx, x, residual, how: B.Dropout):
+        # (the step's tensor is kept as a saved one: whoever advances it before the backward pass is told)
+        ctx.save_for_backward(how.step)
+        ctx.how = how
+        return B.dropout(x, how, residual)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        _ = ctx.saved_tensors
+        dx = B.dropout(dy.contiguous(), ctx.how) if ctx.needs_input_grad[0] else None
+        return dx, dy if ctx.needs_input_grad[1] else None, None
+
+
+class LayerNorm(torch.autograd.Function):
+    """Layer normalisation of rows, x [..., columns] contiguous (hdqt_layernorm_fwd / hdqt_layernorm_bwd): y, or, with a residual or
+    dropout (a binding.Dropout), y and the sum that was normalised, whose gradient past the normalisation is added to its
+    own in the same pass.  What is kept is the sum and the rows' statistics."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, eps: float, how: Optional[B.Dropout]):
+        y, total, saved = B.layernorm_fwd(x, weight, bias, eps, residual, how)
+        ctx.save_for_backward(total, saved, weight, None if how is None else how.step)
+        ctx.how = how
+        ctx.set_materialize_grads(False)
+        return y if total is x else (y, total)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dtotal=None):
+        total, saved, weight, _ = ctx.saved_tensors
+        need = tuple(ctx.needs_input_grad[:4])
+        if dy is None:                               # (nobody asked for y: only the sum's gradient)
+            if dtotal is None:
+                return (None,) * 6
+            dx = dtotal if ctx.how is None or not need[0] else B.dropout(dtotal.contiguous(), ctx.how)
+            return dx if need[0] else None, dtotal if need[1] else None, None, None, None, None
+        dx, dres, dw, db = B.layernorm_bwd(dy.contiguous(), total, saved, weight, None if dtotal is None else dtotal.contiguous(), ctx.how, need)
+        return dx, dres, dw, db, None, None
+
+
+class LowRank(torch.autograd.Function):
+    """base + scale x A B with an adapter for every row (hdqt_adapters_fwd / hdqt_adapters_bwd): x [M, K], base [M, N], A [n, K, r],
+    B [n, r, N], ids int64 [M], scale fp32 [n]; all contiguous."""
+
+    @staticmethod
+    def forward(ctx, x, base, A, Bm, ids, scale):
+        out, saved = B.adapters_fwd(x, A, Bm, ids, scale, base)
+        ctx.save_for_backward(x, A, Bm, ids, scale, saved)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, A, Bm, ids, scale, saved = ctx.saved_tensors
+        need = tuple(ctx.needs_input_grad[k] for k in (0, 2, 3))
+        grads = B.adapters_bwd(dy.contiguous(), x, A, Bm, ids, saved, scale, need=need) if any(need) else (None,) * 3
+        return grads[0], dy if ctx.needs_input_grad[1] else None, grads[1], grads[2], None, None
+
+
+class _Masks:
+    """What a layer with dropout draws its masks by: nothing in evaluation, else a stream of its own (`layer_id`) that moves with every
+    training call, or, where `counter` is set (an int64 tensor of one element on the device, which the program advances), with
+    that: a captured step then takes another mask at every replay."""
+
+    def __init__(self, p: float, seed: int, layer_id: int):
+        if not 0.0 <= p <= 1.0:
+            raise ValueError(f"a share of {p} cannot be dropped")
+        self.p, self.seed, self.layer_id, self.step, self.counter = p, seed, layer_id, 0, None
+
+    def next(self, training: bool) -> Optional[B.Dropout]:
+        if not training or self.p == 0.0:
+            return None
+        how = B.Dropout(self.p, self.seed + self.step, self.layer_id, self.counter)
+        if self.counter is None:
+            self.step += 1
+        return how
+
+
+class ResidualDropout(torch.nn.Module):
+    """residual + dropout(x), or dropout(x); `masks.counter` for captured steps."""
+
+    def __init__(self, p: float, seed: int = 0, layer_id: int = 0):
+        super().__init__()
+        self.masks = _Masks(p, seed, layer_id)
+
+    def forward(self, x, residual=None):
+        how = self.masks.next(self.training)
+        if how is None:
+            return x if residual is None else residual + x
+        return Dropout.apply(x.contiguous(), None if residual is None else residual.contiguous(), how)
+
+
+class ResidualNorm(torch.nn.Module):
+    """A residual block's end: forward(x) is the layer normalisation of x; forward(x, residual) that of the sum
+    residual + dropout(x), and the sum, for what follows.  One pass over the tensors either way; `masks.counter` for captured
+    steps."""
+
+    def __init__(self, columns: int, eps: float = 1e-5, p: float = 0.0, seed: int = 0, layer_id: int = 0, device=None):
+        super().__init__()
+        self.eps, self.masks = eps, _Masks(p, seed, layer_id)
+        self.weight = torch.nn.Parameter(torch.ones(columns, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(columns, device=device))
+
+    def forward(self, x, residual=None):
+        how = self.masks.next(self.training)
+        if residual is None:
+            y = LayerNorm.apply(x.contiguous(), None, self.weight, self.bias, self.eps, how)
+            return y if how is None else y[0]
+        return LayerNorm.apply(x.contiguous(), residual.contiguous(), self.weight, self.bias, self.eps, how)
+
+
+class Adapters(torch.nn.Module):
+    """Low-rank adapters beside a projection of `in_features` to `out_features`, one for each task or request: forward(x, base, ids)
+    is base + alpha / rank x A_a B_a with a = ids of the row (negative: base alone).  x and base of any leading shape, ids of that
+    shape.  A is drawn, B is zero: an adapter starts as nothing."""
+
+    def __init__(self, in_features: int, out_features: int, adapters: int, rank: int, alpha: Optional[float] = None, device=None):
+        super().__init__()
+        self.A = torch.nn.Parameter(torch.randn(adapters, in_features, rank, device=device) * in_features ** -0.5)
+        self.B = torch.nn.Parameter(torch.zeros(adapters, rank, out_features, device=device))
+        self.register_buffer("scale", torch.full((adapters,), (rank if alpha is None else alpha) / rank, device=device))
+
+    def forward(self, x, base, ids):
+        out = LowRank.apply(x.reshape(-1, x.shape[-1]).contiguous(), base.reshape(-1, base.shape[-1]).contiguous(), self.A, self.B,
+                            ids.reshape(-1).contiguous(), self.scale.float())
+        return out.reshape(base.shape)
+
+
 class HdqtLinear(torch.nn.Module):
     """y = x W + bias with the matmul and its gradients quantized; inputs of any
-    leading shape are flattened to [M, K]."""
+    leading shape are flattened to [M, K].  `adapters` (an Adapters of the same features): forward(x, ids) adds those of
+    the rows beside it, in floating point."""
 
     def __init__(self, in_features: int, out_features: int, bias: bool = True,
-                 cfg: Optional[LayerConfig] = None, device=None, relu_input: bool = False):
+                 cfg: Optional[LayerConfig] = None, device=None, relu_input: bool = False, adapters: Optional[Adapters] = None):
         super().__init__()
+        self.adapters = adapters
         self.cfg = cfg or LayerConfig()
         self.relu_input = relu_input      # y = max(x, 0) W + bias, the rectifier's backward pass inside the matmul
         w = torch.empty(in_features, out_features, device=device)
@@ -363,15 +499,20 @@ class HdqtLinear(torch.nn.Module):
         self.bias = torch.nn.Parameter(torch.zeros(out_features, device=device)) if bias else None
         self.step = 0
 
-    def forward(self, x):
+    def forward(self, x, ids=None):
         lead = x.shape[:-1]
+        if ids is not None and self.adapters is None:
+            raise ValueError("ids are for a layer with adapters")
         fn = HdqtReluMatmul if self.relu_input else HdqtMatmul
         z = fn.apply(x.reshape(-1, x.shape[-1]), self.weight, self.cfg, self.step)
         if self.training:
             self.step += 1
         if self.bias is not None:
             z = z + self.bias
-        return z.reshape(*lead, -1)
+        z = z.reshape(*lead, -1)
+        if ids is None:
+            return z
+        return self.adapters(torch.relu(x) if self.relu_input else x, z, ids)
 
 
 class HdqtConv2d(torch.nn.Module):

@@ -333,21 +333,24 @@ struct RowArgs {
 
 // A launch of `inner` x `outer` workgroups.  They go to the eight XCDs in turn: each gets a run of its own, inner after inner, so
 // that tiles of one adapter, which read the same part of its matrix, share an L2.
+// More of them than a launch counts threads for are spread over the grid's other axis, so many `outer` each.
 struct Grid {
     Divisor inner;
-    uint32_t total, per_xcd;
+    uint32_t total, per_xcd, outer, slice;
+    uint32_t slices() const { return (outer + slice - 1) / slice; }
 };
 Grid grid_of(uint32_t inner, uint32_t outer)
 {
-    const uint32_t total = inner * outer;
-    return {make_divisor(inner), total, (total + 7) / 8};
+    const uint32_t most = (1u << 22) / inner, slice = outer < most ? outer : most > 0 ? most : 1, total = inner * slice;
+    return {make_divisor(inner), total, (total + 7) / 8, outer, slice};
 }
 __device__ __forceinline__ bool place_of(const Grid& k, uint32_t& inner, uint32_t& outer)
 {
     const uint32_t idx = (blockIdx.x & 7) * k.per_xcd + (blockIdx.x >> 3);
     outer = divide(idx, k.inner);
     inner = idx - outer * k.inner.d;
-    return idx < k.total;
+    outer += blockIdx.y * k.slice;
+    return idx < k.total && outer < k.outer;
 }
 
 // The rows of workgroup `tile`: none where there is no such tile, or where an earlier row of the few has them.
@@ -970,7 +973,7 @@ void launch_down(const AdapterArgs& a, const void* x, const void* W, float* h, i
     const Parts p = parts_of(a, D);
     const DownArgs d{rows, grid_of(grid_tiles(a), p.parts), x, W, h, D, a.r, p.steps};
     with_types(a, [&](auto dt, auto rt) {
-        const dim3 grid(8 * d.grid.per_xcd), block(64 * kDownWaves);
+        const dim3 grid(8 * d.grid.per_xcd, d.grid.slices()), block(64 * kDownWaves);
         if (D < 8 * lane_of<dt.value>()) hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, d);
         else hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, false>), grid, block, 0, stream, d);
     });
@@ -986,7 +989,7 @@ void launch_up(const AdapterArgs& a, const float* h, const void* W, const void* 
     const uint32_t across = (uint32_t)(most < want ? most : want);
     const UpArgs u{rows, grid_of(across, grid_tiles(a)), across, h, a.scale, W, base, out, N, a.r, parts_of(a, D).parts};
     with_types(a, [&](auto dt, auto rt) {
-        const dim3 grid(8 * u.grid.per_xcd), block(64 * kUpWaves);
+        const dim3 grid(8 * u.grid.per_xcd, u.grid.slices()), block(64 * kUpWaves);
         constexpr int L = lane_of<dt.value>();
         if (N < 16 * L || (MODE == kAlong && a.r < L)) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kShort>), grid, block, 0, stream, u);
         else if (N % L) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kOdd>), grid, block, 0, stream, u);
@@ -1039,7 +1042,7 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
         w.grid = grid_of(w.blocks + (uint32_t)((a.N + columns - 1) / columns), (uint32_t)a.n * w.split);
         if (w.split > 1) w.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + h_bytes(a, a.N));
         with_types(a, [&](auto dt, auto rt) {
-            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(8 * w.grid.per_xcd), dim3(64 * weight_waves(rt.value)), 0, stream, w);
+            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(8 * w.grid.per_xcd, w.grid.slices()), dim3(64 * weight_waves(rt.value)), 0, stream, w);
             if (w.split > 1) {
                 const int64_t all = (int64_t)a.n * a.r * (a.K + a.N);
                 hipLaunchKernelGGL((add_parts_kernel<dt.value>), dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, stream, w);
