@@ -189,6 +189,8 @@ __global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows 
 template <int DT, int R, bool WHOLE, int T>
 __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows k, float* parts)
 {
+    // rows that take more registers than there are beside the gradients' sums are read again for the result
+    constexpr bool kHold = R * T < 4096;
     __shared__ float lds[2][2 * (T / 64)];
     extern __shared__ float columns[];          // [2][C], where a workgroup has several rows at once
     const uint32_t group = threadIdx.x / k.width, t = threadIdx.x & (k.width - 1);
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
             s[r] = dy[r] = more[r] = Eight<DT>{};
             if (at.there) s[r] = at.template load<DT>(a.s, base);
             if (at.there) dy[r] = at.template load<DT>(a.dy, base);
-            if (at.there && a.dsum) more[r] = at.template load<DT>(a.dsum, base);
+            if (kHold && at.there && a.dsum) more[r] = at.template load<DT>(a.dsum, base);
         }
         const float2 stats = there ? reinterpret_cast<const float2*>(a.saved)[row] : make_float2(0.0f, 0.0f);
         float sums[2] = {0.0f, 0.0f};
@@ -237,6 +239,11 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
             s[r].renew();
             dy[r].renew();
             if (!at.there) continue;
+            if (!kHold) {
+                s[r] = at.template load<DT>(a.s, base);
+                dy[r] = at.template load<DT>(a.dy, base);
+                if (a.dsum) more[r] = at.template load<DT>(a.dsum, base);
+            }
             float w[8], v[8];
             at.params(a.weight, a.param_dtype, 1.0f, w);
 #pragma unroll
@@ -328,7 +335,7 @@ Rows rows_of(const LayerNormArgs& a, uint32_t most, uint32_t threads, int64_t wa
     Rows k{};
     const uint32_t vectors = (uint32_t)((a.C + 7) / 8);
     k.width = power_from(vectors) < 1024 ? power_from(vectors) : 1024;
-    auto need = [&](uint32_t width) { return power_from((vectors + width - 1) / width); };
+    auto need = [&](uint32_t width) { return (vectors + width - 1) / width; };
     while (k.width > 64 && need(k.width / 2) <= most && a.M * (k.width / 2) >= waves * 64) k.width /= 2;
     k.R = need(k.width);
     if (threads < k.width) threads = k.width;
@@ -340,7 +347,7 @@ constexpr uint32_t kFwdThreads = 256, kBwdThreads = 512;
 
 Rows fwd_rows(const LayerNormArgs& a)
 {
-    Rows k = rows_of(a, 2, kFwdThreads, 4096);
+    Rows k = rows_of(a, 3, kFwdThreads, 4096);
     const int64_t groups = (a.M + k.at_once - 1) / k.at_once;
     k.groups = (uint32_t)(groups < (1 << 20) ? groups : 1 << 20);
     return k;
@@ -348,7 +355,7 @@ Rows fwd_rows(const LayerNormArgs& a)
 Rows bwd_rows(const LayerNormArgs& a)
 {
     Rows k = rows_of(a, 2, kBwdThreads, 2048);
-    const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.R > 2 ? 1 : k.R > 1 ? 2 : 3);
+    const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.width == 1024 ? 1 : k.R > 1 ? 2 : 3);
     k.groups = (uint32_t)(groups < most ? groups : most);
     return k;
 }
@@ -369,6 +376,7 @@ void with_rows(const LayerNormArgs& a, const Rows& k, F f)
         };
         if (k.R == 1) held(integral_constant<int, 1>{});
         else if (k.R == 2) held(integral_constant<int, 2>{});
+        else if (k.R == 3) held(integral_constant<int, 3>{});
         else held(integral_constant<int, 4>{});
     };
     if (a.dtype == kBf16) of(integral_constant<int, kBf16>{});
