@@ -29,8 +29,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int kSubs = 2, kTile = 16 * kSubs;        // rows of a tile, in blocks of the matrix instruction
-constexpr int kDownWaves = 8, kUpWaves = 4, kMostParts = 4;
-constexpr int weight_waves(int RT) { return RT < 4 ? 4 : RT; }
+constexpr int kDownWaves = 8, kUpWaves = 4, kWeightWaves = 4, kMostParts = 4;
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kMostGroups = kAdaptersMost + 2;
 
 enum Mode { kAlong, kDown };        // memory runs along the contraction, or across it
@@ -146,26 +145,29 @@ __device__ __forceinline__ v4f multiply(const Piece& a, const Piece& b, v4f d)
     return d;
 }
 
-// 32-bit values as the matrix instructions take them: themselves, or two planes of bfloat16
+// planes of a value of 32 bits as the matrix instructions take it: itself, or two of bfloat16
 template <int DT>
 constexpr int planes_of() { return DT == kF32 ? 1 : 2; }
+
+// A value as two planes of bfloat16 side by side, the first, cut off, in the upper half, the second, rounded, in the lower: off by 2^-16
+// of itself at most.  (Equal: an infinity has no rest.)  So is h held by bfloat16 calls where it is no sum of parts.
+__device__ __forceinline__ uint32_t paired(float v)
+{
+    const float cut = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+    return (__float_as_uint(v) & 0xFFFF0000u) | (two_bf16(v == cut ? 0.0f : v - cut, 0.0f) & 0xFFFFu);
+}
+// the planes of such values, or those themselves
 template <int DT>
-__device__ __forceinline__ void split(const float (&v)[lane_of<DT>()], Piece (&to)[planes_of<DT>()])
+__device__ __forceinline__ void unpaired(const uint32_t (&v)[lane_of<DT>()], Piece (&to)[planes_of<DT>()])
 {
     if constexpr (DT == kF32) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) to[0].w[j] = __float_as_uint(v[j]);
+        for (int j = 0; j < 4; ++j) to[0].w[j] = v[j];
     } else {
-        float rest[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float cut = __uint_as_float(__float_as_uint(v[j]) & 0xFFFF0000u);
-            rest[j] = v[j] == cut ? 0.0f : v[j] - cut;                  // (equal: an infinity has no rest)
-        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            to[0].w[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]), 0x07060302u);
-            to[1].w[j] = two_bf16(rest[2 * j], rest[2 * j + 1]);
+            to[0].w[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x07060302u);
+            to[1].w[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], 0x05040100u);
         }
     }
 }
@@ -209,10 +211,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
     const uint32_t groups = (uint32_t)n + 2;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t rows = (M + 64 * kPlanWaves - 1) / (64 * kPlanWaves) * 64, first = wave * rows, end = first + rows < M ? first + rows : M;
-    // f(a row, its group, lanes with the same) for a wave's rows, 64 at a time, kAhead of those loaded before the first is taken; where
-    // that is all of them, they are loaded once
+    // f(u, a row, its group, lanes with the same) for a wave's rows, 64 at a time, kAhead of those loaded before the first is taken; where
+    // that is all of them, they are loaded, and looked through for their like, once
     constexpr int kAhead = 8;
+    const bool once = rows <= 64 * kAhead;
     int64_t id[kAhead];
+    uint32_t before_it[kAhead];             // rows of the group in the wave before a lane's
     auto load = [&](int64_t i) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -225,20 +229,24 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
     __syncthreads();
     auto each = [&](auto f) {
         for (int64_t i = first; i < end; i += 64 * kAhead) {
-            if (rows > 64 * kAhead) load(i);
+            if (!once) load(i);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int64_t at = i + 64 * u + lane;
                 if (i + 64 * u >= end) break;
-                const bool there = at < end;
-                const uint32_t g = group_of(id[u], n);
-                f(at, g, there, same_lanes(g, bits, __ballot(there)));
+                f(u, at, group_of(id[u], n), at < end);
             }
         }
     };
-    each([&](int64_t, uint32_t g, bool there, uint64_t same) {
-        if (there && (same & ((1ull << lane) - 1)) == 0) counts[wave][g] += (uint32_t)__popcll(same);
-    });
+    // the group's rows of the wave so far, and those of this 64 before a lane's, which are counted
+    auto count = [&](uint32_t g, bool there) {
+        const uint64_t same = same_lanes(g, bits, __ballot(there));
+        const int leader = __ffsll((unsigned long long)same) - 1;
+        uint32_t at = 0;
+        if (there && lane == leader) at = atomicAdd(&counts[wave][g], (uint32_t)__popcll(same));
+        return __shfl(at, leader & 63) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+    };
+    each([&](int u, int64_t, uint32_t g, bool there) { before_it[u] = count(g, there); });
     __syncthreads();
     // a thread's two groups: their rows and tiles, and the sums of those of the groups before
     uint32_t have[2] = {0, 0}, cut[2];
@@ -291,12 +299,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
         }
         const_cast<uint2*>(p.tile)[i] = make_uint2(lo, starts[lo] + kTile * (i - tiles[lo]));
     }
-    each([&](int64_t row, uint32_t g, bool there, uint64_t same) {
-        const int leader = __ffsll((unsigned long long)same) - 1;
-        uint32_t at = 0;
-        if (there && lane == leader) at = atomicAdd(&counts[wave][g], (uint32_t)__popcll(same));
-        at = __shfl(at, leader & 63);
-        if (there) order[starts[g] + at + (uint32_t)__popcll(same & ((1ull << lane) - 1))] = (uint32_t)row;
+    each([&](int u, int64_t row, uint32_t g, bool there) {
+        const uint32_t at = once ? (there ? counts[wave][g] : 0) + before_it[u] : count(g, there);
+        if (there) order[starts[g] + at] = (uint32_t)row;
     });
 }
 
@@ -392,7 +397,7 @@ struct DownArgs {
     float* h;                       // [parts][M][16 RT]
     int64_t D;
     int r;
-    uint32_t steps;                 // of the contraction: how many times 8 kLane a part has
+    uint32_t steps, parts;          // of the contraction: how many times 8 kLane a part has, parts
 };
 
 // The sums of a workgroup's waves, in the first one's
@@ -565,7 +570,8 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
 #pragma unroll
                         for (int t = 0; t < RL; ++t) {
                             const int c = 16 * RL * q + RL * j + t;
-                            to[rank[q] + t] = acc[s][RL * q + t][i];
+                            const float v = acc[s][RL * q + t][i];
+                            to[rank[q] + t] = DT == kBf16 && a.parts == 1 ? __uint_as_float(paired(v)) : v;
                             if (c >= a.r) to[c] = 0.0f;     // (behind the last rank)
                         }
                 }
@@ -589,26 +595,39 @@ struct UpArgs {
     uint32_t parts;
 };
 
-// a row's values, all parts together (four are asked for at once), times `scale`
-template <int N>
-__device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t parts, float scale, float (&v)[N])
+// Planes of a row's values, all parts together (four are asked for at once), the first `skip` taken for zeros: P of them, or, of two in one
+// (P = 1), a lane's own.  (Chosen word by word: a choice between the two in memory would put them into LDS, at an address that a load from
+// the host's queue decides, 10 us of a small call.)
+template <int DT, int P>
+__device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t parts, int skip, bool second, Piece (&to)[P])
 {
-    constexpr int B = kMostParts, V = N / 4;
-    v4f q[B][V];
+    constexpr int N = lane_of<DT>(), V = N / 4;
+    v4f q[V];
 #pragma unroll
-    for (int u = 0; u < B; ++u)
-        if (u == 0 || parts > 1)
+    for (int j = 0; j < V; ++j) q[j] = reinterpret_cast<const v4f*>(h)[j];
+    if (parts > 1) {
+        v4f more[kMostParts - 1][V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) q[u][j] = reinterpret_cast<const v4f*>(h + (u < (int)parts ? u : 0) * part)[j];
-        else
+        for (int u = 1; u < kMostParts; ++u)
 #pragma unroll
-            for (int j = 0; j < V; ++j) q[u][j] = v4f{};
+            for (int j = 0; j < V; ++j) more[u - 1][j] = reinterpret_cast<const v4f*>(h + (u < (int)parts ? u : 0) * part)[j];
 #pragma unroll
-    for (int u = 1; u < B; ++u)
+        for (int u = 1; u < kMostParts; ++u)
 #pragma unroll
-        for (int j = 0; j < V; ++j) q[0][j] += u < (int)parts ? q[u][j] : v4f{};
+            for (int j = 0; j < V; ++j) q[j] += u < (int)parts ? more[u - 1][j] : v4f{};
+        if constexpr (DT == kBf16)
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = q[0][j / 4][j % 4] * scale;
+            for (int j = 0; j < N; ++j) q[j / 4][j % 4] = __uint_as_float(paired(q[j / 4][j % 4]));
+    }
+    uint32_t v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = j < skip ? 0u : __float_as_uint(q[j / 4][j % 4]);
+    if constexpr (DT == kBf16 && P == 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[0].w[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], second ? 0x05040100u : 0x07060302u);
+    } else {
+        unpaired<DT>(v, to);
+    }
 }
 
 // How columns end.  kShort: there are fewer than a wave has, or (kAlong) fewer ranks than a load, and W and base are loaded element by
@@ -632,7 +651,8 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
     const bool none = rows.group == (uint32_t)a.rows.n, wrong = rows.group > (uint32_t)a.rows.n;
     if (none && a.base == a.out) return;
     const char* W = static_cast<const char*>(a.W) + (none || wrong ? 0 : (int64_t)rows.group * a.N * a.r * (16 / L));
-    const float scale = a.scale && !none && !wrong ? a.scale[rows.group] : 1.0f;
+    // (rows without an adapter: minus one times zero, which leaves any base as it is)
+    const float scale = wrong ? __builtin_nanf("") : none ? -1.0f : a.scale ? a.scale[rows.group] : 1.0f;
     // a lane's ranks of a chunk: from first(c) on, those before own(c) another lane's
     auto own = [&](int c) { return kChunk * c + L * (kFolded ? g & 1 : g); };
     auto first = [&](int c) { return MODE == kDown || SHORT || own(c) + L <= a.r ? own(c) : a.r - L; };
@@ -646,7 +666,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
         // a lane's columns from c0 on: from col, those from lo to hi its own
         int64_t col;
         int lo, hi;
-        Piece base[kSubs][4], w[L];
+        Piece base[kSubs][4] = {}, w[L];
         auto lines = [&](int c) {
 #pragma unroll
             for (int e = 0; e < L; ++e) {
@@ -679,24 +699,11 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
         for (int f = wave; f < kSubs * C; f += kUpWaves) {
             const int s = f / C, c = f % C;
             const uint32_t of = __shfl(all, 16 * s + j);
-            float v[L] = {};
-            if (!none && !wrong) load_h<L>(a.h + (int64_t)of * kRanks + first(c), a.rows.M * kRanks, a.parts, scale, v);
-            if (MODE == kAlong && !SHORT)
+            Piece planes[P];
+            if (none || wrong) continue;
+            load_h<DT, P>(a.h + (int64_t)of * kRanks + first(c), a.rows.M * kRanks, a.parts, own(c) - first(c), g >= 2, planes);
 #pragma unroll
-                for (int e = 0; e < L; ++e) v[e] = first(c) + e >= own(c) ? v[e] : 0.0f;
-            Piece two[planes_of<DT>()];
-            split<DT>(v, two);
-            if constexpr (kFolded) {
-                // (word by word: a choice between the two in memory would put them into LDS, at an address that a load from the
-                // host's queue decides: 10 us)
-                Piece of_lane;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) of_lane.w[k] = g < 2 ? two[0].w[k] : two[1].w[k];
-                h[f][0][lane] = of_lane;
-            } else {
-#pragma unroll
-                for (int k = 0; k < P; ++k) h[f][k][lane] = two[k];
-            }
+            for (int k = 0; k < P; ++k) h[f][k][lane] = planes[k];
         }
         __syncthreads();
         for (; c0 < a.N; c0 += step) {
@@ -725,8 +732,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
                     float v[L];
 #pragma unroll
                     for (int t = 0; t < L; ++t) {
-                        v[t] = wrong ? __builtin_nanf("") : acc[s][t][i];
-                        if (a.base) v[t] += value<DT>(base[s][i], t);
+                        v[t] = fmaf(scale, acc[s][t][i], value<DT>(base[s][i], t));
                     }
                     if (place + 16 * s + 4 * g + i >= rows.count || hi <= 0 || lo >= L) continue;
                     if constexpr (END == kEven) store_piece<DT>(a.out, row[s][i] * a.N + col, 0, L, piece_of<DT>(v));
@@ -758,14 +764,15 @@ struct WeightArgs {
     __device__ __forceinline__ int64_t of_dA() const { return (int64_t)rows.n * r * N[0]; }
 };
 
-// A workgroup has 128 columns (64 in fp32) and all ranks of one gradient: a wave two tiles of ranks at most, and of the rows what the
-// waves with the same ranks share.
+// A workgroup has 128 columns (64 in fp32) and all ranks of one gradient: a wave four tiles of ranks at most, and of the rows what the
+// waves with the same ranks share.  Tile t of a wave: line m is rank rank0 + RL m + t, so that a load of h has a lane's ranks of all
+// its tiles.
 template <int DT, int RT>
-__global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightArgs a)
+__global__ __launch_bounds__(64 * kWeightWaves, 2) void weights_kernel(WeightArgs a)
 {
-    constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L, P = planes_of<DT>(), RW = 1;
-    constexpr int kWaves = weight_waves(RT), kShares = kWaves / RT;
-    __shared__ v4f sums[kShares > 1 ? kWaves / 2 : 1][RW][L][64];
+    constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L, P = planes_of<DT>(), RL = RT < 2 ? RT : DT == kBf16 || RT < 4 ? 2 : 4;
+    constexpr int kShares = kWeightWaves / (RT / RL);
+    __shared__ v4f sums[kWeightWaves / 2][RL][L][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     uint32_t block, which;
     if (!place_of(a.grid, block, which)) return;
@@ -773,11 +780,11 @@ __global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightAr
     if (!a.out[of]) return;
     const int64_t N = a.N[of], c0 = (int64_t)(block - (of ? a.blocks : 0)) * kColumns, col = c0 + L * j;
     const uint32_t adapter = divide(which, a.by_split), part = which - adapter * a.split;
-    const int rank0 = wave / kShares * (16 * RW), share = wave % kShares;
+    const int half = wave / kShares, rank0 = 16 * RL * half, share = wave % kShares;
     const Group rows = adapter_rows(a.rows, adapter);
-    const float* h = a.h[of] + rank0 + j;
+    const float* h = a.h[of] + rank0 + RL * j;
     const int n = col + L <= N ? L : col < N ? (int)(N - col) : 0;
-    v4f acc[RW][L] = {};
+    v4f acc[RL][L] = {};
     auto sum = [&](auto whole) {
         constexpr bool WHOLE = whole.value;
         // (as often for every lane of a wave: the rows of a few are handed from lane to lane)
@@ -785,37 +792,51 @@ __global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightAr
         uint32_t first = kChunk * (part * kShares + share), next = 0;
         if (first < rows.count) next = rows.rows(first);
         for (; first < rows.count; first += step) {
+            const uint32_t now = next;
             Piece lines[L];
-            float u[RW][L];
+            float u[L][RL];
 #pragma unroll
             for (int e = 0; e < L; ++e) {
-                const int64_t row = __shfl(next, L * g + e);               // (behind the last: one that there is, taken for zeros)
+                const uint32_t row = __shfl(now, L * g + e);               // (behind the last: one that there is, taken for zeros)
                 lines[e] = load_piece<DT, WHOLE>(a.v[of], row * N + (WHOLE || n > 0 ? col : 0), n);
-#pragma unroll
-                for (int t = 0; t < RW; ++t) {
-                    u[t][e] = h[row * (16 * RT) + 16 * t];
-                    for (uint32_t s = 1; s < a.parts[of]; ++s) u[t][e] += h[(s * a.rows.M + row) * (16 * RT) + 16 * t];
-                }
+                __builtin_memcpy(u[e], h + row * (uint32_t)(16 * RT), 4 * RL);
             }
             const uint32_t ahead = first + step;
             if (ahead < rows.count) next = rows.rows(ahead);
+            if (a.parts[of] > 1)
 #pragma unroll
-            for (int e = 0; e < L; ++e) {
-                const bool has = first + L * g + e < rows.count;
-                lines[e] = only_if(has, lines[e]);
+                for (int e = 0; e < L; ++e) {
+                    const uint32_t row = __shfl(now, L * g + e);
+                    for (uint32_t s = 1; s < a.parts[of]; ++s)
 #pragma unroll
-                for (int t = 0; t < RW; ++t) u[t][e] = has ? u[t][e] : 0.0f;
+                        for (int t = 0; t < RL; ++t) u[e][t] += h[(s * a.rows.M + row) * (16 * RT) + t];
+#pragma unroll
+                    for (int t = 0; t < RL; ++t)
+                        if (DT == kBf16) u[e][t] = __uint_as_float(paired(u[e][t]));
+                }
+            if (first + kChunk > rows.count)
+#pragma unroll
+                for (int e = 0; e < L; ++e) {
+                    const bool has = first + L * g + e < rows.count;
+                    lines[e] = only_if(has, lines[e]);
+#pragma unroll
+                    for (int t = 0; t < RL; ++t) u[e][t] = has ? u[e][t] : 0.0f;
+                }
+            Piece up[RL][P];
+#pragma unroll
+            for (int t = 0; t < RL; ++t) {
+                uint32_t v[L];
+#pragma unroll
+                for (int e = 0; e < L; ++e) v[e] = __float_as_uint(u[e][t]);
+                unpaired<DT>(v, up[t]);
             }
-            Piece up[RW][P];
-#pragma unroll
-            for (int t = 0; t < RW; ++t) split<DT>(u[t], up[t]);
 #pragma unroll
             for (int c = 0; c < L; ++c) {
                 const Piece w = turned<DT>(lines, c);
 #pragma unroll
-                for (int t = 0; t < RW; ++t)
+                for (int k = P - 1; k >= 0; --k)
 #pragma unroll
-                    for (int k = P - 1; k >= 0; --k) acc[t][c] = multiply<DT>(up[t][k], w, acc[t][c]);
+                    for (int t = 0; t < RL; ++t) acc[t][c] = multiply<DT>(up[t][k], w, acc[t][c]);
             }
         }
     };
@@ -824,31 +845,31 @@ __global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightAr
     // the waves with the same ranks together, as far as there were rows for them
     const uint32_t begun = part * kShares * kChunk;
 #pragma unroll
-    for (int half = kShares / 2; half; half /= 2) {
-        if (rows.count <= begun + half * kChunk) continue;
+    for (int m = kShares / 2; m; m /= 2) {
+        if (rows.count <= begun + m * kChunk) continue;
         __syncthreads();
-        if (share >= half && share < 2 * half)
+        if (share >= m && share < 2 * m)
 #pragma unroll
-            for (int t = 0; t < RW; ++t)
+            for (int t = 0; t < RL; ++t)
 #pragma unroll
-                for (int c = 0; c < L; ++c) sums[(rank0 / (16 * RW)) * (kShares / 2) + share - half][t][c][lane] = acc[t][c];
+                for (int c = 0; c < L; ++c) sums[half * (kShares / 2) + share - m][t][c][lane] = acc[t][c];
         __syncthreads();
-        if (share < half)
+        if (share < m)
 #pragma unroll
-            for (int t = 0; t < RW; ++t)
+            for (int t = 0; t < RL; ++t)
 #pragma unroll
-                for (int c = 0; c < L; ++c) acc[t][c] += sums[(rank0 / (16 * RW)) * (kShares / 2) + share][t][c][lane];
+                for (int c = 0; c < L; ++c) acc[t][c] += sums[half * (kShares / 2) + share][t][c][lane];
     }
     if (share || n <= 0) return;
     const float scale = a.scale ? a.scale[adapter] : 1.0f;
     float* parts = a.sums ? a.sums + (int64_t)part * a.of_a_part() + (of ? a.of_dA() : 0) : nullptr;
-    // a lane has ranks rank0 + 16 t + 4 g + i of columns col + c: of a rank's run in dB kLane elements, of a column's in dA four
+    // a lane has ranks rank0 + RL (4 g + i) + t of columns col + c: of a rank's run in dB kLane elements, of a column's in dA RL of each i
     if (of) {
 #pragma unroll
-        for (int t = 0; t < RW; ++t)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int rank = rank0 + 16 * t + 4 * g + i;
+            for (int t = 0; t < RL; ++t) {
+                const int rank = rank0 + RL * (4 * g + i) + t;
                 if (rank >= a.r) continue;
                 const int64_t to = ((int64_t)adapter * a.r + rank) * N + col;
                 float v[L];
@@ -864,27 +885,28 @@ __global__ __launch_bounds__(64 * weight_waves(RT)) void weights_kernel(WeightAr
             }
         return;
     }
+    const int rank = rank0 + 4 * RL * g, left = a.r - rank;
 #pragma unroll
     for (int c = 0; c < L; ++c) {
-        if (c >= n) continue;
+        if (c >= n || left <= 0) continue;
+        const int64_t to = ((int64_t)adapter * N + col + c) * a.r + rank;
+        float v[4 * RL];
 #pragma unroll
-        for (int t = 0; t < RW; ++t) {
-            const int rank = rank0 + 16 * t + 4 * g, left = a.r - rank < 4 ? a.r - rank : 4;
-            const int64_t to = ((int64_t)adapter * N + col + c) * a.r + rank;
-            const v4f v = scale * acc[t][c];
-            if (left == 4 && !parts && DT == kBf16) {
-                const uint32_t two[2] = {two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
-                __builtin_memcpy(static_cast<uint16_t*>(a.out[0]) + to, two, 8);
-            } else if (left == 4) {
-                __builtin_memcpy((parts ? parts : static_cast<float*>(a.out[0])) + to, &v, 16);
-            } else {
+        for (int m = 0; m < 4 * RL; ++m) v[m] = scale * acc[m % RL][c][m / RL];
+        if (left >= 4 * RL && !parts && DT == kBf16) {
+            uint32_t two[2 * RL];
 #pragma unroll
-                for (int i = 0; i < 3; ++i)
-                    if (i < left) {
-                        if (parts) parts[to + i] = v[i];
-                        else store_as<DT>(a.out[0], to + i, v[i]);
-                    }
-            }
+            for (int m = 0; m < 2 * RL; ++m) two[m] = two_bf16(v[2 * m], v[2 * m + 1]);
+            __builtin_memcpy(static_cast<uint16_t*>(a.out[0]) + to, two, 8 * RL);
+        } else if (left >= 4 * RL) {
+            __builtin_memcpy((parts ? parts : static_cast<float*>(a.out[0])) + to, v, 16 * RL);
+        } else {
+#pragma unroll
+            for (int m = 0; m < 4 * RL; ++m)
+                if (m < left) {
+                    if (parts) parts[to + m] = v[m];
+                    else store_as<DT>(a.out[0], to + m, v[m]);
+                }
         }
     }
 }
@@ -971,7 +993,7 @@ void launch_down(const AdapterArgs& a, const void* x, const void* W, float* h, i
 {
     ProfileScope ps(K_ADAPT_DOWN, stream);
     const Parts p = parts_of(a, D);
-    const DownArgs d{rows, grid_of(grid_tiles(a), p.parts), x, W, h, D, a.r, p.steps};
+    const DownArgs d{rows, grid_of(grid_tiles(a), p.parts), x, W, h, D, a.r, p.steps, p.parts};
     with_types(a, [&](auto dt, auto rt) {
         const dim3 grid(8 * d.grid.per_xcd, d.grid.slices()), block(64 * kDownWaves);
         if (D < 8 * lane_of<dt.value>()) hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, d);
@@ -1042,7 +1064,7 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
         w.grid = grid_of(w.blocks + (uint32_t)((a.N + columns - 1) / columns), (uint32_t)a.n * w.split);
         if (w.split > 1) w.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + h_bytes(a, a.N));
         with_types(a, [&](auto dt, auto rt) {
-            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(8 * w.grid.per_xcd, w.grid.slices()), dim3(64 * weight_waves(rt.value)), 0, stream, w);
+            hipLaunchKernelGGL((weights_kernel<dt.value, rt.value>), dim3(8 * w.grid.per_xcd, w.grid.slices()), dim3(64 * kWeightWaves), 0, stream, w);
             if (w.split > 1) {
                 const int64_t all = (int64_t)a.n * a.r * (a.K + a.N);
                 hipLaunchKernelGGL((add_parts_kernel<dt.value>), dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, stream, w);
