@@ -177,7 +177,7 @@ __device__ __forceinline__ void unpaired(const uint32_t (&v)[lane_of<DT>()], Pie
 // groups: an adapter's rows for each of n; n: rows without one; n + 1: rows whose number is none
 __device__ __forceinline__ uint32_t group_of(int64_t id, int n) { return id < 0 ? (uint32_t)n : id < n ? (uint32_t)id : (uint32_t)n + 1; }
 
-// The plan in memory: start[groups + 1] (a group's first place in the order), tiles, order[M] (rows), tile[..] (group, first place)
+// The plan in memory, of more rows than a wave sees at once: start[groups + 1] (a group's first place in the order), tiles, order[M] (rows), tile[..] (group, first place)
 struct Plan {
     const uint32_t *start, *tiles, *order;
     const uint2* tile;
@@ -190,7 +190,7 @@ __host__ __device__ inline Plan plan_at(const void* p, int64_t M, int n)
     return {w, w + n + 3, w + n + 4, reinterpret_cast<const uint2*>(w + (plan_words(M, n) + 1) / 2 * 2)};
 }
 
-constexpr int64_t kDirect = 64;         // as many rows a wave sees at once
+constexpr int64_t kDirect = 256;        // as many rows a wave sees at once
 
 // lanes with the same value of `bits` bits
 __device__ __forceinline__ uint64_t same_lanes(uint32_t v, int bits, uint64_t among)
@@ -305,29 +305,28 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
     });
 }
 
-// Rows of one group, for a wave: `count` of them, place p's row by row(p).
+constexpr int kWords = (int)(kDirect / 64);
+
+// Rows of one group, for a wave: `count` of them from place `first` of the group on.
 struct Group {
-    uint32_t group, count;
-    const uint32_t* order;          // the plan's, from the group's or the tile's first place on, or null:
-    uint32_t listed;                // of up to 64 rows, lane p has place p's
-    // lane l's: the row at place `from` + l, the last one's behind it
+    uint32_t group, count, first;
+    const uint32_t* order;          // the plan's, from the group's first place on, or null: of few rows,
+    uint32_t listed[kWords];        // 64 at a time, lane p has the p-th of the group, of which
+    uint32_t start[kWords];         // so many are before these 64
+    // lane l's: the row at place first + `from` + l, the last one's behind it
     __device__ __forceinline__ uint32_t rows(uint32_t from) const
     {
-        const uint32_t at = from + (threadIdx.x & 63), place = at < count ? at : count - 1;
-        return order ? order[place] : __shfl(listed, (int)place);
+        const uint32_t at = from + (threadIdx.x & 63), place = first + (at < count ? at : count - 1);
+        if (order) return order[place];
+        uint32_t row = __shfl(listed[0], (int)place);
+#pragma unroll
+        for (int w = 1; w < kWords; ++w) {
+            const uint32_t other = __shfl(listed[w], (int)(place - start[w]));
+            row = place >= start[w] ? other : row;
+        }
+        return row;
     }
 };
-
-// of up to 64 rows, those of a group
-__device__ __forceinline__ Group listed_group(uint32_t group, uint32_t of_lane, bool there)
-{
-    const int lane = threadIdx.x & 63;
-    const uint64_t same = __ballot(there && of_lane == group);
-    const uint64_t lower = (1ull << lane) - 1;
-    // (the others go behind them, each to a place of its own)
-    const int count = __popcll(same), to = same >> lane & 1 ? __popcll(same & lower) : count + __popcll(~same & lower);
-    return {group, (uint32_t)count, nullptr, (uint32_t)__builtin_amdgcn_ds_permute(4 * to, lane)};
-}
 
 struct RowArgs {
     const int64_t* ids;
@@ -358,34 +357,76 @@ __device__ __forceinline__ bool place_of(const Grid& k, uint32_t& inner, uint32_
     return idx < k.total && outer < k.outer;
 }
 
-// The rows of workgroup `tile`: none where there is no such tile, or where an earlier row of the few has them.
+// of few rows, those of a group; which(a lane's groups of every 64) says which
+template <class F>
+__device__ __forceinline__ Group listed_rows(const RowArgs& a, F which)
+{
+    const int lane = threadIdx.x & 63;
+    const uint64_t lower = (1ull << lane) - 1;
+    uint32_t g[kWords];
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        const int64_t row = 64 * w + lane;
+        g[w] = row < a.M ? group_of(a.ids[row], a.n) : ~0u;
+    }
+    Group of{};
+    of.group = which(g);
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        const uint64_t same = __ballot(g[w] == of.group);
+        // (the others go behind them, each to a place of its own)
+        const int count = __popcll(same), to = same >> lane & 1 ? __popcll(same & lower) : count + __popcll(~same & lower);
+        of.listed[w] = 64 * w + (uint32_t)__builtin_amdgcn_ds_permute(4 * to, lane);
+        of.start[w] = of.count;
+        of.count += (uint32_t)count;
+    }
+    return of;
+}
+
+// The rows of workgroup `tile`, 32 at most: none where there is no such tile.  Of few rows, every 32nd of a group stands for a tile.
 __device__ __forceinline__ Group tile_rows(const RowArgs& a, uint32_t tile)
 {
     if (a.M <= kDirect) {
-        const int lane = threadIdx.x & 63;
-        const bool there = lane < a.M;
-        const uint32_t g = there ? group_of(a.ids[lane], a.n) : 0;
-        const uint32_t mine = __shfl(g, (int)tile);
-        Group of = listed_group(mine, g, there);
-        const uint64_t same = __ballot(there && g == mine);
-        if ((uint32_t)__ffsll((unsigned long long)same) - 1 != tile) of.count = 0;
+        uint32_t before = 0;        // rows of the group before the tile's
+        Group of = listed_rows(a, [&](const uint32_t (&g)[kWords]) {
+            uint32_t mine = 0;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                const uint32_t there = __shfl(g[w], (int)(tile & 63));
+                mine = tile >> 6 == (uint32_t)w ? there : mine;
+            }
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                const uint64_t same = __ballot(g[w] == mine), until = (1ull << (tile & 63)) - 1;
+                before += (uint32_t)w < tile >> 6 ? __popcll(same) : (uint32_t)w == tile >> 6 ? __popcll(same & until) : 0;
+            }
+            return mine;
+        });
+        of.first = before;
+        of.count = before % kTile ? 0 : of.count - before < kTile ? of.count - before : kTile;
         return of;
     }
     const Plan p = plan_at(a.plan, a.M, a.n);
-    if (tile >= *p.tiles) return {0, 0, p.order, 0};
+    Group of{};
+    of.order = p.order;
+    if (tile >= *p.tiles) return of;
     const uint2 t = p.tile[tile];
     const uint32_t left = p.start[t.x + 1] - t.y;
-    return {t.x, left < kTile ? left : kTile, p.order + t.y, 0};
+    of.group = t.x;
+    of.count = left < kTile ? left : kTile;
+    of.first = t.y;
+    return of;
 }
 __device__ __forceinline__ Group adapter_rows(const RowArgs& a, uint32_t adapter)
 {
-    if (a.M <= kDirect) {
-        const int lane = threadIdx.x & 63;
-        const bool there = lane < a.M;
-        return listed_group(adapter, there ? group_of(a.ids[lane], a.n) : 0, there);
-    }
+    if (a.M <= kDirect) return listed_rows(a, [&](const uint32_t (&)[kWords]) { return adapter; });
     const Plan p = plan_at(a.plan, a.M, a.n);
-    return {adapter, p.start[adapter + 1] - p.start[adapter], p.order + p.start[adapter], 0};
+    Group of{};
+    of.group = adapter;
+    of.order = p.order;
+    of.first = p.start[adapter];
+    of.count = p.start[adapter + 1] - of.first;
+    return of;
 }
 
 // ---- down ----
@@ -451,132 +492,129 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
     }
     const int64_t first = (int64_t)part * a.steps, all = (a.D + kStep - 1) / kStep;
     const int64_t last = first + a.steps < all ? first + a.steps : all;
-    for (uint32_t place = 0; place < rows.count; place += kTile) {
-        const uint32_t row = rows.rows(place);
-        v4f acc[kSubs][RT] = {};
-        // the chunk's products: x's fragments, and W's lines across the contraction or fragments along it
-        auto products = [&](const Piece (&x)[kSubs], const Piece (&w)[RQ][MODE == kDown ? L : RL]) {
+    const uint32_t row = rows.rows(0);
+    v4f acc[kSubs][RT] = {};
+    // the chunk's products: x's fragments, and W's lines across the contraction or fragments along it
+    auto products = [&](const Piece (&x)[kSubs], const Piece (&w)[RQ][MODE == kDown ? L : RL]) {
+#pragma unroll
+        for (int q = 0; q < RQ; ++q)
+#pragma unroll
+            for (int t = 0; t < RL; ++t) {
+                Piece b;
+                if constexpr (MODE == kDown) b = turned<DT>(w[q], t);
+                else b = w[q][t];
+#pragma unroll
+                for (int s = 0; s < kSubs; ++s) acc[s][RL * q + t] = multiply<DT>(x[s], b, acc[s][RL * q + t]);
+            }
+    };
+    if constexpr (SHORT) {
+        for (int64_t k0 = (first + wave) * kStep; k0 < a.D && first + wave < last; k0 += kChunk) {
+            const int64_t k = k0 + L * g;
+            const int n = (int)(a.D - k);
+            const int64_t in = n <= 0 ? 0 : k;
+            Piece x[kSubs], w[RQ][MODE == kDown ? L : RL];
+#pragma unroll
+            for (int s = 0; s < kSubs; ++s) x[s] = load_piece<DT, false>(a.x, (int64_t)__shfl(row, 16 * s + j) * a.D + in, n);
 #pragma unroll
             for (int q = 0; q < RQ; ++q)
 #pragma unroll
-                for (int t = 0; t < RL; ++t) {
-                    Piece b;
-                    if constexpr (MODE == kDown) b = turned<DT>(w[q], t);
-                    else b = w[q][t];
-#pragma unroll
-                    for (int s = 0; s < kSubs; ++s) acc[s][RL * q + t] = multiply<DT>(x[s], b, acc[s][RL * q + t]);
+                for (int e = 0; e < (MODE == kDown ? L : RL); ++e) {
+                    if constexpr (MODE == kDown) w[q][e] = only_if(e < n, load_few<DT, RL, true>(W, (e < n ? k + e : 0) * a.r + rank[q], RL));
+                    else w[q][e] = load_piece<DT, false>(W, (int64_t)(rank[q] + e) * a.D + in, n);
                 }
-        };
-        if constexpr (SHORT) {
-            for (int64_t k0 = (first + wave) * kStep; k0 < a.D && first + wave < last; k0 += kChunk) {
-                const int64_t k = k0 + L * g;
-                const int n = (int)(a.D - k);
-                const int64_t in = n <= 0 ? 0 : k;
-                Piece x[kSubs], w[RQ][MODE == kDown ? L : RL];
-#pragma unroll
-                for (int s = 0; s < kSubs; ++s) x[s] = load_piece<DT, false>(a.x, (int64_t)__shfl(row, 16 * s + j) * a.D + in, n);
-#pragma unroll
-                for (int q = 0; q < RQ; ++q)
-#pragma unroll
-                    for (int e = 0; e < (MODE == kDown ? L : RL); ++e) {
-                        if constexpr (MODE == kDown) w[q][e] = only_if(e < n, load_few<DT, RL, true>(W, (e < n ? k + e : 0) * a.r + rank[q], RL));
-                        else w[q][e] = load_piece<DT, false>(W, (int64_t)(rank[q] + e) * a.D + in, n);
-                    }
-                products(x, w);
-            }
-        } else {
-            char* const mine = lds + 128 * kRows * wave;
-            // a lane's pieces: piece l % 8 of rows l / 8, 8 + l / 8, ..: the tile's rows, then the ranks in the fragments' order
-            const char* from[kLoads];
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int at = 8 * i + lane / 8;
-                if (8 * i < kTile) {
-                    from[i] = static_cast<const char*>(a.x) + (int64_t)__shfl(row, at) * a.D * (16 / L);
-                } else {
-                    const int f = at - kTile, c = 16 * RL * (f / (16 * RL)) + RL * (f % 16);        // fragment f / 16 - RL q, line f % 16
-                    from[i] = W + (int64_t)((c + RL <= a.r ? c : a.r - RL) + f / 16 % RL) * a.D * (16 / L);
-                }
-                from[i] += 16 * (lane % 8);
-            }
-            Piece next[kLoads], lines[2][MODE == kDown ? RQ : 1][MODE == kDown ? L : 1];
-            auto load = [&](int64_t step) {
-                const int64_t k = (step + 1) * kStep <= a.D ? step * kStep : a.D - kStep;
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) __builtin_memcpy(next[i].w, from[i] + k * (16 / L), 16);
-                if constexpr (MODE == kDown)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int q = 0; q < RQ; ++q)
-#pragma unroll
-                            for (int e = 0; e < L; ++e) lines[c][q][e] = load_few<DT, RL, true>(W, (k + kChunk * c + L * g + e) * a.r + rank[q], RL);
-            };
-            int64_t step = first + wave;
-            if (step < last) load(step);
-            for (; step < last; step += kDownWaves) {
-                const int skip = (step + 1) * kStep <= a.D ? 0 : (int)((step + 1) * kStep - a.D);
-                if (skip) {
-#pragma unroll
-                    for (int i = 0; i < kLoads; ++i) next[i] = without<DT>(next[i], skip - L * (lane % 8));
-                    if constexpr (MODE == kDown)
-#pragma unroll
-                        for (int c = 0; c < 2; ++c)
-#pragma unroll
-                            for (int q = 0; q < RQ; ++q)
-#pragma unroll
-                                for (int e = 0; e < L; ++e) lines[c][q][e] = only_if(kChunk * c + L * g + e >= skip, lines[c][q][e]);
-                }
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i)
-                    *reinterpret_cast<Piece*>(mine + 1024 * i + 128 * (lane / 8) + 16 * ((lane ^ lane / 8) % 8)) = next[i];
-                Piece w[2][RQ][MODE == kDown ? L : RL];
-                if constexpr (MODE == kDown)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int q = 0; q < RQ; ++q)
-#pragma unroll
-                            for (int e = 0; e < L; ++e) w[c][q][e] = lines[c][q][e];
-                if (step + kDownWaves < last) load(step + kDownWaves);
-                auto fragment = [&](int f, int c) {         // 16 rows from 16 f on
-                    return *reinterpret_cast<const Piece*>(mine + 2048 * f + 128 * j + 16 * ((4 * c + g) ^ (j & 7)));
-                };
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    Piece x[kSubs];
-#pragma unroll
-                    for (int s = 0; s < kSubs; ++s) x[s] = fragment(s, c);
-                    if constexpr (MODE == kAlong)
-#pragma unroll
-                        for (int q = 0; q < RQ; ++q)
-#pragma unroll
-                            for (int t = 0; t < RL; ++t) w[c][q][t] = fragment(kSubs + RL * q + t, c);
-                    products(x, w[c]);
-                }
-            }
+            products(x, w);
         }
-        join_waves<RT>(acc, reinterpret_cast<v4f*>(lds), wave, lane);
-        if (wave == 0)
+    } else {
+        char* const mine = lds + 128 * kRows * wave;
+        // a lane's pieces: piece l % 8 of rows l / 8, 8 + l / 8, ..: the tile's rows, then the ranks in the fragments' order
+        const char* from[kLoads];
 #pragma unroll
-            for (int s = 0; s < kSubs; ++s)
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = 8 * i + lane / 8;
+            if (8 * i < kTile) {
+                from[i] = static_cast<const char*>(a.x) + (int64_t)__shfl(row, at) * a.D * (16 / L);
+            } else {
+                const int f = at - kTile, c = 16 * RL * (f / (16 * RL)) + RL * (f % 16);        // fragment f / 16 - RL q, line f % 16
+                from[i] = W + (int64_t)((c + RL <= a.r ? c : a.r - RL) + f / 16 % RL) * a.D * (16 / L);
+            }
+            from[i] += 16 * (lane % 8);
+        }
+        Piece next[kLoads], lines[2][MODE == kDown ? RQ : 1][MODE == kDown ? L : 1];
+        auto load = [&](int64_t step) {
+            const int64_t k = (step + 1) * kStep <= a.D ? step * kStep : a.D - kStep;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t of = __shfl(row, 16 * s + 4 * g + i);
-                    if (place + 16 * s + 4 * g + i >= rows.count) continue;
-                    float* to = a.h + ((int64_t)part * a.rows.M + of) * (16 * RT);
+            for (int i = 0; i < kLoads; ++i) __builtin_memcpy(next[i].w, from[i] + k * (16 / L), 16);
+            if constexpr (MODE == kDown)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int q = 0; q < RQ; ++q)
 #pragma unroll
-                        for (int t = 0; t < RL; ++t) {
-                            const int c = 16 * RL * q + RL * j + t;
-                            const float v = acc[s][RL * q + t][i];
-                            to[rank[q] + t] = DT == kBf16 && a.parts == 1 ? __uint_as_float(paired(v)) : v;
-                            if (c >= a.r) to[c] = 0.0f;     // (behind the last rank)
-                        }
-                }
-        if (place + kTile < rows.count) __syncthreads();
+                        for (int e = 0; e < L; ++e) lines[c][q][e] = load_few<DT, RL, true>(W, (k + kChunk * c + L * g + e) * a.r + rank[q], RL);
+        };
+        int64_t step = first + wave;
+        if (step < last) load(step);
+        for (; step < last; step += kDownWaves) {
+            const int skip = (step + 1) * kStep <= a.D ? 0 : (int)((step + 1) * kStep - a.D);
+            if (skip) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) next[i] = without<DT>(next[i], skip - L * (lane % 8));
+                if constexpr (MODE == kDown)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                            for (int e = 0; e < L; ++e) lines[c][q][e] = only_if(kChunk * c + L * g + e >= skip, lines[c][q][e]);
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                *reinterpret_cast<Piece*>(mine + 1024 * i + 128 * (lane / 8) + 16 * ((lane ^ lane / 8) % 8)) = next[i];
+            Piece w[2][RQ][MODE == kDown ? L : RL];
+            if constexpr (MODE == kDown)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                        for (int e = 0; e < L; ++e) w[c][q][e] = lines[c][q][e];
+            if (step + kDownWaves < last) load(step + kDownWaves);
+            auto fragment = [&](int f, int c) {         // 16 rows from 16 f on
+                return *reinterpret_cast<const Piece*>(mine + 2048 * f + 128 * j + 16 * ((4 * c + g) ^ (j & 7)));
+            };
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                Piece x[kSubs];
+#pragma unroll
+                for (int s = 0; s < kSubs; ++s) x[s] = fragment(s, c);
+                if constexpr (MODE == kAlong)
+#pragma unroll
+                    for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                        for (int t = 0; t < RL; ++t) w[c][q][t] = fragment(kSubs + RL * q + t, c);
+                products(x, w[c]);
+            }
+        }
     }
+    join_waves<RT>(acc, reinterpret_cast<v4f*>(lds), wave, lane);
+    if (wave == 0)
+#pragma unroll
+        for (int s = 0; s < kSubs; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t of = __shfl(row, 16 * s + 4 * g + i);
+                if (16 * s + 4 * g + i >= rows.count) continue;
+                float* to = a.h + ((int64_t)part * a.rows.M + of) * (16 * RT);
+#pragma unroll
+                for (int q = 0; q < RQ; ++q)
+#pragma unroll
+                    for (int t = 0; t < RL; ++t) {
+                        const int c = 16 * RL * q + RL * j + t;
+                        const float v = acc[s][RL * q + t][i];
+                        to[rank[q] + t] = DT == kBf16 && a.parts == 1 ? __uint_as_float(paired(v)) : v;
+                        if (c >= a.r) to[c] = 0.0f;     // (behind the last rank)
+                    }
+            }
 }
 
 // ---- up ----
@@ -656,91 +694,88 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
     // a lane's ranks of a chunk: from first(c) on, those before own(c) another lane's
     auto own = [&](int c) { return kChunk * c + L * (kFolded ? g & 1 : g); };
     auto first = [&](int c) { return MODE == kDown || SHORT || own(c) + L <= a.r ? own(c) : a.r - L; };
-    for (uint32_t place = 0; place < rows.count; place += kTile) {
-        const uint32_t all = rows.rows(place);
-        uint32_t row[kSubs][4];
+    const uint32_t all = rows.rows(0);
+    uint32_t row[kSubs][4];
 #pragma unroll
-        for (int s = 0; s < kSubs; ++s)
+    for (int s = 0; s < kSubs; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) row[s][i] = __shfl(all, 16 * s + 4 * g + i);
-        // a lane's columns from c0 on: from col, those from lo to hi its own
-        int64_t col;
-        int lo, hi;
-        Piece base[kSubs][4] = {}, w[L];
-        auto lines = [&](int c) {
+        for (int i = 0; i < 4; ++i) row[s][i] = __shfl(all, 16 * s + 4 * g + i);
+    // a lane's columns from c0 on: from col, those from lo to hi its own
+    int64_t col;
+    int lo, hi;
+    Piece base[kSubs][4] = {}, w[L];
+    auto lines = [&](int c) {
 #pragma unroll
-            for (int e = 0; e < L; ++e) {
-                if constexpr (MODE == kDown) {             // line own(c) + e
-                    const int rank = own(c) + e < a.r ? own(c) + e : 0;
-                    w[e] = load_piece<DT, !SHORT>(W, rank * a.N + col, hi);
-                } else {                                   // column col + e
-                    const int rank = first(c) < a.r ? first(c) : 0;
-                    w[e] = load_piece<DT, !SHORT>(W, (col + (SHORT && e >= hi ? 0 : e)) * a.r + rank, a.r - first(c));
-                }
+        for (int e = 0; e < L; ++e) {
+            if constexpr (MODE == kDown) {             // line own(c) + e
+                const int rank = own(c) + e < a.r ? own(c) + e : 0;
+                w[e] = load_piece<DT, !SHORT>(W, rank * a.N + col, hi);
+            } else {                                   // column col + e
+                const int rank = first(c) < a.r ? first(c) : 0;
+                w[e] = load_piece<DT, !SHORT>(W, (col + (SHORT && e >= hi ? 0 : e)) * a.r + rank, a.r - first(c));
             }
-        };
-        auto fetch = [&](int64_t c0) {
-            const int64_t from = SHORT || c0 + kColumns <= a.N ? c0 : a.N - kColumns;
-            lo = (int)(c0 - from) - L * j;
-            hi = SHORT ? (int)(a.N - c0) - L * j : L;
-            col = SHORT && hi <= 0 ? c0 : from + L * j;
-            if (a.base)
+        }
+    };
+    auto fetch = [&](int64_t c0) {
+        const int64_t from = SHORT || c0 + kColumns <= a.N ? c0 : a.N - kColumns;
+        lo = (int)(c0 - from) - L * j;
+        hi = SHORT ? (int)(a.N - c0) - L * j : L;
+        col = SHORT && hi <= 0 ? c0 : from + L * j;
+        if (a.base)
 #pragma unroll
-                for (int s = 0; s < kSubs; ++s)
+            for (int s = 0; s < kSubs; ++s)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) base[s][i] = load_piece<DT, !SHORT>(a.base, row[s][i] * a.N + col, hi);
-            if (!none && !wrong) lines(0);
-        };
-        // the first columns are on their way while the tile's h is split, for all waves
-        int64_t c0 = ((int64_t)over * kUpWaves + wave) * kColumns;
-        const int64_t step = (int64_t)a.across * kUpWaves * kColumns;
-        if (c0 < a.N) fetch(c0);
-        if (place) __syncthreads();
+                for (int i = 0; i < 4; ++i) base[s][i] = load_piece<DT, !SHORT>(a.base, row[s][i] * a.N + col, hi);
+        if (!none && !wrong) lines(0);
+    };
+    // the first columns are on their way while the tile's h is split, for all waves
+    int64_t c0 = ((int64_t)over * kUpWaves + wave) * kColumns;
+    const int64_t step = (int64_t)a.across * kUpWaves * kColumns;
+    if (c0 < a.N) fetch(c0);
         for (int f = wave; f < kSubs * C; f += kUpWaves) {
-            const int s = f / C, c = f % C;
-            const uint32_t of = __shfl(all, 16 * s + j);
-            Piece planes[P];
-            if (none || wrong) continue;
-            load_h<DT, P>(a.h + (int64_t)of * kRanks + first(c), a.rows.M * kRanks, a.parts, own(c) - first(c), g >= 2, planes);
+        const int s = f / C, c = f % C;
+        const uint32_t of = __shfl(all, 16 * s + j);
+        Piece planes[P];
+        if (none || wrong) continue;
+        load_h<DT, P>(a.h + (int64_t)of * kRanks + first(c), a.rows.M * kRanks, a.parts, own(c) - first(c), g >= 2, planes);
 #pragma unroll
-            for (int k = 0; k < P; ++k) h[f][k][lane] = planes[k];
-        }
-        __syncthreads();
-        for (; c0 < a.N; c0 += step) {
-            v4f acc[kSubs][L] = {};
-            if (!none && !wrong)
+        for (int k = 0; k < P; ++k) h[f][k][lane] = planes[k];
+    }
+    __syncthreads();
+    for (; c0 < a.N; c0 += step) {
+        v4f acc[kSubs][L] = {};
+        if (!none && !wrong)
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    if (c) lines(c);
-                    if (a.r != kRanks)                     // (h is zero there, but W may be infinite)
+            for (int c = 0; c < C; ++c) {
+                if (c) lines(c);
+                if (a.r != kRanks)                     // (h is zero there, but W may be infinite)
 #pragma unroll
-                        for (int e = 0; e < L; ++e) w[e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[e]);
+                    for (int e = 0; e < L; ++e) w[e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[e]);
 #pragma unroll
-                    for (int t = 0; t < L; ++t) {
-                        const Piece b = MODE == kDown ? turned<DT>(w, t) : w[t];
+                for (int t = 0; t < L; ++t) {
+                    const Piece b = MODE == kDown ? turned<DT>(w, t) : w[t];
 #pragma unroll
-                        for (int k = P - 1; k >= 0; --k)
+                    for (int k = P - 1; k >= 0; --k)
 #pragma unroll
-                            for (int s = 0; s < kSubs; ++s) acc[s][t] = multiply<DT>(h[s * C + c][k][lane], b, acc[s][t]);
-                    }
-                }
-#pragma unroll
-            for (int s = 0; s < kSubs; ++s) {
-                if (place + 16 * s >= rows.count) break;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v[L];
-#pragma unroll
-                    for (int t = 0; t < L; ++t) {
-                        v[t] = fmaf(scale, acc[s][t][i], value<DT>(base[s][i], t));
-                    }
-                    if (place + 16 * s + 4 * g + i >= rows.count || hi <= 0 || lo >= L) continue;
-                    if constexpr (END == kEven) store_piece<DT>(a.out, row[s][i] * a.N + col, 0, L, piece_of<DT>(v));
-                    else store_piece<DT>(a.out, row[s][i] * a.N + col, lo, hi, piece_of<DT>(v));
+                        for (int s = 0; s < kSubs; ++s) acc[s][t] = multiply<DT>(h[s * C + c][k][lane], b, acc[s][t]);
                 }
             }
-            if (c0 + step < a.N) fetch(c0 + step);
+#pragma unroll
+        for (int s = 0; s < kSubs; ++s) {
+            if (16 * s >= rows.count) break;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[L];
+#pragma unroll
+                for (int t = 0; t < L; ++t) {
+                    v[t] = fmaf(scale, acc[s][t][i], value<DT>(base[s][i], t));
+                }
+                if (16 * s + 4 * g + i >= rows.count || hi <= 0 || lo >= L) continue;
+                if constexpr (END == kEven) store_piece<DT>(a.out, row[s][i] * a.N + col, 0, L, piece_of<DT>(v));
+                else store_piece<DT>(a.out, row[s][i] * a.N + col, lo, hi, piece_of<DT>(v));
+            }
         }
+        if (c0 + step < a.N) fetch(c0 + step);
     }
 }
 
