@@ -185,14 +185,50 @@ __global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows 
     }
 }
 
-// parts[workgroup][2][C]: sums over its rows of dy xh and of dy
-template <int DT, int R, bool WHOLE, int T>
+// Of few rows: both parameters' gradients of 32 columns, over all rows, by one workgroup, beside those that the rows have.
+constexpr int64_t kFewRows = 256;
+template <int DT, int T>
+__device__ __forceinline__ void columns_alone(const LayerNormArgs& a, uint32_t block)
+{
+    __shared__ double lds[2][T / 32][33];
+    const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5, slices = T / 32;
+    const int c = (int)(32 * block + x);
+    float dw = 0.0f, db = 0.0f;
+    if (c < a.C)
+#pragma unroll 8
+        for (int64_t row = y; row < a.M; row += slices) {
+            const float2 stats = reinterpret_cast<const float2*>(a.saved)[row];
+            const float g = load_as<DT>(a.dy, row * a.C + c);
+            dw = fmaf(g, (load_as<DT>(a.s, row * a.C + c) - stats.x) * stats.y, dw);
+            db += g;
+        }
+    lds[0][y][x] = (double)dw;
+    lds[1][y][x] = (double)db;
+    __syncthreads();
+    void* to = y == 0 ? a.dweight : a.dbias;
+    if (y > 1 || c >= a.C || !to) return;
+    double s = 0.0;
+    for (uint32_t i = 0; i < slices; ++i) s += lds[y][i][x];
+    if (a.param_dtype == kBf16) store_as<kBf16>(to, c, (float)s);
+    else store_as<kF32>(to, c, (float)s);
+}
+
+// parts[workgroup][2][C]: sums over its rows of dy xh and of dy; null: they are not wanted.  ALONE: the workgroups behind k.groups have
+// the parameters' gradients.
+template <int DT, int R, bool WHOLE, int T, bool ALONE>
 __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows k, float* parts)
 {
     // rows that take more registers than there are beside the gradients' sums are read again for the result
     constexpr bool kHold = R * T < 4096;
     __shared__ float lds[2][2 * (T / 64)];
     extern __shared__ float columns[];          // [2][C], where a workgroup has several rows at once
+    if (ALONE) {
+        if (blockIdx.x >= k.groups) {
+            columns_alone<DT, T>(a, blockIdx.x - k.groups);
+            return;
+        }
+        if (!a.dx && !a.dresidual) return;
+    }
     const uint32_t group = threadIdx.x / k.width, t = threadIdx.x & (k.width - 1);
     const bool drops = a.drop.on && a.dx;
     const uint64_t key = drops ? drop_key(a.drop) : 0;
@@ -266,7 +302,7 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
             }
         }
     }
-    if (!a.dweight && !a.dbias) return;
+    if (ALONE || !parts) return;
     // the rows that a wave has side by side, then one wave's, or one row's several waves, after the other
     for (uint32_t m = k.width; m < 64; m <<= 1)
 #pragma unroll
@@ -401,16 +437,23 @@ hipError_t launch_layernorm_fwd(const LayerNormArgs& a, hipStream_t stream)
 hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStream_t stream)
 {
     const Rows k = bwd_rows(a);
-    float* parts = static_cast<float*>(workspace);
+    // (a launch less, for reading the rows twice: 128 x 512 in fp32, forward and backward, 17.3 us with three launches)
+    const bool params = a.dweight || a.dbias, alone = params && a.M <= kFewRows && k.R == 1;
+    float* parts = params && !alone ? static_cast<float*>(workspace) : nullptr;
     {
         ProfileScope ps(K_LAYERNORM_BWD, stream);
-        const size_t lds = k.at_once > 1 ? 2 * (size_t)a.C * sizeof(float) : 0;
+        const size_t lds = k.at_once > 1 && parts ? 2 * (size_t)a.C * sizeof(float) : 0;
+        const dim3 grid(k.groups + (alone ? (uint32_t)((a.C + 31) / 32) : 0));
         with_rows(a, k, [&](auto dt, auto r, auto whole, auto t) {
-            hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, r.value, whole.value, t.value>), dim3(k.groups), dim3(k.width * k.at_once), lds,
-                               stream, a, k, parts);
+            if (alone) {
+                if constexpr (r.value == 1)
+                    hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, 1, whole.value, t.value, true>), grid, dim3(t.value), 0, stream, a, k, parts);
+            } else {
+                hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, r.value, whole.value, t.value, false>), grid, dim3(t.value), lds, stream, a, k, parts);
+            }
         });
     }
-    if (a.dweight || a.dbias) {
+    if (parts) {
         ProfileScope ps(K_LAYERNORM_PARAMS, stream);
         hipLaunchKernelGGL(layernorm_params_kernel, dim3((uint32_t)((a.C + 31) / 32), 2), dim3(kParamThreads), 0, stream, a, parts, k.groups);
     }

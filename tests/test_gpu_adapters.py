@@ -90,14 +90,14 @@ def test_ranks(r, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("M", [31, 32, 33, 63, 64, 65, 96, 97, 1023, 1025])
+@pytest.mark.parametrize("M", [31, 32, 33, 63, 64, 65, 96, 97, 128, 129, 255, 256, 257, 1023, 1025])
 def test_rows_around_tiles(M, dtype):
     check(M, 80, 140, 8, 1, dtype, none=0.0)
     check(M, 80, 140, 8, 2, dtype, none=0.9)
     check(M, 80, 140, 8, 2, dtype, none=1.0)
 
 
-@pytest.mark.parametrize("M", [50, 300])
+@pytest.mark.parametrize("M", [50, 150, 300])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_numbers_that_are_none(M, dtype):
     """At n or above: the row is NaN, and nothing is read or added for it."""
@@ -116,7 +116,7 @@ def test_numbers_that_are_none(M, dtype):
     near(dB, want["dB"], dtype)
 
 
-@pytest.mark.parametrize("M", [40, 200])
+@pytest.mark.parametrize("M", [40, 200, 300])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_unusual_values_stay_where_they_belong(M, dtype):
     """A row's NaN is that row's out, and its adapter's gradients; an infinity gives infinities or NaN; other rows have the same bits."""
