@@ -470,17 +470,27 @@ __device__ __forceinline__ void join_waves(v4f (&acc)[kSubs][RT], v4f* lds, int 
 // SHORT: the contraction is shorter than a step; element by element.  Else the last step, where it is no whole one, begins a step
 // before the end, and what it has of the one before is taken for zeros.
 template <int DT, int RT, int MODE, bool SHORT>
+struct Down {
+    static constexpr int L = lane_of<DT>(), kChunk = 4 * L, kStep = 2 * kChunk, RL = RT < L ? RT : L, RQ = RT / RL;
+    static constexpr int kRows = kTile + (MODE == kAlong ? 16 * RT : 0), kLoads = kRows / 8;    // of a step, that go through LDS
+    static constexpr int kBytes = SHORT ? 0 : 128 * kRows * kDownWaves, kSums = kDownWaves / 2 * kSubs * RT * 64 * (int)sizeof(v4f);
+    static constexpr int kLds = kBytes > kSums ? kBytes : kSums;
+    static __device__ __forceinline__ void tile(const DownArgs& a, const Group& rows, uint32_t part, char* lds);
+};
+template <int DT, int RT, int MODE, bool SHORT>
 __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
 {
-    constexpr int L = lane_of<DT>(), kChunk = 4 * L, kStep = 2 * kChunk, RL = RT < L ? RT : L, RQ = RT / RL;
-    constexpr int kRows = kTile + (MODE == kAlong ? 16 * RT : 0), kLoads = kRows / 8;           // of a step, that go through LDS
-    constexpr int kBytes = SHORT ? 0 : 128 * kRows * kDownWaves, kSums = kDownWaves / 2 * kSubs * RT * 64 * (int)sizeof(v4f);
-    __shared__ __attribute__((aligned(16))) char lds[kBytes > kSums ? kBytes : kSums];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+    typedef Down<DT, RT, MODE, SHORT> D;
+    __shared__ __attribute__((aligned(16))) char lds[D::kLds];
     uint32_t tile, part;
     if (!place_of(a.grid, tile, part)) return;
     const Group rows = tile_rows(a.rows, tile);
-    if (!rows.count || rows.group >= (uint32_t)a.rows.n) return;
+    if (rows.count && rows.group < (uint32_t)a.rows.n) D::tile(a, rows, part, lds);
+}
+template <int DT, int RT, int MODE, bool SHORT>
+__device__ __forceinline__ void Down<DT, RT, MODE, SHORT>::tile(const DownArgs& a, const Group& rows, uint32_t part, char* lds)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const char* W = static_cast<const char*>(a.W) + (int64_t)rows.group * a.D * a.r * (16 / L);
     // tile t + RL q of the ranks: a lane's is rank[q] + t.  (16 RL q + RL (l % 16); the last lanes' begin RL before the last rank's end,
     // and have ranks of the lanes before again: r is above RL, where that is more than one)
@@ -622,7 +632,6 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void down_kernel(DownArgs a)
 struct UpArgs {
     RowArgs rows;
     Grid grid;                      // workgroups over the columns, tiles
-    uint32_t across;                // of the former
     const float* h;                 // [parts][M][16 RT]
     const float* scale;             // [n] or null
     const void* W;                  // of an adapter [r, N] (kDown) or [N, r] (kAlong)
@@ -672,20 +681,48 @@ __device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t pa
 // element.  Else the last columns, and the last ranks of a line along them, begin so far before the end that loads are whole; what
 // others have already is not written, and zero in h.  kEven: columns are whole loads, so that a lane writes all of its own or none.
 enum End { kEven, kOdd, kShort };
+template <int DT, int RT, int MODE, int END, int WAVES>
+struct Up {
+    static constexpr bool SHORT = END == kShort;
+    static constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L;
+    // bfloat16, one tile of ranks: both planes are one chunk, the second beside the same lines of W again
+    static constexpr bool kFolded = DT == kBf16 && RT == 1;
+    static constexpr int P = kFolded ? 1 : planes_of<DT>(), C = 16 * RT < kChunk ? 1 : 16 * RT / kChunk, kRanks = 16 * RT;
+    struct Lds {
+        Piece h[kSubs * C][P][64];
+    };
+    // every `across`-th group of WAVES blocks of columns, from `over` on
+    static __device__ __forceinline__ void tile(const UpArgs& a, const Group& rows, uint32_t over, uint32_t across, Lds& lds);
+};
 template <int DT, int RT, int MODE, int END>
 __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
 {
-    constexpr bool SHORT = END == kShort;
-    constexpr int L = lane_of<DT>(), kChunk = 4 * L, kColumns = 16 * L;
-    // bfloat16, one tile of ranks: both planes are one chunk, the second beside the same lines of W again
-    constexpr bool kFolded = DT == kBf16 && RT == 1;
-    constexpr int P = kFolded ? 1 : planes_of<DT>(), C = 16 * RT < kChunk ? 1 : 16 * RT / kChunk, kRanks = 16 * RT;
-    __shared__ Piece h[kSubs * C][P][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+    typedef Up<DT, RT, MODE, END, kUpWaves> U;
+    __shared__ typename U::Lds lds;
     uint32_t tile, over;
     if (!place_of(a.grid, over, tile)) return;
     const Group rows = tile_rows(a.rows, tile);
+    if (rows.count) U::tile(a, rows, over, a.grid.inner.d, lds);
+}
+// Both ways by one workgroup to a tile, h by way of memory.
+template <int DT, int RT, int MODE, int END>
+__global__ __launch_bounds__(64 * kDownWaves, 2) void down_up_kernel(DownArgs d, UpArgs u)
+{
+    typedef Down<DT, RT, MODE, false> D;
+    typedef Up<DT, RT, MODE, END, kDownWaves> U;
+    __shared__ __attribute__((aligned(16))) char lds[D::kLds > (int)sizeof(typename U::Lds) ? D::kLds : (int)sizeof(typename U::Lds)];
+    uint32_t tile, none;
+    if (!place_of(d.grid, tile, none)) return;
+    const Group rows = tile_rows(d.rows, tile);
     if (!rows.count) return;
+    if (rows.group < (uint32_t)d.rows.n) D::tile(d, rows, 0, lds);
+    __syncthreads();
+    U::tile(u, rows, 0, 1, *reinterpret_cast<typename U::Lds*>(lds));
+}
+template <int DT, int RT, int MODE, int END, int WAVES>
+__device__ __forceinline__ void Up<DT, RT, MODE, END, WAVES>::tile(const UpArgs& a, const Group& rows, uint32_t over, uint32_t across, Lds& lds)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const bool none = rows.group == (uint32_t)a.rows.n, wrong = rows.group > (uint32_t)a.rows.n;
     if (none && a.base == a.out) return;
     const char* W = static_cast<const char*>(a.W) + (none || wrong ? 0 : (int64_t)rows.group * a.N * a.r * (16 / L));
@@ -729,17 +766,17 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
         if (!none && !wrong) lines(0);
     };
     // the first columns are on their way while the tile's h is split, for all waves
-    int64_t c0 = ((int64_t)over * kUpWaves + wave) * kColumns;
-    const int64_t step = (int64_t)a.across * kUpWaves * kColumns;
+    int64_t c0 = ((int64_t)over * WAVES + wave) * kColumns;
+    const int64_t step = (int64_t)across * WAVES * kColumns;
     if (c0 < a.N) fetch(c0);
-        for (int f = wave; f < kSubs * C; f += kUpWaves) {
+    for (int f = wave; f < kSubs * C; f += WAVES) {
         const int s = f / C, c = f % C;
         const uint32_t of = __shfl(all, 16 * s + j);
         Piece planes[P];
         if (none || wrong) continue;
         load_h<DT, P>(a.h + (int64_t)of * kRanks + first(c), a.rows.M * kRanks, a.parts, own(c) - first(c), g >= 2, planes);
 #pragma unroll
-        for (int k = 0; k < P; ++k) h[f][k][lane] = planes[k];
+        for (int k = 0; k < P; ++k) lds.h[f][k][lane] = planes[k];
     }
     __syncthreads();
     for (; c0 < a.N; c0 += step) {
@@ -757,7 +794,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void up_kernel(UpArgs a)
 #pragma unroll
                     for (int k = P - 1; k >= 0; --k)
 #pragma unroll
-                        for (int s = 0; s < kSubs; ++s) acc[s][t] = multiply<DT>(h[s * C + c][k][lane], b, acc[s][t]);
+                        for (int s = 0; s < kSubs; ++s) acc[s][t] = multiply<DT>(lds.h[s * C + c][k][lane], b, acc[s][t]);
                 }
             }
 #pragma unroll
@@ -963,7 +1000,18 @@ int tiles_of_rank(int r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }
 // (what a grid has: tiles that may be)
 uint32_t grid_tiles(const AdapterArgs& a) { return (uint32_t)(a.M <= kDirect ? a.M : most_tiles(a.M, a.n)); }
 
-// Parts of a contraction over D: as many as make 512 workgroups, none of fewer than a step for each of the eight waves.
+// Where what a tile's workgroup reads and writes by itself, the adapter and its rows either way, takes less time than a launch, and
+// tiles do not fill the chip by themselves.  A forward call, two launches and one: 64 x 512 x 512 of rank 16 in bfloat16 (96 KB)
+// 9.4 and 6.9 us, 1000 x 512 x 512 of rank 16 in fp32 (192 KB) 14.9 and 14.5, 1 x 4096 x 4096 of rank 16 (272 KB) 9.8 and 15.5,
+// 8192 x 512 x 512 of rank 8 25.6 and 26.2.
+bool small_tile(const AdapterArgs& a)
+{
+    const int64_t rows = a.M < kTile ? a.M : kTile;
+    return a.M <= 4096 && (a.K + a.N) * (a.r + rows) * dtype_size(a.dtype) <= 192 << 10;
+}
+
+// Parts of a contraction over D: as many as make 512 workgroups, none of fewer than a step for each of the eight waves; one of a small
+// tile.
 struct Parts {
     uint32_t parts, steps;
 };
@@ -971,7 +1019,7 @@ Parts parts_of(const AdapterArgs& a, int64_t D)
 {
     const int64_t step = a.dtype == kBf16 ? 64 : 32, steps = (D + step - 1) / step;
     const int64_t tiles = a.M <= kDirect ? (a.M < a.n ? a.M : a.n) : a.M / kTile + (a.n < a.M / kTile ? a.n : a.M / kTile);
-    int64_t parts = 512 / (tiles > 0 ? tiles : 1);
+    int64_t parts = small_tile(a) ? 1 : 512 / (tiles > 0 ? tiles : 1);
     if (parts > kMostParts) parts = kMostParts;
     while (parts > 1 && steps < parts * kDownWaves) --parts;
     if (parts < 1) parts = 1;
@@ -1023,34 +1071,44 @@ void with_types(const AdapterArgs& a, F f)
     else ranks(integral_constant<int, kF32>{});
 }
 
-template <int MODE>
-void launch_down(const AdapterArgs& a, const void* x, const void* W, float* h, int64_t D, const RowArgs& rows, hipStream_t stream)
+// Whether a tile goes both ways in one launch, which needs whole loads.
+bool one_launch(const AdapterArgs& a, int64_t D, int64_t N, bool along)
 {
-    ProfileScope ps(K_ADAPT_DOWN, stream);
-    const Parts p = parts_of(a, D);
-    const DownArgs d{rows, grid_of(grid_tiles(a), p.parts), x, W, h, D, a.r, p.steps, p.parts};
-    with_types(a, [&](auto dt, auto rt) {
-        const dim3 grid(8 * d.grid.per_xcd, d.grid.slices()), block(64 * kDownWaves);
-        if (D < 8 * lane_of<dt.value>()) hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, true>), grid, block, 0, stream, d);
-        else hipLaunchKernelGGL((down_kernel<dt.value, rt.value, MODE, false>), grid, block, 0, stream, d);
-    });
+    const int L = a.dtype == kBf16 ? 8 : 4;
+    return small_tile(a) && D >= 8 * L && N >= 16 * L && a.r <= 64 && !(along && a.r < L);
 }
 
-// (a workgroup has a tile's columns in so many parts: as few as make 2048 workgroups)
 template <int MODE>
-void launch_up(const AdapterArgs& a, const float* h, const void* W, const void* base, void* out, int64_t N, int64_t D, const RowArgs& rows,
-               hipStream_t stream)
+void launch_pass(const AdapterArgs& a, const void* x, const void* W1, float* h, const void* W2, const void* base, void* out, int64_t D, int64_t N,
+                 const RowArgs& rows, hipStream_t stream)
 {
-    ProfileScope ps(K_ADAPT_UP, stream);
-    const int64_t columns = (a.dtype == kBf16 ? 128 : 64) * kUpWaves, most = (N + columns - 1) / columns, want = 2048 / grid_tiles(a) + 1;
+    const Parts p = parts_of(a, D);
+    const uint32_t tiles = grid_tiles(a);
+    const DownArgs d{rows, grid_of(tiles, p.parts), x, W1, h, D, a.r, p.steps, p.parts};
+    // (a workgroup has a tile's columns in so many parts: as few as make 2048 workgroups)
+    const int64_t columns = (a.dtype == kBf16 ? 128 : 64) * kUpWaves, most = (N + columns - 1) / columns, want = 2048 / tiles + 1;
     const uint32_t across = (uint32_t)(most < want ? most : want);
-    const UpArgs u{rows, grid_of(across, grid_tiles(a)), across, h, a.scale, W, base, out, N, a.r, parts_of(a, D).parts};
+    const UpArgs u{rows, grid_of(across, tiles), h, a.scale, W2, base, out, N, a.r, p.parts};
+    const dim3 down(8 * d.grid.per_xcd, d.grid.slices()), up(8 * u.grid.per_xcd, u.grid.slices());
     with_types(a, [&](auto dt, auto rt) {
-        const dim3 grid(8 * u.grid.per_xcd, u.grid.slices()), block(64 * kUpWaves);
-        constexpr int L = lane_of<dt.value>();
-        if (N < 16 * L || (MODE == kAlong && a.r < L)) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kShort>), grid, block, 0, stream, u);
-        else if (N % L) hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kOdd>), grid, block, 0, stream, u);
-        else hipLaunchKernelGGL((up_kernel<dt.value, rt.value, MODE, kEven>), grid, block, 0, stream, u);
+        constexpr int DT = dt.value, RT = rt.value, L = lane_of<DT>();
+        if constexpr (RT <= 4)
+            if (out && one_launch(a, D, N, MODE == kAlong)) {
+                ProfileScope ps(K_ADAPT_DOWN_UP, stream);
+                if (N % L) hipLaunchKernelGGL((down_up_kernel<DT, RT, MODE, kOdd>), down, dim3(64 * kDownWaves), 0, stream, d, u);
+                else hipLaunchKernelGGL((down_up_kernel<DT, RT, MODE, kEven>), down, dim3(64 * kDownWaves), 0, stream, d, u);
+                return;
+            }
+        {
+            ProfileScope ps(K_ADAPT_DOWN, stream);
+            if (D < 8 * L) hipLaunchKernelGGL((down_kernel<DT, RT, MODE, true>), down, dim3(64 * kDownWaves), 0, stream, d);
+            else hipLaunchKernelGGL((down_kernel<DT, RT, MODE, false>), down, dim3(64 * kDownWaves), 0, stream, d);
+        }
+        if (!out) return;
+        ProfileScope ps(K_ADAPT_UP, stream);
+        if (N < 16 * L || (MODE == kAlong && a.r < L)) hipLaunchKernelGGL((up_kernel<DT, RT, MODE, kShort>), up, dim3(64 * kUpWaves), 0, stream, u);
+        else if (N % L) hipLaunchKernelGGL((up_kernel<DT, RT, MODE, kOdd>), up, dim3(64 * kUpWaves), 0, stream, u);
+        else hipLaunchKernelGGL((up_kernel<DT, RT, MODE, kEven>), up, dim3(64 * kUpWaves), 0, stream, u);
     });
 }
 
@@ -1069,8 +1127,7 @@ hipError_t launch_adapters_fwd(const AdapterArgs& a, hipStream_t stream)
         while ((1 << bits) < a.n + 2) ++bits;
         hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a.ids, a.M, a.n, bits, static_cast<uint32_t*>(a.saved));
     }
-    launch_down<kDown>(a, a.x, a.A, h, a.K, rows, stream);
-    launch_up<kDown>(a, h, a.B, a.base, a.out, a.N, a.K, rows, stream);
+    launch_pass<kDown>(a, a.x, a.A, h, a.B, a.base, a.out, a.K, a.N, rows, stream);
     return hipGetLastError();
 }
 
@@ -1079,8 +1136,7 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
     float* h = reinterpret_cast<float*>(static_cast<char*>(a.saved) + plan_bytes(a));
     float* g = static_cast<float*>(workspace);
     const RowArgs rows{a.ids, a.saved, a.M, a.n};
-    if (a.out || a.dA) launch_down<kAlong>(a, a.dy, a.B, g, a.N, rows, stream);
-    if (a.out) launch_up<kAlong>(a, g, a.A, a.base, a.out, a.K, a.N, rows, stream);
+    if (a.out || a.dA) launch_pass<kAlong>(a, a.dy, a.B, g, a.A, a.base, a.out, a.N, a.K, rows, stream);
     if (a.dA || a.dB) {
         ProfileScope ps(K_ADAPT_WEIGHTS, stream);
         const int64_t columns = a.dtype == kBf16 ? 128 : 64;

@@ -41,7 +41,7 @@ const char* kernel_name(int id)
         "groupnorm_bwd_sums", "groupnorm_bwd_finish", "groupnorm_bwd", "xent_logits", "xent_loss", "xent_dlogits",
         "xent_dx", "xent_dw", "xent_dbias", "xent_pack", "xent_add_parts", "groupnorm_params",
         "dropout", "layernorm_fwd", "layernorm_bwd", "layernorm_params", "adapters_plan", "adapters_down", "adapters_up",
-        "adapters_weights"};
+        "adapters_down_up", "adapters_weights"};
     return (id >= 0 && id < K_ALL_COUNT) ? names[id] : "?";
 }
 
