@@ -31,8 +31,8 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const void* x, const 
             dropped(e, q, r);
             store_eight<DT>(y, e, q);
         } else {
-            Eight<DT> q = load_some<DT>(x, e, 0, (int)(n - e));
-            if (residual) r = load_some<DT>(residual, e, 0, (int)(n - e));
+            Eight<DT> q = load_some<DT>(x, e, (int)(n - e));
+            if (residual) r = load_some<DT>(residual, e, (int)(n - e));
             dropped(e, q, r);
             store_some<DT>(y, e, 0, (int)(n - e), q);
         }

@@ -60,19 +60,21 @@ __device__ __forceinline__ void store_eight(void* p, int64_t at, const Eight<DT>
 #pragma unroll
     for (int i = 0; i < Eight<DT>::kWords; i += 4) __builtin_memcpy(to + 4 * i, q.w + i, 16);
 }
-// those of them from `lo` on and before `hi`; the others are zero, and nothing else is read or written
+// the first n of them; the others are zero, and nothing else is read
 template <int DT>
-__device__ __forceinline__ Eight<DT> load_some(const void* p, int64_t at, int lo, int hi)
+__device__ __forceinline__ Eight<DT> load_some(const void* p, int64_t at, int n)
 {
     Eight<DT> q{};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        if (j >= lo && j < hi) {
+        if (j < n) {
             if (DT == kF32) q.w[j % Eight<DT>::kWords] = static_cast<const uint32_t*>(p)[at + j];
             else q.w[j / 2] |= (uint32_t)static_cast<const uint16_t*>(p)[at + j] << 16 * (j & 1);
         }
     return q;
 }
+// those from `lo` on and before `hi`, one by one: a row's end (one, two and four at a time were no faster, at 20011 x 1031 in fp32
+// backward 94 us for 77)
 template <int DT>
 __device__ __forceinline__ void store_some(void* p, int64_t at, int lo, int hi, const Eight<DT>& q)
 {

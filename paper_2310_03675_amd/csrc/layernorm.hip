@@ -68,31 +68,35 @@ __device__ __forceinline__ void row_sums(float (&v)[N], uint32_t width, float* l
     }
 }
 
-// A thread's vector of a row: columns c + lo to c + hi of it.  The last of a row that is no whole vectors begins eight before the
-// row's end, and what it has of the one before is left out.
-template <bool WHOLE>
+// How rows end: whole vectors; with one that begins eight before the row's end, and what it has of the one before is left out; a row
+// is less than a vector.
+enum End { kWhole, kOverlap, kShort };
+
+// A thread's vector of a row: columns c + lo to c + hi of it.  Only the thread's last may be a row's last, or behind it.
+template <int END>
 struct Span {
     int c, lo, hi;
-    bool there;
-    __device__ __forceinline__ Span(uint32_t vector, int C, bool row)
+    bool there, ends;
+    __device__ __forceinline__ Span(uint32_t vector, int C, bool row, bool last)
     {
         const int first = 8 * (int)vector;
-        there = row && first < C;
-        c = WHOLE || first + 8 <= C || C < 8 ? first : C - 8;
-        lo = WHOLE ? 0 : first - c;
-        hi = WHOLE || C >= 8 ? 8 : C;
+        ends = last && END != kWhole;
+        there = row && (!last || first < C);
+        c = END != kOverlap || !last || first + 8 <= C ? first : C - 8;
+        lo = END == kOverlap ? first - c : 0;
+        hi = END == kShort ? C : 8;
     }
-    __device__ __forceinline__ bool has(int j) const { return WHOLE || (j >= lo && j < hi); }
+    __device__ __forceinline__ bool has(int j) const { return !ends || (END == kOverlap ? j >= lo : j < hi); }
     template <int DT>
     __device__ __forceinline__ Eight<DT> load(const void* p, int64_t base) const
     {
-        if (WHOLE || hi == 8) return load_eight<DT>(p, base + c);
-        return load_some<DT>(p, base + c, lo, hi);
+        if constexpr (END == kShort) return load_some<DT>(p, base + c, hi);
+        else return load_eight<DT>(p, base + c);
     }
     template <int DT>
     __device__ __forceinline__ void store(void* p, int64_t base, const Eight<DT>& q) const
     {
-        if (WHOLE || (lo == 0 && hi == 8)) store_eight<DT>(p, base + c, q);
+        if (END != kShort && (!ends || lo == 0)) store_eight<DT>(p, base + c, q);
         else store_some<DT>(p, base + c, lo, hi, q);
     }
     // of the parameters, or `otherwise`
@@ -113,7 +117,7 @@ struct Span {
     }
 };
 
-template <int DT, int R, bool WHOLE, int T>
+template <int DT, int R, int END, int T>
 __global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows k)
 {
     __shared__ float lds[2][T / 64];
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows 
         Eight<DT> q[R], res[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            const Span<END> at(t + r * k.width, a.C, there, r + 1 == R);
             q[r] = res[r] = Eight<DT>{};
             if (at.there) q[r] = at.template load<DT>(a.x, base);
             if (at.there && a.residual) res[r] = at.template load<DT>(a.residual, base);
@@ -136,7 +140,7 @@ __global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows 
         float sum[1] = {0.0f}, squares[1] = {0.0f};
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            const Span<END> at(t + r * k.width, a.C, there, r + 1 == R);
             if (!at.there) continue;
             if (changed) {
                 const uint32_t keep = drops ? kept_eight(a.drop, key, base + at.c) : 0;
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows 
         const float mean = sum[0] / count;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            const Span<END> at(t + r * k.width, a.C, there, r + 1 == R);
             q[r].renew();
             if (!at.there) continue;
 #pragma unroll
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(T) void layernorm_fwd_kernel(LayerNormArgs a, Rows 
         if (a.saved && there && t == 0) reinterpret_cast<float2*>(a.saved)[row] = make_float2(mean, rstd);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            const Span<END> at(t + r * k.width, a.C, there, r + 1 == R);
             q[r].renew();
             if (!at.there) continue;
             float w[8], b[8], v[8];
@@ -215,7 +219,7 @@ __device__ __forceinline__ void columns_alone(const LayerNormArgs& a, uint32_t b
 
 // parts[workgroup][2][C]: sums over its rows of dy xh and of dy; null: they are not wanted.  ALONE: the workgroups behind k.groups have
 // the parameters' gradients.
-template <int DT, int R, bool WHOLE, int T, bool ALONE>
+template <int DT, int R, int END, int T, bool ALONE>
 __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows k, float* parts)
 {
     // rows that take more registers than there are beside the gradients' sums are read again for the result
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
         Eight<DT> s[R], dy[R], more[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            const Span<END> at(t + r * k.width, a.C, there, r + 1 == R);
             s[r] = dy[r] = more[r] = Eight<DT>{};
             if (at.there) s[r] = at.template load<DT>(a.s, base);
             if (at.there) dy[r] = at.template load<DT>(a.dy, base);
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            const Span<END> at(t + r * k.width, a.C, there, r + 1 == R);
             if (!at.there) continue;
             float w[8];
             at.params(a.weight, a.param_dtype, 1.0f, w);
@@ -271,7 +275,7 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
         const float m1 = sums[0] / count, m2 = sums[1] / count;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const Span<WHOLE> at(t + r * k.width, a.C, there);
+            const Span<END> at(t + r * k.width, a.C, there, r + 1 == R);
             s[r].renew();
             dy[r].renew();
             if (!at.there) continue;
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
             float* const into = g + 1 == turns ? to : columns;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const Span<WHOLE> at(t + r * k.width, a.C, true);
+                const Span<END> at(t + r * k.width, a.C, true, r + 1 == R);
                 if (!at.there) continue;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -379,36 +383,38 @@ Rows rows_of(const LayerNormArgs& a, uint32_t most, uint32_t threads, int64_t wa
     return k;
 }
 
-constexpr uint32_t kFwdThreads = 256, kBwdThreads = 512;
+constexpr uint32_t kFwdThreads = 256, kBwdThreads = 512, kFwdMost = 3, kBwdMost = 2;
 
 Rows fwd_rows(const LayerNormArgs& a)
 {
-    Rows k = rows_of(a, 3, kFwdThreads, 4096);
+    Rows k = rows_of(a, kFwdMost, kFwdThreads, 4096);
     const int64_t groups = (a.M + k.at_once - 1) / k.at_once;
     k.groups = (uint32_t)(groups < (1 << 20) ? groups : 1 << 20);
     return k;
 }
 Rows bwd_rows(const LayerNormArgs& a)
 {
-    Rows k = rows_of(a, 2, kBwdThreads, 2048);
+    Rows k = rows_of(a, kBwdMost, kBwdThreads, 2048);
     const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.width == 1024 ? 1 : k.R > 1 ? 2 : 3);
     k.groups = (uint32_t)(groups < most ? groups : most);
     return k;
 }
 
-// f(type, R, whether rows are whole vectors, whether a workgroup has 1024 threads)
-template <class F>
+// f(type, R, how rows end, how many threads a workgroup has at most): of more than MOST vectors only 1024
+template <int MOST, class F>
 void with_rows(const LayerNormArgs& a, const Rows& k, F f)
 {
     using std::integral_constant;
     auto of = [&](auto dt) {
-        auto whole = [&](auto r, auto w) {
-            if (k.width * k.at_once > 512) f(dt, r, w, integral_constant<int, 1024>{});
-            else f(dt, r, w, integral_constant<int, 512>{});
+        auto ended = [&](auto r, auto e) {
+            if constexpr (e.value != kShort)
+                if (r.value > MOST || k.width * k.at_once > 512) return f(dt, r, e, integral_constant<int, 1024>{});
+            if constexpr (r.value <= MOST) f(dt, r, e, integral_constant<int, 512>{});
         };
         auto held = [&](auto r) {
-            if (a.C % 8) whole(r, std::false_type{});
-            else whole(r, std::true_type{});
+            if (a.C % 8 == 0) ended(r, integral_constant<int, kWhole>{});
+            else if (a.C > 8) ended(r, integral_constant<int, kOverlap>{});
+            else if constexpr (r.value == 1) ended(r, integral_constant<int, kShort>{});
         };
         if (k.R == 1) held(integral_constant<int, 1>{});
         else if (k.R == 2) held(integral_constant<int, 2>{});
@@ -427,8 +433,8 @@ hipError_t launch_layernorm_fwd(const LayerNormArgs& a, hipStream_t stream)
 {
     const Rows k = fwd_rows(a);
     ProfileScope ps(K_LAYERNORM_FWD, stream);
-    with_rows(a, k, [&](auto dt, auto r, auto whole, auto t) {
-        hipLaunchKernelGGL((layernorm_fwd_kernel<dt.value, r.value, whole.value, t.value>), dim3(k.groups), dim3(k.width * k.at_once), 0, stream,
+    with_rows<kFwdMost>(a, k, [&](auto dt, auto r, auto end, auto t) {
+        hipLaunchKernelGGL((layernorm_fwd_kernel<dt.value, r.value, end.value, t.value>), dim3(k.groups), dim3(k.width * k.at_once), 0, stream,
                            a, k);
     });
     return hipGetLastError();
@@ -444,12 +450,12 @@ hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStre
         ProfileScope ps(K_LAYERNORM_BWD, stream);
         const size_t lds = k.at_once > 1 && parts ? 2 * (size_t)a.C * sizeof(float) : 0;
         const dim3 grid(k.groups + (alone ? (uint32_t)((a.C + 31) / 32) : 0));
-        with_rows(a, k, [&](auto dt, auto r, auto whole, auto t) {
+        with_rows<kBwdMost>(a, k, [&](auto dt, auto r, auto end, auto t) {
             if (alone) {
                 if constexpr (r.value == 1)
-                    hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, 1, whole.value, t.value, true>), grid, dim3(t.value), 0, stream, a, k, parts);
+                    hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, 1, end.value, t.value, true>), grid, dim3(t.value), 0, stream, a, k, parts);
             } else {
-                hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, r.value, whole.value, t.value, false>), grid, dim3(t.value), lds, stream, a, k, parts);
+                hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, r.value, end.value, t.value, false>), grid, dim3(t.value), lds, stream, a, k, parts);
             }
         });
     }
