@@ -5,15 +5,20 @@
 // Four products with an axis of r, at most 128: memory bounds them, reading x, dy and the adapters and writing what is as large.
 //
 // Rows are grouped by adapter, in their order, first: tiles of 32 rows of one adapter, which a launch of one workgroup writes down
-// (the plan); up to 64 rows need none, a wave sees them all by a ballot.  Then "down": a tile's h, or g, the contraction over K or N
+// (the plan); few rows need none, every wave sees them all by ballots.  Then "down": a tile's h, or g, the contraction over K or N
 // split over a workgroup's eight waves and, where tiles are few, over workgroups, whose parts whoever reads h adds up; "up": a
-// tile's part of out or dx; "weights": an adapter's gradients, 128 columns (64 in fp32) to a workgroup.
+// tile's part of out or dx; "weights": an adapter's gradients, 128 columns (64 in fp32) to a workgroup.  A small tile goes down and up
+// in one launch.
 //
-// All three take their operands from memory straight into the matrix instructions' registers, 16 bytes a lane and load: the order
-// of a contraction is free as long as both operands have the same, and so is which of the product's columns a lane's are.  Where
-// memory runs along the contraction, a load is a fragment; where it runs across it, a lane loads as many lines of the contraction as
-// a fragment has, and turns them in registers: lane i then has the columns i kLane to i kLane + kLane - 1, in as many
-// products.  Nothing goes through LDS but the sums of waves.
+// Operands come in loads of 16 bytes a lane: the order of a contraction is free as long as both operands have the same, and so is
+// which of the product's columns a lane's are.  Where memory runs across the contraction, a lane loads as many lines of it as a
+// fragment has, and turns them in registers: lane i then has the columns i kLane to i kLane + kLane - 1, in as many products.  Where it
+// runs along the contraction a load is a fragment, but sixteen lines apart from lane to lane: what is long so, x and dy, is loaded
+// line by line and takes the way through LDS.  h, which all of a workgroup's columns take, lies there as fragments.
+//
+// Measured in a step of 8192 x 4096 x 16384, rank 64, 32 adapters, bfloat16 (a large copy: 5.1 TB/s): plan 12 us; forward down 42 (x
+// and A read: 2.0 TB/s), up 136 (base read, out written: 4.0 TB/s); backward down 131 (dy and B: 2.6 TB/s; every tile of 32 rows
+// reads its adapter's B again, twice its rows' bytes, from L2), up 40 (dx and A), weights 124 (x, dy and the gradients: 3.3 TB/s).
 //
 // bfloat16: h, g and their sums are held in 32 bits.  Where they are multiplied again each is taken as two bfloat16 values, the first
 // cut off and the second rounded: off by 2^-16 of itself at most.  fp32: products in 32 bits.
@@ -190,7 +195,7 @@ __host__ __device__ inline Plan plan_at(const void* p, int64_t M, int n)
     return {w, w + n + 3, w + n + 4, reinterpret_cast<const uint2*>(w + (plan_words(M, n) + 1) / 2 * 2)};
 }
 
-constexpr int64_t kDirect = 256;        // as many rows a wave sees at once
+constexpr int64_t kDirect = 256;        // as many rows a wave sees at once (without a plan)
 
 // lanes with the same value of `bits` bits
 __device__ __forceinline__ uint64_t same_lanes(uint32_t v, int bits, uint64_t among)
@@ -313,6 +318,7 @@ struct Group {
     const uint32_t* order;          // the plan's, from the group's first place on, or null: of few rows,
     uint32_t listed[kWords];        // 64 at a time, lane p has the p-th of the group, of which
     uint32_t start[kWords];         // so many are before these 64
+    uint32_t words;                 // how many 64 there are
     // lane l's: the row at place first + `from` + l, the last one's behind it
     __device__ __forceinline__ uint32_t rows(uint32_t from) const
     {
@@ -321,6 +327,7 @@ struct Group {
         uint32_t row = __shfl(listed[0], (int)place);
 #pragma unroll
         for (int w = 1; w < kWords; ++w) {
+            if (w >= (int)words) break;
             const uint32_t other = __shfl(listed[w], (int)(place - start[w]));
             row = place >= start[w] ? other : row;
         }
@@ -330,7 +337,7 @@ struct Group {
 
 struct RowArgs {
     const int64_t* ids;
-    const void* plan;
+    const void* plan;               // null: none, there are few rows
     int64_t M;
     int n;
 };
@@ -357,53 +364,51 @@ __device__ __forceinline__ bool place_of(const Grid& k, uint32_t& inner, uint32_
     return idx < k.total && outer < k.outer;
 }
 
-// of few rows, those of a group; which(a lane's groups of every 64) says which
-template <class F>
-__device__ __forceinline__ Group listed_rows(const RowArgs& a, F which)
+// of few rows, a lane's groups of every 64
+__device__ __forceinline__ void groups_of(const RowArgs& a, uint32_t (&g)[kWords])
+{
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        const int64_t row = 64 * w + (threadIdx.x & 63);
+        g[w] = row < a.M ? group_of(a.ids[row], a.n) : ~0u;
+    }
+}
+__device__ __forceinline__ Group listed_rows(const RowArgs& a, const uint32_t (&g)[kWords], uint32_t group)
 {
     const int lane = threadIdx.x & 63;
     const uint64_t lower = (1ull << lane) - 1;
-    uint32_t g[kWords];
-#pragma unroll
-    for (int w = 0; w < kWords; ++w) {
-        const int64_t row = 64 * w + lane;
-        g[w] = row < a.M ? group_of(a.ids[row], a.n) : ~0u;
-    }
     Group of{};
-    of.group = which(g);
+    of.group = group;
 #pragma unroll
     for (int w = 0; w < kWords; ++w) {
-        const uint64_t same = __ballot(g[w] == of.group);
+        of.start[w] = of.count;
+        if (w && 64 * w >= a.M) continue;
+        const uint64_t same = __ballot(g[w] == group);
         // (the others go behind them, each to a place of its own)
         const int count = __popcll(same), to = same >> lane & 1 ? __popcll(same & lower) : count + __popcll(~same & lower);
         of.listed[w] = 64 * w + (uint32_t)__builtin_amdgcn_ds_permute(4 * to, lane);
-        of.start[w] = of.count;
         of.count += (uint32_t)count;
     }
+    of.words = (uint32_t)(a.M + 63) / 64;
     return of;
 }
 
 // The rows of workgroup `tile`, 32 at most: none where there is no such tile.  Of few rows, every 32nd of a group stands for a tile.
 __device__ __forceinline__ Group tile_rows(const RowArgs& a, uint32_t tile)
 {
-    if (a.M <= kDirect) {
-        uint32_t before = 0;        // rows of the group before the tile's
-        Group of = listed_rows(a, [&](const uint32_t (&g)[kWords]) {
-            uint32_t mine = 0;
+    if (!a.plan) {
+        uint32_t g[kWords], before = 0;         // rows of the group before the tile's
+        groups_of(a, g);
+        const uint32_t mine = group_of(a.ids[tile], a.n);
 #pragma unroll
-            for (int w = 0; w < kWords; ++w) {
-                const uint32_t there = __shfl(g[w], (int)(tile & 63));
-                mine = tile >> 6 == (uint32_t)w ? there : mine;
-            }
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) {
-                const uint64_t same = __ballot(g[w] == mine), until = (1ull << (tile & 63)) - 1;
-                before += (uint32_t)w < tile >> 6 ? __popcll(same) : (uint32_t)w == tile >> 6 ? __popcll(same & until) : 0;
-            }
-            return mine;
-        });
+        for (int w = 0; w < kWords; ++w) {
+            const uint64_t same = __ballot(g[w] == mine), until = (1ull << (tile & 63)) - 1;
+            before += (uint32_t)w < tile >> 6 ? __popcll(same) : (uint32_t)w == tile >> 6 ? __popcll(same & until) : 0;
+        }
+        if (before % kTile) return Group{};
+        Group of = listed_rows(a, g, mine);
         of.first = before;
-        of.count = before % kTile ? 0 : of.count - before < kTile ? of.count - before : kTile;
+        of.count = of.count - before < kTile ? of.count - before : kTile;
         return of;
     }
     const Plan p = plan_at(a.plan, a.M, a.n);
@@ -419,7 +424,11 @@ __device__ __forceinline__ Group tile_rows(const RowArgs& a, uint32_t tile)
 }
 __device__ __forceinline__ Group adapter_rows(const RowArgs& a, uint32_t adapter)
 {
-    if (a.M <= kDirect) return listed_rows(a, [&](const uint32_t (&)[kWords]) { return adapter; });
+    if (!a.plan) {
+        uint32_t g[kWords];
+        groups_of(a, g);
+        return listed_rows(a, g, adapter);
+    }
     const Plan p = plan_at(a.plan, a.M, a.n);
     Group of{};
     of.group = adapter;
@@ -997,12 +1006,9 @@ __global__ __launch_bounds__(256) void add_parts_kernel(WeightArgs a)
 
 int tiles_of_rank(int r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }
 
-// (what a grid has: tiles that may be)
-uint32_t grid_tiles(const AdapterArgs& a) { return (uint32_t)(a.M <= kDirect ? a.M : most_tiles(a.M, a.n)); }
-
 // Where what a tile's workgroup reads and writes by itself, the adapter and its rows either way, takes less time than a launch, and
 // tiles do not fill the chip by themselves.  A forward call, two launches and one: 64 x 512 x 512 of rank 16 in bfloat16 (96 KB)
-// 9.4 and 6.9 us, 1000 x 512 x 512 of rank 16 in fp32 (192 KB) 14.9 and 14.5, 1 x 4096 x 4096 of rank 16 (272 KB) 9.8 and 15.5,
+// 9.4 and 6.9 us, 256 x 512 x 512 of rank 16 10.9 and 8.5, 1000 x 512 x 512 of rank 16 in fp32 (192 KB) 14.9 and 14.5, 1 x 4096 x 4096 of rank 16 (272 KB) 9.8 and 15.5,
 // 8192 x 512 x 512 of rank 8 25.6 and 26.2.
 bool small_tile(const AdapterArgs& a)
 {
@@ -1010,16 +1016,26 @@ bool small_tile(const AdapterArgs& a)
     return a.M <= 4096 && (a.K + a.N) * (a.r + rows) * dtype_size(a.dtype) <= 192 << 10;
 }
 
-// Parts of a contraction over D: as many as make 512 workgroups, none of fewer than a step for each of the eight waves; one of a small
-// tile.
+// Rows without a plan: every workgroup, of a tile for every row, of which all but the first of 32 have none, looks through all of them.
+// With a launch for the plan, a forward call: 32 x 4096 x 4096 of 64 adapters in bfloat16 14.0 us for 9.9, 100 x 4096 x 4096 of 64 20.5 for
+// 16.1, 200 x 1024 x 1024 of 10, a small tile, 14.0 for 9.8; the other way round 256 x 4096 x 4096 of 4 15.7 for 18.3, and 20.9 for 28.2
+// backward.
+bool direct(const AdapterArgs& a) { return a.M <= 128 || (a.M <= kDirect && small_tile(a)); }
+// (what a grid has: tiles that may be)
+uint32_t grid_tiles(const AdapterArgs& a) { return (uint32_t)(direct(a) ? a.M : most_tiles(a.M, a.n)); }
+
+// Parts of a contraction over D: as many as make 128 workgroups, none of fewer than a step for each of the eight waves; one of a small
+// tile.  (Whoever reads h reads all parts.  In bfloat16, rank 16, as many as make 64, 128 and 256, and one: 32 x 4096 x 4096 of 64 adapters
+// forward 11.5, 9.9, 10.0 and 14.1 us; 100 rows 18.8, 16.1, 17.6 and 18.8; 1000 rows of 10 adapters 23.8, 19.7, 18.8 and 23.7, and
+// backward 21.4, 23.9, 25.8 and 21.4.)
 struct Parts {
     uint32_t parts, steps;
 };
 Parts parts_of(const AdapterArgs& a, int64_t D)
 {
     const int64_t step = a.dtype == kBf16 ? 64 : 32, steps = (D + step - 1) / step;
-    const int64_t tiles = a.M <= kDirect ? (a.M < a.n ? a.M : a.n) : a.M / kTile + (a.n < a.M / kTile ? a.n : a.M / kTile);
-    int64_t parts = small_tile(a) ? 1 : 512 / (tiles > 0 ? tiles : 1);
+    const int64_t tiles = direct(a) ? (a.M < a.n ? a.M : a.n) : a.M / kTile + (a.n < a.M / kTile ? a.n : a.M / kTile);
+    int64_t parts = small_tile(a) ? 1 : 128 / (tiles > 0 ? tiles : 1);
     if (parts > kMostParts) parts = kMostParts;
     while (parts > 1 && steps < parts * kDownWaves) --parts;
     if (parts < 1) parts = 1;
@@ -1030,20 +1046,21 @@ Parts parts_of(const AdapterArgs& a, int64_t D)
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t plan_bytes(const AdapterArgs& a)
 {
-    return a.M <= kDirect ? 0 : rounded((plan_words(a.M, a.n) + 1) / 2 * 8 + sizeof(uint2) * (size_t)most_tiles(a.M, a.n));
+    return direct(a) ? 0 : rounded((plan_words(a.M, a.n) + 1) / 2 * 8 + sizeof(uint2) * (size_t)most_tiles(a.M, a.n));
 }
 size_t h_bytes(const AdapterArgs& a, int64_t D)
 {
     return rounded((size_t)parts_of(a, D).parts * (size_t)a.M * 16 * tiles_of_rank(a.r) * sizeof(float));
 }
 
-// Parts of the rows that the adapters' gradients are added up over: where columns and adapters are few workgroups, as many as make 1024
-// of them, none of fewer than 128 rows to an adapter.
+// Parts of the rows that the adapters' gradients are added up over: where columns and adapters are few workgroups, as many as make 256
+// of them, none of fewer than 128 rows to an adapter.  (Backward, 8192 x 4096 x 4096 of rank 16 in bfloat16, one part, 256 workgroups and
+// 1024: of one adapter 102, 66 and 68 us, of four 64, 64 and 66; 8192 x 1024 x 1024 of rank 8 and four in fp32 51, 44 and 43.)
 uint32_t split_of(const AdapterArgs& a)
 {
     const int64_t columns = a.dtype == kBf16 ? 128 : 64;
     const int64_t groups = ((a.K + columns - 1) / columns + (a.N + columns - 1) / columns) * a.n;
-    int64_t split = 1024 / groups;
+    int64_t split = 256 / groups;
     const int64_t most = a.M / (128 * (int64_t)a.n);
     if (split > most) split = most;
     return (uint32_t)(split < 1 ? 1 : split > 16 ? 16 : split);
@@ -1085,7 +1102,8 @@ void launch_pass(const AdapterArgs& a, const void* x, const void* W1, float* h, 
     const Parts p = parts_of(a, D);
     const uint32_t tiles = grid_tiles(a);
     const DownArgs d{rows, grid_of(tiles, p.parts), x, W1, h, D, a.r, p.steps, p.parts};
-    // (a workgroup has a tile's columns in so many parts: as few as make 2048 workgroups)
+    // (a workgroup has a tile's columns in so many parts: as few as make 2048 workgroups.  With 512 and 8192, 8192 x 4096 x 16384 of rank 64
+    // in bfloat16 forward 245 and 214 us for 207)
     const int64_t columns = (a.dtype == kBf16 ? 128 : 64) * kUpWaves, most = (N + columns - 1) / columns, want = 2048 / tiles + 1;
     const uint32_t across = (uint32_t)(most < want ? most : want);
     const UpArgs u{rows, grid_of(across, tiles), h, a.scale, W2, base, out, N, a.r, p.parts};
@@ -1120,8 +1138,8 @@ size_t adapters_workspace(const AdapterArgs& a) { return h_bytes(a, a.N) + sums_
 hipError_t launch_adapters_fwd(const AdapterArgs& a, hipStream_t stream)
 {
     float* h = reinterpret_cast<float*>(static_cast<char*>(a.saved) + plan_bytes(a));
-    const RowArgs rows{a.ids, a.saved, a.M, a.n};
-    if (a.M > kDirect) {
+    const RowArgs rows{a.ids, direct(a) ? nullptr : a.saved, a.M, a.n};
+    if (rows.plan) {
         ProfileScope ps(K_ADAPT_PLAN, stream);
         int bits = 1;
         while ((1 << bits) < a.n + 2) ++bits;
@@ -1135,7 +1153,7 @@ hipError_t launch_adapters_bwd(const AdapterArgs& a, void* workspace, hipStream_
 {
     float* h = reinterpret_cast<float*>(static_cast<char*>(a.saved) + plan_bytes(a));
     float* g = static_cast<float*>(workspace);
-    const RowArgs rows{a.ids, a.saved, a.M, a.n};
+    const RowArgs rows{a.ids, direct(a) ? nullptr : a.saved, a.M, a.n};
     if (a.out || a.dA) launch_pass<kAlong>(a, a.dy, a.B, g, a.A, a.base, a.out, a.N, a.K, rows, stream);
     if (a.dA || a.dB) {
         ProfileScope ps(K_ADAPT_WEIGHTS, stream);

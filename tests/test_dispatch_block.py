@@ -28,10 +28,12 @@ def test_launches():
     names = lambda *c: [k.replace("_kernel", "") for k in dispatch([c])[0].kernels]
     assert names("dropout", 1000, F32) == ["dropout"]
     assert names("norm_fwd", 1000, 64, F32) == ["layernorm_fwd"]
-    assert names("norm_bwd", 1000, 64, F32, 15) == ["layernorm_bwd", "layernorm_params"]
-    assert names("norm_bwd", 1000, 64, F32, 3) == ["layernorm_bwd"] and names("norm_bwd", 100, 64, F32, 15) == ["layernorm_bwd"]
+    assert names("norm_bwd", 1025, 64, F32, 15) == ["layernorm_bwd", "layernorm_params"]
+    assert names("norm_bwd", 1025, 64, F32, 3) == ["layernorm_bwd"] and names("norm_bwd", 1024, 64, F32, 15) == ["layernorm_bwd"]
     assert names("adapt_fwd", 100, 256, 256, 8, 4, F32) == ["down_up"]
     assert names("adapt_fwd", 257, 256, 256, 8, 4, F32) == ["plan", "down_up"]
+    assert names("adapt_fwd", 256, 256, 256, 8, 4, F32) == ["down_up"] and names("adapt_fwd", 128, 4096, 4096, 16, 4, BF16) == ["down", "up"]
+    assert names("adapt_fwd", 129, 4096, 4096, 16, 4, BF16) == ["plan", "down", "up"]
     assert names("adapt_fwd", 100, 256, 63, 8, 4, F32) == ["down", "up"] and names("adapt_fwd", 100, 31, 256, 8, 4, F32) == ["down", "up"]
     assert names("adapt_fwd", 100, 256, 256, 65, 4, F32) == ["down", "up"] and names("adapt_fwd", 5000, 256, 256, 8, 4, F32) == ["plan", "down", "up"]
     assert names("adapt_fwd", 100, 4096, 4096, 8, 4, F32) == ["down", "up"]
