@@ -454,7 +454,9 @@ hipError_t launch_layernorm_fwd(const LayerNormArgs& a, hipStream_t stream)
 hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStream_t stream)
 {
     const Rows k = bwd_rows(a);
-    const bool params = a.dweight || a.dbias, alone = params && a.M <= kFewRows && k.R == 1;
+    // (in the same launch only where no row's gradients are written over what the columns' sums read)
+    const bool over = a.dx && (a.dx == a.dy || a.dx == a.s), over_too = a.dresidual && (a.dresidual == a.dy || a.dresidual == a.s);
+    const bool params = a.dweight || a.dbias, alone = params && a.M <= kFewRows && k.R == 1 && !over && !over_too;
     float* parts = params && !alone ? static_cast<float*>(workspace) : nullptr;
     {
         ProfileScope ps(K_LAYERNORM_BWD, stream);

@@ -21,11 +21,11 @@ int main()
             rc = hdqt_dropout(at(0), at(1), at(2), v[0], (int)v[1], &drop, nullptr);
         if (!strcmp(what, "norm_fwd"))              // rows, columns, type
             rc = hdqt_layernorm_fwd(at(0), at(1), &drop, at(2), at(3), at(4), at(5), f(6), v[0], v[1], 1e-5f, (int)v[2], HDQT_F32, nullptr);
-        if (!strcmp(what, "norm_bwd")) {            // rows, columns, type, wanted (1 dx, 2 dresidual, 4 dweight, 8 dbias)
+        if (!strcmp(what, "norm_bwd")) {            // rows, columns, type, wanted (1 dx, 2 dresidual, 4 dweight, 8 dbias; 16: dx is dy, 32: dresidual is)
             auto want = [&](int bit, int k) { return v[3] & bit ? at(k) : nullptr; };
             ws = hdqt_layernorm_bwd_workspace_size(v[0], v[1], (int)v[2]);
-            rc = hdqt_layernorm_bwd(at(0), at(1), at(2), &drop, at(3), f(4), want(1, 5), want(2, 6), want(4, 7), want(8, 8), v[0], v[1], (int)v[2],
-                                    HDQT_F32, at(9), ws, nullptr);
+            rc = hdqt_layernorm_bwd(at(0), at(1), at(2), &drop, at(3), f(4), want(1, v[3] & 16 ? 0 : 5), want(2, v[3] & 32 ? 0 : 6), want(4, 7), want(8, 8), v[0],
+                                    v[1], (int)v[2], HDQT_F32, at(9), ws, nullptr);
         }
         if (!strncmp(what, "adapt", 5)) {           // rows, features, outputs, rank, adapters, type, wanted (1 dx, 2 dA, 4 dB)
             const int r = (int)v[3], n = (int)v[4], t = (int)v[5];

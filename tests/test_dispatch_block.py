@@ -30,6 +30,8 @@ def test_launches():
     assert names("norm_fwd", 1000, 64, F32) == ["layernorm_fwd"]
     assert names("norm_bwd", 1025, 64, F32, 15) == ["layernorm_bwd", "layernorm_params"]
     assert names("norm_bwd", 1025, 64, F32, 3) == ["layernorm_bwd"] and names("norm_bwd", 1024, 64, F32, 15) == ["layernorm_bwd"]
+    # (over dy only behind whoever else reads it)
+    assert names("norm_bwd", 1024, 64, F32, 15 + 16) == ["layernorm_bwd", "layernorm_params"] == names("norm_bwd", 1024, 64, F32, 15 + 32)
     assert names("adapt_fwd", 100, 256, 256, 8, 4, F32) == ["down_up"]
     assert names("adapt_fwd", 257, 256, 256, 8, 4, F32) == ["plan", "down_up"]
     assert names("adapt_fwd", 256, 256, 256, 8, 4, F32) == ["down_up"] and names("adapt_fwd", 128, 4096, 4096, 16, 4, BF16) == ["down", "up"]

@@ -5,6 +5,8 @@ sums whose error is that of a few partial sums: 2e-6 (32 roundings).  bfloat16, 
 more.  What is formed from the sum is compared with what the formulas make of the sum as it was held, the sum with its own.  ds is a
 difference: against the 2-norm of its terms.  dweight and dbias: sums of terms of either sign, whose result may be smaller than its terms by the square root
 of their number; against the 2-norm over the terms' own."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -223,3 +225,23 @@ def test_gradients_against_differences():
         step = lambda t: {**at, name: at[name] + t * u}
         want = (value(step(h)) - value(step(-h))) / (2 * h)
         assert abs(want - float((grad.double().cpu() * u).sum())) <= 1e-4 * float(grad.double().norm()) * float(u.norm()) / 10
+
+
+@pytest.mark.parametrize("M", [1, 128, 300, 1024, 1025])
+def test_gradients_over_their_own_inputs(M):
+    """dx over dy and dresidual over dsum, as the interface allows: of few rows too, whose columns' sums read dy beside them."""
+    x, res, dy, dsum, w, b = inputs((M, 512), F32)
+    d = B.Dropout(0.3, 77, 5)
+    _, total, saved = B.layernorm_fwd(x, w, b, residual=res, dropout=d)
+    want = B.layernorm_bwd(dy, total, saved, w, dsum, d)
+    first, apart = dy.clone(), [torch.empty_like(w), torch.empty_like(w)]
+    lib = B.load()
+    ws = torch.empty(lib.hdqt_layernorm_bwd_workspace_size(M, 512, 0), dtype=torch.uint8, device="cuda")
+    p = lambda t: C.c_void_p(t.data_ptr())
+    rc = lib.hdqt_layernorm_bwd(p(dy), p(dsum), p(total), C.byref(d.c()), p(w), p(saved), p(dy), p(dsum), p(apart[0]), p(apart[1]), M, 512, 0, 0,
+                                p(ws), ws.numel(), C.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert rc == 0
+    assert torch.equal(dy, want[0]) and torch.equal(dsum, want[1])
+    exact = layer_norm(x, first, w, b, res, None, d, held=total)
+    for got, name, terms in zip(apart, ("dweight", "dbias"), ("dw_terms", "db_terms")):
+        near(got, exact[name], 1.0, norm=2e-6 * exact[terms])
