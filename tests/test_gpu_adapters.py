@@ -116,6 +116,21 @@ def test_numbers_that_are_none(M, dtype):
     near(dB, want["dB"], dtype)
 
 
+@pytest.mark.parametrize("M", [40, 300])
+def test_an_adapter_without_rows(M):
+    """Zeros for its gradients, whatever its matrices and its scale hold; the others as without it."""
+    i = inputs(M, 96, 200, 8, 4, F32)
+    ids = torch.where(i["ids"] == 2, torch.full_like(i["ids"], 1), i["ids"])
+    run = lambda: (B.adapters_fwd(i["x"], i["A"], i["Bm"], ids, i["scale"], i["base"]))
+    out, saved = run()
+    grads = B.adapters_bwd(i["dy"], i["x"], i["A"], i["Bm"], ids, saved, i["scale"])
+    i["scale"][2], i["A"][2], i["Bm"][2] = float("inf"), float("nan"), float("inf")
+    out2, saved = run()
+    got = B.adapters_bwd(i["dy"], i["x"], i["A"], i["Bm"], ids, saved, i["scale"])
+    assert torch.equal(out2, out) and all(torch.equal(p, q) for p, q in zip(got, grads))
+    assert not got[1][2].any() and not got[2][2].any()
+
+
 @pytest.mark.parametrize("M", [40, 200, 300])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_unusual_values_stay_where_they_belong(M, dtype):
