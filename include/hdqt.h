@@ -77,7 +77,7 @@ typedef enum { HDQT_GEMM_FWD = 0, HDQT_GEMM_BWD_INPUT = 1, HDQT_GEMM_BWD_WEIGHT 
 
 #define HDQT_EINVAL_DTYPE (-15)    /* unknown element type */
 #define HDQT_EINVAL_OPTION (-16)   /* unknown reduction, activation or kind of norm, or a number (eps,
-                                      max_norm) out of its range */
+                                      max_norm, p) out of its range */
 
 /* One quantized operand; names follow the paper's quantizer Q. */
 typedef struct {
