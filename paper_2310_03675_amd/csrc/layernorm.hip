@@ -400,13 +400,15 @@ Rows fwd_rows(const LayerNormArgs& a)
     k.groups = (uint32_t)(groups < (1 << 20) ? groups : 1 << 20);
     return k;
 }
-// Two workgroups to a compute unit, of 1024 threads one: what registers leave room for, each with one part of the parameters' gradients.
-// (One, two and three, bfloat16: 20011 x 1031 70, 52 and 64 us, 8192 x 4096 70, 65 and 74; of 1024 threads one and two: 2048 x 16384 83
-// and 110.)
+// Two workgroups to a compute unit, what registers leave room for, each with one part of the parameters' gradients; one, and half as many
+// parts, where they have 1024 threads, or come round to fewer than four turns each.  (One, two and three, bfloat16: 20011 x 1031 70, 52 and
+// 64 us, 8192 x 4096 70, 65 and 74; 2000 x 1031, few turns, one and two: 15.6 and 18.7, 2048 x 4096 27 and 31; of 1024 threads 2048 x 16384
+// 83 and 110.  Few rows leave no parts: 300 x 4096 6.1 and 5.1.)
+bool few_rows(const LayerNormArgs& a, const Rows& k) { return a.M <= kFewRows && k.R <= kBwdMost; }
 Rows bwd_rows(const LayerNormArgs& a)
 {
     Rows k = rows_of(a, kBwdMost, kBwdThreads, 2048);
-    const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.width == 1024 ? 1 : 2);
+    const int64_t groups = (a.M + k.at_once - 1) / k.at_once, most = 256 * (k.width == 1024 || (groups < 2048 && !few_rows(a, k)) ? 1 : 2);
     k.groups = (uint32_t)(groups < most ? groups : most);
     return k;
 }
@@ -456,7 +458,7 @@ hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStre
     const Rows k = bwd_rows(a);
     // (in the same launch only where no row's gradients are written over what the columns' sums read)
     const bool over = a.dx && (a.dx == a.dy || a.dx == a.s), over_too = a.dresidual && (a.dresidual == a.dy || a.dresidual == a.s);
-    const bool params = a.dweight || a.dbias, alone = params && a.M <= kFewRows && k.R == 1 && !over && !over_too;
+    const bool params = a.dweight || a.dbias, alone = params && few_rows(a, k) && !over && !over_too;
     float* parts = params && !alone ? static_cast<float*>(workspace) : nullptr;
     {
         ProfileScope ps(K_LAYERNORM_BWD, stream);
@@ -465,8 +467,8 @@ hipError_t launch_layernorm_bwd(const LayerNormArgs& a, void* workspace, hipStre
         const dim3 grid(k.groups + (alone ? (uint32_t)((a.C + 31) / 32) : 0));
         with_rows<kBwdMost>(a, k, [&](auto dt, auto r, auto end, auto t) {
             if (alone) {
-                if constexpr (r.value == 1)
-                    hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, 1, end.value, t.value, true>), grid, dim3(t.value), 0, stream, a, k, parts);
+                if constexpr (r.value <= kBwdMost)
+                    hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, r.value, end.value, t.value, true>), grid, dim3(t.value), 0, stream, a, k, parts);
             } else {
                 hipLaunchKernelGGL((layernorm_bwd_kernel<dt.value, r.value, end.value, t.value, false>), grid, dim3(t.value), lds, stream, a, k, parts);
             }
