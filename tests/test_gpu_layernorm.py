@@ -77,6 +77,13 @@ def test_against_64_bits(shape, dtype, how):
     check(shape, dtype, how)
 
 
+@pytest.mark.parametrize("shape", [(1000, 2051), (1000, 2048), (1023, 2056), (520, 4096), (1025, 2051), (2047, 1031), (2049, 1031)], ids=str)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_two_vectors(shape, dtype):
+    """Two vectors to a thread, on both sides of how many rows take one launch, and of how many make parts."""
+    check(shape, dtype, "both")
+
+
 @pytest.mark.parametrize("how", ["plain", "both"])
 def test_parameters(how):
     for dtype in (F32, BF16):
