@@ -347,7 +347,8 @@ __global__ __launch_bounds__(T) void layernorm_bwd_kernel(LayerNormArgs a, Rows 
     }
 }
 
-// dw and db: the parts' sums of 32 columns
+// dw and db: the parts' sums of 32 columns (backward, 16, 32 and 64 of them: 8192 x 4096 in bfloat16 68.5, 65 and 66 us, 131072 x 64 27.8, 28.3
+// and 29.9)
 constexpr int kParamThreads = 512;
 __global__ __launch_bounds__(kParamThreads) void layernorm_params_kernel(LayerNormArgs a, const float* parts, uint32_t groups)
 {
