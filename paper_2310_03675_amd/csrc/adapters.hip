@@ -4,8 +4,8 @@
 //   dx_i = base_i + g_i A_a^T,   dA_a = sum x_i^T g_i,   dB_a = sum scale_a h_i^T dy_i   (over the rows that have a)
 // Four products with an axis of r, at most 128: memory bounds them, reading x, dy and the adapters and writing what is as large.
 //
-// Rows are grouped by adapter, in their order, first: tiles of 32 rows of one adapter, which a launch of one workgroup writes down
-// (the plan); few rows need none, every wave sees them all by ballots.  Then "down": a tile's h, or g, the contraction over K or N
+// Rows are grouped by adapter, in their order, first: tiles of 32 rows of one adapter, which a launch of one workgroup writes down,
+// or three of more than 8192 rows (the plan); few rows need none, every wave sees them all by ballots.  Then "down": a tile's h, or g, the contraction over K or N
 // split over a workgroup's eight waves and, where tiles are few, over workgroups, whose parts whoever reads h adds up; "up": a
 // tile's part of out or dx; "weights": an adapter's gradients, 128 columns (64 in fp32) to a workgroup.  A small tile goes down and up
 // in one launch.
@@ -207,66 +207,66 @@ __device__ __forceinline__ uint64_t same_lanes(uint32_t v, int bits, uint64_t am
     return among;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, int64_t M, int n, int bits, uint32_t* plan)
+// A workgroup looks through 8192 rows, eight times 64 to a wave, all loaded before the first is taken.
+constexpr int kAhead = 8;
+constexpr int64_t kChunkRows = 64 * kPlanWaves * kAhead;
+__host__ __device__ inline int64_t chunks_of(int64_t M) { return (M + kChunkRows - 1) / kChunkRows; }
+
+struct Chunk {
+    int64_t first, end;                     // a wave's rows
+    uint32_t group[kAhead], before[kAhead]; // of a lane's: the group, and its rows in the wave before it
+};
+// Leaves in counts[wave] how many rows of every group the wave has.  (No barrier behind it.)
+__device__ __forceinline__ void look_through(const int64_t* ids, int64_t from, int64_t M, int n, int bits, uint32_t (*counts)[kMostGroups], Chunk& c)
 {
-    __shared__ uint32_t counts[kPlanWaves][kMostGroups];
-    __shared__ uint32_t starts[kMostGroups + 1], tiles[kMostGroups + 1], waves[2][kPlanWaves];
-    const Plan p = plan_at(plan, M, n);
-    uint32_t *start = const_cast<uint32_t*>(p.start), *order = const_cast<uint32_t*>(p.order);
-    const uint32_t groups = (uint32_t)n + 2;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t rows = (M + 64 * kPlanWaves - 1) / (64 * kPlanWaves) * 64, first = wave * rows, end = first + rows < M ? first + rows : M;
-    // f(u, a row, its group, lanes with the same) for a wave's rows, 64 at a time, kAhead of those loaded before the first is taken; where
-    // that is all of them, they are loaded, and looked through for their like, once
-    constexpr int kAhead = 8;
-    const bool once = rows <= 64 * kAhead;
+    const int64_t left = M - from < kChunkRows ? M - from : kChunkRows, rows = (left + 64 * kPlanWaves - 1) / (64 * kPlanWaves) * 64;
+    c.first = from + wave * rows;
+    c.end = c.first + rows < from + left ? c.first + rows : from + left;
     int64_t id[kAhead];
-    uint32_t before_it[kAhead];             // rows of the group in the wave before a lane's
-    auto load = [&](int64_t i) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int64_t at = i + 64 * u + lane;
-            id[u] = at < end ? ids[at] : 0;
-        }
-    };
-    if (first < end) load(first);
-    for (uint32_t i = lane; i < groups; i += 64) counts[wave][i] = 0;
+    for (int u = 0; u < kAhead; ++u) {
+        const int64_t at = c.first + 64 * u + lane;
+        id[u] = at < c.end ? ids[at] : 0;
+    }
+    for (uint32_t i = lane; i < (uint32_t)n + 2; i += 64) counts[wave][i] = 0;
     __syncthreads();
-    auto each = [&](auto f) {
-        for (int64_t i = first; i < end; i += 64 * kAhead) {
-            if (!once) load(i);
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int64_t at = i + 64 * u + lane;
-                if (i + 64 * u >= end) break;
-                f(u, at, group_of(id[u], n), at < end);
-            }
-        }
-    };
-    // the group's rows of the wave so far, and those of this 64 before a lane's, which are counted
-    auto count = [&](uint32_t g, bool there) {
-        const uint64_t same = same_lanes(g, bits, __ballot(there));
+    for (int u = 0; u < kAhead; ++u) {
+        if (c.first + 64 * u >= c.end) break;
+        const bool there = c.first + 64 * u + lane < c.end;
+        c.group[u] = group_of(id[u], n);
+        // the group's rows of the wave so far, and those of this 64 before a lane's, which are counted
+        const uint64_t same = same_lanes(c.group[u], bits, __ballot(there));
         const int leader = __ffsll((unsigned long long)same) - 1;
         uint32_t at = 0;
-        if (there && lane == leader) at = atomicAdd(&counts[wave][g], (uint32_t)__popcll(same));
-        return __shfl(at, leader & 63) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-    };
-    each([&](int u, int64_t, uint32_t g, bool there) { before_it[u] = count(g, there); });
-    __syncthreads();
-    // a thread's two groups: their rows and tiles, and the sums of those of the groups before
-    uint32_t have[2] = {0, 0}, cut[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const uint32_t g = 2 * threadIdx.x + u;
-        if (g < groups)
-            for (int w = 0; w < kPlanWaves; ++w) {
-                const uint32_t c = counts[w][g];
-                counts[w][g] = have[u];             // (of the group's rows, those of the waves before)
-                have[u] += c;
-            }
-        cut[u] = (have[u] + kTile - 1) / kTile;
+        if (there && lane == leader) at = atomicAdd(&counts[wave][c.group[u]], (uint32_t)__popcll(same));
+        c.before[u] = __shfl(at, leader & 63) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
     }
-    uint32_t before[2] = {have[0] + have[1], cut[0] + cut[1]};
+}
+// Writes the rows to their places, counts[wave][group] being where the wave's rows of the group begin.
+__device__ __forceinline__ void put_in_order(const Chunk& c, const uint32_t (*counts)[kMostGroups], uint32_t* order)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int64_t row = c.first + 64 * u + lane;
+        if (row < c.end) order[counts[wave][c.group[u]] + c.before[u]] = (uint32_t)row;
+    }
+}
+
+struct PlanLds {
+    uint32_t starts[kMostGroups + 1], tiles[kMostGroups + 1], waves[2][kPlanWaves];
+};
+// From how many rows a thread's two groups have: where groups begin, and the tiles
+__device__ __forceinline__ void lay_out(const uint32_t (&have)[2], const Plan& p, uint32_t groups, PlanLds& lds)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    uint32_t cut[2], before[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) cut[u] = (have[u] + kTile - 1) / kTile;
+    before[0] = have[0] + have[1];
+    before[1] = cut[0] + cut[1];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const uint32_t own = before[u];
@@ -274,40 +274,131 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, 
             const uint32_t up = __shfl_up(before[u], m);
             if (lane >= m) before[u] += up;
         }
-        if (lane == 63) waves[u][wave] = before[u];
+        if (lane == 63) lds.waves[u][wave] = before[u];
         before[u] -= own;
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-        for (int w = 0; w < wave; ++w) before[u] += waves[u][w];
+        for (int w = 0; w < wave; ++w) before[u] += lds.waves[u][w];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const uint32_t g = 2 * threadIdx.x + u;
         if (g <= groups) {
-            starts[g] = before[0];
-            tiles[g] = before[1];
-            start[g] = before[0];
+            lds.starts[g] = before[0];
+            lds.tiles[g] = before[1];
+            const_cast<uint32_t*>(p.start)[g] = before[0];
         }
         before[0] += have[u];
         before[1] += cut[u];
     }
     __syncthreads();
-    const uint32_t total = tiles[groups];
+    const uint32_t total = lds.tiles[groups];
     if (threadIdx.x == 0) *const_cast<uint32_t*>(p.tiles) = total;
     for (uint32_t i = threadIdx.x; i < total; i += kPlanThreads) {
         uint32_t lo = 0, hi = groups;               // the last group whose first tile is not behind this one
         while (hi - lo > 1) {
             const uint32_t mid = (lo + hi) / 2;
-            if (tiles[mid] <= i) lo = mid;
+            if (lds.tiles[mid] <= i) lo = mid;
             else hi = mid;
         }
-        const_cast<uint2*>(p.tile)[i] = make_uint2(lo, starts[lo] + kTile * (i - tiles[lo]));
+        const_cast<uint2*>(p.tile)[i] = make_uint2(lo, lds.starts[lo] + kTile * (i - lds.tiles[lo]));
     }
-    each([&](int u, int64_t row, uint32_t g, bool there) {
-        const uint32_t at = once ? (there ? counts[wave][g] : 0) + before_it[u] : count(g, there);
-        if (there) order[starts[g] + at] = (uint32_t)row;
-    });
+}
+
+// Up to 8192 rows, by one workgroup.
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int64_t* ids, int64_t M, int n, int bits, uint32_t* plan)
+{
+    __shared__ uint32_t counts[kPlanWaves][kMostGroups];
+    __shared__ PlanLds lds;
+    const Plan p = plan_at(plan, M, n);
+    const uint32_t groups = (uint32_t)n + 2;
+    Chunk c;
+    look_through(ids, 0, M, n, bits, counts, c);
+    __syncthreads();
+    uint32_t have[2] = {0, 0};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t g = 2 * threadIdx.x + u;
+        if (g < groups)
+            for (int w = 0; w < kPlanWaves; ++w) have[u] += counts[w][g];
+    }
+    lay_out(have, p, groups, lds);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t g = 2 * threadIdx.x + u;
+        if (g < groups) {
+            uint32_t at = lds.starts[g];
+            for (int w = 0; w < kPlanWaves; ++w) {
+                const uint32_t own = counts[w][g];
+                counts[w][g] = at;
+                at += own;
+            }
+        }
+    }
+    __syncthreads();
+    put_in_order(c, counts, const_cast<uint32_t*>(p.order));
+}
+
+// Of more rows: how many of every group each 8192 have; where those begin; the order.  (Three launches: 16384 rows 19 us, 65536 of ten adapters
+// 21, a million 41; one workgroup for all of them 23, 76 and 1095.)
+__global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(const int64_t* ids, int64_t M, int n, int bits, uint32_t* chunks)
+{
+    __shared__ uint32_t counts[kPlanWaves][kMostGroups];
+    const uint32_t groups = (uint32_t)n + 2;
+    Chunk c;
+    look_through(ids, blockIdx.x * kChunkRows, M, n, bits, counts, c);
+    __syncthreads();
+    for (uint32_t g = threadIdx.x; g < groups; g += kPlanThreads) {
+        uint32_t s = 0;
+        for (int w = 0; w < kPlanWaves; ++w) s += counts[w][g];
+        chunks[(int64_t)blockIdx.x * groups + g] = s;
+    }
+}
+__global__ __launch_bounds__(kPlanThreads) void plan_starts_kernel(int64_t M, int n, uint32_t* plan, uint32_t* chunks, uint32_t of_them)
+{
+    __shared__ PlanLds lds;
+    const uint32_t groups = (uint32_t)n + 2;
+    uint32_t have[2] = {0, 0};
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t g = 2 * threadIdx.x + u;
+        if (g < groups)
+#pragma unroll 8
+            for (uint32_t i = 0; i < of_them; ++i) have[u] += chunks[(int64_t)i * groups + g];
+    }
+    lay_out(have, plan_at(plan, M, n), groups, lds);
+    for (uint32_t g = threadIdx.x; g < groups; g += kPlanThreads) {
+        uint32_t at = lds.starts[g];
+        for (uint32_t i = 0; i < of_them; i += 8) {
+            uint32_t own[8];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) own[k] = i + k < of_them ? chunks[(int64_t)(i + k) * groups + g] : 0;
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) {
+                if (i + k < of_them) chunks[(int64_t)(i + k) * groups + g] = at;
+                at += own[k];
+            }
+        }
+    }
+}
+__global__ __launch_bounds__(kPlanThreads) void plan_order_kernel(const int64_t* ids, int64_t M, int n, int bits, uint32_t* plan, const uint32_t* chunks)
+{
+    __shared__ uint32_t counts[kPlanWaves][kMostGroups];
+    const uint32_t groups = (uint32_t)n + 2;
+    Chunk c;
+    look_through(ids, blockIdx.x * kChunkRows, M, n, bits, counts, c);
+    __syncthreads();
+    for (uint32_t g = threadIdx.x; g < groups; g += kPlanThreads) {
+        uint32_t at = chunks[(int64_t)blockIdx.x * groups + g];
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const uint32_t own = counts[w][g];
+            counts[w][g] = at;
+            at += own;
+        }
+    }
+    __syncthreads();
+    put_in_order(c, counts, const_cast<uint32_t*>(plan_at(plan, M, n).order));
 }
 
 constexpr int kWords = (int)(kDirect / 64);
@@ -1044,9 +1135,12 @@ Parts parts_of(const AdapterArgs& a, int64_t D)
 }
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+// the plan, and behind it, of more than one workgroup's rows, their counts
+size_t counts_at(const AdapterArgs& a) { return (plan_words(a.M, a.n) + 1) / 2 * 8 + sizeof(uint2) * (size_t)most_tiles(a.M, a.n); }
 size_t plan_bytes(const AdapterArgs& a)
 {
-    return direct(a) ? 0 : rounded((plan_words(a.M, a.n) + 1) / 2 * 8 + sizeof(uint2) * (size_t)most_tiles(a.M, a.n));
+    if (direct(a)) return 0;
+    return rounded(counts_at(a) + (a.M > kChunkRows ? sizeof(uint32_t) * (size_t)chunks_of(a.M) * (a.n + 2) : 0));
 }
 size_t h_bytes(const AdapterArgs& a, int64_t D)
 {
@@ -1143,7 +1237,15 @@ hipError_t launch_adapters_fwd(const AdapterArgs& a, hipStream_t stream)
         ProfileScope ps(K_ADAPT_PLAN, stream);
         int bits = 1;
         while ((1 << bits) < a.n + 2) ++bits;
-        hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a.ids, a.M, a.n, bits, static_cast<uint32_t*>(a.saved));
+        uint32_t *plan = static_cast<uint32_t*>(a.saved), *counts = reinterpret_cast<uint32_t*>(static_cast<char*>(a.saved) + counts_at(a));
+        const uint32_t chunks = (uint32_t)chunks_of(a.M);
+        if (chunks == 1) {
+            hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a.ids, a.M, a.n, bits, plan);
+        } else {
+            hipLaunchKernelGGL(plan_count_kernel, dim3(chunks), dim3(kPlanThreads), 0, stream, a.ids, a.M, a.n, bits, counts);
+            hipLaunchKernelGGL(plan_starts_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a.M, a.n, plan, counts, chunks);
+            hipLaunchKernelGGL(plan_order_kernel, dim3(chunks), dim3(kPlanThreads), 0, stream, a.ids, a.M, a.n, bits, plan, counts);
+        }
     }
     launch_pass<kDown>(a, a.x, a.A, h, a.B, a.base, a.out, a.K, a.N, rows, stream);
     return hipGetLastError();

@@ -36,6 +36,8 @@ def test_launches():
     assert names("adapt_fwd", 257, 256, 256, 8, 4, F32) == ["plan", "down_up"]
     assert names("adapt_fwd", 256, 256, 256, 8, 4, F32) == ["down_up"] and names("adapt_fwd", 128, 4096, 4096, 16, 4, BF16) == ["down", "up"]
     assert names("adapt_fwd", 129, 4096, 4096, 16, 4, BF16) == ["plan", "down", "up"]
+    assert names("adapt_fwd", 8192, 256, 256, 8, 4, F32)[0] == "plan"
+    assert names("adapt_fwd", 8193, 256, 256, 8, 4, F32) == ["plan_count", "plan_starts", "plan_order", "down", "up"]
     assert names("adapt_fwd", 100, 256, 63, 8, 4, F32) == ["down", "up"] and names("adapt_fwd", 100, 31, 256, 8, 4, F32) == ["down", "up"]
     assert names("adapt_fwd", 100, 256, 256, 65, 4, F32) == ["down", "up"] and names("adapt_fwd", 5000, 256, 256, 8, 4, F32) == ["plan", "down", "up"]
     assert names("adapt_fwd", 100, 4096, 4096, 8, 4, F32) == ["down", "up"]

@@ -97,6 +97,24 @@ def test_rows_around_tiles(M, dtype):
     check(M, 80, 140, 8, 2, dtype, none=1.0)
 
 
+@pytest.mark.parametrize("M, n", [(8191, 3), (8192, 1024), (8193, 3), (16385, 1), (24577, 1024), (70001, 10)])
+def test_plans_of_many_rows(M, n):
+    """On both sides of what one workgroup of the plan looks through, rows without an adapter and with a wrong one among them."""
+    i = inputs(M, 40, 72, 4, n, BF16)
+    i["ids"][M // 2], i["ids"][M - 1] = n, n - 1
+    bad = torch.zeros(M, dtype=torch.bool, device="cuda")
+    bad[M // 2] = True
+    out, saved = B.adapters_fwd(i["x"], i["A"], i["Bm"], i["ids"], i["scale"], i["base"])
+    dx, dA, dB = B.adapters_bwd(i["dy"], i["x"], i["A"], i["Bm"], i["ids"], saved, i["scale"])
+    want = adapters(i["x"], i["A"], i["Bm"], torch.where(bad, torch.full_like(i["ids"], -1), i["ids"]), i["scale"], i["base"], i["dy"])
+    assert bool(out[bad].isnan().all()) and bool(dx[bad].isnan().all())
+    good = ~bad.cpu()
+    near(out[~bad], want["out"][good], BF16)
+    near(dx[~bad], want["dx"][good], BF16)
+    near(dA, want["dA"], BF16)
+    near(dB, want["dB"], BF16)
+
+
 @pytest.mark.parametrize("M", [50, 150, 300])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_numbers_that_are_none(M, dtype):
