@@ -39,6 +39,15 @@ constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kMostGroups =
 
 enum Mode { kAlong, kDown };        // memory runs along the contraction, or across it
 
+// What the lanes of a wave have done in LDS that is the wave's own is before what they do there next.  (A wave's LDS operations are carried
+// out in order: it is the compiler that is kept from moving them across each other.)
+__device__ __forceinline__ void wave_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // 16 bytes of a line: eight bfloat16 values or four of 32 bits
 struct __attribute__((aligned(16))) Piece {
     uint32_t w[4];
@@ -242,6 +251,7 @@ __device__ __forceinline__ void look_through(const int64_t* ids, int64_t from, i
         uint32_t at = 0;
         if (there && lane == leader) at = atomicAdd(&counts[wave][c.group[u]], (uint32_t)__popcll(same));
         c.before[u] = __shfl(at, leader & 63) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+        wave_in_order();                        // (the next 64 rows' leader of the group may be another lane)
     }
 }
 // Writes the rows to their places, counts[wave][group] being where the wave's rows of the group begin.
@@ -689,6 +699,7 @@ __device__ __forceinline__ void Down<DT, RT, MODE, SHORT>::tile(const DownArgs& 
 #pragma unroll
                         for (int e = 0; e < L; ++e) w[c][q][e] = lines[c][q][e];
             if (step + kDownWaves < last) load(step + kDownWaves);
+            wave_in_order();                            // the pieces are there for the lanes that take them
             auto fragment = [&](int f, int c) {         // 16 rows from 16 f on
                 return *reinterpret_cast<const Piece*>(mine + 2048 * f + 128 * j + 16 * ((4 * c + g) ^ (j & 7)));
             };
@@ -704,6 +715,7 @@ __device__ __forceinline__ void Down<DT, RT, MODE, SHORT>::tile(const DownArgs& 
                         for (int t = 0; t < RL; ++t) w[c][q][t] = fragment(kSubs + RL * q + t, c);
                 products(x, w[c]);
             }
+            wave_in_order();                            // and are taken before the next step's are put over them
         }
     }
     join_waves<RT>(acc, reinterpret_cast<v4f*>(lds), wave, lane);
