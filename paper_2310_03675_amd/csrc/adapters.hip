@@ -754,7 +754,7 @@ struct UpArgs {
     uint32_t parts;
 };
 
-// Planes of a row's values, all parts together (four are asked for at once), the first `skip` taken for zeros: P of them, or, of two in one
+// Planes of a row's values from any of them on, all parts together (four are asked for at once), the first `skip` taken for zeros: P of them, or, of two in one
 // (P = 1), a lane's own.  (Chosen word by word: a choice between the two in memory would put them into LDS, at an address that a load from
 // the host's queue decides, 10 us of a small call.)
 template <int DT, int P>
@@ -763,13 +763,13 @@ __device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t pa
     constexpr int N = lane_of<DT>(), V = N / 4;
     v4f q[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) q[j] = reinterpret_cast<const v4f*>(h)[j];
+    for (int j = 0; j < V; ++j) __builtin_memcpy(&q[j], h + 4 * j, 16);
     if (parts > 1) {
         v4f more[kMostParts - 1][V];
 #pragma unroll
         for (int u = 1; u < kMostParts; ++u)
 #pragma unroll
-            for (int j = 0; j < V; ++j) more[u - 1][j] = reinterpret_cast<const v4f*>(h + (u < (int)parts ? u : 0) * part)[j];
+            for (int j = 0; j < V; ++j) __builtin_memcpy(&more[u - 1][j], h + (u < (int)parts ? u : 0) * part + 4 * j, 16);
 #pragma unroll
         for (int u = 1; u < kMostParts; ++u)
 #pragma unroll

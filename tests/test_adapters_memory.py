@@ -29,3 +29,12 @@ def test_a_waves_turns_in_lds_are_in_order():
     with_lds = [name for name, m in tiles.items() if m and m[4] == "0"]
     assert len(with_lds) == 16 and all(calls[name] == 2 for name in with_lds)
     assert [n for name, n in calls.items() if "12look_through" in name] == [1]
+
+
+def test_h_is_loaded_from_any_of_its_values_on():
+    """Of a rank that is no multiple of a load the last lanes begin at its end minus a load: at 4 or 8 bytes."""
+    bodies = [body for name, body in functions().items() if "6load_hI" in name]
+    assert len(bodies) == 3
+    for body in bodies:
+        copies = re.findall(r"@llvm\.memcpy[^(]*\([^,]*, ptr align (\d+) [^,]*, i64 16,", body)
+        assert copies == ["4", "4"], copies
