@@ -897,9 +897,15 @@ __device__ __forceinline__ void Up<DT, RT, MODE, END, WAVES>::tile(const UpArgs&
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 if (c) lines(c);
-                if (a.r != kRanks)                     // (h is zero there, but W may be infinite)
+                if (a.r != kRanks) {                   // (h is zero there, but W may be infinite)
+                    if (MODE == kAlong && !SHORT && a.r % L) {
 #pragma unroll
-                    for (int e = 0; e < L; ++e) w[e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[e]);
+                        for (int e = 0; e < L; ++e) w[e] = without<DT>(w[e], own(c) - first(c));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < L; ++e) w[e] = only_if(own(c) + (MODE == kDown ? e : 0) < a.r, w[e]);
+                    }
+                }
 #pragma unroll
                 for (int t = 0; t < L; ++t) {
                     const Piece b = MODE == kDown ? turned<DT>(w, t) : w[t];

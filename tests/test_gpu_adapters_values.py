@@ -40,3 +40,31 @@ def test_every_step_of_a_contraction_counts(M, K, r, dtype):
     _, saved = B.adapters_fwd(dev(x0), dev(Aw), dev(Bw), ids.cuda())
     dx, dA, dB = B.adapters_bwd(dev(x), dev(x0), dev(Aw), dev(Bw), ids.cuda(), saved)
     assert torch.equal(dx.double().cpu(), want) and not dA.any() and not dB.any()
+
+
+@pytest.mark.parametrize("r", [3, 4, 5, 6, 7, 9, 18, 30, 33, 66, 127])
+@pytest.mark.parametrize("M", [20, 300])
+def test_an_infinity_in_a_matrix_gives_infinities(M, r):
+    """fp32: dx and out have the formula's infinities, with their signs, where it has them, and the same bits everywhere else."""
+    g = torch.Generator().manual_seed(r)
+    K, N, n = 70, 140, 2
+    f = lambda *s: torch.randn(*s, generator=g).cuda()
+    x, dy, base, A, Bm = f(M, K), f(M, N), f(M, N), f(n, K, r), f(n, r, N)
+    ids = torch.randint(0, n, (M,), generator=g).cuda()
+    out0, saved0 = B.adapters_fwd(x, A, Bm, ids, base=base)
+    dx0 = B.adapters_bwd(dy, x, A, Bm, ids, saved0, need=(True, False, False))[0]
+    h = torch.stack([x[i].double() @ A[ids[i]].double() for i in range(M)])
+    back = torch.stack([dy[i].double() @ Bm[ids[i]].double().t() for i in range(M)])
+    for rank in {0, r // 2, max(r - 2, 0), r - 1}:
+        infinite = A.clone()
+        infinite[1, 33, rank] = float("inf")
+        dx = B.adapters_bwd(dy, x, infinite, Bm, ids, saved0, need=(True, False, False))[0]
+        want = dx0.clone()
+        want[ids == 1, 33] = float("inf") * back[ids == 1, rank].sign().float()
+        assert torch.equal(dx, want), rank
+        infinite = Bm.clone()
+        infinite[1, rank, 77] = float("inf")
+        out, _ = B.adapters_fwd(x, A, infinite, ids, base=base)
+        want = out0.clone()
+        want[ids == 1, 77] = float("inf") * h[ids == 1, rank].sign().float()
+        assert torch.equal(out, want), rank
