@@ -1051,7 +1051,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void weights_kernel(WeightArg
                 for (int c = 0; c < L; ++c) acc[t][c] += sums[half * (kShares / 2) + share][t][c][lane];
     }
     if (share || n <= 0) return;
-    const float scale = a.scale && rows.count ? a.scale[adapter] : 1.0f;     // (of no rows: zeros, whatever the scale)
+    const float scale = a.scale && rows.count > begun ? a.scale[adapter] : 1.0f;     // (of no rows, or none in this part: zeros, whatever the scale)
     float* parts = a.sums ? a.sums + (int64_t)part * a.of_a_part() + (of ? a.of_dA() : 0) : nullptr;
     // a lane has ranks rank0 + RL (4 g + i) + t of columns col + c: of a rank's run in dB kLane elements, of a column's in dA RL of each i
     if (of) {

@@ -68,3 +68,22 @@ def test_an_infinity_in_a_matrix_gives_infinities(M, r):
         want = out0.clone()
         want[ids == 1, 77] = float("inf") * h[ids == 1, rank].sign().float()
         assert torch.equal(out, want), rank
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [1, 5, 70, 200])
+def test_an_infinite_scale_of_an_adapter_of_few_rows(rows, dtype):
+    """Its gradients are infinite, also where they are added up over parts of the rows of which some have none of its."""
+    g = torch.Generator().manual_seed(rows)
+    M, K, N, r, n = 1100, 64, 72, 4, 2
+    f = lambda *s: (torch.rand(*s, generator=g) + 0.5).to(dtype).cuda()
+    x, dy, A, Bm, scale = f(M, K), f(M, N), f(n, K, r), f(n, r, N), torch.tensor([1.0, float("inf")], device="cuda")
+    ids = torch.zeros(M, dtype=torch.int64)
+    ids[torch.randperm(M, generator=g)[:rows]] = 1
+    ids = ids.cuda()
+    out, saved = B.adapters_fwd(x, A, Bm, ids, scale)
+    dx, dA, dB = B.adapters_bwd(dy, x, A, Bm, ids, saved, scale)
+    for t in (out[ids == 1], dx[ids == 1], dA[1], dB[1]):
+        assert bool((t == float("inf")).all())
+    for t in (out[ids == 0], dx[ids == 0], dA[0], dB[0]):
+        assert bool(t.isfinite().all())
