@@ -682,8 +682,9 @@ int hdqt_layernorm_bwd(const void *dy, const void *dsum, const void *s, const hd
  *             backward call with the same x, A, ids and sizes; private to the library
  *   dx, dA, dB   any may be NULL (one must not).  An adapter that no row has gets zeros
  *   workspace of the backward call, 16-byte aligned, hdqt_adapters_bwd_workspace_size (0 for invalid arguments)
- * h and g are held in fp32.  fp32: as exact as products in 32 bits.  bfloat16: products of bfloat16 with sums in 32 bits, h and g in
- * the second product as two bfloat16 values each, off by 2^-16 of themselves at most; an infinity among A or B may give NaN
+ * h and g are sums in fp32.  fp32: held and multiplied as such, as exact as products in 32 bits.  bfloat16: products of bfloat16 with
+ * sums in 32 bits; h and g are taken into the second product, and held where that reads them as they are, as two bfloat16 values
+ * each, off by 2^-16 of themselves at most.  There an infinity that meets them, in B (out), A (dx), x (dA) or dy (dB), may give NaN
  * where the formula has an infinity.
  * HDQT_EINVAL_DIM for M above 4 194 240, K or N above 2^21, r above 128, n above 1024.
  */

@@ -20,8 +20,9 @@
 // and A read: 2.0 TB/s), up 136 (base read, out written: 4.0 TB/s); backward down 131 (dy and B: 2.6 TB/s; every tile of 32 rows
 // reads its adapter's B again, twice its rows' bytes, from L2), up 40 (dx and A), weights 124 (x, dy and the gradients: 3.3 TB/s).
 //
-// bfloat16: h, g and their sums are held in 32 bits.  Where they are multiplied again each is taken as two bfloat16 values, the first
-// cut off and the second rounded: off by 2^-16 of itself at most.  fp32: products in 32 bits.
+// bfloat16: h and g are sums in 32 bits.  Where they are multiplied again each is taken as two bfloat16 values, the first cut off and the
+// second rounded: off by 2^-16 of itself at most; so they are left in memory, in as many bytes, but where parts are still to be added up,
+// which are in fp32.  fp32: products in 32 bits.
 #include "dropout.hpp"
 
 #include <type_traits>
