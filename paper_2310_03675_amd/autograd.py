@@ -416,20 +416,47 @@ class LowRank(torch.autograd.Function):
 class _Masks:
     """What a layer with dropout draws its masks by: nothing in evaluation, else a stream of its own (`layer_id`) that moves with every
     training call, or, where `counter` is set (an int64 tensor of one element on the device, which the program advances), with
-    that: a captured step then takes another mask at every replay."""
+    that: a captured step then takes another mask at every replay.
+
+    A call that the backward pass makes again (activation checkpointing) takes the mask it had.  Which call that is, torch's random state
+    on the host says, which checkpointing sets back as torch's own dropout needs it to: every call draws a number of it, and one
+    whose number the layer has seen takes the step that it had then.  With a counter nothing is drawn: the program advances it behind
+    the backward pass."""
+
+    REMEMBERED = 4096               # calls whose steps are kept
 
     def __init__(self, p: float, seed: int, layer_id: int):
         if not 0.0 <= p <= 1.0:
             raise ValueError(f"a share of {p} cannot be dropped")
-        self.p, self.seed, self.layer_id, self.step, self.counter = p, seed, layer_id, 0, None
+        self.p, self.seed, self.layer_id, self.counter = p, seed, layer_id, None
+        self.step = 0
+
+    @property
+    def step(self) -> int:
+        return self._step
+
+    @step.setter
+    def step(self, value: int):
+        self._step, self._drawn = int(value), {}
+
+    def _step_of_this_call(self) -> int:
+        drawn = torch.empty((), dtype=torch.int64, device="cpu").random_().item()
+        step = self._drawn.get(drawn)
+        if step is None:
+            if torch._C._current_graph_task_id() != -1:
+                raise RuntimeError("a forward pass of a layer with dropout, made again by the backward pass, under another random state: its mask is "
+                                   "not known (checkpoint with preserve_rng_state, or set masks.counter)")
+            step = self._drawn[drawn] = self._step
+            self._step += 1
+            if len(self._drawn) > self.REMEMBERED:
+                del self._drawn[next(iter(self._drawn))]
+        return step
 
     def next(self, training: bool) -> Optional[B.Dropout]:
         if not training or self.p == 0.0:
             return None
-        how = B.Dropout(self.p, self.seed + self.step, self.layer_id, self.counter)
-        if self.counter is None:
-            self.step += 1
-        return how
+        step = self._step_of_this_call() if self.counter is None else self._step
+        return B.Dropout(self.p, self.seed + step, self.layer_id, self.counter)
 
 
 class ResidualDropout(torch.nn.Module):

@@ -1,0 +1,72 @@
+"""Which masks the layers of a residual block draw (no GPU: the mask's definition in the kernel's place)."""
+import pytest
+import torch
+from torch.utils.checkpoint import checkpoint
+
+from paper_2310_03675_amd import autograd as A
+from residual_block import dropped, kept
+
+
+@pytest.fixture
+def on_the_host(monkeypatch):
+    def dropout(x, d, residual=None):
+        y = dropped(x, d).to(x.dtype)
+        return y if residual is None else residual + y
+
+    monkeypatch.setattr(A.B, "dropout", dropout)
+
+
+@pytest.mark.parametrize("reentrant", [True, False])
+def test_a_forward_pass_made_again_has_its_masks(on_the_host, reentrant):
+    """Two layers, one of them called twice, in segments that the backward pass makes again in the other order: the gradient goes through
+    the output's masks."""
+    one, two = A.ResidualDropout(0.5, seed=1, layer_id=1), A.ResidualDropout(0.3, seed=1, layer_id=2)
+    first, second = (lambda v: two(one(v))), (lambda v: one(v))
+    for step in range(3):
+        x = torch.ones(400, requires_grad=True)
+        y = checkpoint(second, checkpoint(first, x, use_reentrant=reentrant), use_reentrant=reentrant)
+        y.sum().backward()
+        assert torch.equal(x.grad, y.detach())                  # (linear in x, which is one)
+        masks = [kept(400, p, 1 + s, i) for p, s, i in ((0.5, 2 * step, 1), (0.3, step, 2), (0.5, 2 * step + 1, 1))]
+        assert torch.equal(y != 0, masks[0] & masks[1] & masks[2])
+    assert one.masks.step == 6 and two.masks.step == 3
+
+
+def test_several_passes_before_their_backward_passes(on_the_host):
+    m = A.ResidualDropout(0.5, seed=4)
+    xs = [torch.ones(300, requires_grad=True) for _ in range(5)]
+    ys = [checkpoint(m, x, use_reentrant=True) for x in xs]
+    for x, y in list(zip(xs, ys))[::-1]:
+        y.sum().backward()
+        assert torch.equal(x.grad, y.detach())
+    assert len({tuple(y.tolist()) for y in ys}) == 5
+
+
+def test_a_forward_pass_that_cannot_be_told_is_refused(on_the_host):
+    m = A.ResidualDropout(0.5)
+    x = torch.ones(100, requires_grad=True)
+    y = checkpoint(m, x, use_reentrant=True, preserve_rng_state=False)
+    with pytest.raises(RuntimeError, match="random state"):
+        y.sum().backward()
+
+
+def test_a_counters_pass_made_again(on_the_host):
+    m = A.ResidualDropout(0.5, seed=2)
+    m.masks.counter = torch.zeros(1, dtype=torch.int64)
+    state = torch.get_rng_state()
+    for _ in range(2):
+        x = torch.ones(300, requires_grad=True)
+        y = checkpoint(m, x, use_reentrant=True, preserve_rng_state=False)
+        y.sum().backward()
+        assert torch.equal(x.grad, y.detach())
+        m.masks.counter.add_(1)
+    assert torch.equal(torch.get_rng_state(), state)
+
+
+def test_how_many_calls_are_kept():
+    m = A.ResidualDropout(0.5).masks
+    for k in range(m.REMEMBERED + 10):
+        assert m.next(True).seed == k
+    assert len(m._drawn) == m.REMEMBERED
+    m.step = 5
+    assert m.next(True).seed == 5 and len(m._drawn) == 1
