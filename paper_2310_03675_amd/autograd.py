@@ -7,6 +7,8 @@ The activation is not kept in fp32 for the backward pass: hdqt_layer_fwd leaves
 X's codes along the batch dimension (what the weight gradient contracts over)
 in a byte buffer one eighth the size of X at 4 bits.
 """
+import copy
+import itertools
 from dataclasses import dataclass, field
 from typing import Optional
 
@@ -413,10 +415,15 @@ class LowRank(torch.autograd.Function):
         return grads[0], dy if ctx.needs_input_grad[1] else None, grads[1], grads[2], None, None
 
 
+# ids of the layers that are given none, one after the other: above those that a program counts up
+_unnamed = itertools.count(1 << 31)
+
+
 class _Masks:
-    """What a layer with dropout draws its masks by: nothing in evaluation, else a stream of its own (`layer_id`) that moves with every
-    training call, or, where `counter` is set (an int64 tensor of one element on the device, which the program advances), with
-    that: a captured step then takes another mask at every replay.
+    """What a layer with dropout draws its masks by: nothing in evaluation, else a stream of its own (`layer_id`; a layer that is given
+    none, and a copy of it, has the next that no other such layer has) that moves with every training call, or, where `counter` is set
+    (an int64 tensor of one element on the device, which the program advances), with that: a captured step then takes another
+    mask at every replay.  Calls of one layer at one value of the counter have one mask.
 
     A call that the backward pass makes again (activation checkpointing) takes the mask it had.  Which call that is, torch's random state
     on the host says, which checkpointing sets back as torch's own dropout needs it to: every call draws a number of it, and one
@@ -425,11 +432,19 @@ class _Masks:
 
     REMEMBERED = 4096               # calls whose steps are kept
 
-    def __init__(self, p: float, seed: int, layer_id: int):
+    def __init__(self, p: float, seed: int, layer_id: Optional[int]):
         if not 0.0 <= p <= 1.0:
             raise ValueError(f"a share of {p} cannot be dropped")
-        self.p, self.seed, self.layer_id, self.counter = p, seed, layer_id, None
+        self.p, self.seed, self.counter, self.unnamed = p, seed, None, layer_id is None
+        self.layer_id = next(_unnamed) if self.unnamed else layer_id
         self.step = 0
+
+    def __deepcopy__(self, memo):
+        other = copy.copy(self)
+        other.counter, other._drawn = copy.deepcopy(self.counter, memo), dict(self._drawn)
+        if self.unnamed:
+            other.layer_id = next(_unnamed)
+        return other
 
     @property
     def step(self) -> int:
@@ -462,7 +477,7 @@ class _Masks:
 class ResidualDropout(torch.nn.Module):
     """residual + dropout(x), or dropout(x); `masks.counter` for captured steps."""
 
-    def __init__(self, p: float, seed: int = 0, layer_id: int = 0):
+    def __init__(self, p: float, seed: int = 0, layer_id: Optional[int] = None):
         super().__init__()
         self.masks = _Masks(p, seed, layer_id)
 
@@ -478,7 +493,7 @@ class ResidualNorm(torch.nn.Module):
     residual + dropout(x), and the sum, for what follows.  One pass over the tensors either way; `masks.counter` for captured
     steps."""
 
-    def __init__(self, columns: int, eps: float = 1e-5, p: float = 0.0, seed: int = 0, layer_id: int = 0, device=None):
+    def __init__(self, columns: int, eps: float = 1e-5, p: float = 0.0, seed: int = 0, layer_id: Optional[int] = None, device=None):
         super().__init__()
         self.eps, self.masks = eps, _Masks(p, seed, layer_id)
         self.weight = torch.nn.Parameter(torch.ones(columns, device=device))

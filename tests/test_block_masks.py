@@ -1,4 +1,6 @@
 """Which masks the layers of a residual block draw (no GPU: the mask's definition in the kernel's place)."""
+import copy
+
 import pytest
 import torch
 from torch.utils.checkpoint import checkpoint
@@ -70,3 +72,19 @@ def test_how_many_calls_are_kept():
     assert len(m._drawn) == m.REMEMBERED
     m.step = 5
     assert m.next(True).seed == 5 and len(m._drawn) == 1
+
+
+def test_layers_without_an_id_have_masks_of_their_own(on_the_host):
+    layers = [A.ResidualDropout(0.5) for _ in range(4)]
+    layers += [copy.deepcopy(layers[0]), copy.deepcopy(torch.nn.Sequential(layers[0]))[0]]
+    ys = [m(torch.ones(400)) for m in layers]
+    for i, y in enumerate(ys):
+        for z in ys[:i]:
+            assert 0.35 < float(((y != 0) == (z != 0)).double().mean()) < 0.65         # (half; six standard deviations of 400 draws)
+    ids = [m.masks.layer_id for m in layers + [A.ResidualNorm(8, p=0.1), A.ResidualNorm(8)]]
+    assert len(set(ids)) == 8 and all(2 ** 31 <= i < 2 ** 32 for i in ids)
+    # one that has an id keeps it
+    m = A.ResidualDropout(0.5, layer_id=3)
+    assert m.masks.layer_id == 3 and copy.deepcopy(m).masks.layer_id == 3
+    m.masks.counter = torch.zeros(1, dtype=torch.int64)
+    assert torch.equal(m(torch.ones(400)), copy.deepcopy(m)(torch.ones(400)))
