@@ -474,7 +474,23 @@ class _Masks:
         return B.Dropout(self.p, self.seed + step, self.layer_id, self.counter)
 
 
-class ResidualDropout(torch.nn.Module):
+class _Masked(torch.nn.Module):
+    """A layer with dropout (`masks`): how far its masks have come is in its state, as `step`, so that a run that is taken up again goes on with
+    the next.  A state without it leaves the layer's as it is."""
+
+    def _save_to_state_dict(self, destination, prefix, keep_vars):
+        super()._save_to_state_dict(destination, prefix, keep_vars)
+        if self.masks.p:
+            destination[prefix + "step"] = torch.tensor(self.masks.step, device="cpu")
+
+    def _load_from_state_dict(self, state_dict, prefix, *args):
+        step = state_dict.pop(prefix + "step", None)
+        if step is not None:
+            self.masks.step = int(step)
+        super()._load_from_state_dict(state_dict, prefix, *args)
+
+
+class ResidualDropout(_Masked):
     """residual + dropout(x), or dropout(x); `masks.counter` for captured steps."""
 
     def __init__(self, p: float, seed: int = 0, layer_id: Optional[int] = None):
@@ -488,7 +504,7 @@ class ResidualDropout(torch.nn.Module):
         return Dropout.apply(x.contiguous(), None if residual is None else residual.contiguous(), how)
 
 
-class ResidualNorm(torch.nn.Module):
+class ResidualNorm(_Masked):
     """A residual block's end: forward(x) is the layer normalisation of x; forward(x, residual) that of the sum
     residual + dropout(x), and the sum, for what follows.  One pass over the tensors either way; `masks.counter` for captured
     steps."""

@@ -88,3 +88,30 @@ def test_layers_without_an_id_have_masks_of_their_own(on_the_host):
     assert m.masks.layer_id == 3 and copy.deepcopy(m).masks.layer_id == 3
     m.masks.counter = torch.zeros(1, dtype=torch.int64)
     assert torch.equal(m(torch.ones(400)), copy.deepcopy(m)(torch.ones(400)))
+
+
+def test_a_run_that_is_taken_up_again_goes_on_with_its_masks(on_the_host, tmp_path):
+    new = lambda: torch.nn.Sequential(A.ResidualDropout(0.5, seed=7, layer_id=1), A.ResidualDropout(0.2, layer_id=2))
+    x, net, again = torch.ones(300), new(), new()
+    for _ in range(3):
+        net(x)
+    torch.save(net.state_dict(), tmp_path / "state")
+    want = [net(x) for _ in range(2)]
+    held = torch.load(tmp_path / "state", weights_only=True)
+    again.load_state_dict(held)
+    assert list(held) == ["0.step", "1.step"] and all(torch.equal(again(x), y) for y in want)
+    again.load_state_dict(held)                                 # (it is not used up)
+    assert torch.equal(again(x), want[0])
+
+
+def test_states_of_layers_with_and_without_dropout():
+    norm, plain = A.ResidualNorm(8, p=0.1), A.ResidualNorm(8)
+    assert list(norm.state_dict()) == ["weight", "bias", "step"] and list(plain.state_dict()) == ["weight", "bias"]
+    norm.masks.step = 9
+    norm.load_state_dict(plain.state_dict())                    # one from before has no step
+    assert norm.masks.step == 9
+    plain.load_state_dict(norm.state_dict())
+    with pytest.raises(RuntimeError, match="bias"):
+        norm.load_state_dict({"weight": torch.ones(8), "step": torch.tensor(2)})
+    with pytest.raises(RuntimeError, match="other"):
+        norm.load_state_dict({**norm.state_dict(), "other": torch.ones(8)})
