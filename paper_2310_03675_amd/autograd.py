@@ -350,6 +350,11 @@ def clip_gradients(parameters, max_norm: float, norm_type: float = 2.0, eps: flo
     return B.clip_grad_norm(grads, max_norm, norm_type, eps)
 
 
+def _as_it_is(how: Optional[B.Dropout]) -> Optional[B.Dropout]:
+    """A description for the backward pass, whatever the program does with its own until then."""
+    return None if how is None else B.Dropout(how.p, how.seed, how.tensor_id, how.step)
+
+
 class Dropout(torch.autograd.Function):
     """residual + dropout(x) (hdqt_dropout): no mask is kept, the backward pass forms it again.  x contiguous, residual of its
     shape or None, `how` a binding.Dropout."""
@@ -358,7 +363,7 @@ class Dropout(torch.autograd.Function):
     def forward(ctx, x, residual, how: B.Dropout):
         # (the step's tensor is kept as a saved one: whoever advances it before the backward pass is told)
         ctx.save_for_backward(how.step)
-        ctx.how = how
+        ctx.how = _as_it_is(how)
         return B.dropout(x, how, residual)
 
     @staticmethod
@@ -378,7 +383,7 @@ class LayerNorm(torch.autograd.Function):
     def forward(ctx, x, residual, weight, bias, eps: float, how: Optional[B.Dropout]):
         y, total, saved = B.layernorm_fwd(x, weight, bias, eps, residual, how)
         ctx.save_for_backward(total, saved, weight, None if how is None else how.step)
-        ctx.how = how
+        ctx.how = _as_it_is(how)
         ctx.set_materialize_grads(False)
         return y if total is x else (y, total)
 

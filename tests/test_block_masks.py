@@ -115,3 +115,20 @@ def test_states_of_layers_with_and_without_dropout():
         norm.load_state_dict({"weight": torch.ones(8), "step": torch.tensor(2)})
     with pytest.raises(RuntimeError, match="other"):
         norm.load_state_dict({**norm.state_dict(), "other": torch.ones(8)})
+
+
+def test_a_description_that_changes_before_the_backward_pass(on_the_host, monkeypatch):
+    """One object for two calls, with another id for the second."""
+    how, x = A.B.Dropout(0.5, seed=1, tensor_id=1), torch.ones(300, requires_grad=True)
+    y = A.Dropout.apply(x, None, how)
+    how.tensor_id, how.seed, how.p = 2, 5, 0.1
+    y.sum().backward()
+    assert torch.equal(x.grad, y.detach())
+
+    seen = []
+    monkeypatch.setattr(A.B, "layernorm_fwd", lambda x, w, b, eps, r, d: (x * 1, x * 1, torch.zeros(x.shape[:-1] + (2,))))
+    monkeypatch.setattr(A.B, "layernorm_bwd", lambda dy, s, saved, w, ds, d, need: (seen.append((d.p, d.seed, d.tensor_id)), (dy, None, None, None))[1])
+    y, _ = A.LayerNorm.apply(x.reshape(3, 100), None, None, None, 1e-5, how)
+    how.tensor_id = 3
+    y.sum().backward()
+    assert seen == [(0.1, 5, 2)]
