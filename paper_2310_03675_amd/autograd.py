@@ -548,7 +548,7 @@ class Adapters(torch.nn.Module):
 class HdqtLinear(torch.nn.Module):
     """y = x W + bias with the matmul and its gradients quantized; inputs of any
     leading shape are flattened to [M, K].  `adapters` (an Adapters of the same features): forward(x, ids) adds those of
-    the rows beside it, in floating point."""
+    the rows beside it, in floating point; ids are then asked for (negative: none)."""
 
     def __init__(self, in_features: int, out_features: int, bias: bool = True,
                  cfg: Optional[LayerConfig] = None, device=None, relu_input: bool = False, adapters: Optional[Adapters] = None):
@@ -564,8 +564,9 @@ class HdqtLinear(torch.nn.Module):
 
     def forward(self, x, ids=None):
         lead = x.shape[:-1]
-        if ids is not None and self.adapters is None:
-            raise ValueError("ids are for a layer with adapters")
+        if (ids is None) != (self.adapters is None):
+            raise ValueError("ids are for a layer with adapters" if self.adapters is None else
+                             "a layer with adapters asks for ids, one for each row (negative: none)")
         fn = HdqtReluMatmul if self.relu_input else HdqtMatmul
         z = fn.apply(x.reshape(-1, x.shape[-1]), self.weight, self.cfg, self.step)
         if self.training:
