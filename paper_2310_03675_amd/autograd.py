@@ -539,6 +539,14 @@ class Adapters(torch.nn.Module):
         self.B = torch.nn.Parameter(torch.zeros(adapters, rank, out_features, device=device))
         self.register_buffer("scale", torch.full((adapters,), (rank if alpha is None else alpha) / rank, device=device))
 
+    def _apply(self, fn, recurse=True):
+        # (the scales stay in 32 bits, as the kernels take them, whatever type the module is put into)
+        scale = self.scale
+        super()._apply(fn, recurse)
+        if self.scale.dtype != scale.dtype:
+            self.scale = scale.to(self.scale.device)
+        return self
+
     def forward(self, x, base, ids):
         out = LowRank.apply(x.reshape(-1, x.shape[-1]).contiguous(), base.reshape(-1, base.shape[-1]).contiguous(), self.A, self.B,
                             ids.reshape(-1).contiguous(), self.scale.float())
