@@ -11,8 +11,8 @@
 // which a second launch adds up in 64 bits: no atomics, results do not depend on what finishes first.
 //
 // Measured, with a residual forward and a gradient of s backward (a large copy: 5.1 TB/s): 8192 x 4096 in bfloat16 44 us (6.1 TB/s) and 65 us
-// (4.1), in fp32 102 us (5.3) and 116 us (4.6); 20011 x 1031 in bfloat16 43 and 52 us (3.8 and 3.2 TB/s: a row's end costs a wave as much as a
-// whole vector); 131072 x 64 in fp32 22 and 28 us; 128 x 512 in fp32 3.6 and 3.5 us, a launch each.
+// (4.1), in fp32 102 us (5.3) and 116 us (4.6); 20011 x 1031 in bfloat16 43 and 52 us (3.8 and 3.2 TB/s: its vectors are one more than
+// places, and rows start and end anywhere; 1024 columns 30 and 39); 131072 x 64 in fp32 22 and 28 us; 128 x 512 in fp32 3.6 and 3.5 us, a launch each.
 #include "dropout.hpp"
 #include "lane_ops.hpp"
 
