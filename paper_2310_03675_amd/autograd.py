@@ -432,8 +432,8 @@ class _Masks:
 
     A call that the backward pass makes again (activation checkpointing) takes the mask it had.  Which call that is, torch's random state
     on the host says, which checkpointing sets back as torch's own dropout needs it to: every call draws a number of it, and one
-    whose number the layer has seen takes the step that it had then.  With a counter nothing is drawn: the program advances it behind
-    the backward pass."""
+    whose number the layer has seen takes the step that it had then (so does one behind a program's own setting back of that state).
+    With a counter nothing is drawn: the program advances it behind the backward pass."""
 
     REMEMBERED = 4096               # calls whose steps are kept
 

@@ -756,9 +756,9 @@ struct UpArgs {
     uint32_t parts;
 };
 
-// Planes of a row's values from any of them on, all parts together (four are asked for at once), the first `skip` taken for zeros: P of them, or, of two in one
-// (P = 1), a lane's own.  (Chosen word by word: a choice between the two in memory would put them into LDS, at an address that a load from
-// the host's queue decides, 10 us of a small call.)
+// Planes of a row's values from any of them on, all parts together (four are asked for at once), the first `skip` taken for zeros: P of
+// them, or, of two in one (P = 1), a lane's own.  (Chosen word by word: a choice between the two in memory would put them into LDS, at an
+// address that a load from the host's queue decides, 10 us of a small call.)
 template <int DT, int P>
 __device__ __forceinline__ void load_h(const float* h, int64_t part, uint32_t parts, int skip, bool second, Piece (&to)[P])
 {
